@@ -9,6 +9,12 @@
  *   ann_cross_attn_fwd   the same selection and the attention over it in one launch
  *   sparse_attn_fwd      softmax attention over the selected keys only, with the log-multiplicity bias
  *
+ * and, for programs that serve several requests at a time, dense attention with grouped heads over packed sequences:
+ *   prompt_attn_fwd      causal or full attention over whole prompts
+ *   kv_pages_plan        block tables and slot maps of a paged cache from the requests' lengths
+ *   kv_pages_write       new keys and values into its pages: E4M3 codes with a scale per page and head
+ *   paged_attn_fwd       attention over those pages, for single tokens and chunks
+ *
  * Conventions (all entry points):
  *   - Every pointer is a DEVICE pointer unless it points to one of the small structs below, which
  *     are read on the host at call time.  The caller owns every buffer; the library allocates
@@ -17,7 +23,7 @@
  *     (fastar_init, or lazily and thread-safely by the first call that needs it).
  *   - `stream` is a hipStream_t passed as void*.  Work is enqueued on it and the call returns.
  *   - Tensors are DENSE row-major: [H, N, d] means element (h, n, t) at (h*N + n)*d + t; there are no
- *     stride arguments.  The key/value tiles of the attention kernels are fetched straight into LDS
+ *     stride arguments (the calls that take fastar_rows have them).  The key/value tiles of the attention kernels are fetched straight into LDS
  *     from one base address per tile with fixed row pitch d * sizeof(element), and the cache arrays
  *     K, V, code, cnt, stamp are indexed by one slot number; a strided view would put an address
  *     computation per row back into those loops.  A caller that holds a strided view passes a
@@ -61,6 +67,7 @@ extern "C" {
 #define FASTAR_OP_SELECT_LSH 4
 #define FASTAR_OP_SELECT_BUCKETS 5 /* pass the number of prompt tokens as r */
 #define FASTAR_OP_ATTN 6           /* sparse_attn_fwd_ws, sparse_attn_fwd_fp8_ws: a fixed amount, whatever the shape */
+#define FASTAR_OP_PAGED_ATTN 7     /* paged_attn_fwd: a fixed amount, whatever the shape */
 
 /* representative key of a merged TempCache group (tempcache_compress, rep_mode) */
 #define FASTAR_REP_LAST 0
@@ -418,6 +425,108 @@ int sparse_attn_fwd_fp8(const void *Q, int n_q, const uint8_t *K8, const uint8_t
 int sparse_attn_fwd_fp8_ws(const void *Q, int n_q, const uint8_t *K8, const uint8_t *V8T, const int32_t *cnt,
                            const int32_t *len, int H, int C, int d, const int32_t *sel, const int32_t *nsel, int BQ,
                            int BK, int n_sel, float scale, void *O, float *lse, void *ws, size_t ws_bytes, void *stream);
+
+/* ================================================================================================================
+ * Several requests at a time.  The tokens of B sequences lie one sequence after the other in arrays of n_tok rows
+ * (packed): sequence b owns rows cu[b] .. cu[b+1]-1, cu [B+1] int32 on the device, not falling.  Offsets are cut to
+ * [0, n_tok]; rows outside of every sequence are neither read nor written.  A sequence may have no rows.
+ *
+ * Grouped heads: Hq query heads share Hkv key heads, Hq a multiple of Hkv; query head h reads key head h / (Hq / Hkv).
+ *
+ * Causal: the last query of a sequence is its last key.  With a queries and n keys, query i sees keys j <= n - a + i; for
+ * a > n the first a - n queries see nothing.  A query without a key: o = 0, lse = -inf.
+ * ================================================================================================================ */
+
+/*
+ * A strided view [H, n, d]: element (h, i, t) at p + h*head + i*row + t, strides in elements, >= 0, every row 16-byte
+ * aligned.  [H, n, d] and [n, H, d] arrays and the parts of a fused projection's output are such views.  Rows of an
+ * output must not overlap: one of the strides is at least d, the other at least the first one's extent.
+ */
+typedef struct {
+    void *p;
+    int64_t head, row;
+} fastar_rows;
+
+/*
+ * Attention over whole prompts: l_j = scale * q_i.k_j over the keys j that query i sees, o_i = sum_j softmax(l)_j v_j,
+ * lse_i = ln sum_j exp(l_j).
+ *   Q [Hq,n_tok_q,d], K, V [Hkv,n_tok_k,d], O [Hq,n_tok_q,d] views of dtype;  lse [Hq,n_tok_q] float (dense) or NULL
+ *   cu_q [B+1] rows of Q and O;  cu_k [B+1] rows of K and V, or NULL: cu_q
+ *   causal  0: every query sees all keys of its sequence;  1: as above
+ * bf16: bf16 products (the weights are rounded to bf16), fp32 softmax and sums; fp32: plain fp32 arithmetic.
+ * Supported: d in {64, 128}; scale positive, scale * log2(e) finite.  No workspace.  n_tok_q = 0 or B = 0 launches nothing.
+ */
+int prompt_attn_fwd(const fastar_rows *Q, const fastar_rows *K, const fastar_rows *V, const int32_t *cu_q,
+                    const int32_t *cu_k, int B, int n_tok_q, int n_tok_k, int Hq, int Hkv, int d, int dtype, int causal,
+                    float scale, const fastar_rows *O, float *lse, void *stream);
+
+/*
+ * A cache in pages of P tokens.  Keys and values are E4M3 codes (the format of fastar_kv_to_fp8) in cells of 16 tokens x
+ * 16 coordinates, 256 bytes: a cell of K8 holds a token's 16 coordinates together, one of V8 a coordinate's 16 tokens, so
+ * that 16 consecutive bytes are an operand of the matrix instructions for either product.
+ *   K8 [n_pages, Hkv, P/16, d/16, 16 tokens, 16 coordinates], V8 [n_pages, Hkv, P/16, d/16, 16 coordinates, 16 tokens]
+ *   kscale, vscale [n_pages, Hkv] float, powers of two: a code stands for its E4M3 value times the scale of its page and
+ *   head.  E4M3 has an exponent of its own, so that a finer scale would not make codes more precise; a power of two lets
+ *   the codes of a page be carried to a larger scale without a second rounding (but for those that become subnormal).
+ * P in {16, 32, 64}, n_pages * P < 2^31.  Token i of a sequence lies in page table[b][i / P] of its block table, at i % P.
+ */
+typedef struct {
+    uint8_t *K8, *V8;
+    float *kscale, *vscale;
+    int32_t n_pages, Hkv, P, d;
+} fastar_pages;
+
+/*
+ * Block tables and slot maps for the next step of B requests.
+ *   n_new [B]             tokens that request b appends; 0: none; negative: the request has ended
+ *   len [B]               tokens that it holds
+ *   table [B, max_pages]  block tables, updated;  the first ceil(len/P) entries of a row count, others mean nothing
+ *   pool [n_pages]        free pages, a stack whose first pool_n[0] entries count, updated
+ * 1. The pages of ended requests go on top of the stack, in the order of the requests and of their tables.
+ * 2. Request b needs ceil((len+n_new)/P) - ceil(len/P) pages.  They are taken from the top, in the order of the requests.
+ *    A request is refused, and keeps what it has, if its table is too short (status 2), if its rows go beyond n_tok
+ *    (status 3), or if it needs pages and those needed up to and including it are more than there are (status 1; requests
+ *    refused for status 2 or 3 need none).
+ * Outputs:
+ *   len_out [B]       tokens after the step (0 for ended requests); may be len itself
+ *   pool_n_out [1]    free pages after the step; may be pool_n itself
+ *   cu [B+1]          rows of the requests' new tokens: the prefix sums of max(n_new, 0), cut to n_tok
+ *   slot [n_tok]      page * P + offset of each new token; -1 where the request is refused.  Rows from cu[B] on stay.
+ *   status [B]        0 (also for ended requests), 1, 2 or 3
+ * Lengths and counts are cut to what the arrays hold; a table entry outside of [0, n_pages) gives slot -1.
+ * Supported: P in {16, 32, 64}; max_pages * P and n_pages * P < 2^31.  One launch for few tokens, two for many; no workspace.
+ */
+int kv_pages_plan(const int32_t *n_new, const int32_t *len, int32_t *table, int B, int max_pages, int32_t *pool,
+                  const int32_t *pool_n, int n_pages, int P, int n_tok, int32_t *len_out, int32_t *pool_n_out, int32_t *cu,
+                  int32_t *slot, int32_t *status, void *stream);
+
+/*
+ * New keys and values into their pages.  K_new, V_new [Hkv,n_tok,d] views of dtype; slot [n_tok] int32 as kv_pages_plan
+ * writes it: rows of one page follow one another, in the order of their slots, and a page has one such run of rows in a
+ * call; negative slots and those >= n_pages * P are passed over.
+ * Of a run the largest finite |x| per head asks for the scale s = 2^max(-100, ceil(log2(|x| / 448))).  A run that begins at
+ * offset 0 begins the page anew: the page takes s, and codes behind the run stay as they are (they mean nothing).  Any other
+ * run raises the page's scale to s if that is larger; all other codes of the page and head are then carried over to it (value
+ * of the code times the old scale over the new one, rounded to nearest, ties to even).  New codes: x / scale rounded to
+ * nearest, ties to even; infinities become the largest code of their sign, NaN stays NaN.
+ */
+int kv_pages_write(const fastar_pages *pages, const fastar_rows *K_new, const fastar_rows *V_new, int dtype,
+                   const int32_t *slot, int n_tok, void *stream);
+
+/*
+ * Attention over such a cache: prompt_attn_fwd's definition with the keys and values that the codes stand for.
+ *   Q, O [Hq,n_tok,d] bf16 views;  cu_q [B+1];  len [B] keys of every sequence (those of the queries among them, written
+ *   before);  table [B, max_pages];  lse [Hq,n_tok] float or NULL;  causal as for prompt_attn_fwd
+ * Keys on pages outside of [0, n_pages) are left out, like masked ones; len is cut to [0, max_pages * P].
+ * Products in bf16 (codes are widened exactly), fp32 softmax and sums.  Sequences share the chip by their lengths, which
+ * the device reads: long ones are cut into pieces whose fragments lie in ws, and a second launch puts them together.
+ *   ws / ws_bytes  fastar_workspace_bytes(FASTAR_OP_PAGED_ATTN, ...) bytes, 256-byte aligned; contents need not be kept.
+ *                  Calls that may be in flight at the same time need a workspace each.
+ * Supported: bf16, d in {64, 128}, scales of the pages 2^-100 .. 2^120; scale as for prompt_attn_fwd.
+ */
+int paged_attn_fwd(const fastar_rows *Q, const int32_t *cu_q, const int32_t *len, const int32_t *table, int B, int max_pages,
+                   int n_tok, int Hq, const fastar_pages *pages, int dtype, int causal, float scale, const fastar_rows *O,
+                   float *lse, void *ws, size_t ws_bytes, void *stream);
 
 #ifdef __cplusplus
 }

@@ -17,7 +17,7 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libfastar.so")
 
 F32, BF16 = 0, 1
-OP_COMPRESS, OP_SELECT_SELF, OP_SELECT_CROSS, OP_SELECT_LSH, OP_SELECT_BUCKETS, OP_ATTN = 1, 2, 3, 4, 5, 6
+OP_COMPRESS, OP_SELECT_SELF, OP_SELECT_CROSS, OP_SELECT_LSH, OP_SELECT_BUCKETS, OP_ATTN, OP_PAGED_ATTN = 1, 2, 3, 4, 5, 6, 7
 REP_LAST, REP_MEAN, REP_MEDOID = 0, 1, 2
 
 _lib = None
@@ -35,6 +35,15 @@ class _CacheStruct(ctypes.Structure):
 
 class _CodecStruct(ctypes.Structure):
     _fields_ = [("R", ctypes.c_void_p), ("qscale", ctypes.c_float), ("shift", ctypes.c_int32)]
+
+
+class _RowsStruct(ctypes.Structure):
+    _fields_ = [("p", ctypes.c_void_p), ("head", ctypes.c_int64), ("row", ctypes.c_int64)]
+
+
+class _PagesStruct(ctypes.Structure):
+    _fields_ = [("K8", ctypes.c_void_p), ("V8", ctypes.c_void_p), ("kscale", ctypes.c_void_p), ("vscale", ctypes.c_void_p),
+                ("n_pages", ctypes.c_int32), ("Hkv", ctypes.c_int32), ("P", ctypes.c_int32), ("d", ctypes.c_int32)]
 
 
 def lib() -> ctypes.CDLL:
@@ -120,6 +129,20 @@ def lib() -> ctypes.CDLL:
         L.ann_select_lsh.restype = ctypes.c_int
         L.ann_select_lsh.argtypes = [ctypes.c_void_p, ctypes.c_int, ctypes.c_void_p, ctypes.c_void_p] + \
             [ctypes.c_int] * 7 + [ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p, ctypes.c_size_t, ctypes.c_void_p]
+        rows = ctypes.POINTER(_RowsStruct)
+        L.prompt_attn_fwd.restype = ctypes.c_int
+        L.prompt_attn_fwd.argtypes = [rows, rows, rows, ctypes.c_void_p, ctypes.c_void_p] + [ctypes.c_int] * 8 + \
+            [ctypes.c_float, rows, ctypes.c_void_p, ctypes.c_void_p]
+        L.kv_pages_plan.restype = ctypes.c_int
+        L.kv_pages_plan.argtypes = [ctypes.c_void_p] * 3 + [ctypes.c_int] * 2 + [ctypes.c_void_p] * 2 + [ctypes.c_int] * 3 + \
+            [ctypes.c_void_p] * 6
+        L.kv_pages_write.restype = ctypes.c_int
+        L.kv_pages_write.argtypes = [ctypes.POINTER(_PagesStruct), rows, rows, ctypes.c_int, ctypes.c_void_p, ctypes.c_int,
+                                     ctypes.c_void_p]
+        L.paged_attn_fwd.restype = ctypes.c_int
+        L.paged_attn_fwd.argtypes = [rows, ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p] + [ctypes.c_int] * 4 + \
+            [ctypes.POINTER(_PagesStruct), ctypes.c_int, ctypes.c_int, ctypes.c_float, rows, ctypes.c_void_p, ctypes.c_void_p,
+             ctypes.c_size_t, ctypes.c_void_p]
         L.fastar_probe_mfma_bf16.restype = ctypes.c_int
         L.fastar_probe_mfma_bf16.argtypes = [ctypes.c_int, ctypes.c_int, ctypes.c_void_p, ctypes.POINTER(ctypes.c_double), ctypes.c_void_p]
         L.fastar_probe_copy.restype = ctypes.c_int
@@ -136,6 +159,7 @@ EXPORTS = ("fastar_init", "fastar_version", "fastar_strerror", "fastar_workspace
            "ann_cross_attn_fwd",
            "ann_select_self", "ann_select_self_forced", "ann_select_self_static", "ann_prompt_buckets", "ann_select_buckets", "fastar_encode_packed", "ann_select_self_packed", "ann_select_cross", "sparse_attn_fwd", "sparse_attn_fwd_ws", "fastar_kv_to_fp8",
            "sparse_attn_fwd_fp8", "sparse_attn_fwd_fp8_ws", "fastar_encode_sign", "ann_select_lsh", "ann_select_lsh_buckets",
+           "prompt_attn_fwd", "kv_pages_plan", "kv_pages_write", "paged_attn_fwd",
            "fastar_probe_mfma_bf16", "fastar_probe_copy", "fastar_probe_attn_route", "fastar_debug_plan_wait")
 
 
@@ -577,6 +601,133 @@ def sparse_attn_fwd_fp8(Q, K8, V8T, cnt, length, C: int, sel, nsel, BQ: int, BK:
     _check(lib().sparse_attn_fwd_fp8(Q.data_ptr(), n_q, K8.data_ptr(), V8T.data_ptr(), _ptr(cnt), length.data_ptr(), H, C,
                                      d, sel.data_ptr(), nsel.data_ptr(), BQ, BK, n_sel, float(scale), O.data_ptr(),
                                      _ptr(lse), _stream()), "sparse_attn_fwd_fp8")
+    return O, lse
+
+
+# ---------------------------------------------------------------------------------------------- several requests at a time
+
+
+def _rows(t: torch.Tensor, H: int, n: int, d: int, dtype) -> _RowsStruct:
+    """A view [H, n, d] of any head and row strides."""
+    if t.dtype != dtype:
+        raise TypeError(f"expected {dtype}, got {t.dtype}")
+    if t.shape != (H, n, d) or not t.is_cuda or t.stride(2) != 1:
+        raise ValueError(f"expected a device tensor [{H}, {n}, {d}] whose rows are contiguous, got {tuple(t.shape)}")
+    return _RowsStruct(t.data_ptr(), t.stride(0), t.stride(1))
+
+
+def _ints(t: torch.Tensor, *shape):
+    if tuple(t.shape) != shape:
+        raise ValueError(f"expected shape {shape}, got {tuple(t.shape)}")
+    return _dev(t, torch.int32).data_ptr()
+
+
+def _lse_out(lse, Hq: int, n: int):
+    if lse is None:
+        return None
+    if tuple(lse.shape) != (Hq, n):
+        raise ValueError(f"lse must be [{Hq}, {n}]")
+    return _dev(lse, torch.float32).data_ptr()
+
+
+def _grouped(Q, Hkv: int):
+    if Q.dim() != 3:
+        raise ValueError("Q must be [Hq, n, d]")
+    Hq, n, d = Q.shape
+    if Hkv <= 0 or Hq % Hkv:
+        raise ValueError(f"{Hq} query heads cannot share {Hkv} key heads")
+    return Hq, n, d
+
+
+def prompt_attn_fwd(Q, K, V, cu_q, cu_k=None, causal: bool = True, scale: float | None = None, out=None, want_lse: bool = True):
+    """Attention over whole packed prompts.  Q [Hq,n_q,d], K, V [Hkv,n_k,d]: views of any head and row strides; cu_q, cu_k
+    [B+1] int32 (cu_k None: cu_q); scale None: d ** -0.5.  Returns (O [Hq,n_q,d] in Q's dtype, lse [Hq,n_q] or None); rows
+    outside of every sequence are not written."""
+    Hq, n_q, d = _grouped(Q, K.shape[0])
+    Hkv, n_k = K.shape[0], K.shape[1]
+    dt = _dtype_code(Q)
+    B = cu_q.numel() - 1
+    if out is None:
+        out = (torch.empty_like(Q), torch.empty((Hq, n_q), dtype=torch.float32, device=Q.device) if want_lse else None)
+    O, lse = out
+    q, k, v, o = _rows(Q, Hq, n_q, d, Q.dtype), _rows(K, Hkv, n_k, d, Q.dtype), _rows(V, Hkv, n_k, d, Q.dtype), _rows(O, Hq, n_q, d, Q.dtype)
+    _check(lib().prompt_attn_fwd(q, k, v, _ints(cu_q, B + 1), None if cu_k is None else _ints(cu_k, B + 1), B, n_q, n_k, Hq, Hkv, d,
+                                 dt, 1 if causal else 0, d ** -0.5 if scale is None else float(scale), o, _lse_out(lse, Hq, n_q),
+                                 _stream()), "prompt_attn_fwd")
+    return O, lse
+
+
+@dataclass
+class Pages:
+    """Device buffers of a paged cache of E4M3 codes with a scale per page and head (fastar_pages)."""
+    K8: torch.Tensor      # [n_pages, Hkv, P/16, d/16, 16 tokens, 16 coordinates] uint8
+    kscale: torch.Tensor  # [n_pages, Hkv] float32
+    V8: torch.Tensor      # [n_pages, Hkv, P/16, d/16, 16 coordinates, 16 tokens] uint8
+    vscale: torch.Tensor  # [n_pages, Hkv] float32
+
+    @classmethod
+    def empty(cls, n_pages: int, Hkv: int, P: int, d: int, device="cuda") -> "Pages":
+        code = lambda: torch.zeros((n_pages, Hkv, P // 16, d // 16, 16, 16), dtype=torch.uint8, device=device)
+        one = lambda: torch.ones((n_pages, Hkv), dtype=torch.float32, device=device)
+        return cls(code(), one(), code(), one())
+
+    @property
+    def shape(self):
+        """(n_pages, Hkv, P, d)"""
+        n, H, pb, db = self.K8.shape[:4]
+        return n, H, 16 * pb, 16 * db
+
+    def struct(self) -> _PagesStruct:
+        n, H, P, d = self.shape
+        if self.K8.shape[4:] != (16, 16) or self.V8.shape != self.K8.shape or self.kscale.shape != (n, H) or self.vscale.shape != (n, H):
+            raise ValueError("K8 and V8 must be [n_pages, Hkv, P/16, d/16, 16, 16], kscale and vscale [n_pages, Hkv]")
+        _dev(self.K8, torch.uint8), _dev(self.V8, torch.uint8), _dev(self.kscale, torch.float32), _dev(self.vscale, torch.float32)
+        return _PagesStruct(self.K8.data_ptr(), self.V8.data_ptr(), self.kscale.data_ptr(), self.vscale.data_ptr(), n, H, P, d)
+
+    def nbytes(self) -> int:
+        return sum(t.numel() * t.element_size() for t in (self.K8, self.V8, self.kscale, self.vscale))
+
+
+def kv_pages_plan(n_new, length, table, pool, pool_n, P: int, n_tok: int, out=None):
+    """Block tables and slot maps of the next step: n_new, length [B] int32, table [B,max_pages] and pool [n_pages] int32
+    (updated in place), pool_n [1] int32, n_tok rows for new tokens.  Returns (length after, pool_n after, cu [B+1],
+    slot [n_tok], status [B]), all int32; out may name `length` and `pool_n` themselves for the first two."""
+    B, max_pages = table.shape
+    if out is None:
+        i = lambda *n: torch.empty(n, dtype=torch.int32, device=table.device)
+        out = (i(B), i(1), i(B + 1), torch.full((n_tok,), -1, dtype=torch.int32, device=table.device), i(B))
+    after, free, cu, slot, status = out
+    _check(lib().kv_pages_plan(_ints(n_new, B), _ints(length, B), _ints(table, B, max_pages), B, max_pages, _ints(pool, pool.numel()),
+                               _ints(pool_n, 1), pool.numel(), P, n_tok, _ints(after, B), _ints(free, 1), _ints(cu, B + 1),
+                               _ints(slot, n_tok), _ints(status, B), _stream()), "kv_pages_plan")
+    return out
+
+
+def kv_pages_write(pages: Pages, slot, K_new, V_new) -> None:
+    """New keys and values [Hkv,n,d] (views of any head and row strides) into the pages' slots [n] int32 (kv_pages_plan)."""
+    ps = pages.struct()
+    n = slot.numel()
+    dt = _dtype_code(K_new)
+    k, v = _rows(K_new, ps.Hkv, n, ps.d, K_new.dtype), _rows(V_new, ps.Hkv, n, ps.d, K_new.dtype)
+    _check(lib().kv_pages_write(ps, k, v, dt, _ints(slot, n), n, _stream()), "kv_pages_write")
+
+
+def paged_attn_fwd(Q, cu_q, length, table, pages: Pages, causal: bool = True, scale: float | None = None, out=None,
+                   want_lse: bool = True, ws=None):
+    """Attention of packed queries Q [Hq,n,d] bf16 (a view of any head and row strides) over the pages of their sequences:
+    cu_q [B+1], length [B] and table [B,max_pages] int32.  Returns (O [Hq,n,d], lse [Hq,n] or None).
+    ws: workspace of workspace_bytes(OP_PAGED_ATTN, ...); calls that may be in flight at the same time need one each."""
+    ps = pages.struct()
+    Hq, n, d = _grouped(Q, ps.Hkv)
+    B, max_pages = table.shape
+    ws = _workspace(ws, workspace_bytes(OP_PAGED_ATTN, Hq, n, 0), Q.device)
+    if out is None:
+        out = (torch.empty_like(Q), torch.empty((Hq, n), dtype=torch.float32, device=Q.device) if want_lse else None)
+    O, lse = out
+    q, o = _rows(Q, Hq, n, ps.d, Q.dtype), _rows(O, Hq, n, ps.d, Q.dtype)
+    _check(lib().paged_attn_fwd(q, _ints(cu_q, B + 1), _ints(length, B), _ints(table, B, max_pages), B, max_pages, n, Hq, ps,
+                                _dtype_code(Q), 1 if causal else 0, d ** -0.5 if scale is None else float(scale), o,
+                                _lse_out(lse, Hq, n), ws.data_ptr(), ws.numel() * ws.element_size(), _stream()), "paged_attn_fwd")
     return O, lse
 
 

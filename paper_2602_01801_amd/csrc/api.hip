@@ -8,6 +8,7 @@ size_t select_cross_ws_bytes(int H, int n_q, int n_p, int BQ);
 size_t select_lsh_ws_bytes(int H, int n_q, int C, int n_bits, int BQ, int BK, int n_rep);
 size_t select_buckets_ws_bytes(int H, int n_q, int C, int n_p, int BQ, int BK);
 size_t attn_sk_ws_bytes();
+size_t paged_attn_ws_bytes();
 }  // namespace fastar
 
 namespace fastar {
@@ -104,6 +105,7 @@ extern "C" size_t fastar_workspace_bytes(int op, int H, int n_q, int n_k, int r,
         case FASTAR_OP_SELECT_LSH: return fastar::select_lsh_ws_bytes(H, n_q, n_k, r, BQ, BK, n_rep);
         case FASTAR_OP_SELECT_BUCKETS: return fastar::select_buckets_ws_bytes(H, n_q, n_k, r, BQ, BK);
         case FASTAR_OP_ATTN: return fastar::attn_sk_ws_bytes();
+        case FASTAR_OP_PAGED_ATTN: return fastar::paged_attn_ws_bytes();
         default: return 0;
     }
 }

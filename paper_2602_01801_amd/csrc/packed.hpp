@@ -1,0 +1,39 @@
+// What the calls over packed sequences share: argument checks on the host, and a sequence's rows on the device.
+#pragma once
+
+#include <cmath>
+
+#include "common.hpp"
+
+namespace fastar {
+
+// Views as the kernels take them: strides in bytes.
+struct View {
+    char *p;
+    int64_t head, row;
+};
+inline View view_of(const fastar_rows *r, int elt) { return View{(char *)r->p, r->head * elt, r->row * elt}; }
+
+inline bool view_ok(const fastar_rows *r, int elt) {
+    return r && r->p && !((uintptr_t)r->p & 15) && r->head >= 0 && r->row >= 0 && !((r->head * elt) & 15) && !((r->row * elt) & 15);
+}
+// Rows of an output lie apart: the smaller stride clears a row, the larger one all that the smaller one spans.
+inline bool rows_apart(const fastar_rows *r, int H, int64_t n, int d) {
+    if (H == 1 && n == 1) return true;
+    if (H == 1) return r->row >= d;
+    if (n == 1) return r->head >= d;
+    return (r->head >= d && r->row >= (H - 1) * r->head + d) || (r->row >= d && r->head >= (n - 1) * r->row + d);
+}
+inline bool scale_ok(float scale) { return scale > 0.0f && std::isfinite(scale * 1.4426950408889634f); }
+inline bool page_size_ok(int P) { return P == 16 || P == 32 || P == 64; }
+
+// Rows [first, first + n) of sequence b, inside [0, n_tok).
+struct Rows {
+    int first, n;
+};
+__device__ __forceinline__ Rows rows_of(const int32_t *__restrict__ cu, int b, int n_tok) {
+    const int a = min(max(cu[b], 0), n_tok), e = min(max(cu[b + 1], 0), n_tok);
+    return Rows{a, max(e - a, 0)};
+}
+
+}  // namespace fastar

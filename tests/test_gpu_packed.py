@@ -1,0 +1,533 @@
+"""Attention over packed prompts, and over a paged cache of 8-bit codes with its planning and writing, against plain loops in
+64 bits (packed_ref.py).
+
+Tolerances, from arithmetic.  A score is a sum of d products in fp32, exact for bf16 and E4M3 operands: its error is at most
+(d + 4) 2^-24 S, S = scale * sum |q||k| (the 4: scaling, and the exponent's argument); a weight's relative error is twice that
+(weight and sum), plus 2^-20 for the exponential and the sum's roundings per 16 steps, here `delta`.  bf16: weights are rounded
+to bf16 (2^-8 relative at most) for the product with the values, and the output is rounded to bf16 (2^-8 of it).  So
+|o - o_ref| <= 2^-8 |o_ref| + (2^-8 + delta + n 2^-24) * 1.02 * sum w|v|;  fp32: the same without the 2^-8, 2^-24 |o_ref| for
+the rounding.  lse: the largest score error, 2^-20 and 2^-22 of itself (logarithm, rounding).
+Codes, scales, tables and slots are exact.
+"""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+import packed_ref as ref
+import paper_2602_01801_amd as fa
+
+pytestmark = pytest.mark.gpu
+
+DT = {"bf16": torch.bfloat16, "f32": torch.float32}
+
+
+def f64(t):
+    return t.detach().to(torch.float64).cpu().numpy()
+
+
+def i32(x):
+    return torch.tensor(x, dtype=torch.int32, device="cuda")
+
+
+def prefix(n):
+    return np.concatenate([[0], np.cumsum(n)]).astype(np.int64)
+
+
+def check(O, lse, want, n, d, bf16, what=""):
+    Or, lr, A, S = want
+    o, l = f64(O), f64(lse)
+    delta = 2 * (d + 4) * 2.0 ** -24 * S[..., None] + 2.0 ** -20
+    unit = 2.0 ** -8 if bf16 else 2.0 ** -24
+    tol = unit * np.abs(Or) + ((2.0 ** -8 if bf16 else 0.0) + delta + n * 2.0 ** -24) * 1.02 * A + 1e-37
+    assert np.isfinite(o).all() == np.isfinite(Or).all(), what
+    bad = ~(np.abs(o - Or) <= tol) & ~(np.isnan(o) & np.isnan(Or))
+    assert not bad.any(), (what, np.argwhere(bad)[:4], o[bad][:4], Or[bad][:4], tol[bad][:4])
+    if l is not None:
+        with np.errstate(invalid="ignore"):
+            tl = (d + 4) * 2.0 ** -24 * S + 2.0 ** -20 + n * 2.0 ** -24 + 2.0 ** -22 * np.abs(lr)
+            ok = (np.abs(l - lr) <= tl) | (l == lr) | (np.isnan(l) & np.isnan(lr))
+        assert ok.all(), (what, np.argwhere(~ok)[:4], l[~ok][:4], lr[~ok][:4])
+
+
+def view(g, H, n, d, dtype, layout, mul=1.0):
+    """[H, n, d] view of random values: head-major, token-major, or part of a fused projection's output."""
+    x = torch.randn((n, H, d) if layout != "heads" else (H, n, d), generator=g) * mul
+    if layout == "heads":
+        return x.to(dtype).cuda()
+    if layout == "tokens":
+        return x.to(dtype).cuda().transpose(0, 1)
+    buf = torch.full((n, H + 3, d), math.nan, dtype=dtype)
+    buf[:, 1:H + 1] = x.to(dtype)
+    return buf.cuda()[:, 1:H + 1].transpose(0, 1)
+
+
+PROMPTS = [   # queries, keys (None: the same)
+    ([1], None), ([2, 0, 31, 33], None), ([64, 65], None), ([127, 1, 129], None), ([300, 77, 200], None), ([515], None),
+    ([5, 70, 3, 0], [9, 40, 0, 50]), ([257], [64]), ([130], [700]), ([1, 1, 1], [1, 129, 400]), ([0], [5]),
+]
+
+
+@pytest.mark.parametrize("q,k", PROMPTS, ids=lambda x: "-".join(map(str, x)) if x else "same")
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("dtype,d,Hq,Hkv,layout", [("bf16", 128, 4, 2, "tokens"), ("bf16", 64, 3, 1, "fused"), ("bf16", 128, 5, 5, "heads"),
+                                                   ("bf16", 64, 8, 8, "tokens"), ("f32", 128, 6, 2, "fused"), ("f32", 64, 2, 2, "heads")])
+def test_prompt_attention(q, k, causal, dtype, d, Hq, Hkv, layout):
+    g = torch.Generator().manual_seed(sum(q) * 31 + d + Hq)
+    kk = q if k is None else k
+    pad_q, pad_k = 3, 3 if k is None else 2   # rows in front of the first sequence and behind the last
+    nq, nk = sum(q) + 2 * pad_q, sum(kk) + 2 * pad_k
+    Q = view(g, Hq, nq, d, DT[dtype], layout, 1.5)
+    K = view(g, Hkv, nk, d, DT[dtype], layout)
+    V = view(g, Hkv, nk, d, DT[dtype], layout)
+    for t, n, p in ((K, nk, pad_k), (V, nk, pad_k), (Q, nq, pad_q)):   # rows of nobody
+        t[:, :p] = math.nan
+        t[:, n - p:] = math.inf
+    cq, ck = prefix(q) + pad_q, prefix(kk) + pad_k
+    O = view(g, Hq, nq, d, DT[dtype], layout)
+    O[:] = 7.0
+    lse = torch.full((Hq, nq), 7.0, device="cuda")
+    fa.prompt_attn_fwd(Q, K, V, i32(cq), None if k is None else i32(ck), causal=causal, out=(O, lse))
+    for b in range(len(q)):
+        i, j = slice(cq[b], cq[b + 1]), slice(ck[b], ck[b + 1])
+        want = ref.attend(f64(Q[:, i]), f64(K[:, j]), f64(V[:, j]), causal, d ** -0.5)
+        check(O[:, i], lse[:, i], want, kk[b], d, dtype == "bf16", f"sequence {b}")
+    for t in (O, lse):
+        assert (t[:, :cq[0]] == 7.0).all() and (t[:, cq[-1]:] == 7.0).all()
+
+
+@pytest.mark.parametrize("dtype,d,Hq,Hkv,n", [("bf16", 128, 3, 1, 2200), ("bf16", 64, 2, 1, 1777), ("f32", 128, 2, 1, 900), ("bf16", 128, 8, 1, 1025)])
+def test_prompt_attention_over_long_prompts(dtype, d, Hq, Hkv, n):
+    g = torch.Generator().manual_seed(n)
+    Q, K, V = (view(g, h, n, d, DT[dtype], "tokens", m) for h, m in ((Hq, 2.0), (Hkv, 1.0), (Hkv, 1.0)))
+    K[:, n // 3: n // 3 + 40] *= 4     # maxima that climb in the middle
+    O, lse = fa.prompt_attn_fwd(Q, K, V, i32([0, n]))
+    check(O, lse, ref.attend(f64(Q), f64(K), f64(V), True, d ** -0.5), n, d, dtype == "bf16")
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("causal", [True, False])
+def test_what_a_query_does_not_see_does_not_reach_it(dtype, causal):
+    """Keys and values of later tokens and of other sequences that are not finite."""
+    g = torch.Generator().manual_seed(9)
+    q = [150, 90, 70]
+    n, d = sum(q), 128
+    Q, K, V = (view(g, h, n, d, DT[dtype], "tokens") for h in (4, 2, 2))
+    cu = prefix(q)
+    bad = [cu[0] + 100, cu[2] + 69, cu[2] + 5]   # within a sequence; the last one's last and an early one
+    for x, t in zip((math.nan, math.inf, -math.inf), bad):
+        K[:, t], V[:, t] = x, x
+    O, lse = fa.prompt_attn_fwd(Q, K, V, i32(cu), causal=causal)
+    for b in range(3):
+        i = slice(cu[b], cu[b + 1])
+        with np.errstate(invalid="ignore", over="ignore"):
+            want = ref.attend(f64(Q[:, i]), f64(K[:, i]), f64(V[:, i]), causal, d ** -0.5)
+        a = q[b] if b == 1 else (100 if b == 0 else 5) if causal else 0   # queries that see nothing of it
+        check(O[:, i][:, :a], lse[:, i][:, :a], [w[:, :a] for w in want], q[b], d, dtype == "bf16", f"sequence {b}")
+        if a < q[b]:
+            assert not torch.isfinite(O[:, i][:, a:]).all(-1).any()
+
+
+def test_prompt_attention_with_shared_rows_and_extreme_scales():
+    g = torch.Generator().manual_seed(11)
+    n, d = 200, 128
+    Q, K = view(g, 4, n, d, torch.bfloat16, "tokens"), view(g, 1, n, d, torch.bfloat16, "tokens")
+    V = K[:, :1].expand(1, n, d)    # one value row for all keys: stride 0
+    for scale in (2.0 ** -140, 1e-20, 3.0, 40.0):
+        O, lse = fa.prompt_attn_fwd(Q, K, V, i32([0, n]), scale=scale)
+        want = ref.attend(f64(Q), f64(K), f64(V), True, float(np.float32(scale)))
+        check(O, lse, want, n, d, True, str(scale))
+
+
+# ------------------------------------------------------------------------------------------------ the paged cache
+
+
+def random_pages(rng, n_pages, Hkv, P, d, nan_from=None):
+    """Codes of every finite kind and scales of several powers of two, as numpy and on the device."""
+    K = rng.integers(0, 256, size=(n_pages, Hkv, P // 16, d // 16, 16, 16)).astype(np.uint8)
+    V = rng.integers(0, 256, size=K.shape).astype(np.uint8)
+    for c in (K, V):   # mostly values around one
+        c[...] = np.where(rng.random(c.shape) < 0.9, (c & 0x8F) | 0x30, c)
+        c[(c & 127) == 127] = 0x30
+    ks = 2.0 ** rng.integers(-2, 2, size=(n_pages, Hkv))
+    vs = 2.0 ** rng.integers(-6, 7, size=(n_pages, Hkv))
+    dev = fa.Pages(*(torch.from_numpy(x.astype(np.float32) if x.dtype == np.float64 else x).cuda() for x in (K, ks, V, vs)))
+    return K, ks, V, vs, dev
+
+
+def gather(code, scale, ids, n, tr):
+    """[Hkv, n, d] float64 of a sequence; zeros for pages that do not exist."""
+    n_pages = code.shape[0]
+    rows = ref.VALUES[ref.rows_of_cells(code, tr)] * scale[:, :, None, None]
+    out = np.stack([rows[p] if 0 <= p < n_pages else np.zeros_like(rows[0]) for p in ids], 1) if len(ids) else rows[:0].swapaxes(0, 1).reshape(code.shape[1], 0, 16, rows.shape[3])
+    return out.reshape(code.shape[1], -1, rows.shape[3])[:, :n]
+
+
+def paged_case(q, k, Hq, Hkv, P, d, causal, seed, bad=(), layout="tokens", poison=False):
+    rng = np.random.default_rng(seed)
+    per = [-(-x // P) for x in k]
+    n_pages = sum(per) + 2
+    K, ks, V, vs, dev = random_pages(rng, n_pages, Hkv, P, d)
+    order = rng.permutation(n_pages)
+    mp = max(max(per, default=1), 1) + 1
+    table = rng.integers(-5, n_pages + 5, size=(len(q), mp)).astype(np.int32)   # beyond the length: anything
+    at = 0
+    for b, n in enumerate(per):
+        table[b, :n] = order[at:at + n]
+        at += n
+    for b, j, x in bad:
+        table[b, j] = x
+    if poison:   # what lies behind a sequence on its last page is not a number
+        for b, n in enumerate(k):
+            if n % P:
+                p = table[b, n // P]
+                for code, tr in ((K, False), (V, True)):
+                    rows = ref.rows_of_cells(code[p:p + 1], tr).copy()
+                    rows[0, :, n % P:] = 0x7F
+                    code[p:p + 1] = ref.cells_of_rows(rows, tr)
+        dev = fa.Pages(*(torch.from_numpy(x.astype(np.float32) if x.dtype == np.float64 else x).cuda() for x in (K, ks, V, vs)))
+    g = torch.Generator().manual_seed(seed)
+    nq = sum(q) + 2
+    Q = view(g, Hq, nq, d, torch.bfloat16, layout)
+    cu = prefix(q) + 1
+    O = view(g, Hq, nq, d, torch.bfloat16, layout)
+    O[:] = 7.0
+    lse = torch.full((Hq, nq), 7.0, device="cuda")
+    ws = torch.full((fa.workspace_bytes(fa.OP_PAGED_ATTN, Hq, nq, 0),), 0xFF, dtype=torch.uint8, device="cuda")
+    fa.paged_attn_fwd(Q, i32(cu), i32(k), i32(table), dev, causal=causal, out=(O, lse), ws=ws)
+    for b in range(len(q)):
+        i = slice(cu[b], cu[b + 1])
+        ids = table[b, :per[b]]
+        live = np.repeat([0 <= p < n_pages for p in ids], P)[:k[b]] if len(ids) else np.zeros(0, bool)
+        want = ref.attend(f64(Q[:, i]), gather(K, ks, ids, k[b], False), gather(V, vs, ids, k[b], True), causal, d ** -0.5, live)
+        check(O[:, i], lse[:, i], want, k[b], d, True, f"sequence {b}")
+    for t in (O, lse):
+        assert (t[:, :cu[0]] == 7.0).all() and (t[:, cu[-1]:] == 7.0).all()
+
+
+TOKENS = [([1], [1]), ([1], [2]), ([1] * 4, [15, 16, 17, 64]), ([1] * 5, [63, 65, 0, 130, 1000]), ([1, 0, 1], [300, 40, 77]),
+          ([2, 1, 7], [2, 500, 129]), ([3], [1]), ([17, 1], [40, 333]), ([70, 1, 140], [70, 900, 517]), ([300], [1300])]
+
+
+@pytest.mark.parametrize("q,k", TOKENS, ids=lambda x: "-".join(map(str, x)))
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("Hq,Hkv,P,d", [(4, 4, 16, 128), (10, 2, 64, 128), (6, 2, 32, 64), (16, 1, 64, 64), (24, 1, 16, 128)])
+def test_paged_attention(q, k, causal, Hq, Hkv, P, d):
+    paged_case(q, k, Hq, Hkv, P, d, causal, seed=sum(q) + 3 * sum(k) + P + d, poison=True)
+
+
+@pytest.mark.parametrize("Hq,Hkv,P,d,q,k", [(2, 1, 64, 128, [1, 1], [20000, 3]), (5, 1, 16, 64, [1], [9001]), (2, 2, 32, 128, [4, 9], [7000, 4097]),
+                                            (40, 8, 64, 128, [1] * 9, [1, 700, 64, 65, 2000, 3, 1999, 128, 5]), (4, 1, 64, 128, [130], [5000])])
+def test_paged_attention_over_long_caches_in_pieces(Hq, Hkv, P, d, q, k):
+    paged_case(q, k, Hq, Hkv, P, d, True, seed=sum(k), layout="heads")
+
+
+@pytest.mark.parametrize("P", [16, 32, 64])
+def test_keys_on_pages_that_do_not_exist_are_left_out(P):
+    n = 5 * P + 3
+    paged_case([1, 3, 60], [n, n, n], 4, 2, P, 128, True, seed=P, bad=[(0, 1, -1), (0, 2, 2 ** 30), (1, 0, -2 ** 31), (1, 5, 10 ** 6), (2, 3, -7)])
+    paged_case([1, 40], [2 * P, 2 * P], 4, 2, P, 64, True, seed=P + 1, bad=[(b, j, -1) for b in (0, 1) for j in (0, 1)])
+
+
+def test_paged_attention_of_codes_that_are_no_numbers_among_later_tokens():
+    """Causal chunk: tokens 20 and on of the chunk hold NaN; the queries before do not see them."""
+    rng = np.random.default_rng(4)
+    P, d, a, n = 32, 128, 50, 100
+    K, ks, V, vs, _ = random_pages(rng, 4, 1, P, d)
+    table = np.array([[2, 0, 3, 1]], np.int32)
+    first = n - a + 20
+    for code, tr in ((K, False), (V, True)):
+        rows = ref.rows_of_cells(code, tr).copy()
+        for j in range(first, n):
+            rows[table[0, j // P], :, j % P] = 0x7F
+        code[...] = ref.cells_of_rows(rows, tr)
+    dev = fa.Pages(*(torch.from_numpy(x.astype(np.float32) if x.dtype == np.float64 else x).cuda() for x in (K, ks, V, vs)))
+    Q = view(torch.Generator().manual_seed(1), 2, a, d, torch.bfloat16, "tokens")
+    O, lse = fa.paged_attn_fwd(Q, i32([0, a]), i32([n]), i32(table), dev)
+    want = ref.attend(f64(Q), gather(K, ks, table[0], n, False), gather(V, vs, table[0], n, True), True, d ** -0.5)
+    check(O[:, :20], lse[:, :20], [w[:, :20] for w in want], n, d, True)
+    assert torch.isnan(O[:, 20:]).all()
+
+
+def test_lengths_beyond_the_table_are_cut():
+    rng = np.random.default_rng(6)
+    K, ks, V, vs, dev = random_pages(rng, 3, 2, 16, 64)
+    Q = view(torch.Generator().manual_seed(2), 2, 2, 64, torch.bfloat16, "heads")
+    O, lse = fa.paged_attn_fwd(Q, i32([0, 1, 2]), i32([2 ** 31 - 1, -5]), i32([[1, 2], [0, 0]]), dev)
+    want = ref.attend(f64(Q[:, :1]), gather(K, ks, [1, 2], 32, False), gather(V, vs, [1, 2], 32, True), True, 64 ** -0.5)
+    check(O[:, :1], lse[:, :1], want, 32, 64, True)
+    assert (O[:, 1] == 0).all() and torch.isneginf(lse[:, 1]).all()
+
+
+# ------------------------------------------------------------------------------------------------ planning
+
+
+def run_plan(n_new, length, table, pool, free, P, n_tok, in_place):
+    t, p = i32(table).reshape(len(n_new), -1) if n_new else torch.zeros((0, 3), dtype=torch.int32, device="cuda"), i32(pool)
+    L, F = i32(length), i32([free])
+    slot = torch.full((n_tok,), -9, dtype=torch.int32, device="cuda")
+    z = lambda n: torch.full((n,), -9, dtype=torch.int32, device="cuda")
+    out = (L if in_place else z(len(n_new)), F if in_place else z(1), z(len(n_new) + 1), slot, z(len(n_new)))
+    fa.kv_pages_plan(i32(n_new), L, t, p, F, P, n_tok, out=out)
+    want_t, want_p = [list(r) for r in table], list(pool)
+    after, top, cu, slots, status = ref.plan(n_new, length, want_t, want_p, free, P, n_tok)
+    assert out[0].tolist() == after and out[1].tolist() == [top] and out[2].tolist() == cu and out[4].tolist() == status
+    assert t.tolist() == want_t and p.tolist() == want_p
+    got = slot.tolist()
+    assert got == [slots.get(i, -9) for i in range(n_tok)]
+
+
+@pytest.mark.parametrize("B", [0, 1, 2, 64, 65, 1000, 1025, 2500])
+@pytest.mark.parametrize("P", [16, 32, 64])
+def test_plan(B, P):
+    rng = np.random.default_rng(B + P)
+    mp = 9
+    length = [int(x) for x in rng.integers(0, 6 * P, size=B)]
+    n_new = [int(x) for x in rng.choice([-1, 0, 1, 2, P, 3 * P + 1, 20 * P], size=B, p=[0.1, 0.1, 0.5, 0.1, 0.1, 0.07, 0.03])]
+    held = [-(-x // P) for x in length]
+    n_pages = sum(held) + max(3, B // 3)
+    order = [int(x) for x in rng.permutation(n_pages)]
+    table, at = [[-3] * mp for _ in range(B)], 0
+    for b in range(B):
+        table[b][:held[b]] = order[at:at + held[b]]
+        at += held[b]
+    pool = order[at:] + [-1] * at
+    total = sum(max(x, 0) for x in n_new)
+    for n_tok in (total, total + 7, max(total * 2 // 3, 1), 5000 + total):
+        run_plan(n_new, length, table, pool, n_pages - at, P, n_tok, in_place=bool(n_tok & 1))
+
+
+def test_plan_of_lengths_and_pools_that_make_no_sense():
+    """Counts are cut to what the arrays hold; pages that do not exist give no slot."""
+    run_plan([5, 2 ** 31 - 1, -7, 3], [-10, 5, 2 ** 31 - 1, 10], [[0, 1], [1, 2], [50, -4], [2 ** 30, 3]], [3, 1, 2, 0, 9, 9], 99, 16, 40, False)
+    run_plan([4, 4], [0, 20], [[7, 7], [0, 1]], [5, 6, 7], -2, 16, 8, True)
+    run_plan([1, 1], [15, 16], [[3, 3], [4, 4]], [-1, 77], 2, 16, 2, True)
+
+
+# ------------------------------------------------------------------------------------------------ writing
+
+
+def run_write(rng, runs, Hkv, P, d, dtype, layout, mag, spoil=None):
+    """runs: (page, offset, rows) in the order of the array; None: a row without a slot."""
+    n_pages = 1 + max(r[0] for r in runs if r)
+    K, ks, V, vs, dev = random_pages(rng, n_pages, Hkv, P, d)
+    slot = []
+    for r in runs:
+        slot += [rng.choice([-1, -2 ** 31, n_pages * P, 2 ** 31 - 1])] if r is None else [r[0] * P + r[1] + i for i in range(r[2])]
+    n = len(slot)
+    g = torch.Generator().manual_seed(int(rng.integers(1 << 30)))
+    Kn, Vn = view(g, Hkv, n, d, DT[dtype], layout), view(g, Hkv, n, d, DT[dtype], layout)
+    m = torch.from_numpy(2.0 ** rng.integers(-mag, mag + 1, size=(n,))).to(DT[dtype]).cuda()
+    Kn *= m[None, :, None]
+    Vn *= m.flip(0)[None, :, None]
+    if spoil:
+        spoil(Kn, Vn)
+    for x, code, scale, tr in ((Kn, K, ks, False), (Vn, V, vs, True)):
+        ref.write(code, scale, tr, f64(x), [int(s) for s in slot], P)
+    fa.kv_pages_write(dev, i32([int(s) for s in slot]), Kn, Vn)
+    for got, want in ((dev.K8, K), (dev.V8, V)):
+        a, b = got.cpu().numpy(), want
+        nan = (a & 127) == 127
+        off = np.argwhere(np.where(nan, (b & 127) != 127, a != b))
+        assert len(off) == 0, (len(off), off[:4], [(a[tuple(i)], b[tuple(i)]) for i in off[:4]])
+    for got, want in ((dev.kscale, ks), (dev.vscale, vs)):
+        assert np.array_equal(got.cpu().numpy().astype(np.float64), want)
+
+
+@pytest.mark.parametrize("dtype,d,Hkv,layout", [("bf16", 128, 2, "tokens"), ("bf16", 64, 3, "fused"), ("f32", 128, 1, "heads"), ("f32", 64, 5, "tokens")])
+@pytest.mark.parametrize("P", [16, 32, 64])
+@pytest.mark.parametrize("mag", [0, 12, 40])
+def test_write(P, dtype, d, Hkv, layout, mag):
+    rng = np.random.default_rng(P + d + Hkv + mag)
+    run_write(rng, [(0, 0, 1)], Hkv, P, d, dtype, layout, mag)
+    run_write(rng, [(2, 0, P), (0, 0, P), (1, 0, P - 1)], Hkv, P, d, dtype, layout, mag)
+    run_write(rng, [(3, P - 1, 1), (1, 5, 7), None, (0, 1, P - 1), (2, 0, 3), None, None, (5, P - 3, 3), (4, 9, 1)], Hkv, P, d, dtype, layout, mag)
+    run_write(rng, [(p, int(rng.integers(0, P)), 1) for p in rng.permutation(70)], Hkv, P, d, dtype, layout, mag)
+    # pages whose numbers follow one another are runs of their own
+    run_write(rng, [(0, 3, P - 3), (1, 0, P), (2, 0, 5)], Hkv, P, d, dtype, layout, mag)
+
+
+def test_write_of_values_at_the_ends_of_the_range():
+    rng = np.random.default_rng(8)
+
+    def spoil(K, V):
+        K[:, 0], V[:, 1] = 0.0, 0.0
+        K[:, 2, :3], V[:, 2, 4] = torch.tensor([math.inf, -math.inf, math.nan]).to(K), math.nan
+        K[:, 3], V[:, 3] = 3.38e38, -3.38e38
+        K[:, 4], V[:, 4] = 1e-39, 2.0 ** -110
+        V[:, 5] = math.inf
+        K[:, 6, 0], K[:, 6, 1:] = 448.0, 2.0 ** -10      # a tie with zero, and just above
+        K[:, 7, 0], K[:, 7, 1:] = 448.0, 1.5 * 2.0 ** -10
+        K[:, 8, 0], K[:, 8, 1:], V[:, 8] = 464.0, 232.0, 449.0
+    for dtype in ("bf16", "f32"):
+        run_write(rng, [(p, 0, 1) for p in range(9)], 2, 16, 64, dtype, "tokens", 0, spoil)
+        run_write(rng, [(p, 7, 1) for p in range(9)], 2, 16, 128, dtype, "tokens", 0, spoil)
+        run_write(rng, [(0, 0, 9)], 2, 16, 64, dtype, "tokens", 0, spoil)
+
+
+# ------------------------------------------------------------------------------------------------ together
+
+
+def serve(steps, graph=False):
+    """Requests come, grow by chunks and single tokens, and end; the attention over the pages against the one over the values that
+    the codes stand for, and prompts in one piece against both."""
+    rng = np.random.default_rng(77)
+    Hq, Hkv, d, P, B, mp = 6, 2, 128, 16, 5, 40
+    n_pages = 60
+    pages = fa.Pages.empty(n_pages, Hkv, P, d)
+    table = torch.full((B, mp), -1, dtype=torch.int32, device="cuda")
+    pool = torch.from_numpy(rng.permutation(n_pages).astype(np.int32)).cuda()
+    length, pool_n = i32([0] * B), i32([n_pages])
+    hold = [([], []) for _ in range(B)]     # what was written, per request
+    refused = 0
+    for step in range(steps):
+        n_new = [int(rng.choice([33, 100, 257])) if not hold[b][0] else int(rng.choice([1, 1, 1, 1, 9, -1])) for b in range(B)]
+        n_tok = sum(max(x, 0) for x in n_new)
+        before = length.tolist()
+        _, _, cu, slot, status = fa.kv_pages_plan(i32(n_new), length, table, pool, pool_n, P, n_tok,
+                                                  out=(length, pool_n, i32([0] * (B + 1)), i32([0] * n_tok), i32([0] * B)))
+        g = torch.Generator().manual_seed(step)
+        qkv = (torch.randn((n_tok, Hq + 2 * Hkv, d), generator=g) * 1.2).bfloat16().cuda()
+        Q, K, V = (x.transpose(0, 1) for x in qkv.split([Hq, Hkv, Hkv], 1))
+        fa.kv_pages_write(pages, slot, K, V)
+        O, lse = fa.paged_attn_fwd(Q, cu, length, table, pages)
+        c, st = cu.tolist(), status.tolist()
+        codes = [x.cpu().numpy() for x in (pages.K8, pages.kscale, pages.V8, pages.vscale)]
+        for b in range(B):
+            if n_new[b] < 0:
+                hold[b] = ([], [])
+                assert length[b] == 0
+                continue
+            if st[b]:
+                refused += 1
+                assert length[b] == before[b]
+                continue
+            i = slice(c[b], c[b + 1])
+            hold[b][0].append(f64(K[:, i]))
+            hold[b][1].append(f64(V[:, i]))
+            n = int(length[b])
+            kb, vb = np.concatenate(hold[b][0], 1), np.concatenate(hold[b][1], 1)
+            assert n == kb.shape[1] == before[b] + n_new[b]
+            ids = table[b, : -(-n // P)].tolist()
+            k8, v8 = gather(codes[0], codes[1].astype(np.float64), ids, n, False), gather(codes[2], codes[3].astype(np.float64), ids, n, True)
+            # a code is off by 2^-4 of the value, or half the least step (2^-10) of the page's scale, twice if it was carried over
+            for x8, x, s in ((k8, kb, codes[1]), (v8, vb, codes[3])):
+                assert (np.abs(x8 - x) <= 2.0 ** -4 * np.abs(x) + 2.0 ** -9 * s.max()).all()
+            check(O[:, i], lse[:, i], ref.attend(f64(Q[:, i]), k8, v8, True, d ** -0.5), n, d, True, f"step {step} request {b}")
+            if before[b] == 0:
+                Op, lp = fa.prompt_attn_fwd(Q[:, i], K[:, i], V[:, i], i32([0, n]))
+                check(Op, lp, ref.attend(f64(Q[:, i]), kb, vb, True, d ** -0.5), n, d, True, f"prompt, step {step} request {b}")
+    assert refused > 0
+
+
+def test_requests_are_served():
+    serve(14)
+
+
+@pytest.mark.parametrize("Hq,Hkv,k", [(4, 2, [40, 3, 17]), (2, 1, [5000, 64, 900])])
+def test_a_step_is_captured_and_replayed(Hq, Hkv, k):
+    """Plan, write and attend in one graph; replays with eager work between them, each against the same calls made eagerly."""
+    rng = np.random.default_rng(12)
+    P, d, B = 16, 128, 3
+    per = [-(-(x + 8) // P) + 1 for x in k]
+    n_pages, mp = sum(per) + 4, max(per) + 2
+    _, _, _, _, pages = random_pages(rng, n_pages, Hkv, P, d)
+    order, table, at = rng.permutation(n_pages).astype(np.int32), np.full((B, mp), -1, np.int32), 0
+    for b in range(B):
+        n = -(-k[b] // P)
+        table[b, :n] = order[at:at + n]
+        at += n
+    state = dict(table=i32(table), pool=i32(np.concatenate([order[at:], order[:at]])), length=i32(k), pool_n=i32([n_pages - at]),
+                 n_new=i32([1] * B), pages=pages)
+    Q, K, V = (view(torch.Generator().manual_seed(i), h, B, d, torch.bfloat16, "tokens") for i, h in enumerate((Hq, Hkv, Hkv)))
+    ws = torch.empty(fa.workspace_bytes(fa.OP_PAGED_ATTN, Hq, B, 0), dtype=torch.uint8, device="cuda")
+    O, lse = torch.empty_like(Q), torch.empty((Hq, B), device="cuda")
+    plan_out = (state["length"], state["pool_n"], i32([0] * (B + 1)), i32([0] * B), i32([0] * B))
+
+    def step(s, O, lse, out, ws):
+        fa.kv_pages_plan(s["n_new"], s["length"], s["table"], s["pool"], s["pool_n"], P, B, out=out)
+        fa.kv_pages_write(s["pages"], out[3], K, V)
+        fa.paged_attn_fwd(Q, out[2], s["length"], s["table"], s["pages"], out=(O, lse), ws=ws)
+        fa.prompt_attn_fwd(Q, K, V, out[2], out=(O2, lse2))
+
+    O2, lse2 = torch.empty_like(Q), torch.empty_like(lse)
+    clone = lambda s: {a: fa.Pages(*(x.clone() for x in (v.K8, v.kscale, v.V8, v.vscale))) if a == "pages" else v.clone() for a, v in s.items()}
+    eager = clone(state)
+    fa.init()
+    graph = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph):
+        step(state, O, lse, plan_out, ws)
+    torch.cuda.synchronize()
+    assert state["length"].tolist() == k   # captured, not run
+    for i in range(5):
+        for x in (Q, K, V):
+            x.copy_(torch.randn(x.shape, generator=torch.Generator().manual_seed(100 + i)).bfloat16())
+        graph.replay()
+        got = [x.clone() for x in (O, lse, O2, lse2, state["length"], state["pages"].K8, state["pages"].V8, state["table"])]
+        O_e, lse_e = torch.empty_like(O), torch.empty_like(lse)
+        step(eager, O_e, lse_e, (eager["length"], eager["pool_n"], i32([0] * (B + 1)), i32([0] * B), i32([0] * B)), torch.empty_like(ws))
+        torch.cuda.synchronize()
+        for a, b in zip(got, (O_e, lse_e, O2, lse2, eager["length"], eager["pages"].K8, eager["pages"].V8, eager["table"])):
+            assert torch.equal(a, b)
+
+
+def test_calls_on_other_streams_with_a_workspace_each():
+    rng = np.random.default_rng(3)
+    _, _, _, _, dev = random_pages(rng, 300, 2, 64, 128)
+    table = i32(rng.permutation(300).reshape(2, 150))
+    Q = view(torch.Generator().manual_seed(1), 4, 2, 128, torch.bfloat16, "tokens")
+    args = (i32([0, 1, 2]), i32([9600, 7000]), table, dev)
+    want = fa.paged_attn_fwd(Q, *args)
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    got = []
+    for s in streams:
+        with torch.cuda.stream(s):
+            for _ in range(5):
+                got.append(fa.paged_attn_fwd(Q, *args, ws=torch.empty(fa.workspace_bytes(fa.OP_PAGED_ATTN, 4, 2, 0), dtype=torch.uint8, device="cuda")))
+    torch.cuda.synchronize()
+    for O, lse in got:
+        assert torch.equal(O, want[0]) and torch.equal(lse, want[1])
+
+
+def test_the_binding_refuses_what_does_not_fit():
+    Q = torch.zeros((4, 8, 128), dtype=torch.bfloat16, device="cuda")
+    K = torch.zeros((2, 8, 128), dtype=torch.bfloat16, device="cuda")
+    cu = i32([0, 8])
+    with pytest.raises(ValueError):
+        fa.prompt_attn_fwd(Q[:3], K, K, cu)
+    with pytest.raises(ValueError):
+        fa.prompt_attn_fwd(Q, K, K[:, :7], cu)
+    with pytest.raises(ValueError):
+        fa.prompt_attn_fwd(Q, K.transpose(1, 2).contiguous().transpose(1, 2), K, cu)
+    with pytest.raises(TypeError):
+        fa.prompt_attn_fwd(Q, K.float(), K, cu)
+    with pytest.raises(TypeError):
+        fa.prompt_attn_fwd(Q.half(), K.half(), K.half(), cu)
+    with pytest.raises(TypeError):
+        fa.prompt_attn_fwd(Q, K, K, cu.long())
+    with pytest.raises(ValueError):
+        fa.prompt_attn_fwd(Q, K, K, cu, i32([0, 4, 8]))
+    with pytest.raises(ValueError):
+        fa.prompt_attn_fwd(Q, K, K, cu, out=(Q[:, :4], None))
+    with pytest.raises(fa.FastarError):
+        fa.prompt_attn_fwd(Q, K, K, cu, scale=0.0)
+    with pytest.raises(fa.FastarError):
+        fa.prompt_attn_fwd(Q[..., :96], K[..., :96], K[..., :96], cu)
+    pages = fa.Pages.empty(4, 2, 16, 128)
+    with pytest.raises(ValueError):
+        fa.paged_attn_fwd(Q[:3], cu, i32([8]), i32([[0]]), pages)
+    with pytest.raises(ValueError):
+        fa.paged_attn_fwd(Q, cu, i32([8, 8]), i32([[0]]), pages)
+    with pytest.raises(fa.FastarError):
+        fa.paged_attn_fwd(Q.float(), cu, i32([8]), i32([[0]]), pages)
+    with pytest.raises(fa.FastarError):
+        fa.paged_attn_fwd(Q, cu, i32([8]), i32([[0]]), pages, ws=torch.empty(64, dtype=torch.uint8, device="cuda"))
+    with pytest.raises(ValueError):
+        fa.kv_pages_write(pages, i32([0] * 7), K, K)
+    with pytest.raises(ValueError):
+        fa.kv_pages_write(fa.Pages(pages.K8, pages.kscale[:2], pages.V8, pages.vscale), i32([0] * 8), K, K)
+    with pytest.raises(ValueError):
+        fa.kv_pages_plan(i32([1]), i32([0, 0]), i32([[0]]), i32([0]), i32([1]), 16, 1)
