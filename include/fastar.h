@@ -453,7 +453,8 @@ typedef struct {
  *   Q [Hq,n_tok_q,d], K, V [Hkv,n_tok_k,d], O [Hq,n_tok_q,d] views of dtype;  lse [Hq,n_tok_q] float (dense) or NULL
  *   cu_q [B+1] rows of Q and O;  cu_k [B+1] rows of K and V, or NULL: cu_q
  *   causal  0: every query sees all keys of its sequence;  1: as above
- * bf16: bf16 products (the weights are rounded to bf16), fp32 softmax and sums; fp32: plain fp32 arithmetic.
+ * bf16: bf16 products (the weights are rounded to bf16; those below 2^-126 of a row's largest are zero), fp32 softmax and
+ * sums; fp32: plain fp32 arithmetic.
  * Supported: d in {64, 128}; scale positive, scale * log2(e) finite.  No workspace.  n_tok_q = 0 or B = 0 launches nothing.
  */
 int prompt_attn_fwd(const fastar_rows *Q, const fastar_rows *K, const fastar_rows *V, const int32_t *cu_q,

@@ -109,8 +109,6 @@ __global__ __launch_bounds__(256) void attn_simple_kernel(View Q, View K, View V
 
 }  // namespace packed
 
-size_t paged_attn_ws_bytes() { return 256; }
-
 }  // namespace fastar
 
 extern "C" int prompt_attn_fwd(const fastar_rows *Q, const fastar_rows *K, const fastar_rows *V, const int32_t *cu_q,
@@ -141,35 +139,6 @@ extern "C" int prompt_attn_fwd(const fastar_rows *Q, const fastar_rows *K, const
         else FASTAR_SIMPLE(false, 64);
     }
 #undef FASTAR_SIMPLE
-    FASTAR_LAUNCH_CHECK();
-    return FASTAR_OK;
-}
-
-extern "C" int paged_attn_fwd(const fastar_rows *Q, const int32_t *cu_q, const int32_t *len, const int32_t *table, int B,
-                              int max_pages, int n_tok, int Hq, const fastar_pages *pages, int dtype, int causal, float scale,
-                              const fastar_rows *O, float *lse, void *ws, size_t ws_bytes, void *stream) {
-    using namespace fastar;
-    if (dtype != FASTAR_F32 && dtype != FASTAR_BF16) return FASTAR_ERR_INVALID_ARG;
-    if (B < 0 || n_tok < 0 || max_pages <= 0 || Hq <= 0) return FASTAR_ERR_INVALID_ARG;
-    if (!scale_ok(scale) || (causal & ~1)) return FASTAR_ERR_INVALID_ARG;
-    if (const int rc = pages_check(pages); rc != FASTAR_OK) return rc;
-    if (Hq % pages->Hkv) return FASTAR_ERR_INVALID_ARG;
-    if (dtype != FASTAR_BF16 || (int64_t)max_pages * pages->P > INT32_MAX) return FASTAR_ERR_UNSUPPORTED;
-    if (!ws || ((uintptr_t)ws & 255)) return FASTAR_ERR_INVALID_ARG;
-    if (ws_bytes < paged_attn_ws_bytes()) return FASTAR_ERR_WORKSPACE;
-    if (n_tok == 0 || B == 0) return FASTAR_OK;
-    if (!cu_q || !len || !table || !view_ok(Q, 2) || !view_ok(O, 2) || !rows_apart(O, Hq, n_tok, pages->d)) return FASTAR_ERR_INVALID_ARG;
-    const View none{nullptr, 0, 0};
-    const View q = view_of(Q, 2), o = view_of(O, 2);
-    const dim3 grid((unsigned)(((int64_t)n_tok * Hq + 3) / 4));
-    const float sl = scale * 1.4426950408889634f;
-    const int pshift = __builtin_ctz((unsigned)pages->P);
-    if (pages->d == 128)
-        hipLaunchKernelGGL((packed::attn_simple_kernel<true, 128, true>), grid, dim3(256), 0, (hipStream_t)stream, q, none, none, cu_q,
-                           nullptr, len, table, max_pages, *pages, pshift, B, n_tok, 0, Hq, pages->Hkv, causal, sl, o, lse);
-    else
-        hipLaunchKernelGGL((packed::attn_simple_kernel<true, 64, true>), grid, dim3(256), 0, (hipStream_t)stream, q, none, none, cu_q,
-                           nullptr, len, table, max_pages, *pages, pshift, B, n_tok, 0, Hq, pages->Hkv, causal, sl, o, lse);
     FASTAR_LAUNCH_CHECK();
     return FASTAR_OK;
 }

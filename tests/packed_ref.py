@@ -52,7 +52,7 @@ def cells_of_rows(x, transposed):
 
 
 def attend(Q, K, V, causal, scale, live=None):
-    """One sequence.  Q [Hq,a,d], K, V [Hkv,n,d] float64; live [n] keys that exist (None: all).  Returns (O, lse, A, S):
+    """One sequence.  Q [Hq,a,d], K, V [Hkv,n,d] float64; live [n] keys that exist (None: all).  Returns (O, lse, A, S, max|v|):
     A = sum of weights times |v| per output, S = the largest sum |q||k| * scale of a query, for tolerances."""
     Hq, a, d = Q.shape
     Hkv, n, _ = K.shape
@@ -72,7 +72,8 @@ def attend(Q, K, V, causal, scale, live=None):
             O[h, i], A[h, i] = w @ v[see] / z, w @ np.abs(v[see]) / z
             lse[h, i] = m + math.log(z)
             S[h, i] = (np.abs(k[see]) @ np.abs(Q[h, i])).max() * scale
-    return O, lse, A, S
+    fin = np.abs(V[np.isfinite(V)])
+    return O, lse, A, S, fin.max() if fin.size else 0.0
 
 
 def plan(n_new, length, table, pool, pool_n, P, n_tok):

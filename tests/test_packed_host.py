@@ -156,12 +156,12 @@ def test_plan_reference_hands_every_page_to_one_request():
 def test_attend_leaves_out_what_a_query_does_not_see():
     rng = np.random.default_rng(5)
     Q, K, V = rng.normal(size=(2, 5, 8)), rng.normal(size=(1, 3, 8)), rng.normal(size=(1, 3, 8))
-    O, lse, _, _ = ref.attend(Q, K, V, True, 0.5)
+    O, lse = ref.attend(Q, K, V, True, 0.5)[:2]
     assert (O[:, :2] == 0).all() and np.isneginf(lse[:, :2]).all()
     assert np.allclose(O[:, 2], V[0, 0])
     K2, V2 = K.copy(), V.copy()
     K2[:, 2], V2[:, 2] = math.nan, math.inf
-    O2, lse2, _, _ = ref.attend(Q, K2, V2, True, 0.5)
+    O2, lse2 = ref.attend(Q, K2, V2, True, 0.5)[:2]
     assert np.array_equal(O2[:, :4], O[:, :4]) and np.array_equal(lse2[:, :4], lse[:, :4])
     O3 = ref.attend(Q, K, V, False, 0.5, live=np.array([True, False, True]))[0]
     assert np.allclose(O3, ref.attend(Q, K[:, ::2], V[:, ::2], False, 0.5)[0])
