@@ -455,7 +455,8 @@ typedef struct {
  *   causal  0: every query sees all keys of its sequence;  1: as above
  * bf16: bf16 products (the weights are rounded to bf16; those below 2^-126 of a row's largest are zero), fp32 softmax and
  * sums; fp32: plain fp32 arithmetic.
- * Supported: d in {64, 128}; scale positive, scale * log2(e) finite.  No workspace.  n_tok_q = 0 or B = 0 launches nothing.
+ * Supported: d in {64, 128}; scale positive, scale * log2(e) finite; rows of K and V at most 2^24 bytes apart;
+ * n_tok_q * Hq < 2^30.  No workspace.  n_tok_q = 0 or B = 0 launches nothing.
  */
 int prompt_attn_fwd(const fastar_rows *Q, const fastar_rows *K, const fastar_rows *V, const int32_t *cu_q,
                     const int32_t *cu_k, int B, int n_tok_q, int n_tok_k, int Hq, int Hkv, int d, int dtype, int causal,
@@ -523,7 +524,8 @@ int kv_pages_write(const fastar_pages *pages, const fastar_rows *K_new, const fa
  * the device reads: long ones are cut into pieces whose fragments lie in ws, and a second launch puts them together.
  *   ws / ws_bytes  fastar_workspace_bytes(FASTAR_OP_PAGED_ATTN, ...) bytes, 256-byte aligned; contents need not be kept.
  *                  Calls that may be in flight at the same time need a workspace each.
- * Supported: bf16, d in {64, 128}, scales of the pages 2^-100 .. 2^120; scale as for prompt_attn_fwd.
+ * Supported: bf16, d in {64, 128}, scales of the pages 2^-100 .. 2^120; scale and n_tok * Hq as for
+ * prompt_attn_fwd.
  */
 int paged_attn_fwd(const fastar_rows *Q, const int32_t *cu_q, const int32_t *len, const int32_t *table, int B, int max_pages,
                    int n_tok, int Hq, const fastar_pages *pages, int dtype, int causal, float scale, const fastar_rows *O,

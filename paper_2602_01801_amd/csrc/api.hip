@@ -80,6 +80,7 @@ extern "C" int fastar_init(void) {
     if (rc == FASTAR_OK) rc = fastar::select_setup();
     if (rc == FASTAR_OK) rc = fastar::tempcache_setup();
     if (rc == FASTAR_OK) rc = fastar::attn_fp8_setup();
+    if (rc == FASTAR_OK) rc = fastar::prompt_setup();
     return rc;
 }
 

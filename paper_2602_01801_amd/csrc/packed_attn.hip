@@ -4,7 +4,8 @@
 
 namespace fastar {
 
-int pages_check(const fastar_pages *pg);
+int launch_prompt_bf16(const View &Q, const View &K, const View &V, const int32_t *cu_q, const int32_t *cu_k, int B, int n_tok_q,
+                       int n_tok_k, int Hq, int Hkv, int d, int causal, float scale_log2, const View &O, float *lse, hipStream_t s);
 
 namespace packed {
 
@@ -120,9 +121,11 @@ extern "C" int prompt_attn_fwd(const fastar_rows *Q, const fastar_rows *K, const
     if (B < 0 || n_tok_q < 0 || n_tok_k < 0 || Hq <= 0 || Hkv <= 0 || Hq % Hkv) return FASTAR_ERR_INVALID_ARG;
     if (!scale_ok(scale) || (causal & ~1)) return FASTAR_ERR_INVALID_ARG;
     if (d != 64 && d != 128) return FASTAR_ERR_UNSUPPORTED;
+    if ((int64_t)n_tok_q * Hq > INT32_MAX / 2) return FASTAR_ERR_UNSUPPORTED;
     if (n_tok_q == 0 || B == 0) return FASTAR_OK;
     if (!cu_q || !view_ok(Q, elt) || !view_ok(O, elt) || !rows_apart(O, Hq, n_tok_q, d)) return FASTAR_ERR_INVALID_ARG;
     if (n_tok_k > 0 && (!view_ok(K, elt) || !view_ok(V, elt))) return FASTAR_ERR_INVALID_ARG;
+    if (n_tok_k > 0 && (K->row * elt > MAX_PITCH || V->row * elt > MAX_PITCH)) return FASTAR_ERR_UNSUPPORTED;
     if (!cu_k) cu_k = cu_q;
     const View none{nullptr, 0, 0};
     const View q = view_of(Q, elt), k = n_tok_k ? view_of(K, elt) : none, v = n_tok_k ? view_of(V, elt) : none, o = view_of(O, elt);
@@ -131,13 +134,10 @@ extern "C" int prompt_attn_fwd(const fastar_rows *Q, const fastar_rows *K, const
 #define FASTAR_SIMPLE(BF16, D)                                                                                                    \
     hipLaunchKernelGGL((packed::attn_simple_kernel<BF16, D, false>), grid, dim3(256), 0, (hipStream_t)stream, q, k, v, cu_q, cu_k, \
                        nullptr, nullptr, 0, fastar_pages{}, 0, B, n_tok_q, n_tok_k, Hq, Hkv, causal, sl, o, lse)
-    if (dtype == FASTAR_BF16) {
-        if (d == 128) FASTAR_SIMPLE(true, 128);
-        else FASTAR_SIMPLE(true, 64);
-    } else {
-        if (d == 128) FASTAR_SIMPLE(false, 128);
-        else FASTAR_SIMPLE(false, 64);
-    }
+    if (dtype == FASTAR_BF16)
+        return launch_prompt_bf16(q, k, v, cu_q, cu_k, B, n_tok_q, n_tok_k, Hq, Hkv, d, causal, sl, o, lse, (hipStream_t)stream);
+    if (d == 128) FASTAR_SIMPLE(false, 128);
+    else FASTAR_SIMPLE(false, 64);
 #undef FASTAR_SIMPLE
     FASTAR_LAUNCH_CHECK();
     return FASTAR_OK;

@@ -1,0 +1,442 @@
+// Attention over packed prompts, bf16 (prompt_attn_fwd).
+//
+// A workgroup owns 256 rows of one sequence and key head, a row being a (token, query head of the group) pair: heads that
+// share keys share the tiles, and the diagonal of a causal prompt costs the fewer masked tiles the larger the group is.
+// Eight wavefronts of 32 rows each walk tiles of 64 keys.  Both contractions are transposed, S^T = K Q^T and O^T = V^T P^T, so
+// that a row's softmax stays in two lanes and P^T is a matrix operand as the score registers hold it.  K and V go straight from
+// global memory into LDS (one copy for all eight wavefronts; 16-byte chunks permuted within a row so that operand reads meet no
+// bank twice), K is read as it is, V through the transposing LDS read.
+//
+// Schedule: a SIMD runs matrix instructions of one wavefront beside vector instructions of another, so the wavefronts of a SIMD
+// are kept half a tile apart.  Wavefronts 0..3 and 4..7 are two groups that take turns, a barrier per half step:
+//     X(t): O += P(t-1) V(t-1), then S(t) = K(t) Q^T       (matrix instructions)
+//     Y(t): loads of tile t+2, softmax of S(t) -> P(t)      (vector instructions)
+// Three stages of K and four of V make room for tiles that one group still reads while the other has asked for the next ones.
+#include "packed.hpp"
+
+#include <type_traits>
+
+namespace fastar {
+
+namespace prompt {
+
+#pragma clang diagnostic ignored "-Winline-asm"   // m0 is named as clobbered where the tile loads set it
+
+constexpr int TK = 64;         // keys per tile
+constexpr int NWG = 4;         // wavefronts per group
+constexpr int R = 256;         // rows per workgroup
+constexpr int NK = 3, NV = 4;  // stages
+constexpr float LN2 = 0.6931471805599453f;
+
+typedef __attribute__((ext_vector_type(4))) short s16x4;
+#define LDS_PTR(T, p) ((__attribute__((address_space(3))) T *)(p))
+
+template <int OFF>
+__device__ __forceinline__ s16x4 lds_read_tr16(unsigned addr) {
+    s16x4 r;
+    asm volatile("ds_read_b64_tr_b16 %0, %1 offset:%2" : "=v"(r) : "v"(addr), "n"(OFF));
+    return r;
+}
+template <int OFF>
+__device__ __forceinline__ bf16x8 lds_read_b128(unsigned addr) {
+    bf16x8 r;
+    asm volatile("ds_read_b128 %0, %1 offset:%2" : "=v"(r) : "v"(addr), "n"(OFF));
+    return r;
+}
+// Waits until at most N LDS operations are outstanding (they complete in order): the operands named have landed then.
+template <int N, int KF>
+__device__ __forceinline__ void wait_k(bf16x8 (&f)[KF]) {
+    if constexpr (KF == 8)
+        asm volatile("s_waitcnt lgkmcnt(%8)"
+                     : "+v"(f[0]), "+v"(f[1]), "+v"(f[2]), "+v"(f[3]), "+v"(f[4]), "+v"(f[5]), "+v"(f[6]), "+v"(f[7])
+                     : "n"(N));
+    else
+        asm volatile("s_waitcnt lgkmcnt(%4)" : "+v"(f[0]), "+v"(f[1]), "+v"(f[2]), "+v"(f[3]) : "n"(N));
+}
+template <int N, int DB>
+__device__ __forceinline__ void wait_v(s16x4 (&f)[2][DB][2]) {
+    if constexpr (DB == 4)
+        asm volatile("s_waitcnt lgkmcnt(%16)"
+                     : "+v"(f[0][0][0]), "+v"(f[0][0][1]), "+v"(f[0][1][0]), "+v"(f[0][1][1]), "+v"(f[0][2][0]),
+                       "+v"(f[0][2][1]), "+v"(f[0][3][0]), "+v"(f[0][3][1]), "+v"(f[1][0][0]), "+v"(f[1][0][1]),
+                       "+v"(f[1][1][0]), "+v"(f[1][1][1]), "+v"(f[1][2][0]), "+v"(f[1][2][1]), "+v"(f[1][3][0]),
+                       "+v"(f[1][3][1])
+                     : "n"(N));
+    else
+        asm volatile("s_waitcnt lgkmcnt(%8)"
+                     : "+v"(f[0][0][0]), "+v"(f[0][0][1]), "+v"(f[0][1][0]), "+v"(f[0][1][1]), "+v"(f[1][0][0]),
+                       "+v"(f[1][0][1]), "+v"(f[1][1][0]), "+v"(f[1][1][1])
+                     : "n"(N));
+}
+// K operands of 32 keys; BASE = byte offset of the first row in the stage.
+template <int BASE, int KF>
+__device__ __forceinline__ void read_k(bf16x8 (&f)[KF], const unsigned (&kaddr)[KF]) {
+#pragma unroll
+    for (int s = 0; s < KF; ++s) f[s] = lds_read_b128<BASE>(kaddr[s]);
+}
+// V^T operands of 32 keys (two steps of 16) for the blocks of 32 columns.
+template <int BASE, int ROWB, int DB>
+__device__ __forceinline__ void read_vt(s16x4 (&f)[2][DB][2], const unsigned (&vaddr)[DB]) {
+#pragma unroll
+    for (int db = 0; db < DB; ++db) {
+        f[0][db][0] = lds_read_tr16<BASE>(vaddr[db]);
+        f[0][db][1] = lds_read_tr16<BASE + 8 * ROWB>(vaddr[db]);
+    }
+#pragma unroll
+    for (int db = 0; db < DB; ++db) {
+        f[1][db][0] = lds_read_tr16<BASE + 16 * ROWB>(vaddr[db]);
+        f[1][db][1] = lds_read_tr16<BASE + 24 * ROWB>(vaddr[db]);
+    }
+}
+template <int DB>
+__device__ __forceinline__ void pv_mfma(f32x16 (&o)[DB], const s16x4 (&f)[2][DB][2], const bf16x8 (&p)[2]) {
+#pragma unroll
+    for (int st = 0; st < 2; ++st)
+#pragma unroll
+        for (int db = 0; db < DB; ++db) {
+            struct { s16x4 a, b; } pr = {f[st][db][0], f[st][db][1]};
+            bf16x8 a;
+            __builtin_memcpy(&a, &pr, 16);
+            o[db] = mfma_bf16_32x32x16(a, p[st], o[db]);
+        }
+}
+__device__ __forceinline__ float max_across_halves(float x) {
+    const unsigned u = __float_as_uint(x);
+    const auto r = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+    return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+// Barrier that waits for this wavefront's LDS traffic but not for its outstanding tile loads; the scheduling fences keep
+// register-only work of one phase from drifting into the next.
+__device__ __forceinline__ void wg_barrier() {
+    __builtin_amdgcn_sched_barrier(0);
+    asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    __builtin_amdgcn_sched_barrier(0);
+}
+
+struct Args {
+    View Q, K, V, O;
+    const int32_t *cu_q, *cu_k;
+    int B, n_tok_q, n_tok_k, Hkv, group, causal;
+    float scale_log2;
+    float *lse;
+};
+
+template <int D>
+__global__ __launch_bounds__(2 * NWG * 64, 1) void attn_bf16_kernel(const Args a) {
+    extern __shared__ __attribute__((aligned(1024))) unsigned char lds[];   // [K stages][V stages]
+    constexpr int KF = D / 16, DB = D / 32, ROWB = D * 2, TILEB = TK * ROWB;
+    constexpr int NT = 2 * NWG * 64;
+    constexpr int IPW = TILEB / 1024 / (2 * NWG);   // direct loads of 1 KiB per wavefront, tensor and tile
+    constexpr int RPI = 1024 / ROWB;                // rows that one of them brings
+    constexpr int CPR = ROWB / 16;                  // 16-byte chunks per row
+    __shared__ int s_part[2 * NWG], s_found[3];
+    const int tid = threadIdx.x, lane = tid & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int grp = wave / NWG;
+    const int col = lane & 31, g = lane >> 5;
+
+    // workgroup -> (sequence, tile of rows, head): sequences in order, of each the last rows first (they have the most keys),
+    // heads next to each other
+    int b, qt, h;
+    {
+        int before = 0, found = 0;
+        const int u = blockIdx.x;
+        for (int b0 = 0; b0 < a.B && !found; b0 += NT) {   // uniform
+            int n = 0;
+            if (b0 + tid < a.B) n = (rows_of(a.cu_q, b0 + tid, a.n_tok_q).n * a.group + R - 1) / R * a.Hkv;
+            int v = (int)wave_incl_scan((unsigned)n);
+            __syncthreads();
+            if (tid == 0) s_found[0] = -1;
+            if (lane == 63) s_part[wave] = v;
+            __syncthreads();
+            int base = before;
+#pragma unroll
+            for (int i = 0; i < 2 * NWG; ++i) {
+                if (i < wave) base += s_part[i];
+                before += s_part[i];
+            }
+            v += base;
+            if (u >= v - n && u < v) {
+                s_found[0] = b0 + tid;
+                s_found[1] = v - n;
+                s_found[2] = n;
+            }
+            __syncthreads();
+            found = s_found[0] >= 0;
+        }
+        if (!found) return;
+        b = __builtin_amdgcn_readfirstlane(s_found[0]);
+        const int local = u - __builtin_amdgcn_readfirstlane(s_found[1]), n_qt = __builtin_amdgcn_readfirstlane(s_found[2]) / a.Hkv;
+        h = local % a.Hkv;
+        qt = n_qt - 1 - local / a.Hkv;
+    }
+    const Rows rq = rows_of(a.cu_q, b, a.n_tok_q), rk = rows_of(a.cu_k, b, a.n_tok_k);
+    const int n_rows = rq.n * a.group, n = rk.n;
+    // keys that row r sees; rising with r
+    auto sees = [&](int r) { return a.causal ? min(max(n - rq.n + min(r, n_rows - 1) / a.group + 1, 0), n) : n; };
+    const int nt = (sees(qt * R + R - 1) + TK - 1) / TK;     // tiles of the workgroup
+    const int row0 = qt * R + wave * 32;                     // rows of the wavefront
+    const int limit_min = sees(row0);   // what its first row sees
+    const int my_row = min(row0 + col, n_rows - 1);
+    const int my_tok = my_row / a.group, my_head = h * a.group + my_row - my_tok * a.group;
+    const int limit = sees(my_row);
+
+    bf16x8 qf[KF];
+    {
+        const char *qp = a.Q.p + my_head * a.Q.head + (int64_t)(rq.first + my_tok) * a.Q.row;
+#pragma unroll
+        for (int s = 0; s < KF; ++s) qf[s] = *(const bf16x8 *)(qp + (16 * s + 8 * g) * 2);
+    }
+    f32x16 o[DB];
+#pragma unroll
+    for (int db = 0; db < DB; ++db)
+#pragma unroll
+        for (int v = 0; v < 16; ++v) o[db][v] = 0.0f;
+    float m = -INFINITY, neg = 0.0f, l0 = 0.0f, l1 = 0.0f;
+    const float scale_log2 = a.scale_log2;
+
+    // ---- tile loads: instruction i of this wavefront brings tile rows RPI (IPW wave + i) .., lane l row + l / CPR, chunk l % CPR
+    // of LDS; which chunk of the row that is in global memory is permuted by the row
+    unsigned char *kbuf = lds, *vbuf = lds + NK * TILEB;
+    const char *Kb = a.K.p + h * a.K.head + (int64_t)rk.first * a.K.row, *Vb = a.V.p + h * a.V.head + (int64_t)rk.first * a.V.row;
+    auto swz_k = [](int row) { return D == 128 ? row & 15 : (row >> 1) & 7; };
+    auto swz_v = [](int row) { return D == 128 ? (row & 7) << 1 : ((row >> 1) & 3) << 1; };
+    auto issue = [&](const char *base, int64_t pitch, unsigned char *dst, int t, auto is_v) __attribute__((always_inline)) {
+        const char *tile = base + (int64_t)t * TK * pitch;   // uniform
+        const bool all = t * TK + TK <= n;
+#pragma unroll
+        for (int i = 0; i < IPW; ++i) {
+            const int r = RPI * (IPW * wave + i) + lane / CPR;
+            const int chunk = (lane % CPR) ^ (decltype(is_v)::value ? swz_v(r) : swz_k(r));
+            const unsigned off = (unsigned)r * (unsigned)pitch + 16 * chunk;
+            const char *src = all || t * TK + r < n ? tile + off : base + 16 * chunk;   // rows past the end: key 0, which is seen wherever a key is
+            __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)src, LDS_PTR(void, dst + (IPW * wave + i) * 1024), 16, 0, 0);
+        }
+    };
+    auto issue_k = [&](int t) __attribute__((always_inline)) { if (t < nt) issue(Kb, a.K.row, kbuf + (t % NK) * TILEB, t, std::false_type{}); };
+    auto issue_v = [&](int t) __attribute__((always_inline)) { if (t < nt) issue(Vb, a.V.row, vbuf + (t % NV) * TILEB, t, std::true_type{}); };
+
+    // per-lane LDS addresses of the operands
+    const unsigned kbuf_lds = (unsigned)(size_t)LDS_PTR(unsigned char, kbuf), vbuf_lds = (unsigned)(size_t)LDS_PTR(unsigned char, vbuf);
+    unsigned kaddr[KF], vaddr[DB];
+#pragma unroll
+    for (int s = 0; s < KF; ++s) kaddr[s] = kbuf_lds + col * ROWB + (((2 * s + g) ^ swz_k(col)) << 4);
+    const int s16 = lane & 15, l16 = lane >> 4;
+    const int vrow = 4 * (l16 >> 1) + (s16 >> 2);
+#pragma unroll
+    for (int db = 0; db < DB; ++db)
+        vaddr[db] = vbuf_lds + vrow * ROWB + (((4 * db + 2 * (l16 & 1) + ((s16 & 3) >> 1)) ^ swz_v(vrow)) << 4) + (s16 & 1) * 8;
+    int ks = 0, vs = 0;   // stages that kaddr and vaddr point into
+
+    f32x16 s_acc[2];
+    bf16x8 pf[2][2];
+    s16x4 va[2][DB][2];
+    float mx_tile = -INFINITY;
+    auto phase_x = [&](int t, auto pv_c, auto qk_c) __attribute__((always_inline)) {
+        constexpr bool PV = decltype(pv_c)::value, QK = decltype(qk_c)::value;
+        __builtin_amdgcn_s_setprio(2);
+        s16x4 vb[2][DB][2];
+        bf16x8 ka[KF], kb[KF];
+        if constexpr (PV) read_vt<32 * ROWB, ROWB>(vb, vaddr);
+        if constexpr (QK) read_k<0>(ka, kaddr);
+        if constexpr (PV) {
+            pv_mfma(o, va, pf[0]);
+            wait_v<QK ? KF : 0>(vb);
+            pv_mfma(o, vb, pf[1]);
+            const int step = vs == NV - 1 ? -(NV - 1) * TILEB : TILEB;
+            vs = vs == NV - 1 ? 0 : vs + 1;
+#pragma unroll
+            for (int db = 0; db < DB; ++db) vaddr[db] += step;
+        }
+        if constexpr (QK) {
+            read_k<32 * ROWB>(kb, kaddr);
+            wait_k<KF>(ka);
+#pragma unroll
+            for (int v = 0; v < 16; ++v) s_acc[0][v] = s_acc[1][v] = 0.0f;
+#pragma unroll
+            for (int s = 0; s < KF; ++s) s_acc[0] = mfma_bf16_32x32x16(ka[s], qf[s], s_acc[0]);
+            wait_k<0>(kb);
+            __builtin_amdgcn_sched_barrier(0);
+            const int step = ks == NK - 1 ? -(NK - 1) * TILEB : TILEB;
+            ks = ks == NK - 1 ? 0 : ks + 1;
+#pragma unroll
+            for (int s = 0; s < KF; ++s) {
+                s_acc[1] = mfma_bf16_32x32x16(kb[s], qf[s], s_acc[1]);
+                kaddr[s] += step;
+            }
+            __builtin_amdgcn_sched_barrier(0);
+            if (t * TK + TK > limit_min) {   // uniform: some row of the wavefront does not see some key of the tile
+#pragma unroll
+                for (int hb = 0; hb < 2; ++hb)
+#pragma unroll
+                    for (int v = 0; v < 16; ++v)
+                        if (t * TK + 32 * hb + 8 * (v >> 2) + 4 * g + (v & 3) >= limit) s_acc[hb][v] = -INFINITY;
+            }
+            float mx = s_acc[0][0];
+#pragma unroll
+            for (int v = 1; v < 16; ++v) mx = fmaxf(mx, s_acc[0][v]);
+#pragma unroll
+            for (int v = 0; v < 16; ++v) mx = fmaxf(mx, s_acc[1][v]);
+            mx_tile = max_across_halves(mx);
+            asm volatile("" : "+v"(s_acc[0]), "+v"(s_acc[1]), "+v"(mx_tile));
+        }
+        __builtin_amdgcn_s_setprio(0);
+    };
+    auto phase_y = [&](int t) __attribute__((always_inline)) {
+        issue_k(t + 2);
+        issue_v(t + 2);
+        if (__any((mx_tile - m) * scale_log2 > 8.0f)) {   // the reference may lag the maximum by 8 octaves
+            const float mn = fmaxf(m, mx_tile);
+            const float alpha = m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f((m - mn) * scale_log2);
+            m = mn;
+            neg = mn == -INFINITY ? 0.0f : -mn * scale_log2;
+            l0 *= alpha;
+            l1 *= alpha;
+#pragma unroll
+            for (int db = 0; db < DB; ++db)
+#pragma unroll
+                for (int v = 0; v < 16; ++v) o[db][v] *= alpha;
+        }
+#pragma unroll
+        for (int hb = 0; hb < 2; ++hb)
+#pragma unroll
+            for (int hh = 0; hh < 2; ++hh) {
+                bf16x2 pr[4];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const float p0 = __builtin_amdgcn_exp2f(fmaf(s_acc[hb][8 * hh + 2 * j], scale_log2, neg));
+                    const float p1 = __builtin_amdgcn_exp2f(fmaf(s_acc[hb][8 * hh + 2 * j + 1], scale_log2, neg));
+                    l0 += p0;
+                    l1 += p1;
+                    pr[j][0] = (__bf16)p0;
+                    pr[j][1] = (__bf16)p1;
+                }
+                __builtin_memcpy(&pf[hb][hh], pr, 16);
+            }
+        asm volatile("" : "+v"(pf[0][0]), "+v"(pf[0][1]), "+v"(pf[1][0]), "+v"(pf[1][1]), "+v"(l0), "+v"(l1));
+        read_vt<0, ROWB>(va, vaddr);
+        wait_v<0>(va);
+    };
+    auto landed = [&]() __attribute__((always_inline)) {   // this wavefront's loads are there before the barrier that publishes them
+        __builtin_amdgcn_s_waitcnt(0x0F70);   // vmcnt(0)
+        wg_barrier();
+    };
+
+    // Half steps: group 0 runs X(t) in half step 2t and Y(t) in 2t+1, group 1 one later.  K(t) is read in half steps 2t and 2t+1,
+    // V(t) in 2t+1 .. 2t+3; Y(t) asks for K(t+2) (stage of K(t-1)) and V(t+2) (stage of V(t-2)), and what it asked for is
+    // waited for before the barrier into Y(t+1): group 1's at the start of half step 2t+4, when K(t+2) is first read.
+    if (nt > 0) {
+        issue_k(0);
+        issue_v(0);
+        issue_k(1);
+        issue_v(1);
+        landed();
+        if (grp == 1) wg_barrier();
+        phase_x(0, std::false_type{}, std::true_type{});
+        for (int t = 0; t < nt - 1; ++t) {
+            landed();
+            phase_y(t);
+            wg_barrier();
+            phase_x(t + 1, std::true_type{}, std::true_type{});
+        }
+        landed();
+        phase_y(nt - 1);
+        wg_barrier();
+        phase_x(nt, std::true_type{}, std::false_type{});
+        if (grp == 0) wg_barrier();
+    }
+
+    const float l_lane = l0 + l1;
+    const float l = l_lane + shfl_xor(l_lane, 32);
+    const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+    bool odd = false;
+#pragma unroll
+    for (int db = 0; db < DB; ++db)
+#pragma unroll
+        for (int v = 0; v < 16; ++v) odd |= !(fabsf(o[db][v]) < INFINITY);
+    __syncthreads();   // the tiles are dead: their LDS takes the rows of the output, so that they are stored whole
+    constexpr int OSTR = D + 8;
+    unsigned short *Os = (unsigned short *)lds + (size_t)wave * 32 * OSTR;
+#pragma unroll
+    for (int db = 0; db < DB; ++db)
+#pragma unroll
+        for (int q4 = 0; q4 < 4; ++q4) {
+            const bf16x4 w = {(__bf16)(o[db][4 * q4] * inv), (__bf16)(o[db][4 * q4 + 1] * inv), (__bf16)(o[db][4 * q4 + 2] * inv),
+                              (__bf16)(o[db][4 * q4 + 3] * inv)};
+            *(bf16x4 *)(Os + col * OSTR + 32 * db + 8 * q4 + 4 * g) = w;
+        }
+    __syncthreads();
+#pragma unroll
+    for (int it = 0; it < 32 * CPR / 64; ++it) {
+        const int r = it * (64 / CPR) + lane / CPR, rr = row0 + r;
+        if (rr < n_rows) {
+            const int tok = rr / a.group, head = h * a.group + rr - tok * a.group;
+            *(u32x4 *)(a.O.p + head * a.O.head + (int64_t)(rq.first + tok) * a.O.row + (lane % CPR) * 16) = *(const u32x4 *)(Os + r * OSTR + (lane % CPR) * 8);
+        }
+    }
+    if (a.lse && g == 0 && row0 + col < n_rows)
+        a.lse[(size_t)my_head * a.n_tok_q + rq.first + my_tok] = l == 0.0f ? -INFINITY : (m * scale_log2 + __log2f(l)) * LN2;
+    // Sums that are no numbers, where rows see different keys: a value that a row does not see may have come in as 0 * x (a
+    // product of tiles has no other way).  Those rows are done again key by key, over the keys that they see.
+    if (a.causal && __any(odd)) {
+        for (int r = 0; r < 32 && row0 + r < n_rows; ++r) {
+            const int rr = row0 + r, tok = rr / a.group, head = h * a.group + rr - tok * a.group, seen = sees(rr);
+            const __bf16 *q = (const __bf16 *)(a.Q.p + head * a.Q.head + (int64_t)(rq.first + tok) * a.Q.row);
+            float mr = -INFINITY, lr = 0.0f, acc[D / 64], qv[D / 64];
+#pragma unroll
+            for (int c = 0; c < D / 64; ++c) {
+                acc[c] = 0.0f;
+                qv[c] = (float)q[64 * c + lane];
+            }
+            for (int j = 0; j < seen; ++j) {
+                const __bf16 *kp = (const __bf16 *)(Kb + (int64_t)j * a.K.row), *vp = (const __bf16 *)(Vb + (int64_t)j * a.V.row);
+                float x = 0.0f;
+#pragma unroll
+                for (int c = 0; c < D / 64; ++c) x = fmaf(qv[c], (float)kp[64 * c + lane], x);
+#pragma unroll
+                for (int i = 32; i > 0; i >>= 1) x += shfl_xor(x, i);
+                const float mn = fmaxf(mr, x);
+                const float al = mr == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f((mr - mn) * scale_log2);
+                const float p = __builtin_amdgcn_exp2f((x - (mn == -INFINITY ? 0.0f : mn)) * scale_log2);
+                mr = mn;
+                lr = lr * al + p;
+#pragma unroll
+                for (int c = 0; c < D / 64; ++c) acc[c] = acc[c] * al + p * (float)vp[64 * c + lane];
+            }
+            __bf16 *op = (__bf16 *)(a.O.p + head * a.O.head + (int64_t)(rq.first + tok) * a.O.row);
+#pragma unroll
+            for (int c = 0; c < D / 64; ++c) op[64 * c + lane] = (__bf16)(lr == 0.0f ? 0.0f : acc[c] / lr);
+            if (lane == 0 && a.lse) a.lse[(size_t)head * a.n_tok_q + rq.first + tok] = lr == 0.0f ? -INFINITY : (mr * scale_log2 + __log2f(lr)) * LN2;
+        }
+    }
+}
+
+template <int D>
+constexpr int lds_bytes() { return (NK + NV) * TK * D * 2; }
+
+}  // namespace prompt
+
+int prompt_setup() {
+    static DeviceOnce once;
+    return once.run([](int) {
+        if (hipFuncSetAttribute((const void *)prompt::attn_bf16_kernel<128>, hipFuncAttributeMaxDynamicSharedMemorySize,
+                                prompt::lds_bytes<128>()) != hipSuccess)
+            return FASTAR_ERR_HIP;
+        return FASTAR_OK;
+    });
+}
+
+int launch_prompt_bf16(const View &Q, const View &K, const View &V, const int32_t *cu_q, const int32_t *cu_k, int B, int n_tok_q,
+                       int n_tok_k, int Hq, int Hkv, int d, int causal, float scale_log2, const View &O, float *lse, hipStream_t s) {
+    using namespace prompt;
+    if (const int rc = prompt_setup(); rc != FASTAR_OK) return rc;
+    const Args a = {Q, K, V, O, cu_q, cu_k, B, n_tok_q, n_tok_k, Hkv, Hq / Hkv, causal, scale_log2, lse};
+    const int64_t items = (((int64_t)n_tok_q * a.group + R - 1) / R + B) * Hkv;   // at most
+    if (items > INT32_MAX) return FASTAR_ERR_UNSUPPORTED;
+    if (d == 128) hipLaunchKernelGGL(attn_bf16_kernel<128>, dim3((unsigned)items), dim3(2 * NWG * 64), lds_bytes<128>(), s, a);
+    else hipLaunchKernelGGL(attn_bf16_kernel<64>, dim3((unsigned)items), dim3(2 * NWG * 64), lds_bytes<64>(), s, a);
+    FASTAR_LAUNCH_CHECK();
+    return FASTAR_OK;
+}
+
+}  // namespace fastar

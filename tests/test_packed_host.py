@@ -46,7 +46,7 @@ BAD, UNSUPPORTED, WORKSPACE = -1, -2, -3
     (dict(cu=None), BAD), (dict(B=-1), BAD), (dict(n_q=-1), BAD), (dict(n_k=-1), BAD), (dict(Hq=5), BAD), (dict(Hq=0), BAD),
     (dict(Hkv=0), BAD), (dict(dtype=2), BAD), (dict(causal=2), BAD), (dict(scale=0.0), BAD), (dict(scale=-1.0), BAD),
     (dict(scale=math.nan), BAD), (dict(scale=math.inf), BAD), (dict(scale=3e38), BAD), (dict(d=96), UNSUPPORTED),
-    (dict(d=256), UNSUPPORTED), (dict(Q=rows(p=None)), BAD), (dict(K=rows(p=None)), BAD), (dict(V=rows(p=P + 8)), BAD),
+    (dict(d=256), UNSUPPORTED), (dict(K=rows(row=1 << 24)), UNSUPPORTED), (dict(n_q=1 << 28), UNSUPPORTED), (dict(Q=rows(p=None)), BAD), (dict(K=rows(p=None)), BAD), (dict(V=rows(p=P + 8)), BAD),
     (dict(Q=rows(row=132)), BAD), (dict(K=rows(head=12804)), BAD), (dict(V=rows(row=-128)), BAD),
     (dict(O=rows(p=P + 2)), BAD), (dict(O=rows(row=0)), BAD), (dict(O=rows(row=64)), BAD), (dict(O=rows(head=64)), BAD),
     (dict(O=rows(head=99 * 128)), BAD), (dict(O=rows(head=128, row=3 * 128)), BAD)])
@@ -69,7 +69,7 @@ def paged(L, Q=None, O=None, cu=P, length=P, table=P, B=1, max_pages=4, n=100, H
     (dict(cu=None), BAD), (dict(length=None), BAD), (dict(table=None), BAD), (dict(B=-1), BAD), (dict(max_pages=0), BAD),
     (dict(n=-1), BAD), (dict(Hq=3), BAD), (dict(Hq=0), BAD), (dict(dtype=0), UNSUPPORTED), (dict(dtype=5), BAD),
     (dict(causal=-1), BAD), (dict(scale=0.0), BAD), (dict(ws=None), BAD), (dict(ws=P + 16), BAD), (dict(ws_bytes=0), WORKSPACE),
-    (dict(max_pages=1 << 26), UNSUPPORTED), (dict(pg=pages(P=48)), UNSUPPORTED), (dict(pg=pages(P=128)), UNSUPPORTED),
+    (dict(n=1 << 28), UNSUPPORTED), (dict(max_pages=1 << 26), UNSUPPORTED), (dict(pg=pages(P=48)), UNSUPPORTED), (dict(pg=pages(P=128)), UNSUPPORTED),
     (dict(pg=pages(d=32)), UNSUPPORTED), (dict(pg=pages(K8=None)), BAD), (dict(pg=pages(V8=P + 4)), BAD),
     (dict(pg=pages(kscale=None)), BAD), (dict(pg=pages(n_pages=0)), BAD), (dict(pg=pages(Hkv=0)), BAD),
     (dict(pg=pages(n_pages=1 << 26)), UNSUPPORTED), (dict(O=rows(row=0)), BAD), (dict(Q=rows(p=P + 4)), BAD)])
