@@ -226,6 +226,7 @@ int select_setup();
 int tempcache_setup();
 int attn_fp8_setup();
 int prompt_setup();
+int prompt_f32_setup();
 
 // Host-side launch check shared by the entry points.
 #define FASTAR_LAUNCH_CHECK()                          \

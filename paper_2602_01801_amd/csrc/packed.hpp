@@ -37,4 +37,35 @@ __device__ __forceinline__ Rows rows_of(const int32_t *__restrict__ cu, int b, i
     return Rows{a, max(e - a, 0)};
 }
 
+// One row key by key over the keys that it sees, a wavefront, lane l coordinates l, l + 64: what tiles whose products brought in
+// numbers that are none fall back to.
+template <typename T, int D>
+__device__ __forceinline__ void row_by_keys(const char *q, const char *K, int64_t k_pitch, const char *V, int64_t v_pitch, int seen,
+                                            float scale_log2, float &m, float &l, float (&o)[D / 64]) {
+    const int lane = lane_id();
+    float qv[D / 64];
+    m = -INFINITY;
+    l = 0.0f;
+#pragma unroll
+    for (int c = 0; c < D / 64; ++c) {
+        o[c] = 0.0f;
+        qv[c] = (float)((const T *)q)[64 * c + lane];
+    }
+    for (int j = 0; j < seen; ++j) {
+        const T *kp = (const T *)(K + (int64_t)j * k_pitch), *vp = (const T *)(V + (int64_t)j * v_pitch);
+        float x = 0.0f;
+#pragma unroll
+        for (int c = 0; c < D / 64; ++c) x = fmaf(qv[c], (float)kp[64 * c + lane], x);
+#pragma unroll
+        for (int i = 32; i > 0; i >>= 1) x += shfl_xor(x, i);
+        const float mn = fmaxf(m, x);
+        const float al = m == -INFINITY ? 0.0f : exp2f((m - mn) * scale_log2);
+        const float p = exp2f((x - (mn == -INFINITY ? 0.0f : mn)) * scale_log2);
+        m = mn;
+        l = l * al + p;
+#pragma unroll
+        for (int c = 0; c < D / 64; ++c) o[c] = o[c] * al + p * (float)vp[64 * c + lane];
+    }
+}
+
 }  // namespace fastar

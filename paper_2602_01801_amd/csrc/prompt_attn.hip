@@ -381,28 +381,8 @@ __global__ __launch_bounds__(2 * NWG * 64, 1) void attn_bf16_kernel(const Args a
     if (a.causal && __any(odd)) {
         for (int r = 0; r < 32 && row0 + r < n_rows; ++r) {
             const int rr = row0 + r, tok = rr / a.group, head = h * a.group + rr - tok * a.group, seen = sees(rr);
-            const __bf16 *q = (const __bf16 *)(a.Q.p + head * a.Q.head + (int64_t)(rq.first + tok) * a.Q.row);
-            float mr = -INFINITY, lr = 0.0f, acc[D / 64], qv[D / 64];
-#pragma unroll
-            for (int c = 0; c < D / 64; ++c) {
-                acc[c] = 0.0f;
-                qv[c] = (float)q[64 * c + lane];
-            }
-            for (int j = 0; j < seen; ++j) {
-                const __bf16 *kp = (const __bf16 *)(Kb + (int64_t)j * a.K.row), *vp = (const __bf16 *)(Vb + (int64_t)j * a.V.row);
-                float x = 0.0f;
-#pragma unroll
-                for (int c = 0; c < D / 64; ++c) x = fmaf(qv[c], (float)kp[64 * c + lane], x);
-#pragma unroll
-                for (int i = 32; i > 0; i >>= 1) x += shfl_xor(x, i);
-                const float mn = fmaxf(mr, x);
-                const float al = mr == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f((mr - mn) * scale_log2);
-                const float p = __builtin_amdgcn_exp2f((x - (mn == -INFINITY ? 0.0f : mn)) * scale_log2);
-                mr = mn;
-                lr = lr * al + p;
-#pragma unroll
-                for (int c = 0; c < D / 64; ++c) acc[c] = acc[c] * al + p * (float)vp[64 * c + lane];
-            }
+            float mr, lr, acc[D / 64];
+            row_by_keys<__bf16, D>(a.Q.p + head * a.Q.head + (int64_t)(rq.first + tok) * a.Q.row, Kb, a.K.row, Vb, a.V.row, seen, scale_log2, mr, lr, acc);
             __bf16 *op = (__bf16 *)(a.O.p + head * a.O.head + (int64_t)(rq.first + tok) * a.O.row);
 #pragma unroll
             for (int c = 0; c < D / 64; ++c) op[64 * c + lane] = (__bf16)(lr == 0.0f ? 0.0f : acc[c] / lr);
