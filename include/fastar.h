@@ -511,6 +511,7 @@ int kv_pages_plan(const int32_t *n_new, const int32_t *len, int32_t *table, int 
  * run raises the page's scale to s if that is larger; all other codes of the page and head are then carried over to it (value
  * of the code times the old scale over the new one, rounded to nearest, ties to even).  New codes: x / scale rounded to
  * nearest, ties to even; infinities become the largest code of their sign, NaN stays NaN.
+ * Supported: rows of K_new and V_new at most 2^24 bytes apart.
  */
 int kv_pages_write(const fastar_pages *pages, const fastar_rows *K_new, const fastar_rows *V_new, int dtype,
                    const int32_t *slot, int n_tok, void *stream);

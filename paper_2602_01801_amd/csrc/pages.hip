@@ -171,98 +171,205 @@ __device__ __forceinline__ int scale_exp(float amax) {
 }
 __device__ __forceinline__ float pow2(int e) { return __uint_as_float((unsigned)(e + 127) << 23); }
 
-template <bool BF16>
-__device__ __forceinline__ void load16(const char *p, float (&x)[16]) {
-    if constexpr (BF16) {
+// EPL consecutive elements of a row as they lie in memory.
+template <bool BF16, int EPL>
+struct Piece {
+    static constexpr int W = EPL * (BF16 ? 2 : 4) / 4;
+    unsigned w[W];
+    __device__ __forceinline__ void load(const char *p) {
+        if constexpr (W == 2) {
+            const u32x2 x = *(const u32x2 *)p;
+            w[0] = x[0], w[1] = x[1];
+        } else {
 #pragma unroll
-        for (int q = 0; q < 2; ++q) {
-            const u32x4 a = ((const u32x4 *)p)[q];
+            for (int q = 0; q < W / 4; ++q) {
+                const u32x4 x = ((const u32x4 *)p)[q];
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                x[8 * q + 2 * e] = bf16_lo(a[e]);
-                x[8 * q + 2 * e + 1] = bf16_hi(a[e]);
+                for (int e = 0; e < 4; ++e) w[4 * q + e] = x[e];
             }
         }
-    } else {
-#pragma unroll
-        for (int q = 0; q < 4; ++q) {
-            const f32x4 a = ((const f32x4 *)p)[q];
-#pragma unroll
-            for (int e = 0; e < 4; ++e) x[4 * q + e] = a[e];
-        }
     }
+    __device__ __forceinline__ void clear() {
+#pragma unroll
+        for (int i = 0; i < W; ++i) w[i] = 0;
+    }
+    // From here on the elements are taken out of the words anew: held as floats from the maximum to the codes, those of bf16 rows
+    // would take twice the registers.
+    __device__ __forceinline__ void hold() {
+#pragma unroll
+        for (int i = 0; i < W; ++i) asm volatile("" : "+v"(w[i]));
+    }
+    __device__ __forceinline__ float operator[](int i) const {
+        if constexpr (BF16) return i & 1 ? bf16_hi(w[i / 2]) : bf16_lo(w[i / 2]);
+        else return __uint_as_float(w[i]);
+    }
+    __device__ __forceinline__ unsigned codes(int i, float inv) const {   // of elements i .. i + 3
+        return f8_of((*this)[i] * inv, (*this)[i + 1] * inv, (*this)[i + 2] * inv, (*this)[i + 3] * inv);
+    }
+};
+// Codes carried over to a scale 1 / ratio times as large.
+__device__ __forceinline__ unsigned rescaled(unsigned w, float ratio) {
+    return f8_of(__builtin_amdgcn_cvt_f32_fp8((int)w, 0) * ratio, __builtin_amdgcn_cvt_f32_fp8((int)w, 1) * ratio,
+                 __builtin_amdgcn_cvt_f32_fp8((int)w, 2) * ratio, __builtin_amdgcn_cvt_f32_fp8((int)w, 3) * ratio);
+}
+// Exchanges bytes among four words: word i of the result holds byte i of the four.
+__device__ __forceinline__ void transpose4(unsigned (&w)[4]) {
+    const unsigned a = __builtin_amdgcn_perm(w[1], w[0], 0x05010400u), b = __builtin_amdgcn_perm(w[1], w[0], 0x07030602u);   // 0: w0.0 w1.0 w0.1 w1.1
+    const unsigned c = __builtin_amdgcn_perm(w[3], w[2], 0x05010400u), d = __builtin_amdgcn_perm(w[3], w[2], 0x07030602u);
+    w[0] = __builtin_amdgcn_perm(c, a, 0x05040100u);
+    w[1] = __builtin_amdgcn_perm(c, a, 0x07060302u);
+    w[2] = __builtin_amdgcn_perm(d, b, 0x05040100u);
+    w[3] = __builtin_amdgcn_perm(d, b, 0x07060302u);
+}
+__device__ __forceinline__ float wave_max(float x) {   // of numbers that are not negative
+    return __uint_as_float((unsigned)__builtin_amdgcn_readlane((int)wave_max_last(__float_as_uint(x)), 63));
 }
 
-// A wavefront looks at `chunk` rows of one head of K or V and writes the runs that begin there.
-template <bool BF16, int D>
-__global__ __launch_bounds__(256) void write_kernel(View Kn, View Vn, const int32_t *__restrict__ slot, int n_tok, int chunk,
-                                                    fastar_pages pg, int pshift) {
-    constexpr int LR = D / 16;   // lanes of a row
+// A wavefront looks at `chunk` rows of one head of K or V and writes the runs that begin there, each held in registers between
+// its maximum and its codes.  Bound by memory: every row is read once and every code written once; a lane's pieces are chosen for
+// whole cells.  K: 8 coordinates of a row per lane (their 8 codes lie together).  V: 4 coordinates of 16 rows per lane, so that
+// their codes, exchanged within the lane, are 16 consecutive bytes per coordinate, with no trip through LDS.
+template <bool BF16, int D, int PSHIFT>
+__global__ __launch_bounds__(256, BF16 ? 3 : 2) void write_kernel(View Kn, View Vn, const int32_t *__restrict__ slot, int n_tok, int chunk,
+                                                    fastar_pages pg) {
+    constexpr int P = 1 << PSHIFT, ELT = BF16 ? 2 : 4, DB = D / 16;
     const int lane = threadIdx.x & 63;
     const int unit = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int h = unit % pg.Hkv, rest = unit / pg.Hkv;
     const bool is_v = rest & 1;
-    const int first = (rest >> 1) * chunk, last = min(first + chunk, n_tok);
+    const int first = (rest >> 1) * chunk;
     if (first >= n_tok) return;
     const View x = is_v ? Vn : Kn;
     const char *xh = x.p + h * x.head;
     uint8_t *codes = is_v ? pg.V8 : pg.K8;
     float *scales = is_v ? pg.vscale : pg.kscale;
-    const int P = 1 << pshift, n_slots = pg.n_pages << pshift;
-    const int lr = lane / LR, lc = lane % LR;
-    auto at = [&](int t) { return t >= 0 && t < n_tok && (unsigned)slot[t] < (unsigned)n_slots ? slot[t] : -1; };
-    for (int t = first; t < last; ++t) {   // uniform
-        const int s0 = at(t);
-        if (s0 < 0) continue;
-        const int page = s0 >> pshift, o = s0 & (P - 1);
-        const int before = at(t - 1);
-        if (before >= 0 && before == s0 - 1 && o > 0) continue;   // inside a run
-        int n = 1;
-        while (o + n < P && at(t + n) == s0 + n) ++n;
-        float amax = 0.0f;
-        for (int r = lr; r < n; r += 64 / LR) {
-            float v[16];
-            load16<BF16>(xh + (int64_t)(t + r) * x.row + lc * 16 * (BF16 ? 2 : 4), v);
-#pragma unroll
-            for (int e = 0; e < 16; ++e) amax = fmaxf(amax, finite_abs(v[e]));
-        }
-#pragma unroll
-        for (int m = 32; m > 0; m >>= 1) amax = fmaxf(amax, __shfl_xor(amax, m, 64));
-        const int e_new = scale_exp(amax);
+    const unsigned n_slots = (unsigned)pg.n_pages << PSHIFT, pitch = (unsigned)x.row;
+    // rows first - 1 .. first + 127: which are valid, and which go on where the row before them ended
+    auto at = [&](int t) { return t >= 0 && t < n_tok ? slot[t] : -1; };
+    const int s0 = at(first + lane), s1 = at(first + 64 + lane);
+    const int s_before = at(first - 1);
+    const bool ok0 = (unsigned)s0 < n_slots, ok1 = (unsigned)s1 < n_slots;
+    int p0 = __shfl_up(s0, 1, 64), p1 = __shfl_up(s1, 1, 64);   // all lanes together: a lane that is not there gives nothing
+    if (lane == 0) {
+        p0 = s_before;
+        p1 = __builtin_amdgcn_readlane(s0, 63);
+    }
+    const unsigned long long valid = __ballot(ok0);
+    const unsigned long long go0 = __ballot(ok0 && (s0 & (P - 1)) && p0 == s0 - 1), go1 = __ballot(ok1 && (s1 & (P - 1)) && p1 == s1 - 1);
+    unsigned long long begin = valid & ~go0;
+    if (chunk < 64) begin &= (1ull << chunk) - 1ull;
+    for (; begin; begin &= begin - 1ull) {   // uniform
+        const int pos = __builtin_ctzll(begin);
+        const unsigned long long after = pos == 63 ? go1 : (go0 >> (pos + 1)) | (go1 << (63 - pos));   // bit i: row pos + 1 + i goes on
+        const int n = 1 + (~after ? __builtin_ctzll(~after) : 63);   // at most P: a run ends with its page
+        const int t0 = first + pos, sl = __builtin_amdgcn_readlane(s0, pos);
+        const int page = sl >> PSHIFT, o = sl & (P - 1), e = o + n;
         const size_t ph = (size_t)page * pg.Hkv + h;
-        uint8_t *cell0 = codes + ph * ((size_t)D << pshift);
-        float scale = pow2(e_new);
-        if (o > 0) {
-            const float old = scales[ph];
-            if (old >= scale) {
-                scale = old;
-            } else {   // the page's codes move to the larger scale, those of the run's rows before they are written
-                const float ratio = old / scale;
-                for (int i = lane; i < (D << pshift) / 4; i += 64) {
-                    const unsigned w = ((unsigned *)cell0)[i];
-                    ((unsigned *)cell0)[i] =
-                        f8_of(__builtin_amdgcn_cvt_f32_fp8((int)w, 0) * ratio, __builtin_amdgcn_cvt_f32_fp8((int)w, 1) * ratio,
-                              __builtin_amdgcn_cvt_f32_fp8((int)w, 2) * ratio, __builtin_amdgcn_cvt_f32_fp8((int)w, 3) * ratio);
+        uint8_t *cell0 = codes + ph * (size_t)(D * P);
+        const float old_scale = o > 0 ? scales[ph] : 0.0f;
+        const char *row0 = xh + (int64_t)(t0 - o) * x.row;   // of offset 0
+        float amax = 0.0f;
+        if (!is_v) {
+            constexpr int LPR = D / 8, RPI = 64 / LPR, IT = P / RPI;
+            const int lr = lane / LPR, lc = lane % LPR;
+            Piece<BF16, 8> v[IT];
+#pragma unroll
+            for (int i = 0; i < IT; ++i) {
+                v[i].clear();
+                if (i * RPI < e && (i + 1) * RPI > o)   // uniform; rows beside the run: one of its own again
+                    v[i].load(row0 + ((unsigned)min(max(i * RPI + lr, o), e - 1) * pitch + (unsigned)(lc * 8 * ELT)));
+            }
+#pragma unroll
+            for (int i = 0; i < IT; ++i)
+#pragma unroll
+                for (int c = 0; c < 8; ++c) amax = fmaxf(amax, finite_abs(v[i][c]));
+            const float scale = fmaxf(pow2(scale_exp(wave_max(amax))), old_scale), inv = 1.0f / scale, ratio = old_scale * inv;
+#pragma unroll
+            for (int i = 0; i < IT; ++i) {
+                const int r = i * RPI + lr;
+                u32x2 *p = (u32x2 *)(cell0 + ((r >> 4) * DB + (lc >> 1)) * 256 + (r & 15) * 16 + (lc & 1) * 8);
+                if (r >= o && r < e) {
+                    v[i].hold();
+                    *p = u32x2{v[i].codes(0, inv), v[i].codes(4, inv)};
+                } else if (o > 0 && ratio < 1.0f) {
+                    const u32x2 w = *p;
+                    *p = u32x2{rescaled(w[0], ratio), rescaled(w[1], ratio)};
                 }
-                __threadfence();   // before other lanes' new codes go to the same words
+                __builtin_amdgcn_sched_barrier(0);
             }
-        }
-        const float inv = 1.0f / scale;
-        for (int r = lr; r < n; r += 64 / LR) {
-            float v[16];
-            load16<BF16>(xh + (int64_t)(t + r) * x.row + lc * 16 * (BF16 ? 2 : 4), v);
-            u32x4 w;
+            if (lane == 0) scales[ph] = scale;
+        } else {
+            constexpr int LPR = D / 4, G = 64 / LPR, NB = (P / 16 + G - 1) / G;   // lanes per row, blocks of 16 rows side by side, and one after the other
+            const int lc = lane % LPR, gi = lane / LPR;
+            Piece<BF16, 4> v[NB][16];
+            u32x4 old[4];   // what is there of the one block that a short run lies in, asked for along with its rows
+            const bool one_block = n < 16 && (o >> 4) == ((e - 1) >> 4);
 #pragma unroll
-            for (int q = 0; q < 4; ++q) w[q] = f8_of(v[4 * q] * inv, v[4 * q + 1] * inv, v[4 * q + 2] * inv, v[4 * q + 3] * inv);
-            uint8_t *cell = cell0 + (((o + r) >> 4) * LR + lc) * 256;
-            if (!is_v) {
-                *(u32x4 *)(cell + ((o + r) & 15) * 16) = w;
-            } else {
+            for (int nb = 0; nb < NB; ++nb) {
+                const int r0 = 16 * (nb * G + gi);
 #pragma unroll
-                for (int e = 0; e < 16; ++e) cell[e * 16 + ((o + r) & 15)] = (uint8_t)(w[e >> 2] >> (8 * (e & 3)));
+                for (int i = 0; i < 16; ++i) v[nb][i].clear();
+                if (r0 < e && r0 + 16 > o) {
+#pragma unroll
+                    for (int i = 0; i < 16; ++i)   // rows beside the run: one of its own again
+                        v[nb][i].load(row0 + ((unsigned)min(max(r0 + i, o), e - 1) * pitch + (unsigned)(lc * 4 * ELT)));
+                }
             }
+            if (one_block && gi == (o >> 4) % G) {
+#pragma unroll
+                for (int c = 0; c < 4; ++c) old[c] = *(const u32x4 *)(cell0 + ((o >> 4) * DB + (lc >> 2)) * 256 + (4 * (lc & 3) + c) * 16);
+            }
+#pragma unroll
+            for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+                for (int i = 0; i < 16; ++i)
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) amax = fmaxf(amax, finite_abs(v[nb][i][c]));
+            const float scale = fmaxf(pow2(scale_exp(wave_max(amax))), old_scale), inv = 1.0f / scale, ratio = old_scale * inv;
+            const bool grows = o > 0 && ratio < 1.0f;
+#pragma unroll
+            for (int nb = 0; nb < NB; ++nb) {
+                const int r0 = 16 * (nb * G + gi);
+                if (r0 >= P) continue;
+                u32x4 *p = (u32x4 *)(cell0 + ((r0 >> 4) * DB + (lc >> 2)) * 256 + 4 * (lc & 3) * 16);
+                const bool touches = r0 < e && r0 + 16 > o;
+                if (!touches && !grows) continue;
+                u32x4 y[4];
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    unsigned w[4];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        v[nb][4 * q + i].hold();
+                        w[i] = v[nb][4 * q + i].codes(0, inv);   // of a row; its four coordinates
+                    }
+                    __builtin_amdgcn_sched_barrier(0);   // four rows at a time: all at once they would not fit the registers
+                    transpose4(w);
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) y[c][q] = w[c];
+                }
+                if (r0 < o || r0 + 16 > e) {   // rows of others on the block
+                    u32x4 mask;
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) {
+                        mask[q] = 0u;
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) mask[q] |= r0 + 4 * q + i >= o && r0 + 4 * q + i < e ? 0xFFu << (8 * i) : 0u;
+                    }
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) {
+                        u32x4 w = one_block && touches ? old[c] : p[c];
+                        if (grows)
+#pragma unroll
+                            for (int q = 0; q < 4; ++q) w[q] = rescaled(w[q], ratio);
+                        y[c] = (y[c] & mask) | (w & ~mask);
+                    }
+                }
+#pragma unroll
+                for (int c = 0; c < 4; ++c) p[c] = y[c];
+            }
+            if (lane == 0) scales[ph] = scale;
         }
-        if (lane == 0) scales[ph] = scale;
     }
 }
 
@@ -316,21 +423,31 @@ extern "C" int kv_pages_write(const fastar_pages *pages, const fastar_rows *K_ne
     if (const int rc = pages_check(pages); rc != FASTAR_OK) return rc;
     if (n_tok == 0) return FASTAR_OK;
     if (!slot || !view_ok(K_new, elt) || !view_ok(V_new, elt)) return FASTAR_ERR_INVALID_ARG;
-    const int chunk = 16;
+    if (K_new->row * elt > MAX_PITCH || V_new->row * elt > MAX_PITCH) return FASTAR_ERR_UNSUPPORTED;
+    // Rows per wavefront: a page's where that leaves the chip with enough wavefronts (sixteen per compute unit); fewer rows, down
+    // to one, so that the runs of single tokens are not done one after the other.
+    int chunk = pages->P;
+    while (chunk > 1 && (int64_t)n_tok * pages->Hkv * 2 / chunk < 4096) chunk /= 2;
     const int64_t units = (int64_t)((n_tok + chunk - 1) / chunk) * pages->Hkv * 2;
     if (units > INT32_MAX - 4) return FASTAR_ERR_UNSUPPORTED;
     const dim3 grid((unsigned)((units + 3) / 4));
-    const int pshift = __builtin_ctz((unsigned)pages->P);
     const View k = view_of(K_new, elt), v = view_of(V_new, elt);
-#define FASTAR_WRITE(BF16, D) \
-    hipLaunchKernelGGL((pages::write_kernel<BF16, D>), grid, dim3(256), 0, (hipStream_t)stream, k, v, slot, n_tok, chunk, *pages, pshift)
+#define FASTAR_WRITE(BF16, D, PSHIFT) \
+    hipLaunchKernelGGL((pages::write_kernel<BF16, D, PSHIFT>), grid, dim3(256), 0, (hipStream_t)stream, k, v, slot, n_tok, chunk, *pages)
+#define FASTAR_WRITE_P(BF16, D)                      \
+    do {                                             \
+        if (pages->P == 64) FASTAR_WRITE(BF16, D, 6); \
+        else if (pages->P == 32) FASTAR_WRITE(BF16, D, 5); \
+        else FASTAR_WRITE(BF16, D, 4);               \
+    } while (0)
     if (dtype == FASTAR_BF16) {
-        if (pages->d == 128) FASTAR_WRITE(true, 128);
-        else FASTAR_WRITE(true, 64);
+        if (pages->d == 128) FASTAR_WRITE_P(true, 128);
+        else FASTAR_WRITE_P(true, 64);
     } else {
-        if (pages->d == 128) FASTAR_WRITE(false, 128);
-        else FASTAR_WRITE(false, 64);
+        if (pages->d == 128) FASTAR_WRITE_P(false, 128);
+        else FASTAR_WRITE_P(false, 64);
     }
+#undef FASTAR_WRITE_P
 #undef FASTAR_WRITE
     FASTAR_LAUNCH_CHECK();
     return FASTAR_OK;

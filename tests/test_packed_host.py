@@ -101,7 +101,7 @@ def write(L, pg=None, K=None, V=None, dtype=1, slot=P, n=5):
 
 @pytest.mark.parametrize("over,code", [
     (dict(slot=None), BAD), (dict(n=-1), BAD), (dict(dtype=3), BAD), (dict(K=rows(p=None)), BAD), (dict(V=rows(p=P + 8)), BAD),
-    (dict(K=rows(row=4)), BAD), (dict(pg=pages(P=20)), UNSUPPORTED), (dict(pg=pages(d=80)), UNSUPPORTED),
+    (dict(K=rows(row=4)), BAD), (dict(V=rows(row=1 << 24)), UNSUPPORTED), (dict(pg=pages(P=20)), UNSUPPORTED), (dict(pg=pages(d=80)), UNSUPPORTED),
     (dict(pg=pages(vscale=None)), BAD), (dict(pg=pages(Hkv=-1)), BAD)])
 def test_write_refuses(L, over, code):
     assert write(L, **over) == code
