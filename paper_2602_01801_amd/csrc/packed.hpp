@@ -37,6 +37,70 @@ __device__ __forceinline__ Rows rows_of(const int32_t *__restrict__ cu, int b, i
     return Rows{a, max(e - a, 0)};
 }
 
+// 16 bytes per lane from global memory straight into LDS, lane after lane from dst on (uniform, as `base` is): from one base
+// address, each lane at an offset of its own, which costs no vector instruction; or from an address per lane.
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"   // m0 is named as clobbered
+__device__ __forceinline__ void to_lds(const char *base, unsigned off, unsigned dst) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" : : "s"(dst), "v"(off), "s"(base) : "memory", "m0");
+}
+#pragma clang diagnostic pop
+__device__ __forceinline__ void to_lds(const char *src, unsigned char *dst) {
+    __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)src, (__attribute__((address_space(3))) void *)dst, 16, 0, 0);
+}
+__device__ __forceinline__ unsigned lds_address(const void *p) {
+    return (unsigned)(size_t)(__attribute__((address_space(3))) const unsigned char *)p;
+}
+
+// Item u of a launch whose sequences have ceil(rows * group / R) * Hkv items each, in their order.  Every wavefront looks for
+// itself, four sequences per lane, so that a launch of up to 256 sequences waits for one round of loads and for no barrier.
+struct Item {
+    int b, local, n;   // sequence, item within it, items that it has
+    Rows q, k;
+};
+template <int R>
+__device__ __forceinline__ bool find_item(const int32_t *__restrict__ cu_q, const int32_t *__restrict__ cu_k, int B, int n_tok_q, int n_tok_k,
+                                          int group, int Hkv, int u, Item &out) {
+    const int lane = lane_id();
+    int before = 0;
+    for (int b0 = 0; b0 < B; b0 += 256) {   // uniform
+        int cq[5], ck[5];
+#pragma unroll
+        for (int i = 0; i < 5; ++i) {
+            const int b = min(b0 + 4 * lane + i, B);
+            cq[i] = min(max(cu_q[b], 0), n_tok_q);
+            ck[i] = min(max(cu_k[b], 0), n_tok_k);
+        }
+        int n[4], all = 0;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            n[i] = (max(cq[i + 1] - cq[i], 0) * group + R - 1) / R * Hkv;
+            all += n[i];
+        }
+        const int upto = before + (int)wave_incl_scan((unsigned)all);
+        const unsigned long long hit = __ballot(u >= upto - all && u < upto);
+        if (hit) {
+            const int src = __builtin_ctzll(hit);
+            int start = upto - all, i = 0;
+            for (; i < 3; ++i) {
+                if (u < start + n[i]) break;
+                start += n[i];
+            }
+            auto pick = [&](const int *x) { return i == 0 ? x[0] : i == 1 ? x[1] : i == 2 ? x[2] : x[3]; };
+            auto bcast = [&](int x) { return __builtin_amdgcn_readlane(x, src); };
+            out.b = bcast(b0 + 4 * lane + i);
+            out.local = u - bcast(start);
+            out.n = bcast(pick(n));
+            const int q0 = bcast(pick(cq)), q1 = bcast(pick(cq + 1)), k0 = bcast(pick(ck)), k1 = bcast(pick(ck + 1));
+            out.q = Rows{q0, max(q1 - q0, 0)};
+            out.k = Rows{k0, max(k1 - k0, 0)};
+            return true;
+        }
+        before = __builtin_amdgcn_readlane(upto, 63);
+    }
+    return false;
+}
+
 // One row key by key over the keys that it sees, a wavefront, lane l coordinates l, l + 64: what tiles whose products brought in
 // numbers that are none fall back to.
 template <typename T, int D>

@@ -125,11 +125,9 @@ template <int D>
 __global__ __launch_bounds__(2 * NWG * 64, 1) void attn_bf16_kernel(const Args a) {
     extern __shared__ __attribute__((aligned(1024))) unsigned char lds[];   // [K stages][V stages]
     constexpr int KF = D / 16, DB = D / 32, ROWB = D * 2, TILEB = TK * ROWB;
-    constexpr int NT = 2 * NWG * 64;
     constexpr int IPW = TILEB / 1024 / (2 * NWG);   // direct loads of 1 KiB per wavefront, tensor and tile
     constexpr int RPI = 1024 / ROWB;                // rows that one of them brings
     constexpr int CPR = ROWB / 16;                  // 16-byte chunks per row
-    __shared__ int s_part[2 * NWG], s_found[3];
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int grp = wave / NWG;
@@ -137,40 +135,10 @@ __global__ __launch_bounds__(2 * NWG * 64, 1) void attn_bf16_kernel(const Args a
 
     // workgroup -> (sequence, tile of rows, head): sequences in order, of each the last rows first (they have the most keys),
     // heads next to each other
-    int b, qt, h;
-    {
-        int before = 0, found = 0;
-        const int u = blockIdx.x;
-        for (int b0 = 0; b0 < a.B && !found; b0 += NT) {   // uniform
-            int n = 0;
-            if (b0 + tid < a.B) n = (rows_of(a.cu_q, b0 + tid, a.n_tok_q).n * a.group + R - 1) / R * a.Hkv;
-            int v = (int)wave_incl_scan((unsigned)n);
-            __syncthreads();
-            if (tid == 0) s_found[0] = -1;
-            if (lane == 63) s_part[wave] = v;
-            __syncthreads();
-            int base = before;
-#pragma unroll
-            for (int i = 0; i < 2 * NWG; ++i) {
-                if (i < wave) base += s_part[i];
-                before += s_part[i];
-            }
-            v += base;
-            if (u >= v - n && u < v) {
-                s_found[0] = b0 + tid;
-                s_found[1] = v - n;
-                s_found[2] = n;
-            }
-            __syncthreads();
-            found = s_found[0] >= 0;
-        }
-        if (!found) return;
-        b = __builtin_amdgcn_readfirstlane(s_found[0]);
-        const int local = u - __builtin_amdgcn_readfirstlane(s_found[1]), n_qt = __builtin_amdgcn_readfirstlane(s_found[2]) / a.Hkv;
-        h = local % a.Hkv;
-        qt = n_qt - 1 - local / a.Hkv;
-    }
-    const Rows rq = rows_of(a.cu_q, b, a.n_tok_q), rk = rows_of(a.cu_k, b, a.n_tok_k);
+    Item it;
+    if (!find_item<R>(a.cu_q, a.cu_k, a.B, a.n_tok_q, a.n_tok_k, a.group, a.Hkv, blockIdx.x, it)) return;
+    const int h = it.local % a.Hkv, qt = it.n / a.Hkv - 1 - it.local / a.Hkv;
+    const Rows rq = it.q, rk = it.k;
     const int n_rows = rq.n * a.group, n = rk.n;
     // keys that row r sees; rising with r
     auto sees = [&](int r) { return a.causal ? min(max(n - rq.n + min(r, n_rows - 1) / a.group + 1, 0), n) : n; };
@@ -201,20 +169,28 @@ __global__ __launch_bounds__(2 * NWG * 64, 1) void attn_bf16_kernel(const Args a
     const char *Kb = a.K.p + h * a.K.head + (int64_t)rk.first * a.K.row, *Vb = a.V.p + h * a.V.head + (int64_t)rk.first * a.V.row;
     auto swz_k = [](int row) { return D == 128 ? row & 15 : (row >> 1) & 7; };
     auto swz_v = [](int row) { return D == 128 ? (row & 7) << 1 : ((row >> 1) & 3) << 1; };
-    auto issue = [&](const char *base, int64_t pitch, unsigned char *dst, int t, auto is_v) __attribute__((always_inline)) {
-        const char *tile = base + (int64_t)t * TK * pitch;   // uniform
-        const bool all = t * TK + TK <= n;
+    unsigned koff[IPW], voff[IPW];
 #pragma unroll
-        for (int i = 0; i < IPW; ++i) {
-            const int r = RPI * (IPW * wave + i) + lane / CPR;
-            const int chunk = (lane % CPR) ^ (decltype(is_v)::value ? swz_v(r) : swz_k(r));
-            const unsigned off = (unsigned)r * (unsigned)pitch + 16 * chunk;
-            const char *src = all || t * TK + r < n ? tile + off : base + 16 * chunk;   // rows past the end: key 0, which is seen wherever a key is
-            __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)src, LDS_PTR(void, dst + (IPW * wave + i) * 1024), 16, 0, 0);
+    for (int i = 0; i < IPW; ++i) {
+        const int r = RPI * (IPW * wave + i) + lane / CPR;
+        koff[i] = (unsigned)r * (unsigned)a.K.row + 16 * ((lane % CPR) ^ swz_k(r));
+        voff[i] = (unsigned)r * (unsigned)a.V.row + 16 * ((lane % CPR) ^ swz_v(r));
+    }
+    auto issue = [&](const char *base, int64_t pitch, const unsigned (&off)[IPW], unsigned char *dst, int t) __attribute__((always_inline)) {
+        if (t * TK + TK <= n) {   // uniform
+            const char *tile = base + (int64_t)t * TK * pitch;
+#pragma unroll
+            for (int i = 0; i < IPW; ++i) to_lds(tile, off[i], lds_address(dst) + (IPW * wave + i) * 1024);
+        } else {
+#pragma unroll
+            for (int i = 0; i < IPW; ++i) {   // rows past the end: key 0, which is seen wherever a key is
+                const int r = RPI * (IPW * wave + i) + lane / CPR;
+                to_lds(base + off[i] + (t * TK + r < n ? (int64_t)t * TK * pitch : -(int64_t)r * pitch), dst + (IPW * wave + i) * 1024);
+            }
         }
     };
-    auto issue_k = [&](int t) __attribute__((always_inline)) { if (t < nt) issue(Kb, a.K.row, kbuf + (t % NK) * TILEB, t, std::false_type{}); };
-    auto issue_v = [&](int t) __attribute__((always_inline)) { if (t < nt) issue(Vb, a.V.row, vbuf + (t % NV) * TILEB, t, std::true_type{}); };
+    auto issue_k = [&](int t) __attribute__((always_inline)) { if (t < nt) issue(Kb, a.K.row, koff, kbuf + (t % NK) * TILEB, t); };
+    auto issue_v = [&](int t) __attribute__((always_inline)) { if (t < nt) issue(Vb, a.V.row, voff, vbuf + (t % NV) * TILEB, t); };
 
     // per-lane LDS addresses of the operands
     const unsigned kbuf_lds = (unsigned)(size_t)LDS_PTR(unsigned char, kbuf), vbuf_lds = (unsigned)(size_t)LDS_PTR(unsigned char, vbuf);
@@ -367,8 +343,8 @@ __global__ __launch_bounds__(2 * NWG * 64, 1) void attn_bf16_kernel(const Args a
         }
     __syncthreads();
 #pragma unroll
-    for (int it = 0; it < 32 * CPR / 64; ++it) {
-        const int r = it * (64 / CPR) + lane / CPR, rr = row0 + r;
+    for (int i = 0; i < 32 * CPR / 64; ++i) {
+        const int r = i * (64 / CPR) + lane / CPR, rr = row0 + r;
         if (rr < n_rows) {
             const int tok = rr / a.group, head = h * a.group + rr - tok * a.group;
             *(u32x4 *)(a.O.p + head * a.O.head + (int64_t)(rq.first + tok) * a.O.row + (lane % CPR) * 16) = *(const u32x4 *)(Os + r * OSTR + (lane % CPR) * 8);

@@ -1,13 +1,18 @@
 // Attention over packed prompts, fp32 (prompt_attn_fwd), on the fp32 matrix instructions, and the entry point for both types.
 //
-// A workgroup owns 64 rows of one sequence and key head ((token, head of the group) pairs), a wavefront 16 of them; tiles of 32
-// keys go straight from global memory into LDS, one copy for all, two stages.  Both contractions are transposed (lane l: row
-// l % 16, quarter q = l / 16) on v_mfma_f32_16x16x4_f32, whose k order is free as long as both operands agree:
+// A workgroup owns 16 RW rows of one sequence and key head ((token, head of the group) pairs); RW wavefronts, a team, take 16
+// rows each and walk tiles of 16 HB keys; teams of a workgroup take turns at the tiles of the same rows and put their sums
+// together at the end.  Both contractions are transposed (lane l: row l % 16, quarter q = l / 16) on v_mfma_f32_16x16x4_f32,
+// whose k order is free as long as both operands agree:
 //     S^T = K Q^T    A = K, lane l: key l % 16, coordinates 16 c + 4 q .. + 3 in one 16-byte read, four products
 //     O^T = V^T P^T  B = the score registers as they are (product v: key 4 q + v); A = V: block 4 e + x of 16 output rows stands
 //                    for coordinates 64 e + 4 (l % 16) + x, so that a lane's 16-byte read feeds four blocks
-// What bounds it where the chip is full are the matrix instructions (32 cycles each, 128 per tile, nothing runs beside them).
-// Launches with fewer workgroups than compute units let two teams of four wavefronts take turns at the tiles (TEAMS = 2).
+// Two forms.  Where workgroups fill the chip: four wavefronts over shared tiles of 32 keys, K and V straight from global memory
+// into LDS, two stages.  Where they do not: a workgroup per 16 rows, whose four wavefronts take every fourth tile of 16 keys
+// without a barrier, K by way of LDS, V from global memory into registers.
+// What bounds the first are the matrix instructions (32 cycles each, nothing runs beside them): 12 heads on 4 key heads x 4680
+// tokens, causal, 621 us = 108 TFLOP/s of 157; the second the chain of one wavefront's tile (0.7 us of scores, 0.1 of softmax, 0.6 of
+// values at one wavefront per SIMD) and 5 us of a launch's ends: 4 sequences of 390 to 780 x 4 heads over prompts of 64 to 512 30 us.
 #include "packed.hpp"
 
 #include <type_traits>
@@ -19,9 +24,6 @@ int launch_prompt_bf16(const View &Q, const View &K, const View &V, const int32_
 
 namespace prompt32 {
 
-constexpr int TK = 32;      // keys per tile
-constexpr int NW = 4;       // wavefronts per team
-constexpr int R = 16 * NW;  // rows per workgroup
 constexpr float LN2 = 0.6931471805599453f;
 
 __device__ __forceinline__ f32x4 mfma_16x16x4(float a, float b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x4f32(a, b, c, 0, 0, 0); }
@@ -38,20 +40,32 @@ __device__ __forceinline__ float sum_of_quarters(float v) {
     return __uint_as_float(b[0]) + __uint_as_float(b[1]);
 }
 // LDS reads as assembly: the compiler would wait for the tile loads in flight before each of its own.
-template <int OFF>
 __device__ __forceinline__ f32x4 lds_read(unsigned addr) {
     f32x4 r;
-    asm volatile("ds_read_b128 %0, %1 offset:%2" : "=v"(r) : "v"(addr), "n"(OFF));
+    asm volatile("ds_read_b128 %0, %1" : "=v"(r) : "v"(addr));
     return r;
 }
 template <int N>
-__device__ __forceinline__ void wait2(f32x4 &a, f32x4 &b) {
-    asm volatile("s_waitcnt lgkmcnt(%2)" : "+v"(a), "+v"(b) : "n"(N));
+__device__ __forceinline__ void wait_vm() {   // until at most N loads are outstanding
+    __builtin_amdgcn_s_waitcnt(0x0F70 | (N & 15) | ((N >> 4) << 14));
 }
+// Waits until at most `behind` batches of N reads later than f are outstanding; f has landed then.
 template <int N>
-__device__ __forceinline__ void wait1(f32x4 &a) {
-    asm volatile("s_waitcnt lgkmcnt(%1)" : "+v"(a) : "n"(N));
+__device__ __forceinline__ void wait_for(f32x4 (&f)[N], int behind) {
+    if constexpr (N == 2) {
+        if (behind == 2) asm volatile("s_waitcnt lgkmcnt(4)" : "+v"(f[0]), "+v"(f[1]));
+        else if (behind == 1) asm volatile("s_waitcnt lgkmcnt(2)" : "+v"(f[0]), "+v"(f[1]));
+        else asm volatile("s_waitcnt lgkmcnt(0)" : "+v"(f[0]), "+v"(f[1]));
+    } else {
+        if (behind == 2) asm volatile("s_waitcnt lgkmcnt(2)" : "+v"(f[0]));
+        else if (behind == 1) asm volatile("s_waitcnt lgkmcnt(1)" : "+v"(f[0]));
+        else asm volatile("s_waitcnt lgkmcnt(0)" : "+v"(f[0]));
+    }
 }
+
+// Workgroups of 64 rows from which on 16 rows no longer take a workgroup of their own (two of the former per compute unit).
+// 16 rows each against 64, causal, d = 128: 300 workgroups of 64 rows 115 / 142 us, 188 (not causal) 69 / 77; d = 64: 264 42 / 49.
+constexpr int FULL = 512;
 
 struct Args {
     View Q, K, V, O;
@@ -61,53 +75,22 @@ struct Args {
     float *lse;
 };
 
-template <int D, int TEAMS>
-__global__ __launch_bounds__(TEAMS * NW * 64, 2) void attn_f32_prompt_kernel(const Args a) {
+template <int D, int RW, int TEAMS, int HB, int NS>
+__global__ __launch_bounds__(TEAMS * RW * 64, 2) void attn_f32_prompt_kernel(const Args a) {
+    constexpr int NW = RW, R = 16 * RW, TK = 16 * HB;
     constexpr int CH = D / 16, ROWB = D * 4, TILEB = TK * ROWB, CPR = ROWB / 16;
     constexpr int RPI = 1024 / ROWB, IPW = TILEB / 1024 / NW;   // rows per direct load of 1 KiB, loads per wavefront, tensor and tile
-    constexpr int NT = TEAMS * NW * 64;
     extern __shared__ __attribute__((aligned(1024))) unsigned char lds[];   // [team][stage][K, V]
-    __shared__ int s_part[TEAMS * NW], s_found[3];
-    __shared__ float s_m[NW][16], s_l[NW][16];
+    __shared__ float s_m[TEAMS][NW][16], s_l[TEAMS][NW][16];
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int team = wave / NW, w = wave % NW;
     const int col = lane & 15, quarter = lane >> 4;
 
-    int b, qt, h;   // as in prompt_attn.hip
-    {
-        int before = 0, found = 0;
-        const int u = blockIdx.x;
-        for (int b0 = 0; b0 < a.B && !found; b0 += NT) {   // uniform
-            int n = 0;
-            if (b0 + tid < a.B) n = (rows_of(a.cu_q, b0 + tid, a.n_tok_q).n * a.group + R - 1) / R * a.Hkv;
-            int v = (int)wave_incl_scan((unsigned)n);
-            __syncthreads();
-            if (tid == 0) s_found[0] = -1;
-            if (lane == 63) s_part[wave] = v;
-            __syncthreads();
-            int base = before;
-#pragma unroll
-            for (int i = 0; i < TEAMS * NW; ++i) {
-                if (i < wave) base += s_part[i];
-                before += s_part[i];
-            }
-            v += base;
-            if (u >= v - n && u < v) {
-                s_found[0] = b0 + tid;
-                s_found[1] = v - n;
-                s_found[2] = n;
-            }
-            __syncthreads();
-            found = s_found[0] >= 0;
-        }
-        if (!found) return;
-        b = __builtin_amdgcn_readfirstlane(s_found[0]);
-        const int local = u - __builtin_amdgcn_readfirstlane(s_found[1]), n_qt = __builtin_amdgcn_readfirstlane(s_found[2]) / a.Hkv;
-        h = local % a.Hkv;
-        qt = n_qt - 1 - local / a.Hkv;
-    }
-    const Rows rq = rows_of(a.cu_q, b, a.n_tok_q), rk = rows_of(a.cu_k, b, a.n_tok_k);
+    Item it;
+    if (!find_item<R>(a.cu_q, a.cu_k, a.B, a.n_tok_q, a.n_tok_k, a.group, a.Hkv, blockIdx.x, it)) return;
+    const int h = it.local % a.Hkv, qt = it.n / a.Hkv - 1 - it.local / a.Hkv;
+    const Rows rq = it.q, rk = it.k;
     const int n_rows = rq.n * a.group, n = rk.n;
     auto sees = [&](int r) { return a.causal ? min(max(n - rq.n + min(r, n_rows - 1) / a.group + 1, 0), n) : n; };
     const int nt = (sees(qt * R + R - 1) + TK - 1) / TK;
@@ -130,71 +113,107 @@ __global__ __launch_bounds__(TEAMS * NW * 64, 2) void attn_f32_prompt_kernel(con
     float m = -INFINITY, neg = 0.0f, l = 0.0f;
 
     const char *Kb = a.K.p + h * a.K.head + (int64_t)rk.first * a.K.row, *Vb = a.V.p + h * a.V.head + (int64_t)rk.first * a.V.row;
-    unsigned char *mine = lds + team * 4 * TILEB;
+    unsigned char *mine = lds + team * NS * (RW == 1 ? 1 : 2) * TILEB;
     // one 16-byte piece per lane; K's pieces are permuted within a row, piece c of row w at c ^ (w & 15)
-    auto issue = [&](const char *base, int64_t pitch, unsigned char *dst, int t, bool is_k) __attribute__((always_inline)) {
-        const char *tile = base + (int64_t)t * TK * pitch;
-        const bool all = t * TK + TK <= n;
+    unsigned koff[IPW], voff[IPW];
 #pragma unroll
-        for (int i = 0; i < IPW; ++i) {
-            const int r = RPI * (IPW * w + i) + lane / CPR;
-            const int piece = (lane % CPR) ^ (is_k ? r & 15 : 0);
-            const unsigned off = (unsigned)r * (unsigned)pitch + 16 * piece;
-            const char *src = all || t * TK + r < n ? tile + off : base + 16 * piece;   // rows past the end: key 0, which is seen wherever a key is
-            __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)src,
-                                             (__attribute__((address_space(3))) void *)(dst + (IPW * w + i) * 1024), 16, 0, 0);
+    for (int i = 0; i < IPW; ++i) {
+        const int r = RPI * (IPW * w + i) + lane / CPR;
+        koff[i] = (unsigned)r * (unsigned)a.K.row + 16 * ((lane % CPR) ^ (r & 15));
+        voff[i] = (unsigned)r * (unsigned)a.V.row + 16 * (lane % CPR);
+    }
+    auto issue = [&](const char *base, int64_t pitch, const unsigned (&off)[IPW], unsigned char *dst, int t) __attribute__((always_inline)) {
+        if (RW > 1 && t * TK + TK <= n) {   // uniform
+            const char *tile = base + (int64_t)t * TK * pitch;
+#pragma unroll
+            for (int i = 0; i < IPW; ++i) to_lds(tile, off[i], lds_address(dst) + (IPW * w + i) * 1024);
+        } else {
+#pragma unroll
+            for (int i = 0; i < IPW; ++i) {   // rows past the end: key 0, which is seen wherever a key is
+                const int r = RPI * (IPW * w + i) + lane / CPR;
+                to_lds(base + off[i] + (t * TK + r < n ? (int64_t)t * TK * pitch : -(int64_t)r * pitch), dst + (IPW * w + i) * 1024);
+            }
         }
     };
+    constexpr bool OWN = RW == 1;                 // a wavefront's tiles are its own
+    constexpr int STAGEB = (OWN ? 1 : 2) * TILEB;   // K (and V) of a tile
     auto issue_tile = [&](int t, int stage) __attribute__((always_inline)) {
         if (t >= nt) return;
-        issue(Kb, a.K.row, mine + stage * 2 * TILEB, t, true);
-        issue(Vb, a.V.row, mine + stage * 2 * TILEB + TILEB, t, false);
+        issue(Kb, a.K.row, koff, mine + stage * STAGEB, t);
+        if constexpr (!OWN) issue(Vb, a.V.row, voff, mine + stage * STAGEB + TILEB, t);
+    };
+    constexpr int STEPS = 4 * HB;   // of the second product; step i: key 16 (i / 4) + 4 quarter + i % 4
+    f32x4 vown[OWN ? STEPS : 1][D / 64];
+    auto load_v = [&](int t) __attribute__((always_inline)) {   // 16 lanes read 256 bytes of a row
+        if (t >= nt) return;
+#pragma unroll
+        for (int i = 0; i < (OWN ? STEPS : 0); ++i) {
+            const int r = t * TK + (i >> 2) * 16 + 4 * quarter + (i & 3);
+            const char *p = Vb + (int64_t)(r < n ? r : 0) * a.V.row + col * 16;
+#pragma unroll
+            for (int e = 0; e < D / 64; ++e) vown[i][e] = *(const f32x4 *)(p + 256 * e);
+        }
     };
     const unsigned mine_lds = (unsigned)(size_t)(__attribute__((address_space(3))) unsigned char *)mine;
     const unsigned kaddr0 = mine_lds + col * ROWB + ((quarter ^ col) << 4);        // chunk c: exclusive or with 64 c
     const unsigned vaddr0 = mine_lds + TILEB + 4 * quarter * ROWB + col * 16;
 
-    const int turns = (nt + TEAMS - 1) / TEAMS;   // the same for both teams
-    issue_tile(team, 0);
+    const int turns = (nt + TEAMS - 1) / TEAMS;   // the same for all teams
+#pragma unroll
+    for (int i = 0; i < NS - 1; ++i) issue_tile(TEAMS * i + team, i);
+    load_v(team);
+    int stage = 0;
     for (int i = 0; i < turns; ++i) {
-        const int t = TEAMS * i + team, stage = i & 1;
-        __builtin_amdgcn_s_waitcnt(0x0F70);   // vmcnt(0)
-        asm volatile("s_barrier" ::: "memory");   // the tile is there, and nobody reads the other stage any more
-        issue_tile(t + TEAMS, stage ^ 1);
+        const int t = TEAMS * i + team;
+        // tile t is there
+        if constexpr (OWN) {
+            if (t >= nt) break;
+            wait_vm<STEPS * (D / 64)>();   // V was asked for last
+            asm volatile("" ::: "memory");
+        } else {
+            wait_vm<0>();
+            asm volatile("s_barrier" ::: "memory");   // for all of the team; nobody reads the stage of the turn before any more
+        }
+        issue_tile(t + TEAMS * (NS - 1), stage == 0 ? NS - 1 : stage - 1);
+        const unsigned kaddr = kaddr0 + stage * STAGEB, vaddr = vaddr0 + stage * STAGEB;
+        stage = stage == NS - 1 ? 0 : stage + 1;
         if (t >= nt) continue;   // uniform over the team
-        const unsigned kaddr = kaddr0 + stage * 2 * TILEB, vaddr = vaddr0 + stage * 2 * TILEB;
-        f32x4 s[2] = {{0.0f, 0.0f, 0.0f, 0.0f}, {0.0f, 0.0f, 0.0f, 0.0f}};
+        constexpr int NA = 2 / HB;   // two chains of products at least: one waits for its own results
+        f32x4 s[HB], sa[NA][HB];
+#pragma unroll
+        for (int i = 0; i < NA; ++i)
+#pragma unroll
+            for (int hb = 0; hb < HB; ++hb) sa[i][hb] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
         {
-            f32x4 kf[3][2];
-            auto read = [&](int c, f32x4 (&f)[2]) __attribute__((always_inline)) {
-                const unsigned at = kaddr ^ (unsigned)(64 * c);
-                f[0] = lds_read<0>(at);
-                f[1] = lds_read<16 * ROWB>(at);
+            f32x4 kf[3][HB];   // operands are asked for two chunks ahead
+            auto read = [&](int c) __attribute__((always_inline)) {
+#pragma unroll
+                for (int hb = 0; hb < HB; ++hb) kf[c % 3][hb] = lds_read((kaddr ^ (unsigned)(64 * c)) + 16 * hb * ROWB);
             };
-            read(0, kf[0]);
-            read(1, kf[1]);
+            read(0);
+            read(1);
 #pragma unroll
             for (int c = 0; c < CH; ++c) {
-                if (c + 2 < CH) read(c + 2, kf[(c + 2) % 3]);
-                if (c + 2 < CH) wait2<4>(kf[c % 3][0], kf[c % 3][1]);
-                else if (c + 1 < CH) wait2<2>(kf[c % 3][0], kf[c % 3][1]);
-                else wait2<0>(kf[c % 3][0], kf[c % 3][1]);
+                if (c + 2 < CH) read(c + 2);
+                wait_for(kf[c % 3], min(CH - 1 - c, 2));
 #pragma unroll
                 for (int e = 0; e < 4; ++e)
 #pragma unroll
-                    for (int hb = 0; hb < 2; ++hb) s[hb] = mfma_16x16x4(kf[c % 3][hb][e], q[c][e], s[hb]);
+                    for (int hb = 0; hb < HB; ++hb) sa[e % NA][hb] = mfma_16x16x4(kf[c % 3][hb][e], q[c][e], sa[e % NA][hb]);
             }
+#pragma unroll
+            for (int hb = 0; hb < HB; ++hb) s[hb] = NA == 2 ? sa[0][hb] + sa[NA - 1][hb] : sa[0][hb];
         }
         if (t * TK + TK > limit_min) {
 #pragma unroll
-            for (int hb = 0; hb < 2; ++hb)
+            for (int hb = 0; hb < HB; ++hb)
 #pragma unroll
                 for (int v = 0; v < 4; ++v)
                     if (t * TK + 16 * hb + 4 * quarter + v >= limit) s[hb][v] = -INFINITY;
         }
         float mx = s[0][0];
 #pragma unroll
-        for (int hb = 0; hb < 2; ++hb)
+        for (int hb = 0; hb < HB; ++hb)
 #pragma unroll
             for (int v = 0; v < 4; ++v) mx = fmaxf(mx, s[hb][v]);
         mx = max_of_quarters(mx);
@@ -208,7 +227,7 @@ __global__ __launch_bounds__(TEAMS * NW * 64, 2) void attn_f32_prompt_kernel(con
             for (int c = 0; c < CH; ++c) o[c] *= alpha;
         }
 #pragma unroll
-        for (int hb = 0; hb < 2; ++hb)
+        for (int hb = 0; hb < HB; ++hb)
 #pragma unroll
             for (int v = 0; v < 4; ++v) {
                 s[hb][v] = exp2f(fmaf(s[hb][v], scale_log2, neg));   // with its subnormal results: values go up to 2^128
@@ -216,55 +235,60 @@ __global__ __launch_bounds__(TEAMS * NW * 64, 2) void attn_f32_prompt_kernel(con
             }
         {
             f32x4 vf[3][D / 64];
-            auto read = [&](auto step, f32x4 (&f)[D / 64]) __attribute__((always_inline)) {
-                constexpr int row = (decltype(step)::value >> 2) * 16 + (decltype(step)::value & 3);
-                f[0] = lds_read<row * ROWB>(vaddr);
-                if constexpr (D == 128) f[1] = lds_read<row * ROWB + 256>(vaddr);
+            auto read = [&](int i) __attribute__((always_inline)) {
+#pragma unroll
+                for (int e = 0; e < D / 64; ++e) vf[i % 3][e] = lds_read(vaddr + ((i >> 2) * 16 + (i & 3)) * ROWB + 256 * e);
             };
-            auto product = [&](auto step, auto behind) __attribute__((always_inline)) {
-                constexpr int i = decltype(step)::value, n_behind = decltype(behind)::value * (D / 64);
-                f32x4 (&f)[D / 64] = vf[i % 3];
-                if constexpr (D == 128) wait2<n_behind>(f[0], f[1]);
-                else wait1<n_behind>(f[0]);
+            if constexpr (!OWN) {
+                read(0);
+                read(1);
+            }
+#pragma unroll
+            for (int i = 0; i < STEPS; ++i) {
+                if constexpr (!OWN) {
+                    if (i + 2 < STEPS) read(i + 2);
+                    wait_for(vf[i % 3], min(STEPS - 1 - i, 2));
+                }
 #pragma unroll
                 for (int e = 0; e < D / 64; ++e)
 #pragma unroll
-                    for (int x = 0; x < 4; ++x) o[4 * e + x] = mfma_16x16x4(f[e][x], s[i >> 2][i & 3], o[4 * e + x]);
-            };
-#define N(i) std::integral_constant<int, i>{}
-            read(N(0), vf[0]);
-            read(N(1), vf[1]);
-            read(N(2), vf[2]); product(N(0), N(2));
-            read(N(3), vf[0]); product(N(1), N(2));
-            read(N(4), vf[1]); product(N(2), N(2));
-            read(N(5), vf[2]); product(N(3), N(2));
-            read(N(6), vf[0]); product(N(4), N(2));
-            read(N(7), vf[1]); product(N(5), N(2));
-            product(N(6), N(1));
-            product(N(7), N(0));
-#undef N
+                    for (int x = 0; x < 4; ++x)
+                        o[4 * e + x] = mfma_16x16x4(OWN ? vown[OWN ? i : 0][e][x] : vf[i % 3][e][x], s[i >> 2][i & 3], o[4 * e + x]);
+            }
+            load_v(t + TEAMS);
         }
     }
     l = sum_of_quarters(l);
-    if constexpr (TEAMS == 2) {   // team 1 hands its sums to team 0
+    if constexpr (TEAMS > 1) {   // the other teams hand their sums to team 0
         __syncthreads();
-        f32x4 *give = (f32x4 *)lds + (size_t)w * CH * 64;
-        if (team == 1) {
+        static_assert(CH * 1024 <= NS * STAGEB / NW, "a team's sums fit its stages");
+        f32x4 *give = (f32x4 *)lds;   // [team - 1][wavefront][block][lane]
+        if (team > 0) {
 #pragma unroll
-            for (int c = 0; c < CH; ++c) give[c * 64 + lane] = o[c];
-            if (quarter == 0) {
-                s_m[w][col] = m;
-                s_l[w][col] = l;
-            }
+            for (int c = 0; c < CH; ++c) give[(((team - 1) * NW + w) * CH + c) * 64 + lane] = o[c];
+        }
+        if (quarter == 0) {
+            s_m[team][w][col] = m;
+            s_l[team][w][col] = l;
         }
         __syncthreads();
-        if (team == 1) return;
-        const float mo = s_m[w][col], lo = s_l[w][col], m_all = fmaxf(m, mo);
-        const float w_mine = m == -INFINITY ? 0.0f : exp2f((m - m_all) * scale_log2), w_other = mo == -INFINITY ? 0.0f : exp2f((mo - m_all) * scale_log2);
-        m = m_all;
-        l = l * w_mine + lo * w_other;
+        if (team > 0) return;
+        float m_all = m;
 #pragma unroll
-        for (int c = 0; c < CH; ++c) o[c] = o[c] * w_mine + give[c * 64 + lane] * w_other;
+        for (int i = 1; i < TEAMS; ++i) m_all = fmaxf(m_all, s_m[i][w][col]);
+        auto weight = [&](float mi) { return mi == -INFINITY ? 0.0f : exp2f((mi - m_all) * scale_log2); };
+        const float mine_w = weight(m);
+        l *= mine_w;
+#pragma unroll
+        for (int c = 0; c < CH; ++c) o[c] *= mine_w;
+#pragma unroll
+        for (int i = 1; i < TEAMS; ++i) {
+            const float wi = weight(s_m[i][w][col]);
+            l += s_l[i][w][col] * wi;
+#pragma unroll
+            for (int c = 0; c < CH; ++c) o[c] += give[(((i - 1) * NW + w) * CH + c) * 64 + lane] * wi;
+        }
+        m = m_all;
     }
     bool odd = false;
 #pragma unroll
@@ -299,16 +323,26 @@ __global__ __launch_bounds__(TEAMS * NW * 64, 2) void attn_f32_prompt_kernel(con
     }
 }
 
-template <int D, int TEAMS>
-constexpr int lds_bytes() { return TEAMS * 4 * TK * D * 4; }
-
+template <int D, int RW, int TEAMS, int HB, int NS>
+struct Form {
+    static constexpr int R = 16 * RW, LDS = TEAMS * NS * (RW == 1 ? 1 : 2) * 16 * HB * D * 4;
+    static int setup() {
+        if (LDS <= 65536) return FASTAR_OK;
+        return hipFuncSetAttribute((const void *)attn_f32_prompt_kernel<D, RW, TEAMS, HB, NS>, hipFuncAttributeMaxDynamicSharedMemorySize, LDS) == hipSuccess ? FASTAR_OK : FASTAR_ERR_HIP;
+    }
+    static int launch(const Args &a, hipStream_t s) {
+        const int64_t n = items(a);
+        if (n > INT32_MAX) return FASTAR_ERR_UNSUPPORTED;
+        hipLaunchKernelGGL((attn_f32_prompt_kernel<D, RW, TEAMS, HB, NS>), dim3((unsigned)n), dim3(TEAMS * RW * 64), LDS, s, a);
+        FASTAR_LAUNCH_CHECK();
+        return FASTAR_OK;
+    }
+    static int64_t items(const Args &a) { return (((int64_t)a.n_tok_q * a.group + R - 1) / R + a.B) * a.Hkv; }   // at most
+};
 template <int D>
-int launch(const Args &a, int64_t items, hipStream_t s) {
-    // Two teams where one leaves compute units without a workgroup; their LDS allows only one workgroup per unit.
-    if (items <= 256) hipLaunchKernelGGL((attn_f32_prompt_kernel<D, 2>), dim3((unsigned)items), dim3(2 * NW * 64), (lds_bytes<D, 2>()), s, a);
-    else hipLaunchKernelGGL((attn_f32_prompt_kernel<D, 1>), dim3((unsigned)items), dim3(NW * 64), (lds_bytes<D, 1>()), s, a);
-    FASTAR_LAUNCH_CHECK();
-    return FASTAR_OK;
+int launch(const Args &a, hipStream_t s) {
+    if (Form<D, 4, 1, 2, 2>::items(a) > FULL) return Form<D, 4, 1, 2, 2>::launch(a, s);
+    return Form<D, 1, 4, 1, 2>::launch(a, s);
 }
 
 }  // namespace prompt32
@@ -317,11 +351,11 @@ int prompt_f32_setup() {
     using namespace prompt32;
     static DeviceOnce once;
     return once.run([](int) {
-        if (hipFuncSetAttribute((const void *)attn_f32_prompt_kernel<128, 2>, hipFuncAttributeMaxDynamicSharedMemorySize, lds_bytes<128, 2>()) != hipSuccess ||
-            hipFuncSetAttribute((const void *)attn_f32_prompt_kernel<64, 2>, hipFuncAttributeMaxDynamicSharedMemorySize, lds_bytes<64, 2>()) != hipSuccess ||
-            hipFuncSetAttribute((const void *)attn_f32_prompt_kernel<128, 1>, hipFuncAttributeMaxDynamicSharedMemorySize, lds_bytes<128, 1>()) != hipSuccess)
-            return FASTAR_ERR_HIP;
-        return FASTAR_OK;
+        int rc = Form<128, 4, 1, 2, 2>::setup();
+        if (rc == FASTAR_OK) rc = Form<64, 4, 1, 2, 2>::setup();
+        if (rc == FASTAR_OK) rc = Form<128, 1, 4, 1, 2>::setup();
+        if (rc == FASTAR_OK) rc = Form<64, 1, 4, 1, 2>::setup();
+        return rc;
     });
 }
 
@@ -349,7 +383,5 @@ extern "C" int prompt_attn_fwd(const fastar_rows *Q, const fastar_rows *K, const
         return launch_prompt_bf16(q, k, v, cu_q, cu_k, B, n_tok_q, n_tok_k, Hq, Hkv, d, causal, scale_log2, o, lse, (hipStream_t)stream);
     if (const int rc = prompt_f32_setup(); rc != FASTAR_OK) return rc;
     const prompt32::Args a = {q, k, v, o, cu_q, cu_k, B, n_tok_q, n_tok_k, Hkv, Hq / Hkv, causal, scale_log2, lse};
-    const int64_t items = (((int64_t)n_tok_q * a.group + prompt32::R - 1) / prompt32::R + B) * Hkv;   // at most
-    if (items > INT32_MAX) return FASTAR_ERR_UNSUPPORTED;
-    return d == 128 ? prompt32::launch<128>(a, items, (hipStream_t)stream) : prompt32::launch<64>(a, items, (hipStream_t)stream);
+    return d == 128 ? prompt32::launch<128>(a, (hipStream_t)stream) : prompt32::launch<64>(a, (hipStream_t)stream);
 }
