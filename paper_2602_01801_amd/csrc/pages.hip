@@ -35,7 +35,113 @@ __device__ __forceinline__ int slot_of(const int32_t *__restrict__ row, long lon
     return (unsigned)page < (unsigned)n_pages ? (page << pshift) + (int)(pos & ((1 << pshift) - 1)) : -1;
 }
 
-// One workgroup: requests in rounds of PT.  Tables and the pool are updated by wavefronts, a request each, so that requests
+// Up to PT requests: a thread each, sums in 32 bits (the launch sees to it that they fit).  Everything that is read -- lengths, table
+// entries below a request's own pages, the pool below its top -- is left as it is by the call, so that pages which go from one
+// request to another by way of the pool are looked up where they come from, and tables, pool and slots are written side by side:
+// two rounds of loads in all (one for lengths, one for pages), against six of the kernel for more requests.  With many tokens more
+// workgroups repeat the sums and write slots only; that needs the lengths to stay in place, so not if len_out or pool_n_out is an input.
+// 192 requests, a token each 14.1 -> 6.0 us, 64 prompts of 90122 tokens 13 -> 4.6.
+constexpr int SMALL_LIMIT = 1 << 20;   // PT times this much stays below 2^31
+__global__ __launch_bounds__(PT) void plan_small_kernel(const int32_t *__restrict__ n_new, const int32_t *len, int32_t *table, int B,
+                                                        int max_pages, int32_t *pool, const int32_t *pool_n, int n_pages, int pshift,
+                                                        int n_tok, int32_t *len_out, int32_t *pool_n_out, int32_t *__restrict__ cu,
+                                                        int32_t *__restrict__ slot, int32_t *__restrict__ status, int n_slots) {
+    __shared__ int part[3][PT / 64];
+    __shared__ int s_rows[PT], s_back[PT], s_upto[PT], s_have[PT], s_len[PT];   // the first three: inclusive prefix sums
+    const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
+    const int P = 1 << pshift;
+    int n = 0, L = 0;
+    bool ended = false;
+    if (tid < B) {
+        n = n_new[tid];
+        L = (int)min(max((long long)len[tid], 0ll), (long long)max_pages << pshift);
+        ended = n < 0;
+        n = max(n, 0);
+    }
+    const int free0 = min(max(pool_n[0], 0), n_pages);
+    const int have = (L + P - 1) >> pshift;
+    int rows = (int)wave_incl_scan((unsigned)min(n, n_tok + 1)), back = (int)wave_incl_scan(ended ? (unsigned)have : 0u);
+    if (lane == 63) {
+        part[0][wave] = rows;
+        part[1][wave] = back;
+    }
+    __syncthreads();
+    auto add_before = [&](int which, int &v) {
+        int all = 0;
+#pragma unroll
+        for (int i = 0; i < PT / 64; ++i) {
+            const int x = part[which][i];
+            if (i < wave) v += x;
+            all += x;
+        }
+        return all;
+    };
+    const int n_rows = min(add_before(0, rows), n_tok), n_back = add_before(1, back);
+    const int free1 = (int)min((long long)free0 + n_back, (long long)n_pages);
+    const long long want = ((long long)L + n + P - 1) >> pshift;
+    int st = want > max_pages ? 2 : rows > n_tok && n > 0 ? 3 : 0;
+    const int ask = ended || st ? 0 : (int)max(want - have, 0ll);
+    int upto = (int)wave_incl_scan((unsigned)ask);
+    if (lane == 63) part[2][wave] = upto;
+    __syncthreads();
+    const int n_ask = add_before(2, upto);
+    if (ask > 0 && upto > free1) st = 1;
+    s_rows[tid] = min(rows, n_tok);
+    s_back[tid] = back;
+    s_upto[tid] = upto;
+    s_have[tid] = have;
+    s_len[tid] = st ? -1 : L;
+    __syncthreads();
+    auto owner = [&](const int *incl, int x) {   // the request whose part of the sums holds x
+        int lo = 0, hi = B - 1;
+        while (lo < hi) {
+            const int mid = (lo + hi) >> 1;
+            if (incl[mid] > x) hi = mid;
+            else lo = mid + 1;
+        }
+        return lo;
+    };
+    auto given_back = [&](int r) {
+        const int i = owner(s_back, r);
+        return table[(size_t)i * max_pages + r - (s_back[i] - s_have[i])];
+    };
+    auto taken = [&](int f) {   // the f-th page that is taken
+        const int at = free1 - 1 - f;
+        return at < free0 ? pool[at] : given_back(at - free0);
+    };
+    for (int t = blockIdx.x * PT + tid; t < min(n_rows, n_slots); t += gridDim.x * PT) {
+        const int i = owner(s_rows, t);
+        int y = -1;
+        if (s_len[i] >= 0) {
+            const int pos = s_len[i] + t - (i ? s_rows[i - 1] : 0), pg = pos >> pshift;
+            const int page = pg < s_have[i] ? table[(size_t)i * max_pages + pg] : taken((i ? s_upto[i - 1] : 0) + pg - s_have[i]);
+            if ((unsigned)page < (unsigned)n_pages) y = (page << pshift) + (pos & (P - 1));
+        }
+        slot[t] = y;
+    }
+    if (blockIdx.x) return;
+    int n_take = n_ask;   // those asked for by requests before the first for which they do not suffice
+    if (n_ask > free1) {
+        const int i = owner(s_upto, free1);
+        n_take = i ? s_upto[i - 1] : 0;
+    }
+    for (int f = tid; f < n_take; f += PT) {
+        const int i = owner(s_upto, f);
+        table[(size_t)i * max_pages + s_have[i] + f - (i ? s_upto[i - 1] : 0)] = taken(f);
+    }
+    for (int r = tid; r < free1 - free0; r += PT) pool[free0 + r] = given_back(r);
+    if (tid < B) {
+        cu[tid] = tid ? s_rows[tid - 1] : 0;
+        len_out[tid] = ended ? 0 : st ? L : L + n;
+        status[tid] = st;
+    }
+    if (tid == 0) {
+        cu[B] = n_rows;
+        pool_n_out[0] = free1 - n_take;
+    }
+}
+
+// Any number of requests, 64-bit sums.  One workgroup: requests in rounds of PT.  Tables and the pool are updated by wavefronts, a request each, so that requests
 // with many pages are copied 64 entries at a time.
 template <bool SLOTS>
 __global__ __launch_bounds__(PT) void plan_kernel(const int32_t *__restrict__ n_new, const int32_t *len, int32_t *table, int B,
@@ -388,6 +494,22 @@ extern "C" int kv_pages_plan(const int32_t *n_new, const int32_t *len, int32_t *
     if ((int64_t)max_pages * P > INT32_MAX || (int64_t)n_pages * P > INT32_MAX) return FASTAR_ERR_UNSUPPORTED;
     const int pshift = __builtin_ctz((unsigned)P);
     const hipStream_t s = (hipStream_t)stream;
+    if (B <= pages::PT && n_tok < pages::SMALL_LIMIT && max_pages < pages::SMALL_LIMIT) {
+        // one workgroup writes ONE_SLOTS slots beside the rest; beyond that there are more workgroups, or a launch of their own
+        constexpr int ONE_SLOTS = 4096;
+        const bool alone = len_out == len || pool_n_out == pool_n;
+        const int wgs = n_tok <= ONE_SLOTS || alone ? 1 : (n_tok + pages::PT - 1) / pages::PT;
+        const bool later = n_tok > ONE_SLOTS && alone;
+        hipLaunchKernelGGL(pages::plan_small_kernel, dim3((unsigned)wgs), dim3(pages::PT), 0, s, n_new, len, table, B, max_pages, pool,
+                           pool_n, n_pages, pshift, n_tok, len_out, pool_n_out, cu, slot, status, later ? 0 : n_tok);
+        FASTAR_LAUNCH_CHECK();
+        if (later) {
+            hipLaunchKernelGGL(pages::slots_kernel, dim3((unsigned)((n_tok + 255) / 256)), dim3(256), 0, s, table, B, max_pages, n_pages,
+                               pshift, n_tok, len_out, cu, slot, status);
+            FASTAR_LAUNCH_CHECK();
+        }
+        return FASTAR_OK;
+    }
     if (n_tok <= 4096) {
         hipLaunchKernelGGL(pages::plan_kernel<true>, dim3(1), dim3(pages::PT), 0, s, n_new, len, table, B, max_pages, pool, pool_n,
                            n_pages, pshift, n_tok, len_out, pool_n_out, cu, slot, status);
