@@ -82,6 +82,7 @@ extern "C" int fastar_init(void) {
     if (rc == FASTAR_OK) rc = fastar::attn_fp8_setup();
     if (rc == FASTAR_OK) rc = fastar::prompt_setup();
     if (rc == FASTAR_OK) rc = fastar::prompt_f32_setup();
+    if (rc == FASTAR_OK) rc = fastar::paged_chunk_setup();
     return rc;
 }
 

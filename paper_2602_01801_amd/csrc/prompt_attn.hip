@@ -12,6 +12,7 @@
 //     X(t): O += P(t-1) V(t-1), then S(t) = K(t) Q^T       (matrix instructions)
 //     Y(t): loads of tile t+2, softmax of S(t) -> P(t)      (vector instructions)
 // Three stages of K and four of V make room for tiles that one group still reads while the other has asked for the next ones.
+#include "attn_lds.hpp"
 #include "packed.hpp"
 
 #include <type_traits>
@@ -20,98 +21,13 @@ namespace fastar {
 
 namespace prompt {
 
-#pragma clang diagnostic ignored "-Winline-asm"   // m0 is named as clobbered where the tile loads set it
+using namespace attn_lds;
 
 constexpr int TK = 64;         // keys per tile
 constexpr int NWG = 4;         // wavefronts per group
 constexpr int R = 256;         // rows per workgroup
 constexpr int NK = 3, NV = 4;  // stages
 constexpr float LN2 = 0.6931471805599453f;
-
-typedef __attribute__((ext_vector_type(4))) short s16x4;
-#define LDS_PTR(T, p) ((__attribute__((address_space(3))) T *)(p))
-
-template <int OFF>
-__device__ __forceinline__ s16x4 lds_read_tr16(unsigned addr) {
-    s16x4 r;
-    asm volatile("ds_read_b64_tr_b16 %0, %1 offset:%2" : "=v"(r) : "v"(addr), "n"(OFF));
-    return r;
-}
-template <int OFF>
-__device__ __forceinline__ bf16x8 lds_read_b128(unsigned addr) {
-    bf16x8 r;
-    asm volatile("ds_read_b128 %0, %1 offset:%2" : "=v"(r) : "v"(addr), "n"(OFF));
-    return r;
-}
-// Waits until at most N LDS operations are outstanding (they complete in order): the operands named have landed then.
-template <int N, int KF>
-__device__ __forceinline__ void wait_k(bf16x8 (&f)[KF]) {
-    if constexpr (KF == 8)
-        asm volatile("s_waitcnt lgkmcnt(%8)"
-                     : "+v"(f[0]), "+v"(f[1]), "+v"(f[2]), "+v"(f[3]), "+v"(f[4]), "+v"(f[5]), "+v"(f[6]), "+v"(f[7])
-                     : "n"(N));
-    else
-        asm volatile("s_waitcnt lgkmcnt(%4)" : "+v"(f[0]), "+v"(f[1]), "+v"(f[2]), "+v"(f[3]) : "n"(N));
-}
-template <int N, int DB>
-__device__ __forceinline__ void wait_v(s16x4 (&f)[2][DB][2]) {
-    if constexpr (DB == 4)
-        asm volatile("s_waitcnt lgkmcnt(%16)"
-                     : "+v"(f[0][0][0]), "+v"(f[0][0][1]), "+v"(f[0][1][0]), "+v"(f[0][1][1]), "+v"(f[0][2][0]),
-                       "+v"(f[0][2][1]), "+v"(f[0][3][0]), "+v"(f[0][3][1]), "+v"(f[1][0][0]), "+v"(f[1][0][1]),
-                       "+v"(f[1][1][0]), "+v"(f[1][1][1]), "+v"(f[1][2][0]), "+v"(f[1][2][1]), "+v"(f[1][3][0]),
-                       "+v"(f[1][3][1])
-                     : "n"(N));
-    else
-        asm volatile("s_waitcnt lgkmcnt(%8)"
-                     : "+v"(f[0][0][0]), "+v"(f[0][0][1]), "+v"(f[0][1][0]), "+v"(f[0][1][1]), "+v"(f[1][0][0]),
-                       "+v"(f[1][0][1]), "+v"(f[1][1][0]), "+v"(f[1][1][1])
-                     : "n"(N));
-}
-// K operands of 32 keys; BASE = byte offset of the first row in the stage.
-template <int BASE, int KF>
-__device__ __forceinline__ void read_k(bf16x8 (&f)[KF], const unsigned (&kaddr)[KF]) {
-#pragma unroll
-    for (int s = 0; s < KF; ++s) f[s] = lds_read_b128<BASE>(kaddr[s]);
-}
-// V^T operands of 32 keys (two steps of 16) for the blocks of 32 columns.
-template <int BASE, int ROWB, int DB>
-__device__ __forceinline__ void read_vt(s16x4 (&f)[2][DB][2], const unsigned (&vaddr)[DB]) {
-#pragma unroll
-    for (int db = 0; db < DB; ++db) {
-        f[0][db][0] = lds_read_tr16<BASE>(vaddr[db]);
-        f[0][db][1] = lds_read_tr16<BASE + 8 * ROWB>(vaddr[db]);
-    }
-#pragma unroll
-    for (int db = 0; db < DB; ++db) {
-        f[1][db][0] = lds_read_tr16<BASE + 16 * ROWB>(vaddr[db]);
-        f[1][db][1] = lds_read_tr16<BASE + 24 * ROWB>(vaddr[db]);
-    }
-}
-template <int DB>
-__device__ __forceinline__ void pv_mfma(f32x16 (&o)[DB], const s16x4 (&f)[2][DB][2], const bf16x8 (&p)[2]) {
-#pragma unroll
-    for (int st = 0; st < 2; ++st)
-#pragma unroll
-        for (int db = 0; db < DB; ++db) {
-            struct { s16x4 a, b; } pr = {f[st][db][0], f[st][db][1]};
-            bf16x8 a;
-            __builtin_memcpy(&a, &pr, 16);
-            o[db] = mfma_bf16_32x32x16(a, p[st], o[db]);
-        }
-}
-__device__ __forceinline__ float max_across_halves(float x) {
-    const unsigned u = __float_as_uint(x);
-    const auto r = __builtin_amdgcn_permlane32_swap(u, u, false, false);
-    return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
-}
-// Barrier that waits for this wavefront's LDS traffic but not for its outstanding tile loads; the scheduling fences keep
-// register-only work of one phase from drifting into the next.
-__device__ __forceinline__ void wg_barrier() {
-    __builtin_amdgcn_sched_barrier(0);
-    asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
-    __builtin_amdgcn_sched_barrier(0);
-}
 
 struct Args {
     View Q, K, V, O;
@@ -193,7 +109,7 @@ __global__ __launch_bounds__(2 * NWG * 64, 1) void attn_bf16_kernel(const Args a
     auto issue_v = [&](int t) __attribute__((always_inline)) { if (t < nt) issue(Vb, a.V.row, voff, vbuf + (t % NV) * TILEB, t); };
 
     // per-lane LDS addresses of the operands
-    const unsigned kbuf_lds = (unsigned)(size_t)LDS_PTR(unsigned char, kbuf), vbuf_lds = (unsigned)(size_t)LDS_PTR(unsigned char, vbuf);
+    const unsigned kbuf_lds = lds_address(kbuf), vbuf_lds = lds_address(vbuf);
     unsigned kaddr[KF], vaddr[DB];
 #pragma unroll
     for (int s = 0; s < KF; ++s) kaddr[s] = kbuf_lds + col * ROWB + (((2 * s + g) ^ swz_k(col)) << 4);
