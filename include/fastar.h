@@ -470,7 +470,7 @@ int prompt_attn_fwd(const fastar_rows *Q, const fastar_rows *K, const fastar_row
  *   kscale, vscale [n_pages, Hkv] float, powers of two: a code stands for its E4M3 value times the scale of its page and
  *   head.  E4M3 has an exponent of its own, so that a finer scale would not make codes more precise; a power of two lets
  *   the codes of a page be carried to a larger scale without a second rounding (but for those that become subnormal).
- * P in {16, 32, 64}, n_pages * P < 2^31.  Token i of a sequence lies in page table[b][i / P] of its block table, at i % P.
+ * P in {16, 32, 64}, n_pages * P < 2^31, Hkv * P * d < 2^31.  Token i of a sequence lies in page table[b][i / P] of its block table, at i % P.
  */
 typedef struct {
     uint8_t *K8, *V8;

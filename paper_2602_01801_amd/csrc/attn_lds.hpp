@@ -62,6 +62,12 @@ __device__ __forceinline__ void read_k(bf16x8 (&f)[KF], const unsigned (&kaddr)[
 #pragma unroll
     for (int s = 0; s < KF; ++s) f[s] = lds_read_b128<BASE>(kaddr[s]);
 }
+// The same from one address: that of operand s is exclusive or with 32 s.
+template <int BASE, int KF>
+__device__ __forceinline__ void read_k(bf16x8 (&f)[KF], unsigned kaddr) {
+#pragma unroll
+    for (int s = 0; s < KF; ++s) f[s] = lds_read_b128<BASE>(kaddr ^ (32 * s));
+}
 // V^T operands of 32 keys (two steps of 16) for the blocks of 32 columns.
 template <int BASE, int ROWB, int DB>
 __device__ __forceinline__ void read_vt(s16x4 (&f)[2][DB][2], const unsigned (&vaddr)[DB]) {

@@ -103,43 +103,46 @@ __global__ __launch_bounds__(2 * NWG * 64, 1) void attn_chunk_kernel(const Args 
         u32x4 kr, vr;
         float ks, vs;
         bool ok;
+        int kput = 0, vput = 0;   // stages that the next tile goes to, in bytes
+        const unsigned page_stride = (unsigned)(Hkv * page_bytes);   // of all heads
+        const uint8_t *K8 = a.pg.K8 + h * page_bytes, *V8 = a.pg.V8 + h * page_bytes;
+        const float *kscale = a.pg.kscale + h, *vscale = a.pg.vscale + h;
         auto fetch = [&](int ids) __attribute__((always_inline)) {   // returns which blocks' pages exist
             int id = __builtin_amdgcn_readlane(ids, tb);
             ok = page_exists(a, id);
             id = ok ? id : 0;
-            const size_t ph = (size_t)id * Hkv + h;
+            const size_t at = (size_t)(unsigned)id * page_stride;
             if (has_k) {
-                kr = *(const u32x4 *)(a.pg.K8 + ph * page_bytes + piece);
-                ks = a.pg.kscale[ph];
+                kr = *(const u32x4 *)(K8 + at + piece);
+                ks = kscale[(size_t)(unsigned)id * (unsigned)Hkv];
             }
             if (has_v) {
-                vr = *(const u32x4 *)(a.pg.V8 + ph * page_bytes + piece);
-                vs = a.pg.vscale[ph];
+                vr = *(const u32x4 *)(V8 + at + piece);
+                vs = vscale[(size_t)(unsigned)id * (unsigned)Hkv];
             }
             return (int)(__ballot(page_exists(a, ids)) & 15);
         };
         auto put = [&](int t) __attribute__((always_inline)) {
             if (has_k) {
-                unsigned char *p = kbuf + ((t - ta) % NK) * TILEB;
+                unsigned char *p = kbuf + kput;
                 *(bf16x8 *)(p + kw) = widen(kr[0], kr[1], ks);
                 *(bf16x8 *)(p + (kw ^ 16)) = widen(kr[2], kr[3], ks);
             }
             if (has_v) {
                 const int live = ok ? limit_max - (t * TK + 16 * tb) : 0;
                 if (live < 16) vr &= first_bytes(live);   // uniform; values that no row sees need not be numbers
-                unsigned char *p = vbuf + ((t - ta) % NV) * TILEB;
+                unsigned char *p = vbuf + vput;
                 *(bf16x8 *)(p + vw) = widen(vr[0], vr[2], vs);
                 *(bf16x8 *)(p + (vw ^ 16)) = widen(vr[1], vr[3], vs);
             }
+            kput = kput == (NK - 1) * TILEB ? 0 : kput + TILEB;
+            vput = vput == (NV - 1) * TILEB ? 0 : vput + TILEB;
         };
 
-        // per-lane LDS addresses of the operands
-        unsigned kaddr[KF], vaddr[4];
-#pragma unroll
-        for (int s = 0; s < KF; ++s) kaddr[s] = kbuf_lds + col * ROWB + (((2 * s + g) ^ swz_k(col)) << 4);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) vaddr[i] = vbuf_lds + col * VROWB + (((2 * i + g) ^ swz_v(col)) << 4);   // block of 16 tokens i
-        int kst = 0, vst = 0;   // stages that kaddr and vaddr point into
+        // per-lane LDS addresses of the operands: of K's first 16 coordinates (the s-th: exclusive or with 32 s), of V's first 16 tokens
+        // (the i-th: with 32 i)
+        unsigned kaddr = kbuf_lds + col * ROWB + ((g ^ swz_k(col)) << 4), vaddr = vbuf_lds + col * VROWB + ((g ^ swz_v(col)) << 4);
+        int kst = 0, vst = 0;   // stages that they point into
 
         f32x16 s_acc[2];
         bf16x8 pf[2][2], va[2][DB];
@@ -147,11 +150,12 @@ __global__ __launch_bounds__(2 * NWG * 64, 1) void attn_chunk_kernel(const Args 
         auto read_v = [&](int hb, bf16x8 (&f)[2][DB]) __attribute__((always_inline)) {
 #pragma unroll
             for (int st = 0; st < 2; ++st) {
-                f[st][0] = lds_read_b128<0>(vaddr[2 * hb + st]);
-                f[st][1] = lds_read_b128<32 * VROWB>(vaddr[2 * hb + st]);
+                const unsigned at = vaddr ^ (32 * (2 * hb + st));
+                f[st][0] = lds_read_b128<0>(at);
+                f[st][1] = lds_read_b128<32 * VROWB>(at);
                 if constexpr (DB == 4) {
-                    f[st][2] = lds_read_b128<64 * VROWB>(vaddr[2 * hb + st]);
-                    f[st][3] = lds_read_b128<96 * VROWB>(vaddr[2 * hb + st]);
+                    f[st][2] = lds_read_b128<64 * VROWB>(at);
+                    f[st][3] = lds_read_b128<96 * VROWB>(at);
                 }
             }
         };
@@ -171,10 +175,8 @@ __global__ __launch_bounds__(2 * NWG * 64, 1) void attn_chunk_kernel(const Args 
                 pv(va, pf[0]);
                 wait_b<QK ? KF : 0>(vb);
                 pv(vb, pf[1]);
-                const int step = vst == NV - 1 ? -(NV - 1) * TILEB : TILEB;
+                vaddr += vst == NV - 1 ? -(NV - 1) * TILEB : TILEB;
                 vst = vst == NV - 1 ? 0 : vst + 1;
-#pragma unroll
-                for (int i = 0; i < 4; ++i) vaddr[i] += step;
             }
             if constexpr (QK) {
                 read_k<32 * ROWB>(kb, kaddr);
@@ -185,13 +187,10 @@ __global__ __launch_bounds__(2 * NWG * 64, 1) void attn_chunk_kernel(const Args 
                 for (int s = 0; s < KF; ++s) s_acc[0] = mfma_bf16_32x32x16(ka[s], qf[s], s_acc[0]);
                 wait_k<0>(kb);
                 __builtin_amdgcn_sched_barrier(0);
-                const int step = kst == NK - 1 ? -(NK - 1) * TILEB : TILEB;
+                kaddr += kst == NK - 1 ? -(NK - 1) * TILEB : TILEB;
                 kst = kst == NK - 1 ? 0 : kst + 1;
 #pragma unroll
-                for (int s = 0; s < KF; ++s) {
-                    s_acc[1] = mfma_bf16_32x32x16(kb[s], qf[s], s_acc[1]);
-                    kaddr[s] += step;
-                }
+                for (int s = 0; s < KF; ++s) s_acc[1] = mfma_bf16_32x32x16(kb[s], qf[s], s_acc[1]);
                 __builtin_amdgcn_sched_barrier(0);
                 if (t * TK + TK > limit_min || exist != 15) {   // uniform: some row of the wavefront does not see some key of the tile
 #pragma unroll
@@ -210,11 +209,10 @@ __global__ __launch_bounds__(2 * NWG * 64, 1) void attn_chunk_kernel(const Args 
             }
             __builtin_amdgcn_s_setprio(0);
         };
-        // what is on its way: page numbers of tile t + 4 (ids), codes of tile t + 3 (registers, existing pages e3)
-        int ids = 0, e0 = 15, e1 = 15, e2 = 15, e3 = 15;
+        // on their way: page numbers of tile t + 4 (ids), codes of tile t + 3 (registers); which pages of tiles t + 1 .. t + 3 exist
+        int ids = 0, e1 = 15, e2 = 15, e3 = 15;
         auto phase_y = [&](int t) __attribute__((always_inline)) {
             if (t + 2 < t_end) put(t + 2);
-            e0 = e1;
             e1 = e2;
             e2 = e3;
             if (t + 3 < t_end) e3 = fetch(ids);
@@ -254,21 +252,15 @@ __global__ __launch_bounds__(2 * NWG * 64, 1) void attn_chunk_kernel(const Args 
         // Half steps as in prompt_attn.hip; tiles t + 2 are written in Y(t), where prompt_attn.hip asks for them, and are there at the
         // barrier that ends it.
         if (ta < t_end) {
-            {
-                const int i0 = ids_of(ta), i1 = ids_of(ta + 1), i2 = ids_of(ta + 2);
-                ids = ids_of(ta + 3);
-                e0 = fetch(i0);
-                put(ta);
-                if (ta + 1 < t_end) {
-                    e1 = fetch(i1);
-                    put(ta + 1);
-                }
-                if (ta + 2 < t_end) e2 = fetch(i2);
+            const int i0 = ids_of(ta), i1 = ids_of(ta + 1), i2 = ids_of(ta + 2);
+            ids = ids_of(ta + 3);
+            e1 = fetch(i0);
+            put(ta);
+            if (ta + 1 < t_end) {
+                e2 = fetch(i1);
+                put(ta + 1);
             }
-            // fetch(ids) of Y(ta) brings tile ta + 3; e0 .. e2 are moved on by Y before X asks for them
-            e3 = e2;
-            e2 = e1;
-            e1 = e0;
+            if (ta + 2 < t_end) e3 = fetch(i2);
             wg_barrier();
             if (grp == 1) wg_barrier();
             phase_x(ta, e1, std::false_type{}, std::true_type{});
@@ -285,6 +277,12 @@ __global__ __launch_bounds__(2 * NWG * 64, 1) void attn_chunk_kernel(const Args 
             if (grp == 0) wg_barrier();
         }
 
+        // rows anew, so that the loop need not hold them in registers
+        int qt_e = qt, lane_e = lane;
+        asm volatile("" : "+s"(qt_e), "+v"(lane_e));
+        const int row0_e = qt_e * R + wave * 32, col_e = lane_e & 31, g_e = lane_e >> 5;
+        const int my_row_e = min(row0_e + col_e, n_rows - 1);
+        const int my_tok_e = my_row_e / a.group, my_head_e = h * a.group + my_row_e - my_tok_e * a.group;
         const float l_lane = l0 + l1;
         const float l = l_lane + shfl_xor(l_lane, 32);
         bool odd = false;
@@ -304,46 +302,46 @@ __global__ __launch_bounds__(2 * NWG * 64, 1) void attn_chunk_kernel(const Args 
                 for (int q4 = 0; q4 < 4; ++q4) {
                     const bf16x4 w = {(__bf16)(o[db][4 * q4] * inv), (__bf16)(o[db][4 * q4 + 1] * inv), (__bf16)(o[db][4 * q4 + 2] * inv),
                                       (__bf16)(o[db][4 * q4 + 3] * inv)};
-                    *(bf16x4 *)(Os + col * OSTR + 32 * db + 8 * q4 + 4 * g) = w;
+                    *(bf16x4 *)(Os + col_e * OSTR + 32 * db + 8 * q4 + 4 * g_e) = w;
                 }
             __syncthreads();
 #pragma unroll
             for (int i = 0; i < 32 * CPR / 64; ++i) {
-                const int x = i * (64 / CPR) + lane / CPR, rr = row0 + x;
+                const int x = i * (64 / CPR) + lane_e / CPR, rr = row0_e + x;
                 if (rr < n_rows) {
                     const int tok = rr / a.group, head = h * a.group + rr - tok * a.group;
-                    *(u32x4 *)(a.O.p + head * a.O.head + (int64_t)(sq.q0 + tok) * a.O.row + (lane % CPR) * 16) = *(const u32x4 *)(Os + x * OSTR + (lane % CPR) * 8);
+                    *(u32x4 *)(a.O.p + head * a.O.head + (int64_t)(sq.q0 + tok) * a.O.row + (lane_e % CPR) * 16) = *(const u32x4 *)(Os + x * OSTR + (lane_e % CPR) * 8);
                 }
             }
-            if (a.lse && g == 0 && row0 + col < n_rows)
-                a.lse[(size_t)my_head * a.n_tok + sq.q0 + my_tok] = l == 0.0f ? -INFINITY : (m * scale_log2 + __log2f(l)) * LN2;
-        } else {   // [wavefront][block of 32 coordinates][q4][lane] of four floats, then maxima and sums
+            if (a.lse && g_e == 0 && row0_e + col_e < n_rows)
+                a.lse[(size_t)my_head_e * a.n_tok + sq.q0 + my_tok_e] = l == 0.0f ? -INFINITY : (m * scale_log2 + __log2f(l)) * LN2;
+        } else {   // [wavefront][block of 32 coordinates][q4][lane_e] of four floats, then maxima and sums
 #pragma unroll
             for (int db = 0; db < DB; ++db)
 #pragma unroll
                 for (int q4 = 0; q4 < 4; ++q4) {
                     const f32x4 x = {o[db][4 * q4], o[db][4 * q4 + 1], o[db][4 * q4 + 2], o[db][4 * q4 + 3]};
-                    ((f32x4 *)frag)[((wave * DB + db) * 4 + q4) * 64 + lane] = x;
+                    ((f32x4 *)frag)[((wave * DB + db) * 4 + q4) * 64 + lane_e] = x;
                 }
-            if (g == 0) {
-                frag[R * D + wave * 32 + col] = m;
-                frag[R * D + R + wave * 32 + col] = l;
+            if (g_e == 0) {
+                frag[R * D + wave * 32 + col_e] = m;
+                frag[R * D + R + wave * 32 + col_e] = l;
             }
         }
         // as in paged_attn.hip: rows that a value which they do not see may have spoilt
         if (a.causal && sq.n_q > 1 && __any(odd)) {
             __threadfence();
-            for (int x = 0; x < 32 && row0 + x < n_rows; ++x) {
-                const int rr = row0 + x, tok = rr / a.group, head = h * a.group + rr - tok * a.group;
+            for (int x = 0; x < 32 && row0_e + x < n_rows; ++x) {
+                const int rr = row0_e + x, tok = rr / a.group, head = h * a.group + rr - tok * a.group;
                 float mr, lr, acc[D / 64];
                 row_by_paged_keys<D>(a, a.Q.p + head * a.Q.head + (int64_t)(sq.q0 + tok) * a.Q.row, pages, h, ta * TK, min(sees(rr), te * TK), mr, lr, acc);
 #pragma unroll
                 for (int c = 0; c < D / 64; ++c) {
-                    const int co = 64 * c + lane;
+                    const int co = 64 * c + lane_e;
                     if (whole) ((__bf16 *)(a.O.p + head * a.O.head + (int64_t)(sq.q0 + tok) * a.O.row))[co] = (__bf16)(lr == 0.0f ? 0.0f : acc[c] / lr);
                     else frag[(((wave * DB + (co >> 5)) * 4 + ((co & 31) >> 3)) * 64 + ((co & 7) >> 2) * 32 + x) * 4 + (co & 3)] = acc[c];
                 }
-                if (lane == 0) {
+                if (lane_e == 0) {
                     if (whole) {
                         if (a.lse) a.lse[(size_t)head * a.n_tok + sq.q0 + tok] = lr == 0.0f ? -INFINITY : (mr * scale_log2 + __log2f(lr)) * LN2;
                     } else {

@@ -531,7 +531,7 @@ int pages_check(const fastar_pages *pg) {
     if (((uintptr_t)pg->K8 & 15) || ((uintptr_t)pg->V8 & 15)) return FASTAR_ERR_INVALID_ARG;
     if (pg->n_pages <= 0 || pg->Hkv <= 0) return FASTAR_ERR_INVALID_ARG;
     if (!page_size_ok(pg->P) || (pg->d != 64 && pg->d != 128)) return FASTAR_ERR_UNSUPPORTED;
-    if ((int64_t)pg->n_pages * pg->P > INT32_MAX) return FASTAR_ERR_UNSUPPORTED;
+    if ((int64_t)pg->n_pages * pg->P > INT32_MAX || (int64_t)pg->Hkv * pg->P * pg->d > INT32_MAX) return FASTAR_ERR_UNSUPPORTED;
     return FASTAR_OK;
 }
 }  // namespace fastar
