@@ -277,6 +277,9 @@ __device__ __forceinline__ int scale_exp(float amax) {
 }
 __device__ __forceinline__ float pow2(int e) { return __uint_as_float((unsigned)(e + 127) << 23); }
 
+typedef __attribute__((ext_vector_type(2))) unsigned short u16x2;
+typedef __attribute__((ext_vector_type(2))) short s16x2;
+
 // EPL consecutive elements of a row as they lie in memory.
 template <bool BF16, int EPL>
 struct Piece {
@@ -299,20 +302,41 @@ struct Piece {
 #pragma unroll
         for (int i = 0; i < W; ++i) w[i] = 0;
     }
-    // From here on the elements are taken out of the words anew: held as floats from the maximum to the codes, those of bf16 rows
-    // would take twice the registers.
-    __device__ __forceinline__ void hold() {
-#pragma unroll
-        for (int i = 0; i < W; ++i) asm volatile("" : "+v"(w[i]));
-    }
     __device__ __forceinline__ float operator[](int i) const {
         if constexpr (BF16) return i & 1 ? bf16_hi(w[i / 2]) : bf16_lo(w[i / 2]);
         else return __uint_as_float(w[i]);
     }
-    __device__ __forceinline__ unsigned codes(int i, float inv) const {   // of elements i .. i + 3
-        return f8_of((*this)[i] * inv, (*this)[i + 1] * inv, (*this)[i + 2] * inv, (*this)[i + 3] * inv);
+    // Largest |x| by its bits, with what `top` holds (two 16-bit maxima for bf16): numbers that are not finite come out on top.
+    __device__ __forceinline__ unsigned top(unsigned top) const {
+#pragma unroll
+        for (int i = 0; i < W; ++i) {
+            if constexpr (BF16) top = __builtin_bit_cast(unsigned, __builtin_elementwise_max(__builtin_bit_cast(u16x2, top), __builtin_bit_cast(u16x2, w[i] & 0x7FFF7FFFu)));
+            else top = max(top, w[i] & 0x7FFFFFFFu);
+        }
+        return top;
+    }
+    // Codes of elements i .. i + 3: the conversion instructions divide by a power of two and round to nearest, ties to even (what
+    // goes beyond 464 becomes no number; here nothing goes beyond 448).
+    __device__ __forceinline__ unsigned codes(int i, float scale) const {
+        s16x2 r = {0, 0};
+        if constexpr (BF16) {
+            r = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(r, __builtin_bit_cast(bf16x2, w[i / 2]), scale, false);
+            r = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(r, __builtin_bit_cast(bf16x2, w[i / 2 + 1]), scale, true);
+        } else {
+            r = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(r, (*this)[i], (*this)[i + 1], scale, false);
+            r = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(r, (*this)[i + 2], (*this)[i + 3], scale, true);
+        }
+        return __builtin_bit_cast(unsigned, r);
     }
 };
+// The wavefront's largest |x| from its lanes' tops; true: some number is not finite.
+template <bool BF16>
+__device__ __forceinline__ bool wave_top(unsigned top, float &amax) {
+    if constexpr (BF16) top = max(top & 0xFFFFu, top >> 16) << 16;
+    top = (unsigned)__builtin_amdgcn_readlane((int)wave_max_last(top), 63);
+    amax = __uint_as_float(top);
+    return top >= 0x7F800000u;
+}
 // Codes carried over to a scale 1 / ratio times as large.
 __device__ __forceinline__ unsigned rescaled(unsigned w, float ratio) {
     return f8_of(__builtin_amdgcn_cvt_f32_fp8((int)w, 0) * ratio, __builtin_amdgcn_cvt_f32_fp8((int)w, 1) * ratio,
@@ -329,6 +353,31 @@ __device__ __forceinline__ void transpose4(unsigned (&w)[4]) {
 }
 __device__ __forceinline__ float wave_max(float x) {   // of numbers that are not negative
     return __uint_as_float((unsigned)__builtin_amdgcn_readlane((int)wave_max_last(__float_as_uint(x)), 63));
+}
+// Rows o .. e - 1 of a page where some number is not finite, one after the other.
+template <bool BF16, int D>
+__device__ __forceinline__ void write_odd_run(const char *row0, int64_t pitch, int o, int e, bool is_v, uint8_t *cell0, int page_bytes,
+                                              float old_scale, float *scale_out) {
+    const int lane = threadIdx.x & 63;
+    auto at = [&](int r, int c) {
+        const char *p = row0 + r * pitch;
+        if constexpr (BF16) return bf16_bits_to_f32(((const unsigned short *)p)[c]);
+        else return ((const float *)p)[c];
+    };
+    float amax = 0.0f;
+    for (int r = o; r < e; ++r)
+        for (int c = lane; c < D; c += 64) amax = fmaxf(amax, finite_abs(at(r, c)));
+    const float scale = fmaxf(pow2(scale_exp(wave_max(amax))), old_scale), inv = 1.0f / scale, ratio = old_scale * inv;
+    if (o > 0 && ratio < 1.0f) {
+        for (int i = lane; i < page_bytes / 4; i += 64) ((unsigned *)cell0)[i] = rescaled(((unsigned *)cell0)[i], ratio);
+        __threadfence();   // before other lanes' new codes go to the same words
+    }
+    for (int r = o; r < e; ++r)
+        for (int c = lane; c < D; c += 64) {
+            const float x = at(r, c) * inv;
+            cell0[((r >> 4) * (D / 16) + (c >> 4)) * 256 + (is_v ? (c & 15) * 16 + (r & 15) : (r & 15) * 16 + (c & 15))] = (uint8_t)f8_of(x, x, x, x);
+        }
+    if (lane == 0) *scale_out = scale;
 }
 
 // A wavefront looks at `chunk` rows of one head of K or V and writes the runs that begin there, each held in registers between
@@ -374,7 +423,8 @@ __global__ __launch_bounds__(256, BF16 ? 3 : 2) void write_kernel(View Kn, View 
         uint8_t *cell0 = codes + ph * (size_t)(D * P);
         const float old_scale = o > 0 ? scales[ph] : 0.0f;
         const char *row0 = xh + (int64_t)(t0 - o) * x.row;   // of offset 0
-        float amax = 0.0f;
+        unsigned top = 0;
+        float amax;
         if (!is_v) {
             constexpr int LPR = D / 8, RPI = 64 / LPR, IT = P / RPI;
             const int lr = lane / LPR, lc = lane % LPR;
@@ -386,17 +436,18 @@ __global__ __launch_bounds__(256, BF16 ? 3 : 2) void write_kernel(View Kn, View 
                     v[i].load(row0 + ((unsigned)min(max(i * RPI + lr, o), e - 1) * pitch + (unsigned)(lc * 8 * ELT)));
             }
 #pragma unroll
-            for (int i = 0; i < IT; ++i)
-#pragma unroll
-                for (int c = 0; c < 8; ++c) amax = fmaxf(amax, finite_abs(v[i][c]));
-            const float scale = fmaxf(pow2(scale_exp(wave_max(amax))), old_scale), inv = 1.0f / scale, ratio = old_scale * inv;
+            for (int i = 0; i < IT; ++i) top = v[i].top(top);
+            if (wave_top<BF16>(top, amax)) {
+                write_odd_run<BF16, D>(row0, x.row, o, e, is_v, cell0, D * P, old_scale, scales + ph);
+                continue;
+            }
+            const float scale = fmaxf(pow2(scale_exp(amax)), old_scale), ratio = old_scale / scale;
 #pragma unroll
             for (int i = 0; i < IT; ++i) {
                 const int r = i * RPI + lr;
                 u32x2 *p = (u32x2 *)(cell0 + ((r >> 4) * DB + (lc >> 1)) * 256 + (r & 15) * 16 + (lc & 1) * 8);
                 if (r >= o && r < e) {
-                    v[i].hold();
-                    *p = u32x2{v[i].codes(0, inv), v[i].codes(4, inv)};
+                    *p = u32x2{v[i].codes(0, scale), v[i].codes(4, scale)};
                 } else if (o > 0 && ratio < 1.0f) {
                     const u32x2 w = *p;
                     *p = u32x2{rescaled(w[0], ratio), rescaled(w[1], ratio)};
@@ -428,10 +479,12 @@ __global__ __launch_bounds__(256, BF16 ? 3 : 2) void write_kernel(View Kn, View 
 #pragma unroll
             for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
-                for (int i = 0; i < 16; ++i)
-#pragma unroll
-                    for (int c = 0; c < 4; ++c) amax = fmaxf(amax, finite_abs(v[nb][i][c]));
-            const float scale = fmaxf(pow2(scale_exp(wave_max(amax))), old_scale), inv = 1.0f / scale, ratio = old_scale * inv;
+                for (int i = 0; i < 16; ++i) top = v[nb][i].top(top);
+            if (wave_top<BF16>(top, amax)) {
+                write_odd_run<BF16, D>(row0, x.row, o, e, is_v, cell0, D * P, old_scale, scales + ph);
+                continue;
+            }
+            const float scale = fmaxf(pow2(scale_exp(amax)), old_scale), ratio = old_scale / scale;
             const bool grows = o > 0 && ratio < 1.0f;
 #pragma unroll
             for (int nb = 0; nb < NB; ++nb) {
@@ -445,10 +498,7 @@ __global__ __launch_bounds__(256, BF16 ? 3 : 2) void write_kernel(View Kn, View 
                 for (int q = 0; q < 4; ++q) {
                     unsigned w[4];
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        v[nb][4 * q + i].hold();
-                        w[i] = v[nb][4 * q + i].codes(0, inv);   // of a row; its four coordinates
-                    }
+                    for (int i = 0; i < 4; ++i) w[i] = v[nb][4 * q + i].codes(0, scale);   // of a row; its four coordinates
                     __builtin_amdgcn_sched_barrier(0);   // four rows at a time: all at once they would not fit the registers
                     transpose4(w);
 #pragma unroll
