@@ -286,7 +286,9 @@ struct Piece {
     static constexpr int W = EPL * (BF16 ? 2 : 4) / 4;
     unsigned w[W];
     __device__ __forceinline__ void load(const char *p) {
-        if constexpr (W == 2) {
+        if constexpr (W == 1) {
+            w[0] = *(const unsigned *)p;
+        } else if constexpr (W == 2) {
             const u32x2 x = *(const u32x2 *)p;
             w[0] = x[0], w[1] = x[1];
         } else {
@@ -297,10 +299,6 @@ struct Piece {
                 for (int e = 0; e < 4; ++e) w[4 * q + e] = x[e];
             }
         }
-    }
-    __device__ __forceinline__ void clear() {
-#pragma unroll
-        for (int i = 0; i < W; ++i) w[i] = 0;
     }
     __device__ __forceinline__ float operator[](int i) const {
         if constexpr (BF16) return i & 1 ? bf16_hi(w[i / 2]) : bf16_lo(w[i / 2]);
@@ -315,41 +313,19 @@ struct Piece {
         }
         return top;
     }
-    // Codes of elements i .. i + 3: the conversion instructions divide by a power of two and round to nearest, ties to even (what
-    // goes beyond 464 becomes no number; here nothing goes beyond 448).
-    __device__ __forceinline__ unsigned codes(int i, float scale) const {
-        s16x2 r = {0, 0};
-        if constexpr (BF16) {
-            r = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(r, __builtin_bit_cast(bf16x2, w[i / 2]), scale, false);
-            r = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(r, __builtin_bit_cast(bf16x2, w[i / 2 + 1]), scale, true);
-        } else {
-            r = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(r, (*this)[i], (*this)[i + 1], scale, false);
-            r = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(r, (*this)[i + 2], (*this)[i + 3], scale, true);
-        }
-        return __builtin_bit_cast(unsigned, r);
+    // Codes of elements i, i + 1, in the lower or the upper half of r: the conversion instructions divide by a power of two and round
+    // to nearest, ties to even (what goes beyond 464 becomes no number; here nothing goes beyond 448).
+    template <bool UPPER>
+    __device__ __forceinline__ void codes(int i, float scale, unsigned &r) const {
+        const s16x2 old = __builtin_bit_cast(s16x2, r);
+        if constexpr (BF16) r = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(old, __builtin_bit_cast(bf16x2, w[i / 2]), scale, UPPER));
+        else r = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(old, (*this)[i], (*this)[i + 1], scale, UPPER));
     }
 };
-// The wavefront's largest |x| from its lanes' tops; true: some number is not finite.
-template <bool BF16>
-__device__ __forceinline__ bool wave_top(unsigned top, float &amax) {
-    if constexpr (BF16) top = max(top & 0xFFFFu, top >> 16) << 16;
-    top = (unsigned)__builtin_amdgcn_readlane((int)wave_max_last(top), 63);
-    amax = __uint_as_float(top);
-    return top >= 0x7F800000u;
-}
 // Codes carried over to a scale 1 / ratio times as large.
 __device__ __forceinline__ unsigned rescaled(unsigned w, float ratio) {
     return f8_of(__builtin_amdgcn_cvt_f32_fp8((int)w, 0) * ratio, __builtin_amdgcn_cvt_f32_fp8((int)w, 1) * ratio,
                  __builtin_amdgcn_cvt_f32_fp8((int)w, 2) * ratio, __builtin_amdgcn_cvt_f32_fp8((int)w, 3) * ratio);
-}
-// Exchanges bytes among four words: word i of the result holds byte i of the four.
-__device__ __forceinline__ void transpose4(unsigned (&w)[4]) {
-    const unsigned a = __builtin_amdgcn_perm(w[1], w[0], 0x05010400u), b = __builtin_amdgcn_perm(w[1], w[0], 0x07030602u);   // 0: w0.0 w1.0 w0.1 w1.1
-    const unsigned c = __builtin_amdgcn_perm(w[3], w[2], 0x05010400u), d = __builtin_amdgcn_perm(w[3], w[2], 0x07030602u);
-    w[0] = __builtin_amdgcn_perm(c, a, 0x05040100u);
-    w[1] = __builtin_amdgcn_perm(c, a, 0x07060302u);
-    w[2] = __builtin_amdgcn_perm(d, b, 0x05040100u);
-    w[3] = __builtin_amdgcn_perm(d, b, 0x07060302u);
 }
 __device__ __forceinline__ float wave_max(float x) {   // of numbers that are not negative
     return __uint_as_float((unsigned)__builtin_amdgcn_readlane((int)wave_max_last(__float_as_uint(x)), 63));
@@ -380,20 +356,21 @@ __device__ __forceinline__ void write_odd_run(const char *row0, int64_t pitch, i
     if (lane == 0) *scale_out = scale;
 }
 
-// A wavefront looks at `chunk` rows of one head of K or V and writes the runs that begin there, each held in registers between
-// its maximum and its codes.  Bound by memory: every row is read once and every code written once; a lane's pieces are chosen for
-// whole cells.  K: 8 coordinates of a row per lane (their 8 codes lie together).  V: 4 coordinates of 16 rows per lane, so that
-// their codes, exchanged within the lane, are 16 consecutive bytes per coordinate, with no trip through LDS.
+// A workgroup looks at `chunk` rows of one head of K or V and writes the runs that begin there, a wavefront for every 16 tokens of
+// a page, whose rows stay in registers between the run's maximum and the codes.  Bound by memory: every row is read once and every
+// code written once, in whole lines: K by rows, whose halves of a cell's 16 bytes neighbouring lanes exchange; V two coordinates of
+// every row per lane, whose codes over the rows are the lane's 32 consecutive bytes of the page (d = 64: twice 8), exchanged within
+// the lane.  (A wavefront per page and tensor with 64 registers of data, K in pieces of 64 bytes, V of 16: 76 us where this is
+// WRITEPROMPT; a third of the wavefronts were resident, and they read and wrote in turn.)
 template <bool BF16, int D, int PSHIFT>
-__global__ __launch_bounds__(256, BF16 ? 3 : 2) void write_kernel(View Kn, View Vn, const int32_t *__restrict__ slot, int n_tok, int chunk,
-                                                    fastar_pages pg) {
-    constexpr int P = 1 << PSHIFT, ELT = BF16 ? 2 : 4, DB = D / 16;
-    const int lane = threadIdx.x & 63;
-    const int unit = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int h = unit % pg.Hkv, rest = unit / pg.Hkv;
+__global__ __launch_bounds__(4 << PSHIFT) void write_kernel(View Kn, View Vn, const int32_t *__restrict__ slot, int n_tok, int chunk,
+                                                            fastar_pages pg) {
+    constexpr int P = 1 << PSHIFT, ELT = BF16 ? 2 : 4, NW = P / 16;
+    __shared__ unsigned s_top[2][NW];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int h = blockIdx.x % pg.Hkv, rest = blockIdx.x / pg.Hkv;
     const bool is_v = rest & 1;
     const int first = (rest >> 1) * chunk;
-    if (first >= n_tok) return;
     const View x = is_v ? Vn : Kn;
     const char *xh = x.p + h * x.head;
     uint8_t *codes = is_v ? pg.V8 : pg.K8;
@@ -413,118 +390,126 @@ __global__ __launch_bounds__(256, BF16 ? 3 : 2) void write_kernel(View Kn, View 
     const unsigned long long go0 = __ballot(ok0 && (s0 & (P - 1)) && p0 == s0 - 1), go1 = __ballot(ok1 && (s1 & (P - 1)) && p1 == s1 - 1);
     unsigned long long begin = valid & ~go0;
     if (chunk < 64) begin &= (1ull << chunk) - 1ull;
-    for (; begin; begin &= begin - 1ull) {   // uniform
+    for (int turn = 0; begin; begin &= begin - 1ull, turn ^= 1) {   // uniform over the workgroup
         const int pos = __builtin_ctzll(begin);
         const unsigned long long after = pos == 63 ? go1 : (go0 >> (pos + 1)) | (go1 << (63 - pos));   // bit i: row pos + 1 + i goes on
         const int n = 1 + (~after ? __builtin_ctzll(~after) : 63);   // at most P: a run ends with its page
         const int t0 = first + pos, sl = __builtin_amdgcn_readlane(s0, pos);
         const int page = sl >> PSHIFT, o = sl & (P - 1), e = o + n;
         const size_t ph = (size_t)page * pg.Hkv + h;
-        uint8_t *cell0 = codes + ph * (size_t)(D * P);
+        uint8_t *page0 = codes + ph * (size_t)(D * P), *blk = page0 + wave * (16 * D);
         const float old_scale = o > 0 ? scales[ph] : 0.0f;
         const char *row0 = xh + (int64_t)(t0 - o) * x.row;   // of offset 0
+        const int r0 = 16 * wave;
+        const bool touches = r0 < e && r0 + 16 > o, all = r0 >= o && r0 + 16 <= e;   // rows of the run among the wavefront's 16
+        auto row_of = [&](int r) { return row0 + (unsigned)min(max(r0 + r, o), e - 1) * pitch; };   // rows beside the run: one of its own again
+        // K: row i RPI + lr, coordinates 8 lc .. ; V: rows VR g .., coordinates 2 c
+        constexpr int LPR = D / 8, RPI = 64 / LPR, IT = 16 / RPI, VL = D / 2, VR = 16 * VL / 64;
+        const int lr = lane / LPR, lc = lane % LPR, vc = lane % VL, vg = lane / VL;
+        Piece<BF16, 8> k[IT];
+        Piece<BF16, 2> v[VR];
+        u32x2 old[4];   // of V: what is there of a block that the run covers in part
+        u32x2 *vp = (u32x2 *)(blk + vc * 32 + vg * VR);   // a coordinate's VR bytes; the next one's are 16 bytes on
+        auto vword = [&](int i) -> u32x2 & { return D == 128 ? vp[i] : vp[2 * i]; };   // 8 bytes: D = 128: two per coordinate
+        constexpr int VW = VR / 4;   // such words: 4 or 2
         unsigned top = 0;
-        float amax;
+        if (touches) {
+            if (!is_v) {
+#pragma unroll
+                for (int i = 0; i < IT; ++i) k[i].load(row_of(i * RPI + lr) + lc * 8 * ELT);
+#pragma unroll
+                for (int i = 0; i < IT; ++i) top = k[i].top(top);
+            } else {
+#pragma unroll
+                for (int i = 0; i < VR; ++i) v[i].load(row_of(vg * VR + i) + vc * 2 * ELT);
+                if (!all) {
+#pragma unroll
+                    for (int i = 0; i < VW; ++i) old[i] = vword(i);
+                }
+#pragma unroll
+                for (int i = 0; i < VR; ++i) top = v[i].top(top);
+            }
+        }
+        if constexpr (BF16) top = max(top & 0xFFFFu, top >> 16) << 16;
+        top = (unsigned)__builtin_amdgcn_readlane((int)wave_max_last(top), 63);
+        if constexpr (NW > 1) {
+            if (lane == 0) s_top[turn][wave] = top;
+            __syncthreads();   // the other half of s_top is free by the next one
+#pragma unroll
+            for (int i = 0; i < NW; ++i) top = max(top, s_top[turn][i]);
+        }
+        if (top >= 0x7F800000u) {   // some number is not finite
+            if (wave == 0) write_odd_run<BF16, D>(row0, x.row, o, e, is_v, page0, D * P, old_scale, scales + ph);
+            continue;
+        }
+        const float scale = fmaxf(pow2(scale_exp(__uint_as_float(top))), old_scale), ratio = old_scale / scale;
+        const bool grows = o > 0 && ratio < 1.0f;
+        if (lane == 0 && wave == 0) scales[ph] = scale;
+        if (!touches && !grows) continue;
         if (!is_v) {
-            constexpr int LPR = D / 8, RPI = 64 / LPR, IT = P / RPI;
-            const int lr = lane / LPR, lc = lane % LPR;
-            Piece<BF16, 8> v[IT];
+            u32x2 c[IT];
 #pragma unroll
             for (int i = 0; i < IT; ++i) {
-                v[i].clear();
-                if (i * RPI < e && (i + 1) * RPI > o)   // uniform; rows beside the run: one of its own again
-                    v[i].load(row0 + ((unsigned)min(max(i * RPI + lr, o), e - 1) * pitch + (unsigned)(lc * 8 * ELT)));
+                unsigned w0 = 0, w1 = 0;
+                k[i].template codes<false>(0, scale, w0);
+                k[i].template codes<true>(2, scale, w0);
+                k[i].template codes<false>(4, scale, w1);
+                k[i].template codes<true>(6, scale, w1);
+                c[i] = u32x2{w0, w1};
             }
 #pragma unroll
-            for (int i = 0; i < IT; ++i) top = v[i].top(top);
-            if (wave_top<BF16>(top, amax)) {
-                write_odd_run<BF16, D>(row0, x.row, o, e, is_v, cell0, D * P, old_scale, scales + ph);
-                continue;
-            }
-            const float scale = fmaxf(pow2(scale_exp(amax)), old_scale), ratio = old_scale / scale;
+            for (int i = 0; i < IT; i += 2) {   // even lanes take row i of the pair's cell, odd ones row i + 1
+                const bool odd = lane & 1;
+                const u32x2 give = odd ? c[i] : c[i + 1], keep = odd ? c[i + 1] : c[i];
+                const u32x2 got = {lane_of_eight<0>(give[0]), lane_of_eight<0>(give[1])};
+                const int r = (i + (odd ? 1 : 0)) * RPI + lr;
+                u32x4 y = odd ? u32x4{got[0], got[1], keep[0], keep[1]} : u32x4{keep[0], keep[1], got[0], got[1]};
+                u32x4 *p = (u32x4 *)(blk + (lc >> 1) * 256 + r * 16);
+                const bool mine = r0 + r >= o && r0 + r < e;
+                if (!mine && grows) {
+                    y = *p;
 #pragma unroll
-            for (int i = 0; i < IT; ++i) {
-                const int r = i * RPI + lr;
-                u32x2 *p = (u32x2 *)(cell0 + ((r >> 4) * DB + (lc >> 1)) * 256 + (r & 15) * 16 + (lc & 1) * 8);
-                if (r >= o && r < e) {
-                    *p = u32x2{v[i].codes(0, scale), v[i].codes(4, scale)};
-                } else if (o > 0 && ratio < 1.0f) {
-                    const u32x2 w = *p;
-                    *p = u32x2{rescaled(w[0], ratio), rescaled(w[1], ratio)};
+                    for (int q = 0; q < 4; ++q) y[q] = rescaled(y[q], ratio);
                 }
-                __builtin_amdgcn_sched_barrier(0);
+                if (mine || grows) *p = y;
             }
-            if (lane == 0) scales[ph] = scale;
         } else {
-            constexpr int LPR = D / 4, G = 64 / LPR, NB = (P / 16 + G - 1) / G;   // lanes per row, blocks of 16 rows side by side, and one after the other
-            const int lc = lane % LPR, gi = lane / LPR;
-            Piece<BF16, 4> v[NB][16];
-            u32x4 old[4];   // what is there of the one block that a short run lies in, asked for along with its rows
-            const bool one_block = n < 16 && (o >> 4) == ((e - 1) >> 4);
+            unsigned c[VR / 2];   // of rows 2 i, 2 i + 1: codes of the two coordinates
 #pragma unroll
-            for (int nb = 0; nb < NB; ++nb) {
-                const int r0 = 16 * (nb * G + gi);
-#pragma unroll
-                for (int i = 0; i < 16; ++i) v[nb][i].clear();
-                if (r0 < e && r0 + 16 > o) {
-#pragma unroll
-                    for (int i = 0; i < 16; ++i)   // rows beside the run: one of its own again
-                        v[nb][i].load(row0 + ((unsigned)min(max(r0 + i, o), e - 1) * pitch + (unsigned)(lc * 4 * ELT)));
-                }
+            for (int i = 0; i < VR / 2; ++i) {
+                c[i] = 0;
+                v[2 * i].template codes<false>(0, scale, c[i]);
+                v[2 * i + 1].template codes<true>(0, scale, c[i]);
             }
-            if (one_block && gi == (o >> 4) % G) {
+            u32x2 y[VW];   // coordinate by coordinate, four rows a word
 #pragma unroll
-                for (int c = 0; c < 4; ++c) old[c] = *(const u32x4 *)(cell0 + ((o >> 4) * DB + (lc >> 2)) * 256 + (4 * (lc & 3) + c) * 16);
-            }
+            for (int co = 0; co < 2; ++co)
 #pragma unroll
-            for (int nb = 0; nb < NB; ++nb)
+                for (int q = 0; q < VR / 4; ++q)
+                    y[(co * (VR / 4) + q) / 2][(co * (VR / 4) + q) % 2] = __builtin_amdgcn_perm(c[2 * q + 1], c[2 * q], co ? 0x07050301u : 0x06040200u);
+            if (!all) {
 #pragma unroll
-                for (int i = 0; i < 16; ++i) top = v[nb][i].top(top);
-            if (wave_top<BF16>(top, amax)) {
-                write_odd_run<BF16, D>(row0, x.row, o, e, is_v, cell0, D * P, old_scale, scales + ph);
-                continue;
-            }
-            const float scale = fmaxf(pow2(scale_exp(amax)), old_scale), ratio = old_scale / scale;
-            const bool grows = o > 0 && ratio < 1.0f;
+                for (int i = 0; i < VW; ++i) {
+                    u32x2 w = touches ? old[i] : vword(i);
 #pragma unroll
-            for (int nb = 0; nb < NB; ++nb) {
-                const int r0 = 16 * (nb * G + gi);
-                if (r0 >= P) continue;
-                u32x4 *p = (u32x4 *)(cell0 + ((r0 >> 4) * DB + (lc >> 2)) * 256 + 4 * (lc & 3) * 16);
-                const bool touches = r0 < e && r0 + 16 > o;
-                if (!touches && !grows) continue;
-                u32x4 y[4];
+                    for (int j = 0; j < 2; ++j) {
+                        if (grows) w[j] = rescaled(w[j], ratio);
+                        const int row = r0 + vg * VR + ((2 * i + j) % (VR / 4)) * 4;   // of the word's first byte
+                        unsigned mask = 0;
 #pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                    unsigned w[4];
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) w[i] = v[nb][4 * q + i].codes(0, scale);   // of a row; its four coordinates
-                    __builtin_amdgcn_sched_barrier(0);   // four rows at a time: all at once they would not fit the registers
-                    transpose4(w);
-#pragma unroll
-                    for (int c = 0; c < 4; ++c) y[c][q] = w[c];
-                }
-                if (r0 < o || r0 + 16 > e) {   // rows of others on the block
-                    u32x4 mask;
-#pragma unroll
-                    for (int q = 0; q < 4; ++q) {
-                        mask[q] = 0u;
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) mask[q] |= r0 + 4 * q + i >= o && r0 + 4 * q + i < e ? 0xFFu << (8 * i) : 0u;
+                        for (int b = 0; b < 4; ++b) mask |= row + b >= o && row + b < e ? 0xFFu << (8 * b) : 0u;
+                        w[j] = touches ? (y[i][j] & mask) | (w[j] & ~mask) : w[j];
                     }
-#pragma unroll
-                    for (int c = 0; c < 4; ++c) {
-                        u32x4 w = one_block && touches ? old[c] : p[c];
-                        if (grows)
-#pragma unroll
-                            for (int q = 0; q < 4; ++q) w[q] = rescaled(w[q], ratio);
-                        y[c] = (y[c] & mask) | (w & ~mask);
-                    }
+                    y[i] = w;
                 }
-#pragma unroll
-                for (int c = 0; c < 4; ++c) p[c] = y[c];
             }
-            if (lane == 0) scales[ph] = scale;
+            if constexpr (D == 128) {
+                ((u32x4 *)vp)[0] = u32x4{y[0][0], y[0][1], y[1][0], y[1][1]};
+                ((u32x4 *)vp)[1] = u32x4{y[2][0], y[2][1], y[3][0], y[3][1]};
+            } else {
+#pragma unroll
+                for (int i = 0; i < VW; ++i) vword(i) = y[i];
+            }
         }
     }
 }
@@ -596,16 +581,16 @@ extern "C" int kv_pages_write(const fastar_pages *pages, const fastar_rows *K_ne
     if (n_tok == 0) return FASTAR_OK;
     if (!slot || !view_ok(K_new, elt) || !view_ok(V_new, elt)) return FASTAR_ERR_INVALID_ARG;
     if (K_new->row * elt > MAX_PITCH || V_new->row * elt > MAX_PITCH) return FASTAR_ERR_UNSUPPORTED;
-    // Rows per wavefront: a page's where that leaves the chip with enough wavefronts (sixteen per compute unit); fewer rows, down
-    // to one, so that the runs of single tokens are not done one after the other.
+    // Rows per workgroup: a page's where that makes enough of them; fewer, down to one, so that the runs of single tokens are not
+    // done one after the other.
     int chunk = pages->P;
     while (chunk > 1 && (int64_t)n_tok * pages->Hkv * 2 / chunk < 4096) chunk /= 2;
     const int64_t units = (int64_t)((n_tok + chunk - 1) / chunk) * pages->Hkv * 2;
-    if (units > INT32_MAX - 4) return FASTAR_ERR_UNSUPPORTED;
-    const dim3 grid((unsigned)((units + 3) / 4));
+    if (units > INT32_MAX) return FASTAR_ERR_UNSUPPORTED;
+    const dim3 grid((unsigned)units);
     const View k = view_of(K_new, elt), v = view_of(V_new, elt);
 #define FASTAR_WRITE(BF16, D, PSHIFT) \
-    hipLaunchKernelGGL((pages::write_kernel<BF16, D, PSHIFT>), grid, dim3(256), 0, (hipStream_t)stream, k, v, slot, n_tok, chunk, *pages)
+    hipLaunchKernelGGL((pages::write_kernel<BF16, D, PSHIFT>), grid, dim3(4 << PSHIFT), 0, (hipStream_t)stream, k, v, slot, n_tok, chunk, *pages)
 #define FASTAR_WRITE_P(BF16, D)                      \
     do {                                             \
         if (pages->P == 64) FASTAR_WRITE(BF16, D, 6); \
