@@ -56,30 +56,24 @@ __device__ __forceinline__ void wait_b(bf16x8 (&f)[2][DB]) {
     else
         asm volatile("s_waitcnt lgkmcnt(%4)" : "+v"(f[0][0]), "+v"(f[0][1]), "+v"(f[1][0]), "+v"(f[1][1]) : "n"(N));
 }
-// K operands of 32 keys; BASE = byte offset of the first row in the stage.
-template <int BASE, int KF>
-__device__ __forceinline__ void read_k(bf16x8 (&f)[KF], const unsigned (&kaddr)[KF]) {
-#pragma unroll
-    for (int s = 0; s < KF; ++s) f[s] = lds_read_b128<BASE>(kaddr[s]);
-}
-// The same from one address: that of operand s is exclusive or with 32 s.
+// K operands of 32 keys; BASE = byte offset of the first row in the stage.  The address of operand s is exclusive or with 32 s.
 template <int BASE, int KF>
 __device__ __forceinline__ void read_k(bf16x8 (&f)[KF], unsigned kaddr) {
 #pragma unroll
     for (int s = 0; s < KF; ++s) f[s] = lds_read_b128<BASE>(kaddr ^ (32 * s));
 }
-// V^T operands of 32 keys (two steps of 16) for the blocks of 32 columns.
+// V^T operands of 32 keys (two steps of 16) for the blocks of 32 columns; the address of block db is exclusive or with 64 db.
 template <int BASE, int ROWB, int DB>
-__device__ __forceinline__ void read_vt(s16x4 (&f)[2][DB][2], const unsigned (&vaddr)[DB]) {
+__device__ __forceinline__ void read_vt(s16x4 (&f)[2][DB][2], unsigned vaddr) {
 #pragma unroll
     for (int db = 0; db < DB; ++db) {
-        f[0][db][0] = lds_read_tr16<BASE>(vaddr[db]);
-        f[0][db][1] = lds_read_tr16<BASE + 8 * ROWB>(vaddr[db]);
+        f[0][db][0] = lds_read_tr16<BASE>(vaddr ^ (64 * db));
+        f[0][db][1] = lds_read_tr16<BASE + 8 * ROWB>(vaddr ^ (64 * db));
     }
 #pragma unroll
     for (int db = 0; db < DB; ++db) {
-        f[1][db][0] = lds_read_tr16<BASE + 16 * ROWB>(vaddr[db]);
-        f[1][db][1] = lds_read_tr16<BASE + 24 * ROWB>(vaddr[db]);
+        f[1][db][0] = lds_read_tr16<BASE + 16 * ROWB>(vaddr ^ (64 * db));
+        f[1][db][1] = lds_read_tr16<BASE + 24 * ROWB>(vaddr ^ (64 * db));
     }
 }
 template <int DB>

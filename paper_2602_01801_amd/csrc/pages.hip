@@ -360,8 +360,8 @@ __device__ __forceinline__ void write_odd_run(const char *row0, int64_t pitch, i
 // a page, whose rows stay in registers between the run's maximum and the codes.  Bound by memory: every row is read once and every
 // code written once, in whole lines: K by rows, whose halves of a cell's 16 bytes neighbouring lanes exchange; V two coordinates of
 // every row per lane, whose codes over the rows are the lane's 32 consecutive bytes of the page (d = 64: twice 8), exchanged within
-// the lane.  (A wavefront per page and tensor with 64 registers of data, K in pieces of 64 bytes, V of 16: 76 us where this is
-// WRITEPROMPT; a third of the wavefronts were resident, and they read and wrote in turn.)
+// the lane.  (A wavefront per page and tensor with 64 registers of data, K in pieces of 64 bytes, V of 16: 76 us where this takes
+// 43 for 34612 tokens x 8 heads; a third of the wavefronts were resident, and they read and wrote in turn.)
 template <bool BF16, int D, int PSHIFT>
 __global__ __launch_bounds__(4 << PSHIFT) void write_kernel(View Kn, View Vn, const int32_t *__restrict__ slot, int n_tok, int chunk,
                                                             fastar_pages pg) {

@@ -6,12 +6,16 @@
 // that a row's softmax stays in two lanes and P^T is a matrix operand as the score registers hold it.  K and V go straight from
 // global memory into LDS (one copy for all eight wavefronts; 16-byte chunks permuted within a row so that operand reads meet no
 // bank twice), K is read as it is, V through the transposing LDS read.
+// Launches of few workgroups (SPLIT): 128 rows each, four wavefronts for either half of their keys, put together at the end.
 //
 // Schedule: a SIMD runs matrix instructions of one wavefront beside vector instructions of another, so the wavefronts of a SIMD
 // are kept half a tile apart.  Wavefronts 0..3 and 4..7 are two groups that take turns, a barrier per half step:
 //     X(t): O += P(t-1) V(t-1), then S(t) = K(t) Q^T       (matrix instructions)
 //     Y(t): loads of tile t+2, softmax of S(t) -> P(t)      (vector instructions)
 // Three stages of K and four of V make room for tiles that one group still reads while the other has asked for the next ones.
+// What bounds it: 3300 cycles per tile and pair of wavefronts, 2048 of them matrix instructions, at the 1.6 to 1.7 GHz that the chip
+// holds under it (matrix instructions alone reach 1.73 PFLOP/s on such data): 32760 tokens x 12 heads on 4 key heads, causal,
+// 2.84 ms = 1.16 PFLOP/s.  Short sequences add 5 us of a workgroup's ends (lengths, queries and first tiles 2.5, output 1.2).
 #include "attn_lds.hpp"
 #include "packed.hpp"
 
@@ -25,8 +29,13 @@ using namespace attn_lds;
 
 constexpr int TK = 64;         // keys per tile
 constexpr int NWG = 4;         // wavefronts per group
-constexpr int R = 256;         // rows per workgroup
-constexpr int NK = 3, NV = 4;  // stages
+// Stages of K and of V: shared by both groups, or of each group's own.
+constexpr int NK = 3, NV = 4, OWN_STAGES = 2;
+// Workgroups of 256 rows up to which 128 rows take a workgroup, whose two groups share their tiles: as many of them as compute
+// units; causal ones up to twice that, since the first half of the rows has a quarter of the work.  256 / 128 rows, 12 heads of 128:
+// 60 workgroups (1000 tokens, causal) 32.9 / 23.3 us, 156 (3000) 75.8 / 52.1, 240 (4680) 117 / 88, not causal 140 / 163; 392 (40 heads on
+// 8, 2 x 1200, causal) 49 / 63.
+constexpr int SPLIT_ITEMS = 128;
 constexpr float LN2 = 0.6931471805599453f;
 
 struct Args {
@@ -37,16 +46,18 @@ struct Args {
     float *lse;
 };
 
-template <int D>
+template <int D, bool SPLIT>
 __global__ __launch_bounds__(2 * NWG * 64, 1) void attn_bf16_kernel(const Args a) {
     extern __shared__ __attribute__((aligned(1024))) unsigned char lds[];   // [K stages][V stages]
     constexpr int KF = D / 16, DB = D / 32, ROWB = D * 2, TILEB = TK * ROWB;
-    constexpr int IPW = TILEB / 1024 / (2 * NWG);   // direct loads of 1 KiB per wavefront, tensor and tile
+    constexpr int OS_SPLIT = NWG * (DB * 4 + 1) * 1024;   // behind the sums that group 1 hands over
+    constexpr int R = SPLIT ? 128 : 256, NK = SPLIT ? OWN_STAGES : prompt::NK, NV = SPLIT ? OWN_STAGES : prompt::NV;
+    constexpr int IPW = TILEB / 1024 / (SPLIT ? NWG : 2 * NWG);   // direct loads of 1 KiB per wavefront, tensor and tile
     constexpr int RPI = 1024 / ROWB;                // rows that one of them brings
     constexpr int CPR = ROWB / 16;                  // 16-byte chunks per row
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int grp = wave / NWG;
+    const int grp = wave / NWG, part = SPLIT ? wave % NWG : wave;   // part: of the rows and of a tile's loads
     const int col = lane & 31, g = lane >> 5;
 
     // workgroup -> (sequence, tile of rows, head): sequences in order, of each the last rows first (they have the most keys),
@@ -58,8 +69,10 @@ __global__ __launch_bounds__(2 * NWG * 64, 1) void attn_bf16_kernel(const Args a
     const int n_rows = rq.n * a.group, n = rk.n;
     // keys that row r sees; rising with r
     auto sees = [&](int r) { return a.causal ? min(max(n - rq.n + min(r, n_rows - 1) / a.group + 1, 0), n) : n; };
-    const int nt = (sees(qt * R + R - 1) + TK - 1) / TK;     // tiles of the workgroup
-    const int row0 = qt * R + wave * 32;                     // rows of the wavefront
+    const int nt_all = (sees(qt * R + R - 1) + TK - 1) / TK;   // tiles of the workgroup; of this group: nt from t0 on
+    const int nt0 = SPLIT ? (nt_all + 1) / 2 : nt_all, nt1 = SPLIT ? nt_all - nt0 : nt_all;
+    const int nt = grp == 0 ? nt0 : nt1, t0 = SPLIT && grp == 1 ? nt0 : 0;
+    const int row0 = qt * R + part * 32;                       // rows of the wavefront
     const int limit_min = sees(row0);   // what its first row sees
     const int my_row = min(row0 + col, n_rows - 1);
     const int my_tok = my_row / a.group, my_head = h * a.group + my_row - my_tok * a.group;
@@ -81,14 +94,14 @@ __global__ __launch_bounds__(2 * NWG * 64, 1) void attn_bf16_kernel(const Args a
 
     // ---- tile loads: instruction i of this wavefront brings tile rows RPI (IPW wave + i) .., lane l row + l / CPR, chunk l % CPR
     // of LDS; which chunk of the row that is in global memory is permuted by the row
-    unsigned char *kbuf = lds, *vbuf = lds + NK * TILEB;
+    unsigned char *kbuf = lds + (SPLIT ? grp * 2 * OWN_STAGES * TILEB : 0), *vbuf = kbuf + NK * TILEB;
     const char *Kb = a.K.p + h * a.K.head + (int64_t)rk.first * a.K.row, *Vb = a.V.p + h * a.V.head + (int64_t)rk.first * a.V.row;
     auto swz_k = [](int row) { return D == 128 ? row & 15 : (row >> 1) & 7; };
     auto swz_v = [](int row) { return D == 128 ? (row & 7) << 1 : ((row >> 1) & 3) << 1; };
     unsigned koff[IPW], voff[IPW];
 #pragma unroll
     for (int i = 0; i < IPW; ++i) {
-        const int r = RPI * (IPW * wave + i) + lane / CPR;
+        const int r = RPI * (IPW * part + i) + lane / CPR;
         koff[i] = (unsigned)r * (unsigned)a.K.row + 16 * ((lane % CPR) ^ swz_k(r));
         voff[i] = (unsigned)r * (unsigned)a.V.row + 16 * ((lane % CPR) ^ swz_v(r));
     }
@@ -96,28 +109,25 @@ __global__ __launch_bounds__(2 * NWG * 64, 1) void attn_bf16_kernel(const Args a
         if (t * TK + TK <= n) {   // uniform
             const char *tile = base + (int64_t)t * TK * pitch;
 #pragma unroll
-            for (int i = 0; i < IPW; ++i) to_lds(tile, off[i], lds_address(dst) + (IPW * wave + i) * 1024);
+            for (int i = 0; i < IPW; ++i) to_lds(tile, off[i], lds_address(dst) + (IPW * part + i) * 1024);
         } else {
 #pragma unroll
             for (int i = 0; i < IPW; ++i) {   // rows past the end: key 0, which is seen wherever a key is
-                const int r = RPI * (IPW * wave + i) + lane / CPR;
-                to_lds(base + off[i] + (t * TK + r < n ? (int64_t)t * TK * pitch : -(int64_t)r * pitch), dst + (IPW * wave + i) * 1024);
+                const int r = RPI * (IPW * part + i) + lane / CPR;
+                to_lds(base + off[i] + (t * TK + r < n ? (int64_t)t * TK * pitch : -(int64_t)r * pitch), dst + (IPW * part + i) * 1024);
             }
         }
     };
-    auto issue_k = [&](int t) __attribute__((always_inline)) { if (t < nt) issue(Kb, a.K.row, koff, kbuf + (t % NK) * TILEB, t); };
-    auto issue_v = [&](int t) __attribute__((always_inline)) { if (t < nt) issue(Vb, a.V.row, voff, vbuf + (t % NV) * TILEB, t); };
+    auto issue_k = [&](int t) __attribute__((always_inline)) { if (t < nt) issue(Kb, a.K.row, koff, kbuf + (t % NK) * TILEB, t0 + t); };
+    auto issue_v = [&](int t) __attribute__((always_inline)) { if (t < nt) issue(Vb, a.V.row, voff, vbuf + (t % NV) * TILEB, t0 + t); };
 
     // per-lane LDS addresses of the operands
     const unsigned kbuf_lds = lds_address(kbuf), vbuf_lds = lds_address(vbuf);
-    unsigned kaddr[KF], vaddr[DB];
-#pragma unroll
-    for (int s = 0; s < KF; ++s) kaddr[s] = kbuf_lds + col * ROWB + (((2 * s + g) ^ swz_k(col)) << 4);
     const int s16 = lane & 15, l16 = lane >> 4;
     const int vrow = 4 * (l16 >> 1) + (s16 >> 2);
-#pragma unroll
-    for (int db = 0; db < DB; ++db)
-        vaddr[db] = vbuf_lds + vrow * ROWB + (((4 * db + 2 * (l16 & 1) + ((s16 & 3) >> 1)) ^ swz_v(vrow)) << 4) + (s16 & 1) * 8;
+    // K's first 16 coordinates (the s-th: exclusive or with 32 s), V's first 32 (the db-th: with 64 db)
+    unsigned kaddr = kbuf_lds + col * ROWB + ((g ^ swz_k(col)) << 4);
+    unsigned vaddr = vbuf_lds + vrow * ROWB + (((2 * (l16 & 1) + ((s16 & 3) >> 1)) ^ swz_v(vrow)) << 4) + (s16 & 1) * 8;
     int ks = 0, vs = 0;   // stages that kaddr and vaddr point into
 
     f32x16 s_acc[2];
@@ -135,10 +145,8 @@ __global__ __launch_bounds__(2 * NWG * 64, 1) void attn_bf16_kernel(const Args a
             pv_mfma(o, va, pf[0]);
             wait_v<QK ? KF : 0>(vb);
             pv_mfma(o, vb, pf[1]);
-            const int step = vs == NV - 1 ? -(NV - 1) * TILEB : TILEB;
+            vaddr += vs == NV - 1 ? -(NV - 1) * TILEB : TILEB;
             vs = vs == NV - 1 ? 0 : vs + 1;
-#pragma unroll
-            for (int db = 0; db < DB; ++db) vaddr[db] += step;
         }
         if constexpr (QK) {
             read_k<32 * ROWB>(kb, kaddr);
@@ -149,20 +157,18 @@ __global__ __launch_bounds__(2 * NWG * 64, 1) void attn_bf16_kernel(const Args a
             for (int s = 0; s < KF; ++s) s_acc[0] = mfma_bf16_32x32x16(ka[s], qf[s], s_acc[0]);
             wait_k<0>(kb);
             __builtin_amdgcn_sched_barrier(0);
-            const int step = ks == NK - 1 ? -(NK - 1) * TILEB : TILEB;
+            kaddr += ks == NK - 1 ? -(NK - 1) * TILEB : TILEB;
             ks = ks == NK - 1 ? 0 : ks + 1;
 #pragma unroll
-            for (int s = 0; s < KF; ++s) {
-                s_acc[1] = mfma_bf16_32x32x16(kb[s], qf[s], s_acc[1]);
-                kaddr[s] += step;
-            }
+            for (int s = 0; s < KF; ++s) s_acc[1] = mfma_bf16_32x32x16(kb[s], qf[s], s_acc[1]);
             __builtin_amdgcn_sched_barrier(0);
-            if (t * TK + TK > limit_min) {   // uniform: some row of the wavefront does not see some key of the tile
+            const int key0 = (t0 + t) * TK;
+            if (key0 + TK > limit_min) {   // uniform: some row of the wavefront does not see some key of the tile
 #pragma unroll
                 for (int hb = 0; hb < 2; ++hb)
 #pragma unroll
                     for (int v = 0; v < 16; ++v)
-                        if (t * TK + 32 * hb + 8 * (v >> 2) + 4 * g + (v & 3) >= limit) s_acc[hb][v] = -INFINITY;
+                        if (key0 + 32 * hb + 8 * (v >> 2) + 4 * g + (v & 3) >= limit) s_acc[hb][v] = -INFINITY;
             }
             float mx = s_acc[0][0];
 #pragma unroll
@@ -176,7 +182,7 @@ __global__ __launch_bounds__(2 * NWG * 64, 1) void attn_bf16_kernel(const Args a
     };
     auto phase_y = [&](int t) __attribute__((always_inline)) {
         issue_k(t + 2);
-        issue_v(t + 2);
+        issue_v(SPLIT ? t + 1 : t + 2);
         if (__any((mx_tile - m) * scale_log2 > 8.0f)) {   // the reference may lag the maximum by 8 octaves
             const float mn = fmaxf(m, mx_tile);
             const float alpha = m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f((m - mn) * scale_log2);
@@ -217,13 +223,22 @@ __global__ __launch_bounds__(2 * NWG * 64, 1) void attn_bf16_kernel(const Args a
     // Half steps: group 0 runs X(t) in half step 2t and Y(t) in 2t+1, group 1 one later.  K(t) is read in half steps 2t and 2t+1,
     // V(t) in 2t+1 .. 2t+3; Y(t) asks for K(t+2) (stage of K(t-1)) and V(t+2) (stage of V(t-2)), and what it asked for is
     // waited for before the barrier into Y(t+1): group 1's at the start of half step 2t+4, when K(t+2) is first read.
+    // SPLIT: a group reads only what it has asked for itself; Y(t) asks for K(t+2) (stage of K(t)) and V(t+1) (of V(t-1)), both of
+    // which X(t) was the last to read.
+    const int n_bar = max(nt0 > 0 ? 2 * nt0 + 1 : 0, nt1 > 0 ? 2 * nt1 + 2 : 1) + 1;   // barriers that every wavefront passes
+    int done = 0;
     if (nt > 0) {
         issue_k(0);
         issue_v(0);
         issue_k(1);
-        issue_v(1);
-        landed();
-        if (grp == 1) wg_barrier();
+        if constexpr (!SPLIT) issue_v(1);
+    }
+    landed();
+    if (grp == 1) {
+        wg_barrier();
+        ++done;
+    }
+    if (nt > 0) {
         phase_x(0, std::false_type{}, std::true_type{});
         for (int t = 0; t < nt - 1; ++t) {
             landed();
@@ -235,20 +250,49 @@ __global__ __launch_bounds__(2 * NWG * 64, 1) void attn_bf16_kernel(const Args a
         phase_y(nt - 1);
         wg_barrier();
         phase_x(nt, std::true_type{}, std::false_type{});
-        if (grp == 0) wg_barrier();
+        done += 2 * nt;
     }
+    for (++done; done < n_bar; ++done) wg_barrier();
 
     const float l_lane = l0 + l1;
-    const float l = l_lane + shfl_xor(l_lane, 32);
+    float l = l_lane + shfl_xor(l_lane, 32);
+    if constexpr (SPLIT) {   // group 1 hands its sums to group 0
+        __syncthreads();   // the tiles are dead
+        f32x4 *give = (f32x4 *)lds + (size_t)part * (DB * 4 + 1) * 64;
+        if (grp == 1) {
+#pragma unroll
+            for (int db = 0; db < DB; ++db)
+#pragma unroll
+                for (int q4 = 0; q4 < 4; ++q4) give[(db * 4 + q4) * 64 + lane] = f32x4{o[db][4 * q4], o[db][4 * q4 + 1], o[db][4 * q4 + 2], o[db][4 * q4 + 3]};
+            give[DB * 4 * 64 + lane] = f32x4{m, l, 0.0f, 0.0f};
+        }
+        __syncthreads();
+        if (grp == 1) return;
+        const f32x4 ml = give[DB * 4 * 64 + lane];
+        const float m_all = fmaxf(m, ml[0]);
+        const float w_mine = m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f((m - m_all) * scale_log2);
+        const float w_other = ml[0] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f((ml[0] - m_all) * scale_log2);
+        m = m_all;
+        l = l * w_mine + ml[1] * w_other;
+#pragma unroll
+        for (int db = 0; db < DB; ++db)
+#pragma unroll
+            for (int q4 = 0; q4 < 4; ++q4) {
+                const f32x4 x = give[(db * 4 + q4) * 64 + lane];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) o[db][4 * q4 + e] = o[db][4 * q4 + e] * w_mine + x[e] * w_other;
+            }
+    }
     const float inv = l == 0.0f ? 0.0f : 1.0f / l;
     bool odd = false;
 #pragma unroll
     for (int db = 0; db < DB; ++db)
 #pragma unroll
         for (int v = 0; v < 16; ++v) odd |= !(fabsf(o[db][v]) < INFINITY);
-    __syncthreads();   // the tiles are dead: their LDS takes the rows of the output, so that they are stored whole
+    // LDS takes the rows of the output, a wavefront's own each, so that they are stored whole
     constexpr int OSTR = D + 8;
-    unsigned short *Os = (unsigned short *)lds + (size_t)wave * 32 * OSTR;
+    unsigned short *Os = (unsigned short *)(lds + (SPLIT ? OS_SPLIT : 0)) + (size_t)part * 32 * OSTR;
+    if constexpr (!SPLIT) __syncthreads();   // the tiles are dead
 #pragma unroll
     for (int db = 0; db < DB; ++db)
 #pragma unroll
@@ -257,7 +301,7 @@ __global__ __launch_bounds__(2 * NWG * 64, 1) void attn_bf16_kernel(const Args a
                               (__bf16)(o[db][4 * q4 + 3] * inv)};
             *(bf16x4 *)(Os + col * OSTR + 32 * db + 8 * q4 + 4 * g) = w;
         }
-    __syncthreads();
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
 #pragma unroll
     for (int i = 0; i < 32 * CPR / 64; ++i) {
         const int r = i * (64 / CPR) + lane / CPR, rr = row0 + r;
@@ -283,18 +327,29 @@ __global__ __launch_bounds__(2 * NWG * 64, 1) void attn_bf16_kernel(const Args a
     }
 }
 
-template <int D>
-constexpr int lds_bytes() { return (NK + NV) * TK * D * 2; }
+template <int D, bool SPLIT>
+constexpr int lds_bytes() { return (SPLIT ? 4 * OWN_STAGES : NK + NV) * TK * D * 2; }
+static_assert(NWG * (4 * 4 + 1) * 1024 + NWG * 32 * (128 + 8) * 2 <= lds_bytes<128, true>() && NWG * (2 * 4 + 1) * 1024 + NWG * 32 * (64 + 8) * 2 <= lds_bytes<64, true>(),
+              "sums and rows fit");
+
+template <int D, bool SPLIT>
+int setup() {
+    return hipFuncSetAttribute((const void *)attn_bf16_kernel<D, SPLIT>, hipFuncAttributeMaxDynamicSharedMemorySize, lds_bytes<D, SPLIT>()) == hipSuccess ? FASTAR_OK : FASTAR_ERR_HIP;
+}
+template <int D, bool SPLIT>
+int launch(const Args &a, int64_t items, hipStream_t s) {
+    hipLaunchKernelGGL((attn_bf16_kernel<D, SPLIT>), dim3((unsigned)items), dim3(2 * NWG * 64), (lds_bytes<D, SPLIT>()), s, a);
+    FASTAR_LAUNCH_CHECK();
+    return FASTAR_OK;
+}
 
 }  // namespace prompt
 
 int prompt_setup() {
     static DeviceOnce once;
     return once.run([](int) {
-        if (hipFuncSetAttribute((const void *)prompt::attn_bf16_kernel<128>, hipFuncAttributeMaxDynamicSharedMemorySize,
-                                prompt::lds_bytes<128>()) != hipSuccess)
-            return FASTAR_ERR_HIP;
-        return FASTAR_OK;
+        const int rc = prompt::setup<128, false>();
+        return rc == FASTAR_OK ? prompt::setup<128, true>() : rc;
     });
 }
 
@@ -303,12 +358,11 @@ int launch_prompt_bf16(const View &Q, const View &K, const View &V, const int32_
     using namespace prompt;
     if (const int rc = prompt_setup(); rc != FASTAR_OK) return rc;
     const Args a = {Q, K, V, O, cu_q, cu_k, B, n_tok_q, n_tok_k, Hkv, Hq / Hkv, causal, scale_log2, lse};
-    const int64_t items = (((int64_t)n_tok_q * a.group + R - 1) / R + B) * Hkv;   // at most
-    if (items > INT32_MAX) return FASTAR_ERR_UNSUPPORTED;
-    if (d == 128) hipLaunchKernelGGL(attn_bf16_kernel<128>, dim3((unsigned)items), dim3(2 * NWG * 64), lds_bytes<128>(), s, a);
-    else hipLaunchKernelGGL(attn_bf16_kernel<64>, dim3((unsigned)items), dim3(2 * NWG * 64), lds_bytes<64>(), s, a);
-    FASTAR_LAUNCH_CHECK();
-    return FASTAR_OK;
+    auto items = [&](int rows) { return (((int64_t)n_tok_q * a.group + rows - 1) / rows + B) * Hkv; };   // at most
+    if (items(128) > INT32_MAX) return FASTAR_ERR_UNSUPPORTED;
+    const bool split = items(256) <= (causal ? 2 : 1) * SPLIT_ITEMS;
+    if (d == 128) return split ? launch<128, true>(a, items(128), s) : launch<128, false>(a, items(256), s);
+    return split ? launch<64, true>(a, items(128), s) : launch<64, false>(a, items(256), s);
 }
 
 }  // namespace fastar
