@@ -607,27 +607,27 @@ def sparse_attn_fwd_fp8(Q, K8, V8T, cnt, length, C: int, sel, nsel, BQ: int, BK:
 # ---------------------------------------------------------------------------------------------- several requests at a time
 
 
+# The checks below are what a call costs on the host, next to the foreign call itself: one condition each where all is well.
 def _rows(t: torch.Tensor, H: int, n: int, d: int, dtype) -> _RowsStruct:
     """A view [H, n, d] of any head and row strides."""
-    if t.dtype != dtype:
-        raise TypeError(f"expected {dtype}, got {t.dtype}")
-    if t.shape != (H, n, d) or not t.is_cuda or t.stride(2) != 1:
+    head, row, one = t.stride() if t.dim() == 3 else (0, 0, 0)
+    if one != 1 or t.dtype is not dtype or t.shape != (H, n, d) or not t.is_cuda:
+        if t.dtype != dtype:
+            raise TypeError(f"expected {dtype}, got {t.dtype}")
         raise ValueError(f"expected a device tensor [{H}, {n}, {d}] whose rows are contiguous, got {tuple(t.shape)}")
-    return _RowsStruct(t.data_ptr(), t.stride(0), t.stride(1))
+    return _RowsStruct(t.data_ptr(), head, row)
 
 
-def _ints(t: torch.Tensor, *shape):
-    if tuple(t.shape) != shape:
-        raise ValueError(f"expected shape {shape}, got {tuple(t.shape)}")
-    return _dev(t, torch.int32).data_ptr()
+def _ints(t: torch.Tensor, *shape, dtype=torch.int32) -> int:
+    if t.shape != shape or t.dtype is not dtype or not t.is_cuda or not t.is_contiguous():
+        if t.shape != shape:
+            raise ValueError(f"expected shape {shape}, got {tuple(t.shape)}")
+        _dev(t, dtype)
+    return t.data_ptr()
 
 
 def _lse_out(lse, Hq: int, n: int):
-    if lse is None:
-        return None
-    if tuple(lse.shape) != (Hq, n):
-        raise ValueError(f"lse must be [{Hq}, {n}]")
-    return _dev(lse, torch.float32).data_ptr()
+    return None if lse is None else _ints(lse, Hq, n, dtype=torch.float32)
 
 
 def _grouped(Q, Hkv: int):
@@ -678,11 +678,13 @@ class Pages:
         return n, H, 16 * pb, 16 * db
 
     def struct(self) -> _PagesStruct:
-        n, H, P, d = self.shape
-        if self.K8.shape[4:] != (16, 16) or self.V8.shape != self.K8.shape or self.kscale.shape != (n, H) or self.vscale.shape != (n, H):
+        K8, V8, ks, vs = self.K8, self.V8, self.kscale, self.vscale
+        shape = K8.shape
+        if len(shape) != 6 or shape[4:] != (16, 16) or V8.shape != shape or ks.shape != shape[:2] or vs.shape != shape[:2]:
             raise ValueError("K8 and V8 must be [n_pages, Hkv, P/16, d/16, 16, 16], kscale and vscale [n_pages, Hkv]")
-        _dev(self.K8, torch.uint8), _dev(self.V8, torch.uint8), _dev(self.kscale, torch.float32), _dev(self.vscale, torch.float32)
-        return _PagesStruct(self.K8.data_ptr(), self.V8.data_ptr(), self.kscale.data_ptr(), self.vscale.data_ptr(), n, H, P, d)
+        n, H, pb, db = shape[:4]
+        return _PagesStruct(_ints(K8, *shape, dtype=torch.uint8), _ints(V8, *shape, dtype=torch.uint8), _ints(ks, n, H, dtype=torch.float32),
+                            _ints(vs, n, H, dtype=torch.float32), n, H, 16 * pb, 16 * db)
 
     def nbytes(self) -> int:
         return sum(t.numel() * t.element_size() for t in (self.K8, self.V8, self.kscale, self.vscale))

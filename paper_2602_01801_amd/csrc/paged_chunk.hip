@@ -24,13 +24,14 @@ constexpr int R = 256;         // rows per item
 constexpr int NK = 3, NV = 4;  // stages
 constexpr int SHARES = 256;
 constexpr int LEAST = 8;       // tiles of a share at least: a fragment costs as much as some of them
+constexpr int FEW_KEYS = 512;  // longer ones are cut while items leave compute units idle (one item of 300 rows x 4 heads x 2000 keys: 72 us whole)
 constexpr int FRAG_FLOATS = R * 128 + 2 * R;
 static_assert(SHARES <= MAX_SHARES, "descriptors");
 
 template <int D>
 constexpr int lds_bytes() { return (NK + NV) * TK * D * 2; }
 
-template <int D>
+template <int D, bool SPLIT>
 __global__ __launch_bounds__(2 * NWG * 64, 1) void attn_chunk_kernel(const Args a) {
     extern __shared__ __attribute__((aligned(1024))) unsigned char lds[];   // [K stages: a row per key][V stages: a row per coordinate]
     constexpr int KF = D / 16, DB = D / 32, ROWB = D * 2, TILEB = TK * ROWB, VROWB = TK * 2, CPR = ROWB / 16;
@@ -57,19 +58,21 @@ __global__ __launch_bounds__(2 * NWG * 64, 1) void attn_chunk_kernel(const Args 
 
     Range r;
     Seq sq;
-    if (!first_unit<R, true>(a, SHARES, LEAST, r, sq)) {
-        if (tid == 0) a.desc[r.share].last = -1;
+    if (!first_unit<R, SPLIT>(a, SHARES, LEAST, r, sq)) {
+        if (SPLIT && tid == 0) a.desc[r.share].last = -1;
         return;
     }
     Desc d = {0, 0, 0, -1};
     while (r.u < r.u_end) {   // uniform: one piece of one item per turn
-        if (r.u >= r.base + (long long)sq.n_qt * Hkv * sq.n_tiles) find_unit<R, true>(a, r.u, r.b, r.base, sq);
+        if (SPLIT && r.u >= r.base + (long long)sq.n_qt * Hkv * sq.n_tiles) find_unit<R, SPLIT>(a, r.u, r.b, r.base, sq);
+        const int units = SPLIT ? sq.n_tiles : 1;
         const long long local = r.u - r.base;
-        const int item = (int)(local / sq.n_tiles);
+        const int item = (int)(local / units);
         const int h = item / sq.n_qt, qt = item - h * sq.n_qt;
-        const int ta = (int)(local - (long long)item * sq.n_tiles), te = (int)min((long long)sq.n_tiles, ta + (r.u_end - r.u));
-        const bool begins = ta == 0, ends = te == sq.n_tiles, whole = begins && ends;
-        r.u += te - ta;
+        const int ta = SPLIT ? (int)(local - (long long)item * units) : 0;
+        const int te = SPLIT ? (int)min((long long)units, ta + (r.u_end - r.u)) : sq.n_tiles;
+        const bool begins = ta == 0, ends = te == sq.n_tiles, whole = !SPLIT || (begins && ends);
+        r.u += SPLIT ? te - ta : 1;
 
         const int n_rows = sq.n_q * a.group;
         auto sees = [&](int x) {
@@ -352,9 +355,9 @@ __global__ __launch_bounds__(2 * NWG * 64, 1) void attn_chunk_kernel(const Args 
             }
         }
         __syncthreads();   // the next piece's tiles go where this one's rows were
-        if (begins && !ends) d = Desc{r.b, h, qt, share_of(r, r.base + (long long)(item + 1) * sq.n_tiles - 1)};
+        if (SPLIT && begins && !ends) d = Desc{r.b, h, qt, share_of(r, r.base + (long long)(item + 1) * units - 1)};
     }
-    if (tid == 0) a.desc[r.share] = d;
+    if (SPLIT && tid == 0) a.desc[r.share] = d;
 }
 
 // Puts the fragments of an item together: a workgroup per share, 32 rows and 32 coordinates; most find nothing to do.
@@ -370,9 +373,11 @@ __global__ __launch_bounds__(256) void combine_chunk_kernel(const Args a) {
     const int lane = threadIdx.x & 63, q4 = threadIdx.x >> 6, col = lane & 31, g = lane >> 5;
     const int first = blockIdx.x, n = d.last - first + 1;
     float m_all = -INFINITY;
+#pragma unroll 4
     for (int i = 0; i < n; ++i) m_all = fmaxf(m_all, fragment<FRAG_FLOATS>(a, first, i)[R * D + wave * 32 + col]);
     f32x4 x = {0.0f, 0.0f, 0.0f, 0.0f};
     float l = 0.0f;
+#pragma unroll 4
     for (int i = 0; i < n; ++i) {
         const float *f = fragment<FRAG_FLOATS>(a, first, i);
         const float wt = weight_of(f[R * D + wave * 32 + col], m_all, a.scale_log2);
@@ -395,30 +400,45 @@ __global__ __launch_bounds__(256) void combine_chunk_kernel(const Args a) {
 
 size_t paged_chunk_frag_bytes() { return (size_t)2 * paged::chunk::SHARES * paged::chunk::FRAG_FLOATS * 4; }
 
-int paged_chunk_setup() {
-    using namespace paged::chunk;
-    static DeviceOnce once;
-    return once.run([](int) {
-        return hipFuncSetAttribute((const void *)attn_chunk_kernel<128>, hipFuncAttributeMaxDynamicSharedMemorySize, lds_bytes<128>()) == hipSuccess
-                   ? FASTAR_OK
-                   : FASTAR_ERR_HIP;
-    });
-}
+namespace paged {
 
-int launch_paged_chunk(const paged::Args &a, hipStream_t s) {
-    using namespace paged::chunk;
-    if (const int rc = paged_chunk_setup(); rc != FASTAR_OK) return rc;
-    if (a.pg.d == 128) {
-        hipLaunchKernelGGL(attn_chunk_kernel<128>, dim3(SHARES), dim3(2 * NWG * 64), lds_bytes<128>(), s, a);
+namespace chunk {
+
+template <int D>
+int setup() {
+    for (const void *f : {(const void *)attn_chunk_kernel<D, true>, (const void *)attn_chunk_kernel<D, false>})
+        if (hipFuncSetAttribute(f, hipFuncAttributeMaxDynamicSharedMemorySize, lds_bytes<D>()) != hipSuccess) return FASTAR_ERR_HIP;
+    return FASTAR_OK;
+}
+template <int D>
+int launch(const Args &a, int64_t items, bool split, hipStream_t s) {
+    if (!split) {
+        hipLaunchKernelGGL((attn_chunk_kernel<D, false>), dim3((unsigned)items), dim3(2 * NWG * 64), lds_bytes<D>(), s, a);
         FASTAR_LAUNCH_CHECK();
-        hipLaunchKernelGGL(combine_chunk_kernel<128>, dim3(SHARES, 8 * 128 / 32), dim3(256), 0, s, a);
-    } else {
-        hipLaunchKernelGGL(attn_chunk_kernel<64>, dim3(SHARES), dim3(2 * NWG * 64), lds_bytes<64>(), s, a);
-        FASTAR_LAUNCH_CHECK();
-        hipLaunchKernelGGL(combine_chunk_kernel<64>, dim3(SHARES, 8 * 64 / 32), dim3(256), 0, s, a);
+        return FASTAR_OK;
     }
+    hipLaunchKernelGGL((attn_chunk_kernel<D, true>), dim3(SHARES), dim3(2 * NWG * 64), lds_bytes<D>(), s, a);
+    FASTAR_LAUNCH_CHECK();
+    hipLaunchKernelGGL(combine_chunk_kernel<D>, dim3(SHARES, 8 * D / 32), dim3(256), 0, s, a);
     FASTAR_LAUNCH_CHECK();
     return FASTAR_OK;
+}
+
+}  // namespace chunk
+
+}  // namespace paged
+
+int paged_chunk_setup() {
+    static DeviceOnce once;
+    return once.run([](int) { return paged::chunk::setup<128>(); });   // the tiles of d = 64 fit without
+}
+
+int launch_paged_chunk(const paged::Args &a, int64_t rows, int64_t keys, bool one_launch, hipStream_t s) {
+    using namespace paged::chunk;
+    if (const int rc = paged_chunk_setup(); rc != FASTAR_OK) return rc;
+    const int64_t items = ((rows + R - 1) / R + a.B) * a.pg.Hkv;   // at most
+    const bool split = !one_launch || (items < SHARES && keys > FEW_KEYS) || items > INT32_MAX;
+    return a.pg.d == 128 ? launch<128>(a, items, split, s) : launch<64>(a, items, split, s);
 }
 
 }  // namespace fastar
