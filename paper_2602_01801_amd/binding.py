@@ -607,22 +607,28 @@ def sparse_attn_fwd_fp8(Q, K8, V8T, cnt, length, C: int, sel, nsel, BQ: int, BK:
 # ---------------------------------------------------------------------------------------------- several requests at a time
 
 
+def _here() -> int:
+    """The device whose current stream a call is launched on."""
+    return torch.cuda.current_device() if _device_now is None else _device_now()
+
+
 # The checks below are what a call costs on the host, next to the foreign call itself: one condition each where all is well.
 def _rows(t: torch.Tensor, H: int, n: int, d: int, dtype) -> _RowsStruct:
     """A view [H, n, d] of any head and row strides."""
     head, row, one = t.stride() if t.dim() == 3 else (0, 0, 0)
-    if one != 1 or t.dtype is not dtype or t.shape != (H, n, d) or not t.is_cuda:
+    if one != 1 or t.dtype is not dtype or t.shape != (H, n, d) or t.get_device() != _here():
         if t.dtype != dtype:
             raise TypeError(f"expected {dtype}, got {t.dtype}")
-        raise ValueError(f"expected a device tensor [{H}, {n}, {d}] whose rows are contiguous, got {tuple(t.shape)}")
+        raise ValueError(f"expected a tensor [{H}, {n}, {d}] on the current device whose rows are contiguous, got {tuple(t.shape)} on {t.device}")
     return _RowsStruct(t.data_ptr(), head, row)
 
 
 def _ints(t: torch.Tensor, *shape, dtype=torch.int32) -> int:
-    if t.shape != shape or t.dtype is not dtype or not t.is_cuda or not t.is_contiguous():
+    if t.shape != shape or t.dtype is not dtype or t.get_device() != _here() or not t.is_contiguous():
         if t.shape != shape:
             raise ValueError(f"expected shape {shape}, got {tuple(t.shape)}")
         _dev(t, dtype)
+        raise ValueError(f"expected a tensor on the current device, got one on {t.device}")
     return t.data_ptr()
 
 
@@ -657,9 +663,9 @@ def prompt_attn_fwd(Q, K, V, cu_q, cu_k=None, causal: bool = True, scale: float 
     return O, lse
 
 
-@dataclass
+@dataclass(frozen=True)
 class Pages:
-    """Device buffers of a paged cache of E4M3 codes with a scale per page and head (fastar_pages)."""
+    """Device buffers of a paged cache of E4M3 codes with a scale per page and head (fastar_pages); checked once, when it is made."""
     K8: torch.Tensor      # [n_pages, Hkv, P/16, d/16, 16 tokens, 16 coordinates] uint8
     kscale: torch.Tensor  # [n_pages, Hkv] float32
     V8: torch.Tensor      # [n_pages, Hkv, P/16, d/16, 16 coordinates, 16 tokens] uint8
@@ -671,20 +677,18 @@ class Pages:
         one = lambda: torch.ones((n_pages, Hkv), dtype=torch.float32, device=device)
         return cls(code(), one(), code(), one())
 
-    @property
-    def shape(self):
-        """(n_pages, Hkv, P, d)"""
-        n, H, pb, db = self.K8.shape[:4]
-        return n, H, 16 * pb, 16 * db
+    def __post_init__(self):
+        shape = tuple(self.K8.shape)
+        if len(shape) != 6 or shape[4:] != (16, 16):
+            raise ValueError("K8 and V8 must be [n_pages, Hkv, P/16, d/16, 16, 16], kscale and vscale [n_pages, Hkv]")
+        for t, want, dtype in ((self.K8, shape, torch.uint8), (self.V8, shape, torch.uint8), (self.kscale, shape[:2], torch.float32),
+                               (self.vscale, shape[:2], torch.float32)):
+            if tuple(_dev(t, dtype).shape) != want or t.device != self.K8.device:
+                raise ValueError("K8 and V8 must be [n_pages, Hkv, P/16, d/16, 16, 16], kscale and vscale [n_pages, Hkv], on one device")
+        object.__setattr__(self, "shape", (shape[0], shape[1], 16 * shape[2], 16 * shape[3]))   # (n_pages, Hkv, P, d)
 
     def struct(self) -> _PagesStruct:
-        K8, V8, ks, vs = self.K8, self.V8, self.kscale, self.vscale
-        shape = K8.shape
-        if len(shape) != 6 or shape[4:] != (16, 16) or V8.shape != shape or ks.shape != shape[:2] or vs.shape != shape[:2]:
-            raise ValueError("K8 and V8 must be [n_pages, Hkv, P/16, d/16, 16, 16], kscale and vscale [n_pages, Hkv]")
-        n, H, pb, db = shape[:4]
-        return _PagesStruct(_ints(K8, *shape, dtype=torch.uint8), _ints(V8, *shape, dtype=torch.uint8), _ints(ks, n, H, dtype=torch.float32),
-                            _ints(vs, n, H, dtype=torch.float32), n, H, 16 * pb, 16 * db)
+        return _PagesStruct(self.K8.data_ptr(), self.V8.data_ptr(), self.kscale.data_ptr(), self.vscale.data_ptr(), *self.shape)
 
     def nbytes(self) -> int:
         return sum(t.numel() * t.element_size() for t in (self.K8, self.V8, self.kscale, self.vscale))
@@ -708,6 +712,8 @@ def kv_pages_plan(n_new, length, table, pool, pool_n, P: int, n_tok: int, out=No
 def kv_pages_write(pages: Pages, slot, K_new, V_new) -> None:
     """New keys and values [Hkv,n,d] (views of any head and row strides) into the pages' slots [n] int32 (kv_pages_plan)."""
     ps = pages.struct()
+    if pages.K8.get_device() != _here():
+        raise ValueError("the pages are not on the current device")
     n = slot.numel()
     dt = _dtype_code(K_new)
     k, v = _rows(K_new, ps.Hkv, n, ps.d, K_new.dtype), _rows(V_new, ps.Hkv, n, ps.d, K_new.dtype)
@@ -720,6 +726,8 @@ def paged_attn_fwd(Q, cu_q, length, table, pages: Pages, causal: bool = True, sc
     cu_q [B+1], length [B] and table [B,max_pages] int32.  Returns (O [Hq,n,d], lse [Hq,n] or None).
     ws: workspace of workspace_bytes(OP_PAGED_ATTN, ...); calls that may be in flight at the same time need one each."""
     ps = pages.struct()
+    if pages.K8.get_device() != _here():
+        raise ValueError("the pages are not on the current device")
     Hq, n, d = _grouped(Q, ps.Hkv)
     B, max_pages = table.shape
     ws = _workspace(ws, workspace_bytes(OP_PAGED_ATTN, Hq, n, 0), Q.device)

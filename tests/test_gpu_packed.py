@@ -39,7 +39,7 @@ def prefix(n):
 
 def check(O, lse, want, n, d, bf16, what=""):
     Or, lr, A, S, vmax = want
-    o, l = f64(O), f64(lse)
+    o, l = f64(O), None if lse is None else f64(lse)
     delta = 2 * (d + 4) * 2.0 ** -24 * S[..., None] + 2.0 ** -20
     unit = 2.0 ** -8 if bf16 else 2.0 ** -24
     tol = unit * np.abs(Or) + ((2.0 ** -8 if bf16 else 0.0) + delta + n * 2.0 ** -24) * 1.02 * A + n * 2.0 ** -126 * vmax
@@ -131,6 +131,21 @@ def test_what_a_query_does_not_see_does_not_reach_it(dtype, causal):
             assert not torch.isfinite(O[:, i][:, a:]).all(-1).any()
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_what_a_query_does_not_see_does_not_reach_it_in_launches_that_fill_the_chip(dtype):
+    g = torch.Generator().manual_seed(10)
+    Hkv, Hq, n, d = 40, 80, 900, 128
+    Q, K, V = (view(g, h, n, d, DT[dtype], "tokens") for h in (Hq, Hkv, Hkv))
+    for h, t, x in ((0, 850, math.nan), (16, 500, math.inf), (39, 899, -math.inf)):
+        K[h, t], V[h, t] = x, x
+    O, lse = fa.prompt_attn_fwd(Q, K, V, i32([0, n]))
+    for hq, t in ((1, 850), (32, 500), (79, 899), (10, 900)):
+        k, v = f64(K[hq // 2:hq // 2 + 1]), f64(V[hq // 2:hq // 2 + 1])
+        want = ref.attend(f64(Q[hq:hq + 1, :t]), k[:, :t], v[:, :t], True, d ** -0.5)
+        check(O[hq:hq + 1, :t], lse[hq:hq + 1, :t], want, n, d, dtype == "bf16", f"head {hq}")
+        assert not torch.isfinite(O[hq, t:]).all(-1).any()
+
+
 def test_prompt_attention_with_shared_rows_and_extreme_scales():
     g = torch.Generator().manual_seed(11)
     n, d = 200, 128
@@ -140,6 +155,52 @@ def test_prompt_attention_with_shared_rows_and_extreme_scales():
         O, lse = fa.prompt_attn_fwd(Q, K, V, i32([0, n]), scale=scale)
         want = ref.attend(f64(Q), f64(K), f64(V), True, float(np.float32(scale)))
         check(O, lse, want, n, d, True, str(scale))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("B", [256, 257, 300, 1100])
+def test_prompt_attention_of_many_sequences(B, dtype):
+    """More sequences than one look at the offsets takes, empty ones among them; without lse."""
+    rng = np.random.default_rng(B)
+    q = rng.integers(0, 4, size=B)
+    q[rng.integers(0, B, size=3)] = (0, 37, 300)
+    q[-1] = 5
+    g = torch.Generator().manual_seed(B)
+    n, d = int(q.sum()), 64
+    Q, K, V = (view(g, h, n, d, DT[dtype], "tokens") for h in (3, 1, 1))
+    cu = prefix(q)
+    O, none = fa.prompt_attn_fwd(Q, K, V, i32(cu), want_lse=False)
+    assert none is None
+    Qh, Kh, Vh = f64(Q), f64(K), f64(V)
+    for b in range(B):
+        i = slice(cu[b], cu[b + 1])
+        want = ref.attend(Qh[:, i], Kh[:, i], Vh[:, i], True, d ** -0.5)
+        check(O[:, i], None, want, int(q[b]), d, dtype == "bf16", f"sequence {b}")
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("n,causal", [(900, True), (700, False), (2049, True)])
+def test_prompt_attention_in_launches_that_fill_the_chip(n, causal, dtype):
+    """As many heads as it takes for workgroups that are not split; a few rows checked."""
+    g = torch.Generator().manual_seed(n)
+    Hkv, Hq, d, elt = 40, 80, 128, DT[dtype]
+    Q, K, V = (view(g, h, n, d, elt, "tokens", m) for h, m in ((Hq, 1.5), (Hkv, 1.0), (Hkv, 1.0)))
+    O, lse = fa.prompt_attn_fwd(Q, K, V, i32([0, n]), causal=causal)
+    for h in (0, 33, 79):
+        k, v = f64(K[h // 2:h // 2 + 1]), f64(V[h // 2:h // 2 + 1])
+        want = ref.attend(f64(Q[h:h + 1]), k, v, causal, d ** -0.5)
+        check(O[h:h + 1], lse[h:h + 1], want, n, d, dtype == "bf16", f"head {h}")
+
+
+def test_prompt_attention_of_rows_beyond_32_bit_offsets():
+    n, pitch, d = 70000, 1 << 15, 128          # 4.6 GB of rows 64 KB apart
+    big = torch.empty((n, pitch), dtype=torch.bfloat16, device="cuda")
+    g = torch.Generator(device="cuda").manual_seed(3)
+    big[:, :256] = torch.randn((n, 256), generator=g, device="cuda").bfloat16()
+    K, V = big[:, :128].unsqueeze(0), big[:, 128:256].unsqueeze(0)
+    Q = view(torch.Generator().manual_seed(4), 2, 3, d, torch.bfloat16, "tokens", 2.0)
+    O, lse = fa.prompt_attn_fwd(Q, K, V, i32([0, 3]), i32([0, n]))
+    check(O, lse, ref.attend(f64(Q), f64(K), f64(V), True, d ** -0.5), n, d, True)
 
 
 # ------------------------------------------------------------------------------------------------ the paged cache
@@ -232,13 +293,16 @@ def test_keys_on_pages_that_do_not_exist_are_left_out(P):
     paged_case([1, 40], [2 * P, 2 * P], 4, 2, P, 64, True, seed=P + 1, bad=[(b, j, -1) for b in (0, 1) for j in (0, 1)])
 
 
-def test_paged_attention_of_codes_that_are_no_numbers_among_later_tokens():
-    """Causal chunk: tokens 20 and on of the chunk hold NaN; the queries before do not see them."""
+@pytest.mark.parametrize("a,n,few,d", [(50, 100, 20, 128), (6, 90, 4, 128), (150, 2500, 100, 128), (7, 2600, 3, 128), (12, 2200, 11, 64), (90, 130, 45, 64)])
+def test_paged_attention_of_codes_that_are_no_numbers_among_later_tokens(a, n, few, d):
+    """Causal chunk: tokens `few` and on of the chunk hold NaN; the queries before do not see them.  Few rows and chunks, in one piece
+    and in several."""
     rng = np.random.default_rng(4)
-    P, d, a, n = 32, 128, 50, 100
-    K, ks, V, vs, _ = random_pages(rng, 4, 1, P, d)
-    table = np.array([[2, 0, 3, 1]], np.int32)
-    first = n - a + 20
+    P = 32
+    per = -(-n // P)
+    K, ks, V, vs, _ = random_pages(rng, per, 1, P, d)
+    table = rng.permutation(per).astype(np.int32)[None]
+    first = n - a + few
     for code, tr in ((K, False), (V, True)):
         rows = ref.rows_of_cells(code, tr).copy()
         for j in range(first, n):
@@ -248,8 +312,8 @@ def test_paged_attention_of_codes_that_are_no_numbers_among_later_tokens():
     Q = view(torch.Generator().manual_seed(1), 2, a, d, torch.bfloat16, "tokens")
     O, lse = fa.paged_attn_fwd(Q, i32([0, a]), i32([n]), i32(table), dev)
     want = ref.attend(f64(Q), gather(K, ks, table[0], n, False), gather(V, vs, table[0], n, True), True, d ** -0.5)
-    check(O[:, :20], lse[:, :20], [w[:, :20] for w in want[:4]] + [want[4]], n, d, True)
-    assert torch.isnan(O[:, 20:]).all()
+    check(O[:, :few], lse[:, :few], [w[:, :few] for w in want[:4]] + [want[4]], n, d, True)
+    assert torch.isnan(O[:, few:]).all()
 
 
 def test_lengths_beyond_the_table_are_cut():
@@ -260,6 +324,38 @@ def test_lengths_beyond_the_table_are_cut():
     want = ref.attend(f64(Q[:, :1]), gather(K, ks, [1, 2], 32, False), gather(V, vs, [1, 2], 32, True), True, 64 ** -0.5)
     check(O[:, :1], lse[:, :1], want, 32, 64, True)
     assert (O[:, 1] == 0).all() and torch.isneginf(lse[:, 1]).all()
+
+
+@pytest.mark.parametrize("B,q,k", [(257, 1, 70), (300, 2, 2100), (1025, 1, 33), (260, 40, 300), (300, 13, 2300)])
+def test_paged_attention_of_many_sequences(B, q, k):
+    """More sequences than one look at the lengths takes; few rows and chunks, one launch and two."""
+    rng = np.random.default_rng(B + k)
+    qs, ks = rng.integers(0, q + 1, size=B), rng.integers(0, 60, size=B)
+    qs[B // 2], ks[B // 2], qs[-1], ks[-1], qs[0] = q, k, q, k // 2, q
+    if q > 8:
+        qs[:] = np.maximum(qs, q - 3)    # rows on average decide on the kernel
+    paged_case([int(x) for x in qs], [int(x) for x in ks], 4, 1, 16, 64, True, seed=B)
+
+
+def test_paged_attention_and_writing_beyond_32_bit_offsets():
+    """Pages whose codes lie beyond 4 GB, against the same ones in a small cache."""
+    Hkv, P, d, n = 8, 64, 128, 700
+    n_pages = 66000 + 11     # 65536 bytes of K each
+    big = fa.Pages(*(torch.empty((n_pages, Hkv) + s, dtype=t, device="cuda") for s, t in (((4, 8, 16, 16), torch.uint8), ((), torch.float32)) * 2))
+    small = fa.Pages.empty(11, Hkv, P, d)
+    K, V = (view(torch.Generator().manual_seed(i), Hkv, n, d, torch.bfloat16, "tokens") for i in range(2))
+    slot = torch.arange(n, dtype=torch.int32, device="cuda")
+    fa.kv_pages_write(big, slot + 66000 * P, K, V)
+    fa.kv_pages_write(small, slot, K, V)
+    last = n // P * P   # the rest of the last page means nothing
+    assert torch.equal(big.K8[66000:66010], small.K8[:10]) and torch.equal(big.V8[66000:66010], small.V8[:10]) and last == 640
+    assert torch.equal(big.kscale[66000:], small.kscale) and torch.equal(big.vscale[66000:], small.vscale)
+    for a in (1, 200):   # single tokens and chunks
+        Q = view(torch.Generator().manual_seed(9), 16, a, d, torch.bfloat16, "tokens")
+        table = torch.arange(11, dtype=torch.int32, device="cuda")[None]
+        want = fa.paged_attn_fwd(Q, i32([0, a]), i32([n]), table, small)
+        got = fa.paged_attn_fwd(Q, i32([0, a]), i32([n]), table + 66000, big)
+        assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
 
 
 # ------------------------------------------------------------------------------------------------ planning
@@ -298,6 +394,25 @@ def test_plan(B, P):
     total = sum(max(x, 0) for x in n_new)
     for n_tok in (total, total + 7, max(total * 2 // 3, 1), 5000 + total):
         run_plan(n_new, length, table, pool, n_pages - at, P, n_tok, in_place=bool(n_tok & 1))
+
+
+@pytest.mark.parametrize("in_place", [True, False])
+def test_plan_of_many_tokens(in_place):
+    """More slots than one workgroup writes, in place and not; some requests are refused, some end."""
+    rng = np.random.default_rng(5)
+    P, B, mp = 16, 70, 60
+    length = [int(x) for x in rng.integers(0, 300, size=B)]
+    n_new = [int(x) for x in rng.choice([-1, 0, 1, 200, 600], size=B)]
+    held = [-(-x // P) for x in length]
+    n_pages = sum(held) + 700
+    order = [int(x) for x in rng.permutation(n_pages)]
+    table, at = [[-3] * mp for _ in range(B)], 0
+    for b in range(B):
+        table[b][:held[b]] = order[at:at + held[b]]
+        at += held[b]
+    total = sum(max(x, 0) for x in n_new)
+    assert total > 9000
+    run_plan(n_new, length, table, order[at:] + [-1] * at, n_pages - at, P, total, in_place)
 
 
 def test_plan_of_lengths_and_pools_that_make_no_sense():
@@ -530,6 +645,8 @@ def test_the_binding_refuses_what_does_not_fit():
     with pytest.raises(ValueError):
         fa.kv_pages_write(pages, i32([0] * 7), K, K)
     with pytest.raises(ValueError):
-        fa.kv_pages_write(fa.Pages(pages.K8, pages.kscale[:2], pages.V8, pages.vscale), i32([0] * 8), K, K)
+        fa.Pages(pages.K8, pages.kscale[:2], pages.V8, pages.vscale)
+    with pytest.raises(TypeError):
+        fa.Pages(pages.K8, pages.kscale, pages.V8.view(torch.int8), pages.vscale)
     with pytest.raises(ValueError):
         fa.kv_pages_plan(i32([1]), i32([0, 0]), i32([[0]]), i32([0]), i32([1]), 16, 1)
