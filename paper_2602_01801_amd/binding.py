@@ -613,27 +613,33 @@ def _here() -> int:
 
 
 # The checks below are what a call costs on the host, next to the foreign call itself: one condition each where all is well.
-def _rows(t: torch.Tensor, H: int, n: int, d: int, dtype) -> _RowsStruct:
+def _rows(t: torch.Tensor, H: int, n: int, d: int, dtype, dev: int) -> _RowsStruct:
     """A view [H, n, d] of any head and row strides."""
-    head, row, one = t.stride() if t.dim() == 3 else (0, 0, 0)
-    if one != 1 or t.dtype is not dtype or t.shape != (H, n, d) or t.get_device() != _here():
+    if t.dtype is not dtype or t.shape != (H, n, d) or t.get_device() != dev:
         if t.dtype != dtype:
             raise TypeError(f"expected {dtype}, got {t.dtype}")
-        raise ValueError(f"expected a tensor [{H}, {n}, {d}] on the current device whose rows are contiguous, got {tuple(t.shape)} on {t.device}")
+        raise ValueError(f"expected a tensor [{H}, {n}, {d}] on the current device, got {tuple(t.shape)} on {t.device}")
+    head, row, one = t.stride()
+    if one != 1:
+        raise ValueError("rows must be contiguous")
     return _RowsStruct(t.data_ptr(), head, row)
 
 
-def _ints(t: torch.Tensor, *shape, dtype=torch.int32) -> int:
-    if t.shape != shape or t.dtype is not dtype or t.get_device() != _here() or not t.is_contiguous():
-        if t.shape != shape:
-            raise ValueError(f"expected shape {shape}, got {tuple(t.shape)}")
-        _dev(t, dtype)
-        raise ValueError(f"expected a tensor on the current device, got one on {t.device}")
+def _ints(t: torch.Tensor, n: int, dev: int) -> int:
+    """n contiguous int32 numbers."""
+    if t.dtype is not torch.int32 or t.numel() != n or t.get_device() != dev or not t.is_contiguous():
+        _dev(t, torch.int32)
+        raise ValueError(f"expected {n} numbers on the current device, got {tuple(t.shape)} on {t.device}")
     return t.data_ptr()
 
 
-def _lse_out(lse, Hq: int, n: int):
-    return None if lse is None else _ints(lse, Hq, n, dtype=torch.float32)
+def _lse_out(lse, Hq: int, n: int, dev: int):
+    if lse is None:
+        return None
+    if lse.shape != (Hq, n) or lse.dtype is not torch.float32 or lse.get_device() != dev or not lse.is_contiguous():
+        _dev(lse, torch.float32)
+        raise ValueError(f"lse must be [{Hq}, {n}] on the current device, got {tuple(lse.shape)} on {lse.device}")
+    return lse.data_ptr()
 
 
 def _grouped(Q, Hkv: int):
@@ -651,15 +657,15 @@ def prompt_attn_fwd(Q, K, V, cu_q, cu_k=None, causal: bool = True, scale: float 
     outside of every sequence are not written."""
     Hq, n_q, d = _grouped(Q, K.shape[0])
     Hkv, n_k = K.shape[0], K.shape[1]
-    dt = _dtype_code(Q)
+    dt, code, dev = Q.dtype, _dtype_code(Q), _here()
     B = cu_q.numel() - 1
     if out is None:
         out = (torch.empty_like(Q), torch.empty((Hq, n_q), dtype=torch.float32, device=Q.device) if want_lse else None)
     O, lse = out
-    q, k, v, o = _rows(Q, Hq, n_q, d, Q.dtype), _rows(K, Hkv, n_k, d, Q.dtype), _rows(V, Hkv, n_k, d, Q.dtype), _rows(O, Hq, n_q, d, Q.dtype)
-    _check(lib().prompt_attn_fwd(q, k, v, _ints(cu_q, B + 1), None if cu_k is None else _ints(cu_k, B + 1), B, n_q, n_k, Hq, Hkv, d,
-                                 dt, 1 if causal else 0, d ** -0.5 if scale is None else float(scale), o, _lse_out(lse, Hq, n_q),
-                                 _stream()), "prompt_attn_fwd")
+    _check(lib().prompt_attn_fwd(_rows(Q, Hq, n_q, d, dt, dev), _rows(K, Hkv, n_k, d, dt, dev), _rows(V, Hkv, n_k, d, dt, dev),
+                                 _ints(cu_q, B + 1, dev), None if cu_k is None else _ints(cu_k, B + 1, dev), B, n_q, n_k, Hq, Hkv, d,
+                                 code, 1 if causal else 0, d ** -0.5 if scale is None else float(scale), _rows(O, Hq, n_q, d, dt, dev),
+                                 _lse_out(lse, Hq, n_q, dev), _stream()), "prompt_attn_fwd")
     return O, lse
 
 
@@ -687,7 +693,9 @@ class Pages:
                 raise ValueError("K8 and V8 must be [n_pages, Hkv, P/16, d/16, 16, 16], kscale and vscale [n_pages, Hkv], on one device")
         object.__setattr__(self, "shape", (shape[0], shape[1], 16 * shape[2], 16 * shape[3]))   # (n_pages, Hkv, P, d)
 
-    def struct(self) -> _PagesStruct:
+    def struct(self, dev: int) -> _PagesStruct:
+        if self.K8.get_device() != dev:
+            raise ValueError("the pages are not on the current device")
         return _PagesStruct(self.K8.data_ptr(), self.V8.data_ptr(), self.kscale.data_ptr(), self.vscale.data_ptr(), *self.shape)
 
     def nbytes(self) -> int:
@@ -699,25 +707,25 @@ def kv_pages_plan(n_new, length, table, pool, pool_n, P: int, n_tok: int, out=No
     (updated in place), pool_n [1] int32, n_tok rows for new tokens.  Returns (length after, pool_n after, cu [B+1],
     slot [n_tok], status [B]), all int32; out may name `length` and `pool_n` themselves for the first two."""
     B, max_pages = table.shape
+    n_pages, dev = pool.numel(), _here()
     if out is None:
         i = lambda *n: torch.empty(n, dtype=torch.int32, device=table.device)
         out = (i(B), i(1), i(B + 1), torch.full((n_tok,), -1, dtype=torch.int32, device=table.device), i(B))
     after, free, cu, slot, status = out
-    _check(lib().kv_pages_plan(_ints(n_new, B), _ints(length, B), _ints(table, B, max_pages), B, max_pages, _ints(pool, pool.numel()),
-                               _ints(pool_n, 1), pool.numel(), P, n_tok, _ints(after, B), _ints(free, 1), _ints(cu, B + 1),
-                               _ints(slot, n_tok), _ints(status, B), _stream()), "kv_pages_plan")
+    _check(lib().kv_pages_plan(_ints(n_new, B, dev), _ints(length, B, dev), _ints(table, B * max_pages, dev), B, max_pages,
+                               _ints(pool, n_pages, dev), _ints(pool_n, 1, dev), n_pages, P, n_tok, _ints(after, B, dev),
+                               _ints(free, 1, dev), _ints(cu, B + 1, dev), _ints(slot, n_tok, dev), _ints(status, B, dev), _stream()),
+           "kv_pages_plan")
     return out
 
 
 def kv_pages_write(pages: Pages, slot, K_new, V_new) -> None:
     """New keys and values [Hkv,n,d] (views of any head and row strides) into the pages' slots [n] int32 (kv_pages_plan)."""
-    ps = pages.struct()
-    if pages.K8.get_device() != _here():
-        raise ValueError("the pages are not on the current device")
-    n = slot.numel()
-    dt = _dtype_code(K_new)
-    k, v = _rows(K_new, ps.Hkv, n, ps.d, K_new.dtype), _rows(V_new, ps.Hkv, n, ps.d, K_new.dtype)
-    _check(lib().kv_pages_write(ps, k, v, dt, _ints(slot, n), n, _stream()), "kv_pages_write")
+    dev = _here()
+    ps = pages.struct(dev)
+    n, dt, code = slot.numel(), K_new.dtype, _dtype_code(K_new)
+    _check(lib().kv_pages_write(ps, _rows(K_new, ps.Hkv, n, ps.d, dt, dev), _rows(V_new, ps.Hkv, n, ps.d, dt, dev), code,
+                                _ints(slot, n, dev), n, _stream()), "kv_pages_write")
 
 
 def paged_attn_fwd(Q, cu_q, length, table, pages: Pages, causal: bool = True, scale: float | None = None, out=None,
@@ -725,19 +733,19 @@ def paged_attn_fwd(Q, cu_q, length, table, pages: Pages, causal: bool = True, sc
     """Attention of packed queries Q [Hq,n,d] bf16 (a view of any head and row strides) over the pages of their sequences:
     cu_q [B+1], length [B] and table [B,max_pages] int32.  Returns (O [Hq,n,d], lse [Hq,n] or None).
     ws: workspace of workspace_bytes(OP_PAGED_ATTN, ...); calls that may be in flight at the same time need one each."""
-    ps = pages.struct()
-    if pages.K8.get_device() != _here():
-        raise ValueError("the pages are not on the current device")
+    dev = _here()
+    ps = pages.struct(dev)
     Hq, n, d = _grouped(Q, ps.Hkv)
+    dt, code = Q.dtype, _dtype_code(Q)
     B, max_pages = table.shape
     ws = _workspace(ws, workspace_bytes(OP_PAGED_ATTN, Hq, n, 0), Q.device)
     if out is None:
         out = (torch.empty_like(Q), torch.empty((Hq, n), dtype=torch.float32, device=Q.device) if want_lse else None)
     O, lse = out
-    q, o = _rows(Q, Hq, n, ps.d, Q.dtype), _rows(O, Hq, n, ps.d, Q.dtype)
-    _check(lib().paged_attn_fwd(q, _ints(cu_q, B + 1), _ints(length, B), _ints(table, B, max_pages), B, max_pages, n, Hq, ps,
-                                _dtype_code(Q), 1 if causal else 0, d ** -0.5 if scale is None else float(scale), o,
-                                _lse_out(lse, Hq, n), ws.data_ptr(), ws.numel() * ws.element_size(), _stream()), "paged_attn_fwd")
+    _check(lib().paged_attn_fwd(_rows(Q, Hq, n, ps.d, dt, dev), _ints(cu_q, B + 1, dev), _ints(length, B, dev),
+                                _ints(table, B * max_pages, dev), B, max_pages, n, Hq, ps, code, 1 if causal else 0,
+                                d ** -0.5 if scale is None else float(scale), _rows(O, Hq, n, ps.d, dt, dev),
+                                _lse_out(lse, Hq, n, dev), ws.data_ptr(), ws.numel() * ws.element_size(), _stream()), "paged_attn_fwd")
     return O, lse
 
 
