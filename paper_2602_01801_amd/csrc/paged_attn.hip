@@ -64,15 +64,11 @@ __global__ __launch_bounds__(NW * 64, 2) void attn_kernel(const Args a) {
     }
     Desc d = {0, 0, 0, -1};
     while (r.u < r.u_end) {   // uniform: one piece of one item per turn
-        if (r.u >= r.base + (long long)sq.n_qt * Hkv * (SPLIT ? sq.n_tiles : 1)) find_unit<R, SPLIT>(a, r.u, r.b, r.base, sq);
-        const int units = SPLIT ? sq.n_tiles : 1;
-        const long long local = r.u - r.base;
-        const int item = (int)(local / units);
-        const int h = item / sq.n_qt, qt = item - h * sq.n_qt;
-        const int ta = SPLIT ? (int)(local - (long long)item * units) : 0;
-        const int te = SPLIT ? (int)min((long long)units, ta + (r.u_end - r.u)) : sq.n_tiles;
+        if (SPLIT && r.u >= r.base + (long long)sq.n_qt * Hkv * (sq.n_tiles + ENDS)) find_unit<R, SPLIT>(a, r.u, r.b, r.base, sq);
+        const PieceOf piece = next_piece<SPLIT>(r, sq);
+        if (piece.te <= piece.ta) continue;
+        const int h = piece.h, qt = piece.qt, ta = piece.ta, te = piece.te;
         const bool begins = ta == 0, ends = te == sq.n_tiles;
-        r.u += SPLIT ? te - ta : 1;
 
         const int n_rows = sq.n_q * a.group;
         const int tok0 = (qt * R) / a.group, tok1 = min(qt * R + R - 1, n_rows - 1) / a.group;
@@ -314,7 +310,7 @@ __global__ __launch_bounds__(NW * 64, 2) void attn_kernel(const Args a) {
             }
             __syncthreads();
         }
-        if (SPLIT && begins && !ends) d = Desc{r.b, h, qt, share_of(r, r.base + (long long)(item + 1) * units - 1)};
+        if (SPLIT && begins && !ends) d = Desc{r.b, h, qt, share_of(r, piece.last)};
     }
     if (SPLIT && tid == 0) a.desc[r.share] = d;
 }

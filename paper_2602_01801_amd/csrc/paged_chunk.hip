@@ -64,15 +64,11 @@ __global__ __launch_bounds__(2 * NWG * 64, 1) void attn_chunk_kernel(const Args 
     }
     Desc d = {0, 0, 0, -1};
     while (r.u < r.u_end) {   // uniform: one piece of one item per turn
-        if (SPLIT && r.u >= r.base + (long long)sq.n_qt * Hkv * sq.n_tiles) find_unit<R, SPLIT>(a, r.u, r.b, r.base, sq);
-        const int units = SPLIT ? sq.n_tiles : 1;
-        const long long local = r.u - r.base;
-        const int item = (int)(local / units);
-        const int h = item / sq.n_qt, qt = item - h * sq.n_qt;
-        const int ta = SPLIT ? (int)(local - (long long)item * units) : 0;
-        const int te = SPLIT ? (int)min((long long)units, ta + (r.u_end - r.u)) : sq.n_tiles;
+        if (SPLIT && r.u >= r.base + (long long)sq.n_qt * Hkv * (sq.n_tiles + ENDS)) find_unit<R, SPLIT>(a, r.u, r.b, r.base, sq);
+        const PieceOf its = next_piece<SPLIT>(r, sq);
+        if (its.te <= its.ta) continue;
+        const int h = its.h, qt = its.qt, ta = its.ta, te = its.te;
         const bool begins = ta == 0, ends = te == sq.n_tiles, whole = !SPLIT || (begins && ends);
-        r.u += SPLIT ? te - ta : 1;
 
         const int n_rows = sq.n_q * a.group;
         auto sees = [&](int x) {
@@ -355,7 +351,7 @@ __global__ __launch_bounds__(2 * NWG * 64, 1) void attn_chunk_kernel(const Args 
             }
         }
         __syncthreads();   // the next piece's tiles go where this one's rows were
-        if (SPLIT && begins && !ends) d = Desc{r.b, h, qt, share_of(r, r.base + (long long)(item + 1) * units - 1)};
+        if (SPLIT && begins && !ends) d = Desc{r.b, h, qt, share_of(r, its.last)};
     }
     if (SPLIT && tid == 0) a.desc[r.share] = d;
 }
