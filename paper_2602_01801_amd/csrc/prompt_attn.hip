@@ -97,7 +97,8 @@ __global__ __launch_bounds__(2 * NWG * 64, 1) void attn_bf16_kernel(const Args a
     unsigned char *kbuf = lds + (SPLIT ? grp * 2 * OWN_STAGES * TILEB : 0), *vbuf = kbuf + NK * TILEB;
     const char *Kb = a.K.p + h * a.K.head + (int64_t)rk.first * a.K.row, *Vb = a.V.p + h * a.V.head + (int64_t)rk.first * a.V.row;
     auto swz_k = [](int row) { return D == 128 ? row & 15 : (row >> 1) & 7; };
-    auto swz_v = [](int row) { return D == 128 ? (row & 7) << 1 : ((row >> 1) & 3) << 1; };
+    // a transposing read takes 64 bytes of four rows at a time: a quarter of the banks each
+    auto swz_v = [](int row) { return D == 128 ? (row & 3) << 2 : ((row >> 1) & 1) << 2; };
     unsigned koff[IPW], voff[IPW];
 #pragma unroll
     for (int i = 0; i < IPW; ++i) {
