@@ -1,9 +1,10 @@
 // Attention of packed queries over a paged cache of E4M3 codes (paged_attn_fwd): the kernel for chunks of many rows.
 //
-// prompt_attn.hip's schedule -- 256 rows per workgroup, two groups of four wavefronts half a tile apart, three stages of K and
-// four of V -- over tiles that come from pages.  A wavefront of paged_attn.hip widens every code it multiplies with; here a tile's
+// prompt_attn.hip's schedule -- 256 rows per workgroup, two groups of four wavefronts half a tile apart -- over tiles that come
+// from pages.  A wavefront of paged_attn.hip widens every code it multiplies with; here a tile's
 // codes are widened once for all eight wavefronts: each takes an eighth of the tile, 16 bytes of K and of V per lane, into
-// registers, and writes it to LDS as bf16 a tile later.  V's cells hold a coordinate's 16 tokens, so V lies transposed in LDS and
+// registers, and writes it to LDS as bf16 a tile later, in the matrix phase (in the vector phase, which is the longer one, 505 us
+// where this takes 460).  V's cells hold a coordinate's 16 tokens, so V lies transposed in LDS and
 // is read as it is; within 16 tokens the order is 0-3, 8-11, 4-7, 12-15, which is the order that half a wavefront holds P in.
 // The items' tiles are dealt out as in paged_dev.hpp, a workgroup per compute unit.
 #include "attn_lds.hpp"
@@ -21,7 +22,7 @@ using namespace attn_lds;
 
 constexpr int NWG = 4;         // wavefronts per group
 constexpr int R = 256;         // rows per item
-constexpr int NK = 3, NV = 4;  // stages
+constexpr int NK = 2, NV = 3;  // stages
 constexpr int SHARES = 256;
 constexpr int LEAST = 8;       // tiles of a share at least: a fragment costs as much as some of them
 constexpr int FEW_KEYS = 512;  // longer ones are cut while items leave compute units idle (one item of 300 rows x 4 heads x 2000 keys: 72 us whole)
@@ -164,14 +165,23 @@ __global__ __launch_bounds__(2 * NWG * 64, 1) void attn_chunk_kernel(const Args 
 #pragma unroll
                 for (int db = 0; db < DB; ++db) o[db] = mfma_bf16_32x32x16(f[st][db], p[st], o[db]);
         };
-        auto phase_x = [&](int t, int exist, auto pv_c, auto qk_c) __attribute__((always_inline)) {
+        // on their way: page numbers of tile t + 2 (ids), codes of tile t + 1 (registers); which pages of tiles t and t + 1 exist
+        int ids = 0, e1 = 15, e2 = 15;
+        auto phase_x = [&](int t, auto pv_c, auto qk_c) __attribute__((always_inline)) {
             constexpr bool PV = decltype(pv_c)::value, QK = decltype(qk_c)::value;
             __builtin_amdgcn_s_setprio(2);
             bf16x8 vb[2][DB], ka[KF], kb[KF];
             if constexpr (PV) read_v(1, vb);
             if constexpr (QK) read_k<0>(ka, kaddr);
+            const int exist = e1;
             if constexpr (PV) {
                 pv(va, pf[0]);
+                if constexpr (QK) {
+                    if (t + 1 < t_end) put(t + 1);
+                    e1 = e2;
+                    if (t + 2 < t_end) e2 = fetch(ids);
+                    if (t + 3 < t_end) ids = ids_of(t + 3);
+                }
                 wait_b<QK ? KF : 0>(vb);
                 pv(vb, pf[1]);
                 vaddr += vst == NV - 1 ? -(NV - 1) * TILEB : TILEB;
@@ -208,14 +218,7 @@ __global__ __launch_bounds__(2 * NWG * 64, 1) void attn_chunk_kernel(const Args 
             }
             __builtin_amdgcn_s_setprio(0);
         };
-        // on their way: page numbers of tile t + 4 (ids), codes of tile t + 3 (registers); which pages of tiles t + 1 .. t + 3 exist
-        int ids = 0, e1 = 15, e2 = 15, e3 = 15;
         auto phase_y = [&](int t) __attribute__((always_inline)) {
-            if (t + 2 < t_end) put(t + 2);
-            e1 = e2;
-            e2 = e3;
-            if (t + 3 < t_end) e3 = fetch(ids);
-            if (t + 4 < t_end) ids = ids_of(t + 4);
             if (__any((mx_tile - m) * scale_log2 > TAU)) {
                 const float mn = fmaxf(m, mx_tile);
                 const float alpha = weight_of(m, mn, scale_log2);
@@ -248,31 +251,33 @@ __global__ __launch_bounds__(2 * NWG * 64, 1) void attn_chunk_kernel(const Args 
             read_v(0, va);
             wait_b<0>(va);
         };
-        // Half steps as in prompt_attn.hip; tiles t + 2 are written in Y(t), where prompt_attn.hip asks for them, and are there at the
-        // barrier that ends it.
+        // Half steps as in prompt_attn.hip.  X(t) writes tile t + 1 (half steps 2t and 2t+1), whose K group 0 reads from 2t+2 on; the
+        // stages are those of K(t-1) and V(t-2), last read in half step 2t-1.  Tiles ta and ta + 1 are written before the first.
         if (ta < t_end) {
             const int i0 = ids_of(ta), i1 = ids_of(ta + 1), i2 = ids_of(ta + 2);
             ids = ids_of(ta + 3);
             e1 = fetch(i0);
             put(ta);
+            int of_next = 15;
             if (ta + 1 < t_end) {
-                e2 = fetch(i1);
+                of_next = fetch(i1);
                 put(ta + 1);
             }
-            if (ta + 2 < t_end) e3 = fetch(i2);
+            if (ta + 2 < t_end) e2 = fetch(i2);
             wg_barrier();
             if (grp == 1) wg_barrier();
-            phase_x(ta, e1, std::false_type{}, std::true_type{});
+            phase_x(ta, std::false_type{}, std::true_type{});
+            e1 = of_next;
             for (int t = ta; t < t_end - 1; ++t) {
                 wg_barrier();
                 phase_y(t);
                 wg_barrier();
-                phase_x(t + 1, e1, std::true_type{}, std::true_type{});
+                phase_x(t + 1, std::true_type{}, std::true_type{});
             }
             wg_barrier();
             phase_y(t_end - 1);
             wg_barrier();
-            phase_x(t_end, 15, std::true_type{}, std::false_type{});
+            phase_x(t_end, std::true_type{}, std::false_type{});
             if (grp == 0) wg_barrier();
         }
 
