@@ -28,14 +28,10 @@ constexpr int64_t MAX_PITCH = 1 << 24;   // bytes between rows of keys and value
 inline bool scale_ok(float scale) { return scale > 0.0f && std::isfinite(scale * 1.4426950408889634f); }
 inline bool page_size_ok(int P) { return P == 16 || P == 32 || P == 64; }
 
-// Rows [first, first + n) of sequence b, inside [0, n_tok).
+// Rows [first, first + n) of a sequence, inside the array.
 struct Rows {
     int first, n;
 };
-__device__ __forceinline__ Rows rows_of(const int32_t *__restrict__ cu, int b, int n_tok) {
-    const int a = min(max(cu[b], 0), n_tok), e = min(max(cu[b + 1], 0), n_tok);
-    return Rows{a, max(e - a, 0)};
-}
 
 // 16 bytes per lane from global memory straight into LDS, lane after lane from dst on (uniform, as `base` is): from one base
 // address, each lane at an offset of its own, which costs no vector instruction; or from an address per lane.
@@ -50,6 +46,20 @@ __device__ __forceinline__ void to_lds(const char *src, unsigned char *dst) {
 }
 __device__ __forceinline__ unsigned lds_address(const void *p) {
     return (unsigned)(size_t)(__attribute__((address_space(3))) const unsigned char *)p;
+}
+
+// Maximum and sum over the four lanes of a row (lane % 16).
+__device__ __forceinline__ float max_of_quarters(float v) {
+    const auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    v = fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
+    const auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
+}
+__device__ __forceinline__ float sum_of_quarters(float v) {
+    const auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    v = __uint_as_float(a[0]) + __uint_as_float(a[1]);
+    const auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return __uint_as_float(b[0]) + __uint_as_float(b[1]);
 }
 
 // Item u of a launch whose sequences have ceil(rows * group / R) * Hkv items each, in their order.  Every wavefront looks for

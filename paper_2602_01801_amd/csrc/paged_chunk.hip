@@ -1,12 +1,14 @@
 // Attention of packed queries over a paged cache of E4M3 codes (paged_attn_fwd): the kernel for chunks of many rows.
 //
 // prompt_attn.hip's schedule -- 256 rows per workgroup, two groups of four wavefronts half a tile apart -- over tiles that come
-// from pages.  A wavefront of paged_attn.hip widens every code it multiplies with; here a tile's
-// codes are widened once for all eight wavefronts: each takes an eighth of the tile, 16 bytes of K and of V per lane, into
-// registers, and writes it to LDS as bf16 a tile later, in the matrix phase (in the vector phase, which is the longer one, 505 us
-// where this takes 460).  V's cells hold a coordinate's 16 tokens, so V lies transposed in LDS and
-// is read as it is; within 16 tokens the order is 0-3, 8-11, 4-7, 12-15, which is the order that half a wavefront holds P in.
-// The items' tiles are dealt out as in paged_dev.hpp, a workgroup per compute unit.
+// from pages.  A wavefront of paged_attn.hip widens every code it multiplies with; here a tile's codes are widened once for all
+// eight wavefronts: each takes an eighth of the tile, 16 bytes of K and of V per lane, into registers, and writes it to LDS as bf16 a
+// tile later, in the matrix phase (in the vector phase, which is the longer one, 505 us where this takes 460).  V's cells hold a
+// coordinate's 16 tokens, so V lies transposed in LDS and is read as it is; within 16 tokens the order is 0-3, 8-11, 4-7, 12-15,
+// which is the order that half a wavefront holds P in.  The items' tiles are dealt out as in paged_dev.hpp, a workgroup per compute
+// unit.  What bounds it: the two phases' instructions, 4000 cycles per tile and pair of wavefronts, 2048 of them matrix instructions;
+// rows that no token fills (8 % of five chunks of 201 to 780 tokens x 3 heads); 14 us of fragments.  Those chunks over caches of 4680
+// to 37440 keys x 4 key heads: 460 us = 845 TFLOP/s (paged_attn.hip's way with 64 rows per wavefront took 790).
 #include "attn_lds.hpp"
 #include "paged_dev.hpp"
 
@@ -25,7 +27,7 @@ constexpr int R = 256;         // rows per item
 constexpr int NK = 2, NV = 3;  // stages
 constexpr int SHARES = 256;
 constexpr int LEAST = 8;       // tiles of a share at least: a fragment costs as much as some of them
-constexpr int FEW_KEYS = 512;  // longer ones are cut while items leave compute units idle (one item of 300 rows x 4 heads x 2000 keys: 72 us whole)
+constexpr int FEW_KEYS = 512;  // longer tables are cut while items leave compute units idle (100 tokens x 12 heads on 4 x 2000 keys 72 us whole, 34 cut)
 constexpr int FRAG_FLOATS = R * 128 + 2 * R;
 static_assert(SHARES <= MAX_SHARES, "descriptors");
 
@@ -218,7 +220,7 @@ __global__ __launch_bounds__(2 * NWG * 64, 1) void attn_chunk_kernel(const Args 
             }
             __builtin_amdgcn_s_setprio(0);
         };
-        auto phase_y = [&](int t) __attribute__((always_inline)) {
+        auto phase_y = [&]() __attribute__((always_inline)) {
             if (__any((mx_tile - m) * scale_log2 > TAU)) {
                 const float mn = fmaxf(m, mx_tile);
                 const float alpha = weight_of(m, mn, scale_log2);
@@ -270,12 +272,12 @@ __global__ __launch_bounds__(2 * NWG * 64, 1) void attn_chunk_kernel(const Args 
             e1 = of_next;
             for (int t = ta; t < t_end - 1; ++t) {
                 wg_barrier();
-                phase_y(t);
+                phase_y();
                 wg_barrier();
                 phase_x(t + 1, std::true_type{}, std::true_type{});
             }
             wg_barrier();
-            phase_y(t_end - 1);
+            phase_y();
             wg_barrier();
             phase_x(t_end, std::true_type{}, std::false_type{});
             if (grp == 0) wg_barrier();
