@@ -522,8 +522,9 @@ int kv_pages_write(const fastar_pages *pages, const fastar_rows *K_new, const fa
  *   Q, O [Hq,n_tok,d] bf16 views;  cu_q [B+1];  len [B] keys of every sequence (those of the queries among them, written
  *   before);  table [B, max_pages];  lse [Hq,n_tok] float or NULL;  causal as for prompt_attn_fwd
  * Keys on pages outside of [0, n_pages) are left out, like masked ones; len is cut to [0, max_pages * P].
- * Products in bf16 (codes are widened exactly), fp32 softmax and sums.  Sequences share the chip by their lengths, which
- * the device reads: long ones are cut into pieces whose fragments lie in ws, and a second launch puts them together.
+ * Products in bf16 (codes are widened exactly; where a sequence has at most eight query rows on a key head and sequences have
+ * at most 16 on average, weights have 16 bits), fp32 softmax and sums.  Sequences share the chip by their lengths, which the
+ * device reads: long ones are cut into pieces whose fragments lie in ws, and a second launch puts them together.
  *   ws / ws_bytes  fastar_workspace_bytes(FASTAR_OP_PAGED_ATTN, ...) bytes, 256-byte aligned; contents need not be kept.
  *                  Calls that may be in flight at the same time need a workspace each.
  * Supported: bf16, d in {64, 128}, scales of the pages 2^-100 .. 2^120; scale and n_tok * Hq as for

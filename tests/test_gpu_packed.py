@@ -286,6 +286,23 @@ def test_paged_attention_over_long_caches_in_pieces(Hq, Hkv, P, d, q, k):
     paged_case(q, k, Hq, Hkv, P, d, True, seed=sum(k), layout="heads")
 
 
+@pytest.mark.parametrize("Hq,Hkv,P,d,q,k", [(8, 1, 16, 128, 1, 1500), (12, 12, 64, 128, 1, 700), (4, 1, 32, 64, 2, 333), (5, 1, 64, 128, 1, 9000),
+                                            (6, 3, 16, 64, 4, 5000)])
+def test_weights_of_few_rows_have_sixteen_bits(Hq, Hkv, P, d, q, k):
+    """At most eight rows of a key head: what rounding to bf16 takes from a weight is rounded to bf16 again and multiplied too, so that
+    2^-16 of it is missing instead of 2^-8 (or 2^-126 of the largest, where the rest is too small a number)."""
+    rng = np.random.default_rng(k)
+    per = -(-k // P)
+    K, ks, V, vs, dev = random_pages(rng, per, Hkv, P, d)
+    table = rng.permutation(per).astype(np.int32)[None]
+    Q = view(torch.Generator().manual_seed(k), Hq, q, d, torch.bfloat16, "tokens")
+    O, lse = fa.paged_attn_fwd(Q, i32([0, q]), i32([k]), i32(table), dev)
+    Or, _, A, S, vmax = ref.attend(f64(Q), gather(K, ks, table[0], k, False), gather(V, vs, table[0], k, True), True, d ** -0.5)
+    delta = 2 * (d + 4) * 2.0 ** -24 * S[..., None] + 2.0 ** -20
+    tol = 2.0 ** -8 * np.abs(Or) + (2.0 ** -16 + delta + k * 2.0 ** -24) * 1.02 * A + 2 * k * 2.0 ** -126 * vmax
+    assert (np.abs(f64(O) - Or) <= tol).all()
+
+
 @pytest.mark.parametrize("P", [16, 32, 64])
 def test_keys_on_pages_that_do_not_exist_are_left_out(P):
     n = 5 * P + 3
