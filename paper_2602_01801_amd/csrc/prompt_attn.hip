@@ -33,8 +33,8 @@ constexpr int NWG = 4;         // wavefronts per group
 constexpr int NK = 3, NV = 4, OWN_STAGES = 2;
 // Workgroups of 256 rows up to which 128 rows take a workgroup, whose two groups share their tiles: as many of them as compute
 // units; causal ones up to twice that, since the first half of the rows has a quarter of the work.  256 / 128 rows, 12 heads of 128:
-// 60 workgroups (1000 tokens, causal) 32.9 / 23.3 us, 156 (3000) 75.8 / 52.1, 240 (4680) 117 / 88, not causal 140 / 163; 392 (40 heads on
-// 8, 2 x 1200, causal) 49 / 63.
+// 60 workgroups (1000 tokens, causal) 31.8 / 22.2 us, 156 (3000) 73.2 / 49.9, 240 (4680) 111 / 86, not causal 134 / 162; 392 (40 heads on
+// 8, 2 x 1200, causal) 47 / 62.
 constexpr int SPLIT_ITEMS = 128;
 constexpr float LN2 = 0.6931471805599453f;
 
