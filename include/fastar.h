@@ -457,7 +457,9 @@ typedef struct {
  * bf16: bf16 products (the weights are rounded to bf16; those below 2^-126 of a row's largest are zero), fp32 softmax and
  * sums; fp32: plain fp32 arithmetic.
  * Supported: d in {64, 128}; scale positive, scale * log2(e) finite; rows of K and V at most 2^24 bytes apart;
- * n_tok_q * Hq < 2^30.  No workspace.  n_tok_q = 0 or B = 0 launches nothing.
+ * n_tok_q * Hq < 2^30, n_tok_k <= 2^30.  No workspace.  n_tok_q = 0 or B = 0 launches nothing.
+ * Where a causal call meets infinities or NaN among the values, the queries of the tiles concerned are done again key by key, so
+ * that none sees what is masked for it: right, and many times slower.
  */
 int prompt_attn_fwd(const fastar_rows *Q, const fastar_rows *K, const fastar_rows *V, const int32_t *cu_q,
                     const int32_t *cu_k, int B, int n_tok_q, int n_tok_k, int Hq, int Hkv, int d, int dtype, int causal,
@@ -494,7 +496,9 @@ typedef struct {
  *   len_out [B]       tokens after the step (0 for ended requests); may be len itself
  *   pool_n_out [1]    free pages after the step; may be pool_n itself
  *   cu [B+1]          rows of the requests' new tokens: the prefix sums of max(n_new, 0), cut to n_tok
- *   slot [n_tok]      page * P + offset of each new token; -1 where the request is refused.  Rows from cu[B] on stay.
+ *   slot [n_tok]      page * P + offset of each new token; -1 where the request is refused.  Rows from cu[B] on stay as they
+ *                     are: an array that is used again, in a replayed graph say, is set to -1 before, or kv_pages_write finds
+ *                     the slots of an earlier step there
  *   status [B]        0 (also for ended requests), 1, 2 or 3
  * Lengths and counts are cut to what the arrays hold; a table entry outside of [0, n_pages) gives slot -1.
  * Supported: P in {16, 32, 64}; max_pages * P and n_pages * P < 2^31.  One launch for few tokens, two for many; no workspace.
@@ -527,8 +531,8 @@ int kv_pages_write(const fastar_pages *pages, const fastar_rows *K_new, const fa
  * device reads: long ones are cut into pieces whose fragments lie in ws, and a second launch puts them together.
  *   ws / ws_bytes  fastar_workspace_bytes(FASTAR_OP_PAGED_ATTN, ...) bytes, 256-byte aligned; contents need not be kept.
  *                  Calls that may be in flight at the same time need a workspace each.
- * Supported: bf16, d in {64, 128}, scales of the pages 2^-100 .. 2^120; scale and n_tok * Hq as for
- * prompt_attn_fwd.
+ * Supported: bf16, d in {64, 128}, scales of the pages 2^-100 .. 2^120, max_pages * P <= 2^30; scale, n_tok * Hq and values that
+ * are no numbers as for prompt_attn_fwd.
  */
 int paged_attn_fwd(const fastar_rows *Q, const int32_t *cu_q, const int32_t *len, const int32_t *table, int B, int max_pages,
                    int n_tok, int Hq, const fastar_pages *pages, int dtype, int causal, float scale, const fastar_rows *O,

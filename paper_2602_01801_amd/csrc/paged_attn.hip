@@ -408,7 +408,7 @@ extern "C" int paged_attn_fwd(const fastar_rows *Q, const int32_t *cu_q, const i
     if (!scale_ok(scale) || (causal & ~1)) return FASTAR_ERR_INVALID_ARG;
     if (const int rc = pages_check(pages); rc != FASTAR_OK) return rc;
     if (Hq % pages->Hkv) return FASTAR_ERR_INVALID_ARG;
-    if (dtype != FASTAR_BF16 || (int64_t)max_pages * pages->P > INT32_MAX) return FASTAR_ERR_UNSUPPORTED;
+    if (dtype != FASTAR_BF16 || (int64_t)max_pages * pages->P > MAX_KEYS) return FASTAR_ERR_UNSUPPORTED;
     if ((int64_t)n_tok * Hq > INT32_MAX / 2) return FASTAR_ERR_UNSUPPORTED;
     if (!ws || ((uintptr_t)ws & 255)) return FASTAR_ERR_INVALID_ARG;
     if (ws_bytes < paged_attn_ws_bytes()) return FASTAR_ERR_WORKSPACE;

@@ -358,7 +358,7 @@ extern "C" int prompt_attn_fwd(const fastar_rows *Q, const fastar_rows *K, const
     if (B < 0 || n_tok_q < 0 || n_tok_k < 0 || Hq <= 0 || Hkv <= 0 || Hq % Hkv) return FASTAR_ERR_INVALID_ARG;
     if (!scale_ok(scale) || (causal & ~1)) return FASTAR_ERR_INVALID_ARG;
     if (d != 64 && d != 128) return FASTAR_ERR_UNSUPPORTED;
-    if ((int64_t)n_tok_q * Hq > INT32_MAX / 2) return FASTAR_ERR_UNSUPPORTED;
+    if ((int64_t)n_tok_q * Hq > INT32_MAX / 2 || n_tok_k > MAX_KEYS) return FASTAR_ERR_UNSUPPORTED;
     if (n_tok_q == 0 || B == 0) return FASTAR_OK;
     if (!cu_q || !view_ok(Q, elt) || !view_ok(O, elt) || !rows_apart(O, Hq, n_tok_q, d)) return FASTAR_ERR_INVALID_ARG;
     if (n_tok_k > 0 && (!view_ok(K, elt) || !view_ok(V, elt))) return FASTAR_ERR_INVALID_ARG;

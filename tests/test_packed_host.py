@@ -54,6 +54,11 @@ def test_prompt_attn_refuses(L, over, code):
     assert prompt(L, **over) == code
 
 
+def test_key_positions_stay_in_32_bits_tiles_ahead(L):
+    assert prompt(L, n_k=(1 << 30) + 1) == UNSUPPORTED and prompt(L, n_k=(1 << 31) - 1, dtype=0) == UNSUPPORTED
+    assert paged(L, max_pages=(1 << 24) + 1) == UNSUPPORTED and paged(L, max_pages=(1 << 27) - 1, pg=pages(P=16)) == UNSUPPORTED
+
+
 def test_prompt_attn_of_nothing_is_done_at_once(L):
     assert prompt(L, B=0) == 0 and prompt(L, n_q=0) == 0 and prompt(L, B=0, cu=None) == 0
 
