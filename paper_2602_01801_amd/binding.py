@@ -705,7 +705,8 @@ class Pages:
 def kv_pages_plan(n_new, length, table, pool, pool_n, P: int, n_tok: int, out=None):
     """Block tables and slot maps of the next step: n_new, length [B] int32, table [B,max_pages] and pool [n_pages] int32
     (updated in place), pool_n [1] int32, n_tok rows for new tokens.  Returns (length after, pool_n after, cu [B+1],
-    slot [n_tok], status [B]), all int32; out may name `length` and `pool_n` themselves for the first two."""
+    slot [n_tok], status [B]), all int32; out may name `length` and `pool_n` themselves for the first two.  Slots behind the
+    last new token are -1, in an array of the caller's as they were: it sets them to -1 where a step has fewer tokens than n_tok."""
     B, max_pages = table.shape
     n_pages, dev = pool.numel(), _here()
     if out is None:
