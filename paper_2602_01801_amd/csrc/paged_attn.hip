@@ -181,7 +181,10 @@ __global__ __launch_bounds__(NW * 64, 2) void attn_kernel(const Args a) {
 #pragma unroll
                     for (int v = 0; v < 4; ++v) mx = fmaxf(mx, s[rt][j][v]);
                 mx = max_of_quarters(mx);
-                if (__any((mx - m[rt]) * scale_log2 > TAU)) {
+                // The reference is the maximum itself, so that the weight of a row that one key rules is 1 and loses nothing: 20 tokens
+                // of 16 rows an error of 0.0017 instead of 0.0019 with a reference that may lag 8 octaves, 3 of 9 rows 0.0018 instead
+                // of 0.002, for 0 to 1 % (8 tokens of 24 rows on 1560 keys 4 %).
+                if (__any(mx > m[rt])) {
                     const float mn = fmaxf(m[rt], mx);
                     const float alpha = weight_of(m[rt], mn, scale_log2);
                     m[rt] = mn;

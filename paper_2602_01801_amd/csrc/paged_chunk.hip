@@ -25,6 +25,7 @@ using namespace attn_lds;
 constexpr int NWG = 4;         // wavefronts per group
 constexpr int R = 256;         // rows per item
 constexpr int NK = 2, NV = 3;  // stages
+constexpr float TAU = 8.0f;    // the reference maximum may lag the true one by 8 octaves: weights up to 256
 constexpr int SHARES = 256;
 constexpr int LEAST = 8;       // tiles of a share at least: a fragment costs as much as some of them
 constexpr int FEW_KEYS = 512;  // longer tables are cut while items leave compute units idle (100 tokens x 12 heads on 4 x 2000 keys 72 us whole, 34 cut)
