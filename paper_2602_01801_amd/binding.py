@@ -215,6 +215,8 @@ def workspace_bytes(op: int, H: int, n_q: int, n_k: int, r: int = 32, BQ: int = 
 def _workspace(ws, nbytes: int, device):
     if ws is None:
         ws = torch.empty(max(nbytes, 256), dtype=torch.uint8, device=device)
+    elif ws.get_device() != device.index or not ws.is_contiguous():   # a kernel writes through its address
+        raise ValueError(f"the workspace must be a contiguous tensor on {device}, got one on {ws.device}")
     if ws.numel() * ws.element_size() < nbytes:
         raise FastarError("workspace too small")
     return ws

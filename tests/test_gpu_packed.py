@@ -667,3 +667,16 @@ def test_the_binding_refuses_what_does_not_fit():
         fa.Pages(pages.K8, pages.kscale, pages.V8.view(torch.int8), pages.vscale)
     with pytest.raises(ValueError):
         fa.kv_pages_plan(i32([1]), i32([0, 0]), i32([[0]]), i32([0]), i32([1]), 16, 1)
+
+
+def test_workspaces_that_do_not_fit_are_refused():
+    """Nothing is launched."""
+    Q, cu, length, table = torch.zeros((4, 8, 128), dtype=torch.bfloat16, device="cuda"), i32([0, 8]), i32([8]), i32([[0]])
+    pages = fa.Pages.empty(4, 2, 16, 128)
+    n = fa.workspace_bytes(fa.OP_PAGED_ATTN, 4, 8, 0)
+    for ws in (torch.empty(n, dtype=torch.uint8), torch.empty((n, 2), dtype=torch.uint8, device="cuda")[:, 0]):
+        with pytest.raises(ValueError):
+            fa.paged_attn_fwd(Q, cu, length, table, pages, ws=ws)
+    q = torch.zeros((1, 128, 32), dtype=torch.int8, device="cuda")
+    with pytest.raises(ValueError):
+        fa.ann_select_self(q, q, i32([128]), 128, 4, 64, 1, ws=torch.empty(1 << 20, dtype=torch.uint8))

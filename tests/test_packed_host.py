@@ -116,6 +116,17 @@ def test_write_of_nothing_is_done_at_once(L):
     assert write(L, n=0) == 0 and write(L, n=0, slot=None) == 0
 
 
+def test_a_workspace_that_a_kernel_cannot_write_to_is_refused():
+    """Its size alone was looked at: the address of a host tensor went to the kernel."""
+    import torch
+    from paper_2602_01801_amd.binding import _workspace
+    dev = torch.device("cuda", 0)
+    with pytest.raises(ValueError):
+        _workspace(torch.empty(4096, dtype=torch.uint8), 256, dev)
+    with pytest.raises(ValueError):
+        _workspace(torch.empty(4096, dtype=torch.uint8, device="meta"), 256, dev)
+
+
 # ------------------------------------------------------------------------------------------------ the references
 
 
