@@ -313,9 +313,10 @@ __global__ __launch_bounds__(2 * NWG * 64, 1) void attn_bf16_kernel(const Args a
     }
     if (a.lse && g == 0 && row0 + col < n_rows)
         a.lse[(size_t)my_head * a.n_tok_q + rq.first + my_tok] = l == 0.0f ? -INFINITY : (m * scale_log2 + __log2f(l)) * LN2;
-    // Sums that are no numbers, where rows see different keys: a value that a row does not see may have come in as 0 * x (a
-    // product of tiles has no other way).  Those rows are done again key by key, over the keys that they see.
-    if (a.causal && __any(odd)) {
+    // Sums that are not finite: a value that a row does not see, or key 0's, which fills up the last tile, may have come in as 0 * x
+    // (a product of tiles has no other way), or a weight of up to 256 times a value have left the range.  Those rows are done again
+    // key by key, over the keys that they see and against their largest score.
+    if (__any(odd)) {
         for (int r = 0; r < 32 && row0 + r < n_rows; ++r) {
             const int rr = row0 + r, tok = rr / a.group, head = h * a.group + rr - tok * a.group, seen = sees(rr);
             float mr, lr, acc[D / 64];

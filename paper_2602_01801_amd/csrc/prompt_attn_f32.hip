@@ -297,8 +297,8 @@ __global__ __launch_bounds__(TEAMS * RW * 64, 2) void attn_f32_prompt_kernel(con
         if (a.lse && quarter == 0)
             a.lse[(size_t)my_head * a.n_tok_q + rq.first + my_tok] = l == 0.0f ? -INFINITY : (m * scale_log2 + __log2f(l)) * LN2;
     }
-    // as in prompt_attn.hip: rows that a value which they do not see may have spoilt
-    if (a.causal && __any(odd)) {
+    // as in prompt_attn.hip: rows whose sums are not finite
+    if (__any(odd)) {
         for (int r = 0; r < 16 && row0 + r < n_rows; ++r) {
             const int rr = row0 + r, tok = rr / a.group, head = h * a.group + rr - tok * a.group;
             float mr, lr, acc[D / 64];

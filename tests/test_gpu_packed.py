@@ -680,3 +680,59 @@ def test_workspaces_that_do_not_fit_are_refused():
     q = torch.zeros((1, 128, 32), dtype=torch.int8, device="cuda")
     with pytest.raises(ValueError):
         fa.ann_select_self(q, q, i32([128]), 128, 4, 64, 1, ws=torch.empty(1 << 20, dtype=torch.uint8))
+
+
+# ------------------------------------------------------------------------------------------------ the ends of the range
+
+
+def check_kinds(O, lse, want, n, d, bf16, what=""):
+    """Infinities, NaN and finite numbers where the definition has them; the finite ones as everywhere."""
+    Or, lr, A, S, vmax = want
+    o = f64(O)
+    for kind in (np.isnan, np.isposinf, np.isneginf):
+        assert (kind(o) == kind(Or)).all(), (what, kind.__name__, np.argwhere(kind(o) != kind(Or))[:4], o[kind(o) != kind(Or)][:4])
+    fin = np.isfinite(Or)
+    check(torch.from_numpy(np.where(fin, o, 0.0)), lse, (np.where(fin, Or, 0.0), lr, np.where(fin, A, 0.0), S, vmax), n, d, bf16, what)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("Hkv,q", [(2, 5), (40, 420)])   # few workgroups, and launches that fill the chip
+@pytest.mark.parametrize("n", [1, 17, 64, 70, 130])
+def test_infinite_values_of_the_first_key(n, Hkv, q, dtype):
+    """Tiles are filled up with the first key, at weight 0: infinite values of it made the sums no numbers, by the length modulo
+    the tile."""
+    g = torch.Generator().manual_seed(n)
+    d, Hq = 128, 2 * Hkv
+    Q, K, V = (view(g, h, m, d, DT[dtype], "tokens") for h, m in ((Hq, q), (Hkv, n), (Hkv, n)))
+    V[:, 0, 3], V[:, 0, 70], V[:, 0, 127] = math.inf, -math.inf, math.nan
+    V[:, n // 2, 5] = -math.inf
+    O, lse = fa.prompt_attn_fwd(Q, K, V, i32([0, q]), i32([0, n]), causal=False)
+    for h in {0, 1, Hq - 1}:
+        with np.errstate(invalid="ignore"):
+            want = ref.attend(f64(Q[h:h + 1]), f64(K[h // 2:h // 2 + 1]), f64(V[h // 2:h // 2 + 1]), False, d ** -0.5)
+        check_kinds(O[h:h + 1], lse[h:h + 1], want, n, d, dtype == "bf16", f"head {h}")
+
+
+def climbing(Hq, Hkv, q, n, d, at, octaves=7.5):
+    """Scores of 0, and key `at` of so many octaves: Q, K and the scale."""
+    Q, K = torch.zeros((Hq, q, d)), torch.zeros((Hkv, n, d))
+    Q[:, :, 0], K[:, at, 0] = 8.0, octaves
+    return Q, K, math.log(2.0) / 8
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("Hkv,q", [(2, 5), (40, 420)])
+def test_prompt_attention_of_large_values_under_climbing_scores(Hkv, q, causal, dtype):
+    """A value of 2^121 under a key whose score is 7.5 octaves above those before it: its weight against the first tile's maximum
+    is 181, and their product beyond the range."""
+    n, d = 470, 128
+    Q, K, scale = climbing(2 * Hkv, Hkv, q, n, d, at=40 if causal and q == 420 else 100)
+    V = torch.randn((Hkv, n, d), generator=torch.Generator().manual_seed(1))
+    V[:, 40 if causal and q == 420 else 100] = 2.0 ** 121
+    Q, K, V = (x.to(DT[dtype]).cuda() for x in (Q, K, V))
+    O, lse = fa.prompt_attn_fwd(Q, K, V, i32([0, q]), i32([0, n]), causal=causal, scale=scale)
+    for h in {0, 2 * Hkv - 1}:
+        want = ref.attend(f64(Q[h:h + 1]), f64(K[h // 2:h // 2 + 1]), f64(V[h // 2:h // 2 + 1]), causal, float(np.float32(scale)))
+        assert np.isfinite(want[0]).all()
+        check_kinds(O[h:h + 1], lse[h:h + 1], want, n, d, dtype == "bf16", f"head {h}")
