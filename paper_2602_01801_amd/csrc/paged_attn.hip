@@ -42,7 +42,7 @@ template <int D, int RT, bool SPLIT, int NW>
 __global__ __launch_bounds__(NW * 64, 2) void attn_kernel(const Args a) {
     constexpr int R = 16 * RT, DB = D / 16, KS = D / 64;
     constexpr int NS = NW < 4 ? NW : 4;   // wavefronts' sums that LDS holds at a time
-    __shared__ int s_flag;
+    __shared__ int s_odd;   // the last piece with sums that are not finite
     __shared__ float s_m[NW][R], s_l[NW][R];
     __shared__ f32x4 s_o[NS][DB][64];
     const int tid = threadIdx.x, lane = tid & 63;
@@ -58,10 +58,13 @@ __global__ __launch_bounds__(NW * 64, 2) void attn_kernel(const Args a) {
         return;
     }
     Desc d = {0, 0, 0, -1};
+    if (tid == 0) s_odd = 0;   // read behind the first barriers
+    int turn = 0;
     while (r.u < r.u_end) {   // uniform: one piece of one item per turn
         if (SPLIT && r.u >= r.base + (long long)sq.n_qt * Hkv * (sq.n_tiles + ENDS)) find_unit<R, SPLIT>(a, r.u, r.b, r.base, sq);
         const PieceOf piece = next_piece<SPLIT>(r, sq);
         if (piece.te <= piece.ta) continue;
+        ++turn;
         const int h = piece.h, qt = piece.qt, ta = piece.ta, te = piece.te;
         const bool begins = ta == 0, ends = te == sq.n_tiles;
 
@@ -232,7 +235,6 @@ __global__ __launch_bounds__(NW * 64, 2) void attn_kernel(const Args a) {
                 s_l[w][16 * rt + row] = l[rt];
             }
         }
-        if (tid == 0) s_flag = 0;
         __syncthreads();
         const bool whole = begins && ends;
         float *frag = SPLIT ? a.frag + (size_t)(2 * r.share + (begins ? 1 : 0)) * FRAG_FLOATS : nullptr;
@@ -292,36 +294,32 @@ __global__ __launch_bounds__(NW * 64, 2) void attn_kernel(const Args a) {
                     frag[R * D + R + 16 * rt + row] = l_all;
                 }
             }
+            if (odd) s_odd = turn;
             __syncthreads();
         }
-        // Sums that are no numbers, where rows see different keys: a value that a row does not see may have come in as 0 * x
-        // (a product of tiles has no other way).  Those rows are done again key by key, over the keys that they see.
-        if (a.causal && sq.n_q > 1) {
-            if (odd) s_flag = 1;
-            __syncthreads();
-            if (s_flag) {
-                for (int i = w; i < R && qt * R + i < n_rows; i += NW) {
-                    const int rr = qt * R + i, tok = rr / a.group, head = h * a.group + rr - tok * a.group;
-                    float mr, lr, acc[D / 64];
-                    row_by_paged_keys<D>(a, a.Q.p + head * a.Q.head + (int64_t)(sq.q0 + tok) * a.Q.row, pages, h, ta * TK,
-                                         min(min(sq.L - sq.n_q + tok + 1, sq.L), te * TK), mr, lr, acc);
+        // Sums that are not finite: a value that a row does not see may have come in as 0 * x (a product of tiles has no other way), or
+        // they have left the range.  Those rows are done again key by key, over the keys that they see.
+        if (__builtin_amdgcn_readfirstlane(s_odd) == turn) {
+            for (int i = w; i < R && qt * R + i < n_rows; i += NW) {
+                const int rr = qt * R + i, tok = rr / a.group, head = h * a.group + rr - tok * a.group;
+                float mr, lr, acc[D / 64];
+                row_by_paged_keys<D>(a, a.Q.p + head * a.Q.head + (int64_t)(sq.q0 + tok) * a.Q.row, pages, h, ta * TK,
+                                     min(a.causal ? min(sq.L - sq.n_q + tok + 1, sq.L) : sq.L, te * TK), mr, lr, acc);
 #pragma unroll
-                    for (int c = 0; c < D / 64; ++c) {
-                        const int co = 64 * c + lane;
-                        if (whole) ((__bf16 *)(a.O.p + head * a.O.head + (int64_t)(sq.q0 + tok) * a.O.row))[co] = (__bf16)(lr == 0.0f ? 0.0f : acc[c] / lr);
-                        else frag[(((i >> 4) * DB + (co >> 4)) * 64 + ((co & 15) >> 2) * 16 + (i & 15)) * 4 + (co & 3)] = acc[c];
-                    }
-                    if (lane == 0) {
-                        if (whole) {
-                            if (a.lse) a.lse[(size_t)head * a.n_tok + sq.q0 + tok] = lr == 0.0f ? -INFINITY : (mr * scale_log2 + __log2f(lr)) * LN2;
-                        } else {
-                            frag[R * D + i] = mr;
-                            frag[R * D + R + i] = lr;
-                        }
+                for (int c = 0; c < D / 64; ++c) {
+                    const int co = 64 * c + lane;
+                    if (whole) ((__bf16 *)(a.O.p + head * a.O.head + (int64_t)(sq.q0 + tok) * a.O.row))[co] = (__bf16)(lr == 0.0f ? 0.0f : acc[c] / lr);
+                    else frag[(((i >> 4) * DB + (co >> 4)) * 64 + ((co & 15) >> 2) * 16 + (i & 15)) * 4 + (co & 3)] = acc[c];
+                }
+                if (lane == 0) {
+                    if (whole) {
+                        if (a.lse) a.lse[(size_t)head * a.n_tok + sq.q0 + tok] = lr == 0.0f ? -INFINITY : (mr * scale_log2 + __log2f(lr)) * LN2;
+                    } else {
+                        frag[R * D + i] = mr;
+                        frag[R * D + R + i] = lr;
                     }
                 }
             }
-            __syncthreads();
         }
         if (SPLIT && begins && !ends) d = Desc{r.b, h, qt, share_of(r, piece.last)};
     }

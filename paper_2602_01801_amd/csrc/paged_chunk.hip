@@ -335,8 +335,8 @@ __global__ __launch_bounds__(2 * NWG * 64, 1) void attn_chunk_kernel(const Args 
                 frag[R * D + R + wave * 32 + col_e] = l;
             }
         }
-        // as in paged_attn.hip: rows that a value which they do not see may have spoilt
-        if (a.causal && sq.n_q > 1 && __any(odd)) {
+        // as in paged_attn.hip: rows whose sums are not finite (here a weight of up to 256 times a value may have left the range too)
+        if (__any(odd)) {
             __threadfence();
             for (int x = 0; x < 32 && row0_e + x < n_rows; ++x) {
                 const int rr = row0_e + x, tok = rr / a.group, head = h * a.group + rr - tok * a.group;

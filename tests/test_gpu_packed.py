@@ -736,3 +736,41 @@ def test_prompt_attention_of_large_values_under_climbing_scores(Hkv, q, causal, 
         want = ref.attend(f64(Q[h:h + 1]), f64(K[h // 2:h // 2 + 1]), f64(V[h // 2:h // 2 + 1]), causal, float(np.float32(scale)))
         assert np.isfinite(want[0]).all()
         check_kinds(O[h:h + 1], lse[h:h + 1], want, n, d, dtype == "bf16", f"head {h}")
+
+
+def flat_pages(n, Hkv, P, d, seed, kexp=(-8, -6), vexp=(-8, -6)):
+    """Pages of a sequence of n tokens in any order, with two that belong to nobody: codes from 1 to 448 of either sign, so that scores of ordinary queries
+    spread by about one and the values by their sign; and the table."""
+    rng = np.random.default_rng(seed)
+    per = max(-(-n // P), 1)
+    code = lambda: (rng.integers(0x38, 0x7F, size=(per + 2, Hkv, P // 16, d // 16, 16, 16)) | 128 * rng.integers(0, 2, size=(per + 2, Hkv, P // 16, d // 16, 16, 16))).astype(np.uint8)
+    scale = lambda lo, hi: 2.0 ** rng.integers(lo, hi + 1, size=(per + 2, Hkv))
+    return code(), scale(*kexp), code(), scale(*vexp), rng.permutation(per + 2)[:per].astype(np.int32)[None]
+
+
+def on_device(K, ks, V, vs):
+    return fa.Pages(*(torch.from_numpy(x.astype(np.float32) if x.dtype == np.float64 else x).cuda() for x in (K, ks, V, vs)))
+
+
+PAGED_ENDS = [(40, 1, 16, 128, 1, 470), (40, 1, 64, 64, 1, 5000), (4, 2, 32, 128, 50, 470), (4, 1, 64, 128, 130, 9000)]   # chunks: rows > 32 each
+
+
+@pytest.mark.parametrize("Hq,Hkv,P,d,q,n", PAGED_ENDS)
+@pytest.mark.parametrize("causal", [False, True])
+def test_paged_attention_of_large_values_under_climbing_scores(Hq, Hkv, P, d, q, n, causal):
+    """As for prompts, over pages: a value of 2^121 from a code of 2 and a scale of 2^120."""
+    K, ks, V, vs, table = flat_pages(n, Hkv, P, d, n)
+    Q, _, scale = climbing(Hq, Hkv, q, n, d, 100)
+    p, off = table[0, 100 // P], 100 % P
+    rows = np.zeros((K.shape[0], Hkv, P, d), np.uint8)
+    rows[p, :, off, 0] = ref.code_of(7.5)
+    K, ks = ref.cells_of_rows(rows, False), np.ones_like(ks)
+    rows = ref.rows_of_cells(V, True).copy()
+    rows[p] = 0
+    rows[p, :, off] = ref.code_of(2.0)
+    V, vs[p] = ref.cells_of_rows(rows, True), 2.0 ** 120
+    Q = Q.bfloat16().cuda()
+    O, lse = fa.paged_attn_fwd(Q, i32([0, q]), i32([n]), i32(table), on_device(K, ks, V, vs), causal=causal, scale=scale)
+    want = ref.attend(f64(Q), gather(K, ks, table[0], n, False), gather(V, vs, table[0], n, True), causal, float(np.float32(scale)))
+    assert np.isfinite(want[0]).all()
+    check_kinds(O, lse, want, n, d, True)
