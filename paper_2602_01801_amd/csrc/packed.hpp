@@ -112,35 +112,76 @@ __device__ __forceinline__ bool find_item(const int32_t *__restrict__ cu_q, cons
     return false;
 }
 
-// One row key by key over the keys that it sees, a wavefront, lane l coordinates l, l + 64: what tiles whose products brought in
-// numbers that are none fall back to.
-template <typename T, int D>
-__device__ __forceinline__ void row_by_keys(const char *q, const char *K, int64_t k_pitch, const char *V, int64_t v_pitch, int seen,
-                                            float scale_log2, float &m, float &l, float (&o)[D / 64]) {
+// One row over the keys first .. seen - 1, a wavefront: what tiles whose sums are not finite fall back to.  The maximum and the sum of
+// the weights come first, so that values are taken with weights that add up to one and their sum stays where the values are; a
+// key per lane for the scores, then lane l coordinates l, l + 64 for the values.  score(j, q): q.k of key j by this lane, which no
+// other lane shares, or -inf; value(j, c): coordinate 64 c + lane of key j; seen_at(j): whether uniform key j has a value.
+template <int D, class Score, class Seen, class Value>
+__device__ __forceinline__ void row_again(int first, int seen, float scale_log2, Score score, Seen seen_at, Value value, float &m, float &l,
+                                          float (&o)[D / 64]) {
     const int lane = lane_id();
-    float qv[D / 64];
     m = -INFINITY;
     l = 0.0f;
 #pragma unroll
-    for (int c = 0; c < D / 64; ++c) {
-        o[c] = 0.0f;
-        qv[c] = (float)((const T *)q)[64 * c + lane];
-    }
-    for (int j = 0; j < seen; ++j) {
-        const T *kp = (const T *)(K + (int64_t)j * k_pitch), *vp = (const T *)(V + (int64_t)j * v_pitch);
-        float x = 0.0f;
+    for (int c = 0; c < D / 64; ++c) o[c] = 0.0f;
+    auto scored = [&](int j0) __attribute__((always_inline)) {   // all lanes together: they hold the query's coordinates
+        const float x = score(min(j0 + lane, seen - 1));
+        return j0 + lane < seen ? x : -INFINITY;
+    };
+    for (int j0 = first; j0 < seen; j0 += 64) {
+        const float x = scored(j0);
+        float mn = fmaxf(m, x);
 #pragma unroll
-        for (int c = 0; c < D / 64; ++c) x = fmaf(qv[c], (float)kp[64 * c + lane], x);
-#pragma unroll
-        for (int i = 32; i > 0; i >>= 1) x += shfl_xor(x, i);
-        const float mn = fmaxf(m, x);
-        const float al = m == -INFINITY ? 0.0f : exp2f((m - mn) * scale_log2);
-        const float p = exp2f((x - (mn == -INFINITY ? 0.0f : mn)) * scale_log2);
+        for (int i = 32; i > 0; i >>= 1) mn = fmaxf(mn, shfl_xor(mn, i));
+        l = l * (m == -INFINITY ? 0.0f : exp2f((m - mn) * scale_log2)) + exp2f((x - (mn == -INFINITY ? 0.0f : mn)) * scale_log2);
         m = mn;
-        l = l * al + p;
-#pragma unroll
-        for (int c = 0; c < D / 64; ++c) o[c] = o[c] * al + p * (float)vp[64 * c + lane];
+        if (__any(l != l)) break;   // and stays so
     }
+#pragma unroll
+    for (int i = 32; i > 0; i >>= 1) l += shfl_xor(l, i);
+    if (l != l) {
+#pragma unroll
+        for (int c = 0; c < D / 64; ++c) o[c] = l;
+        return;
+    }
+    const float inv = l == 0.0f ? 0.0f : 1.0f / l, m0 = m == -INFINITY ? 0.0f : m;
+    for (int j0 = first; j0 < seen; j0 += 64) {
+        const float w = exp2f((scored(j0) - m0) * scale_log2) * inv;
+        for (int j = j0; j < min(j0 + 64, seen); ++j) {
+            if (!seen_at(j)) continue;
+            const float wj = __uint_as_float((unsigned)__builtin_amdgcn_readlane((int)__float_as_uint(w), j - j0));
+#pragma unroll
+            for (int c = 0; c < D / 64; ++c) o[c] = fmaf(wj, value(j, c), o[c]);
+        }
+    }
+}
+// The query's coordinate 64 h + i of lane i's qv[h].
+__device__ __forceinline__ float of_lane(float x, int i) { return __uint_as_float((unsigned)__builtin_amdgcn_readlane((int)__float_as_uint(x), i)); }
+
+template <typename T, int D>
+__device__ __forceinline__ void row_by_keys(const char *q, const char *K, int64_t k_pitch, const char *V, int64_t v_pitch, int seen,
+                                            float scale_log2, float &m, float &l, float (&o)[D / 64]) {
+    constexpr int E = 16 / sizeof(T);
+    typedef __attribute__((ext_vector_type(E))) T Chunk;
+    const int lane = lane_id();
+    float qv[D / 64];
+#pragma unroll
+    for (int c = 0; c < D / 64; ++c) qv[c] = (float)((const T *)q)[64 * c + lane];
+    row_again<D>(
+        0, seen, scale_log2,
+        [&](int j) __attribute__((always_inline)) {
+            const Chunk *kp = (const Chunk *)(K + (int64_t)j * k_pitch);
+            float x = 0.0f;
+#pragma unroll
+            for (int h = 0; h < D / 64; ++h)
+                for (int i = 0; i < 64; i += E) {
+                    const Chunk k = kp[(64 * h + i) / E];
+#pragma unroll
+                    for (int e = 0; e < E; ++e) x = fmaf(of_lane(qv[h], i + e), (float)k[e], x);
+                }
+            return x;
+        },
+        [](int) { return true; }, [&](int j, int c) __attribute__((always_inline)) { return (float)((const T *)(V + (int64_t)j * v_pitch))[64 * c + lane]; }, m, l, o);
 }
 
 }  // namespace fastar

@@ -308,7 +308,7 @@ __global__ __launch_bounds__(NW * 64, 2) void attn_kernel(const Args a) {
 #pragma unroll
                 for (int c = 0; c < D / 64; ++c) {
                     const int co = 64 * c + lane;
-                    if (whole) ((__bf16 *)(a.O.p + head * a.O.head + (int64_t)(sq.q0 + tok) * a.O.row))[co] = (__bf16)(lr == 0.0f ? 0.0f : acc[c] / lr);
+                    if (whole) ((__bf16 *)(a.O.p + head * a.O.head + (int64_t)(sq.q0 + tok) * a.O.row))[co] = (__bf16)acc[c];
                     else frag[(((i >> 4) * DB + (co >> 4)) * 64 + ((co & 15) >> 2) * 16 + (i & 15)) * 4 + (co & 3)] = acc[c];
                 }
                 if (lane == 0) {
@@ -316,7 +316,7 @@ __global__ __launch_bounds__(NW * 64, 2) void attn_kernel(const Args a) {
                         if (a.lse) a.lse[(size_t)head * a.n_tok + sq.q0 + tok] = lr == 0.0f ? -INFINITY : (mr * scale_log2 + __log2f(lr)) * LN2;
                     } else {
                         frag[R * D + i] = mr;
-                        frag[R * D + R + i] = lr;
+                        frag[R * D + R + i] = -lr;   // its sums add up to one
                     }
                 }
             }
@@ -348,9 +348,9 @@ __global__ __launch_bounds__(256) void combine_kernel(const Args a) {
 #pragma unroll 8
     for (int i = w; i < n; i += NW) {
         const float *f = frag(i);
-        const float wt = weight_of(f[R * D + 16 * rt + row], m_all, a.scale_log2);
-        x += ((const f32x4 *)f)[(rt * DB + db) * 64 + lane] * wt;
-        l += f[R * D + R + 16 * rt + row] * wt;
+        const float wt = weight_of(f[R * D + 16 * rt + row], m_all, a.scale_log2), lf = f[R * D + R + 16 * rt + row];
+        x += ((const f32x4 *)f)[(rt * DB + db) * 64 + lane] * parts_of(lf, wt);
+        l += fabsf(lf) * wt;
     }
     s_o[w][lane] = x;
     if (quarter == 0) s_l[w][row] = l;
@@ -367,7 +367,15 @@ __global__ __launch_bounds__(256) void combine_kernel(const Args a) {
     if (rr >= sq.n_q * a.group) return;
     const int tok = rr / a.group, head = d.h * a.group + rr - tok * a.group;
     const float inv = l == 0.0f ? 0.0f : 1.0f / l;
-    const bf16x4 y = {(__bf16)(x[0] * inv), (__bf16)(x[1] * inv), (__bf16)(x[2] * inv), (__bf16)(x[3] * inv)};
+    x *= inv;
+    if (!finite(x)) {   // sums beyond the range: again with weights that add up to one
+        x = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+        for (int i = 0; i < n; ++i) {
+            const float *f = frag(i);
+            x += ((const f32x4 *)f)[(rt * DB + db) * 64 + lane] * parts_of(f[R * D + R + 16 * rt + row], weight_of(f[R * D + 16 * rt + row], m_all, a.scale_log2) * inv);
+        }
+    }
+    const bf16x4 y = {(__bf16)x[0], (__bf16)x[1], (__bf16)x[2], (__bf16)x[3]};
     *(bf16x4 *)(a.O.p + head * a.O.head + (int64_t)(sq.q0 + tok) * a.O.row + (16 * db + 4 * quarter) * 2) = y;
     if (a.lse && db == 0 && quarter == 0)
         a.lse[(size_t)head * a.n_tok + sq.q0 + tok] = l == 0.0f ? -INFINITY : (m_all * a.scale_log2 + __log2f(l)) * LN2;

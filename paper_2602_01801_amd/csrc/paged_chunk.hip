@@ -345,7 +345,7 @@ __global__ __launch_bounds__(2 * NWG * 64, 1) void attn_chunk_kernel(const Args 
 #pragma unroll
                 for (int c = 0; c < D / 64; ++c) {
                     const int co = 64 * c + lane_e;
-                    if (whole) ((__bf16 *)(a.O.p + head * a.O.head + (int64_t)(sq.q0 + tok) * a.O.row))[co] = (__bf16)(lr == 0.0f ? 0.0f : acc[c] / lr);
+                    if (whole) ((__bf16 *)(a.O.p + head * a.O.head + (int64_t)(sq.q0 + tok) * a.O.row))[co] = (__bf16)acc[c];
                     else frag[(((wave * DB + (co >> 5)) * 4 + ((co & 31) >> 3)) * 64 + ((co & 7) >> 2) * 32 + x) * 4 + (co & 3)] = acc[c];
                 }
                 if (lane_e == 0) {
@@ -353,7 +353,7 @@ __global__ __launch_bounds__(2 * NWG * 64, 1) void attn_chunk_kernel(const Args 
                         if (a.lse) a.lse[(size_t)head * a.n_tok + sq.q0 + tok] = lr == 0.0f ? -INFINITY : (mr * scale_log2 + __log2f(lr)) * LN2;
                     } else {
                         frag[R * D + wave * 32 + x] = mr;
-                        frag[R * D + R + wave * 32 + x] = lr;
+                        frag[R * D + R + wave * 32 + x] = -lr;   // its sums add up to one
                     }
                 }
             }
@@ -384,15 +384,24 @@ __global__ __launch_bounds__(256) void combine_chunk_kernel(const Args a) {
 #pragma unroll 4
     for (int i = 0; i < n; ++i) {
         const float *f = fragment<FRAG_FLOATS>(a, first, i);
-        const float wt = weight_of(f[R * D + wave * 32 + col], m_all, a.scale_log2);
-        x += ((const f32x4 *)f)[((wave * DB + db) * 4 + q4) * 64 + lane] * wt;
-        l += f[R * D + R + wave * 32 + col] * wt;
+        const float wt = weight_of(f[R * D + wave * 32 + col], m_all, a.scale_log2), lf = f[R * D + R + wave * 32 + col];
+        x += ((const f32x4 *)f)[((wave * DB + db) * 4 + q4) * 64 + lane] * parts_of(lf, wt);
+        l += fabsf(lf) * wt;
     }
     const int rr = d.qt * R + wave * 32 + col;
     if (rr >= n_rows) return;
     const int tok = rr / a.group, head = d.h * a.group + rr - tok * a.group;
     const float inv = l == 0.0f ? 0.0f : 1.0f / l;
-    const bf16x4 y = {(__bf16)(x[0] * inv), (__bf16)(x[1] * inv), (__bf16)(x[2] * inv), (__bf16)(x[3] * inv)};
+    x *= inv;
+    if (!finite(x)) {   // sums beyond the range: again with weights that add up to one
+        x = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+        for (int i = 0; i < n; ++i) {
+            const float *f = fragment<FRAG_FLOATS>(a, first, i);
+            x += ((const f32x4 *)f)[((wave * DB + db) * 4 + q4) * 64 + lane] *
+                 parts_of(f[R * D + R + wave * 32 + col], weight_of(f[R * D + wave * 32 + col], m_all, a.scale_log2) * inv);
+        }
+    }
+    const bf16x4 y = {(__bf16)x[0], (__bf16)x[1], (__bf16)x[2], (__bf16)x[3]};
     *(bf16x4 *)(a.O.p + head * a.O.head + (int64_t)(sq.q0 + tok) * a.O.row + (32 * db + 8 * q4 + 4 * g) * 2) = y;
     if (a.lse && db == 0 && q4 == 0 && g == 0)
         a.lse[(size_t)head * a.n_tok + sq.q0 + tok] = l == 0.0f ? -INFINITY : (m_all * a.scale_log2 + __log2f(l)) * LN2;

@@ -190,6 +190,8 @@ __device__ __forceinline__ float weight_of(float m, float m_all, float scale_log
     return m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f((m - m_all) * scale_log2);
 }
 
+__device__ __forceinline__ bool finite(f32x4 x) { return fabsf(x[0]) < INFINITY && fabsf(x[1]) < INFINITY && fabsf(x[2]) < INFINITY && fabsf(x[3]) < INFINITY; }
+
 // Eight codes times a power of two, exactly.
 __device__ __forceinline__ bf16x8 widen(unsigned lo, unsigned hi, float scale) {
     const bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, scale, false), b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, scale, true);
@@ -208,42 +210,51 @@ __device__ __forceinline__ u32x4 first_bytes(int live) {
     return mask;
 }
 
-// One row key by key over keys first .. seen - 1, a wavefront, lane l coordinates l, l + 64 (see row_by_keys).
+// One row over keys first .. seen - 1 of its pages (see row_again).
 template <int D>
 __device__ __forceinline__ void row_by_paged_keys(const Args &a, const char *q, const int32_t *pages, int h, int first, int seen, float &m,
                                                   float &l, float (&o)[D / 64]) {
     const int lane = lane_id();
     float qv[D / 64];
-    m = -INFINITY;
-    l = 0.0f;
 #pragma unroll
-    for (int c = 0; c < D / 64; ++c) {
-        o[c] = 0.0f;
-        qv[c] = (float)((const __bf16 *)q)[64 * c + lane];
-    }
-    for (int j = first; j < seen; ++j) {
-        const int page = pages[j >> a.pshift];
-        if (!page_exists(a, page)) continue;
-        const size_t ph = (size_t)page * a.pg.Hkv + h;
-        const int off = j & ((1 << a.pshift) - 1);
-        const size_t cell = ph * ((size_t)D << a.pshift) + (off >> 4) * (16 * D);
-        float x = 0.0f, v[D / 64];
+    for (int c = 0; c < D / 64; ++c) qv[c] = (float)((const __bf16 *)q)[64 * c + lane];
+    auto cell_of = [&](int page, int off) __attribute__((always_inline)) {   // first byte of the cells of a token's block of 16
+        return ((size_t)page * a.pg.Hkv + h) * ((size_t)D << a.pshift) + (off >> 4) * (16 * D);
+    };
+    const int in_page = (1 << a.pshift) - 1;
+    row_again<D>(
+        first, seen, a.scale_log2,
+        [&](int j) __attribute__((always_inline)) {
+            const int id = pages[j >> a.pshift], page = page_exists(a, id) ? id : 0, off = j & in_page;
+            const uint8_t *k8 = a.pg.K8 + cell_of(page, off) + (off & 15) * 16;
+            float x = 0.0f;
+            const float ks = a.pg.kscale[(size_t)page * a.pg.Hkv + h];
 #pragma unroll
-        for (int c = 0; c < D / 64; ++c) {
-            const int co = 64 * c + lane;
-            x = fmaf(qv[c], __builtin_amdgcn_cvt_f32_fp8((int)a.pg.K8[cell + (co >> 4) * 256 + (off & 15) * 16 + (co & 15)], 0) * a.pg.kscale[ph], x);
-            v[c] = __builtin_amdgcn_cvt_f32_fp8((int)a.pg.V8[cell + (co >> 4) * 256 + (co & 15) * 16 + (off & 15)], 0) * a.pg.vscale[ph];
-        }
+            for (int hh = 0; hh < D / 64; ++hh)
+                for (int i = 0; i < 64; i += 16) {
+                    const u32x4 k = *(const u32x4 *)(k8 + (64 * hh + i) * 16);
 #pragma unroll
-        for (int i = 32; i > 0; i >>= 1) x += shfl_xor(x, i);
-        const float mn = fmaxf(m, x);
-        const float al = m == -INFINITY ? 0.0f : exp2f((m - mn) * a.scale_log2), p = exp2f((x - (mn == -INFINITY ? 0.0f : mn)) * a.scale_log2);
-        m = mn;
-        l = l * al + p;
-#pragma unroll
-        for (int c = 0; c < D / 64; ++c) o[c] = o[c] * al + p * v[c];
-    }
+                    for (int e = 0; e < 4; ++e) {
+                        x = fmaf(of_lane(qv[hh], i + 4 * e), __builtin_amdgcn_cvt_f32_fp8((int)k[e], 0) * ks, x);
+                        x = fmaf(of_lane(qv[hh], i + 4 * e + 1), __builtin_amdgcn_cvt_f32_fp8((int)k[e], 1) * ks, x);
+                        x = fmaf(of_lane(qv[hh], i + 4 * e + 2), __builtin_amdgcn_cvt_f32_fp8((int)k[e], 2) * ks, x);
+                        x = fmaf(of_lane(qv[hh], i + 4 * e + 3), __builtin_amdgcn_cvt_f32_fp8((int)k[e], 3) * ks, x);
+                    }
+                }
+            return page_exists(a, id) ? x : -INFINITY;
+        },
+        [&](int j) __attribute__((always_inline)) { return page_exists(a, pages[j >> a.pshift]); },
+        [&](int j, int c) __attribute__((always_inline)) {
+            const int page = pages[j >> a.pshift], off = j & in_page, co = 64 * c + lane;
+            return __builtin_amdgcn_cvt_f32_fp8((int)a.pg.V8[cell_of(page, off) + (co >> 4) * 256 + (co & 15) * 16 + (off & 15)], 0) *
+                   a.pg.vscale[(size_t)page * a.pg.Hkv + h];
+        },
+        m, l, o);
 }
+
+// What a fragment's sums count for against the others': its weight; sums of rows that were done again add up to one, which the sign of
+// their sum of weights says (theirs is that times its size).
+__device__ __forceinline__ float parts_of(float l, float weight) { return l < 0.0f ? -l * weight : weight; }
 
 }  // namespace paged
 

@@ -314,8 +314,8 @@ __global__ __launch_bounds__(2 * NWG * 64, 1) void attn_bf16_kernel(const Args a
     if (a.lse && g == 0 && row0 + col < n_rows)
         a.lse[(size_t)my_head * a.n_tok_q + rq.first + my_tok] = l == 0.0f ? -INFINITY : (m * scale_log2 + __log2f(l)) * LN2;
     // Sums that are not finite: a value that a row does not see, or key 0's, which fills up the last tile, may have come in as 0 * x
-    // (a product of tiles has no other way), or a weight of up to 256 times a value have left the range.  Those rows are done again
-    // key by key, over the keys that they see and against their largest score.
+    // (a product of tiles has no other way), or weights times values have left the range.  Those rows are done again key by key, over
+    // the keys that they see and with weights that add up to one.
     if (__any(odd)) {
         for (int r = 0; r < 32 && row0 + r < n_rows; ++r) {
             const int rr = row0 + r, tok = rr / a.group, head = h * a.group + rr - tok * a.group, seen = sees(rr);
@@ -323,7 +323,7 @@ __global__ __launch_bounds__(2 * NWG * 64, 1) void attn_bf16_kernel(const Args a
             row_by_keys<__bf16, D>(a.Q.p + head * a.Q.head + (int64_t)(rq.first + tok) * a.Q.row, Kb, a.K.row, Vb, a.V.row, seen, scale_log2, mr, lr, acc);
             __bf16 *op = (__bf16 *)(a.O.p + head * a.O.head + (int64_t)(rq.first + tok) * a.O.row);
 #pragma unroll
-            for (int c = 0; c < D / 64; ++c) op[64 * c + lane] = (__bf16)(lr == 0.0f ? 0.0f : acc[c] / lr);
+            for (int c = 0; c < D / 64; ++c) op[64 * c + lane] = (__bf16)acc[c];
             if (lane == 0 && a.lse) a.lse[(size_t)head * a.n_tok_q + rq.first + tok] = lr == 0.0f ? -INFINITY : (mr * scale_log2 + __log2f(lr)) * LN2;
         }
     }

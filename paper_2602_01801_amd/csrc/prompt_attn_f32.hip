@@ -305,7 +305,7 @@ __global__ __launch_bounds__(TEAMS * RW * 64, 2) void attn_f32_prompt_kernel(con
             row_by_keys<float, D>(a.Q.p + head * a.Q.head + (int64_t)(rq.first + tok) * a.Q.row, Kb, a.K.row, Vb, a.V.row, sees(rr), scale_log2, mr, lr, acc);
             float *op = (float *)(a.O.p + head * a.O.head + (int64_t)(rq.first + tok) * a.O.row);
 #pragma unroll
-            for (int c = 0; c < D / 64; ++c) op[64 * c + lane] = lr == 0.0f ? 0.0f : acc[c] / lr;
+            for (int c = 0; c < D / 64; ++c) op[64 * c + lane] = acc[c];
             if (lane == 0 && a.lse) a.lse[(size_t)head * a.n_tok_q + rq.first + tok] = lr == 0.0f ? -INFINITY : (mr * scale_log2 + __log2f(lr)) * LN2;
         }
     }

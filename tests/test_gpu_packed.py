@@ -774,3 +774,35 @@ def test_paged_attention_of_large_values_under_climbing_scores(Hq, Hkv, P, d, q,
     want = ref.attend(f64(Q), gather(K, ks, table[0], n, False), gather(V, vs, table[0], n, True), causal, float(np.float32(scale)))
     assert np.isfinite(want[0]).all()
     check_kinds(O, lse, want, n, d, True)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("Hkv,q,n", [(2, 5, 3), (2, 5, 200), (1, 130, 1300), (40, 420, 470)])
+def test_prompt_attention_of_values_whose_sums_leave_the_range(Hkv, q, n, causal, dtype):
+    """Means of values between 2^126 and 2^128."""
+    g = torch.Generator().manual_seed(n)
+    d, Hq = 64, 2 * Hkv
+    Q, K = view(g, Hq, q, d, DT[dtype], "tokens"), view(g, Hkv, n, d, DT[dtype], "tokens")
+    V = ((torch.rand((Hkv, n, d), generator=g) + 1.0) * 2.0 ** 126 * 1.9).to(DT[dtype]).cuda()
+    V[:, :, 7] *= -1
+    O, lse = fa.prompt_attn_fwd(Q, K, V, i32([0, q]), i32([0, n]), causal=causal)
+    for h in {0, Hq - 1}:
+        want = ref.attend(f64(Q[h:h + 1]), f64(K[h // 2:h // 2 + 1]), f64(V[h // 2:h // 2 + 1]), causal, d ** -0.5)
+        check_kinds(O[h:h + 1], lse[h:h + 1], want, n, d, dtype == "bf16", f"head {h}")
+
+
+@pytest.mark.parametrize("Hq,Hkv,P,d,q,n", PAGED_ENDS + [(8, 2, 16, 128, 1, 300), (8, 1, 64, 64, 1, 20000), (6, 2, 32, 128, 7, 900), (12, 1, 16, 128, 2, 5000),
+                                                         (40, 2, 64, 128, 1, 3)])
+@pytest.mark.parametrize("causal", [False, True])
+def test_paged_attention_of_values_whose_sums_leave_the_range(Hq, Hkv, P, d, q, n, causal):
+    """Codes from 128 to 448 at a scale of 2^119; sums over fragments leave the range where those in a fragment do not, too."""
+    K, ks, V, vs, table = flat_pages(n, Hkv, P, d, n)
+    V = ((V & 0x07) | 0x70).astype(np.uint8)
+    V[V == 0x77] = 0x7E
+    vs[:] = 2.0 ** 119
+    Q = view(torch.Generator().manual_seed(n), Hq, q, d, torch.bfloat16, "tokens")
+    O, lse = fa.paged_attn_fwd(Q, i32([0, q]), i32([n]), i32(table), on_device(K, ks, V, vs), causal=causal)
+    want = ref.attend(f64(Q), gather(K, ks, table[0], n, False), gather(V, vs, table[0], n, True), causal, d ** -0.5)
+    assert np.isfinite(want[0]).all()
+    check_kinds(O, lse, want, n, d, True)
