@@ -112,6 +112,16 @@ __device__ __forceinline__ bool find_item(const int32_t *__restrict__ cu_q, cons
     return false;
 }
 
+// ln of a row's sum of weights from its reference score and the sum l against it, from log2 but where scaled scores leave its range.
+__device__ __forceinline__ float lse_of(float m, float l, float scale_log2) {
+    constexpr float LN2 = 0.6931471805599453f;
+    const float x = m * scale_log2 + __log2f(l);
+    return l == 0.0f ? -INFINITY : fabsf(x) < INFINITY ? x * LN2 : m * (scale_log2 * LN2) + __log2f(l) * LN2;
+}
+// Whether a row with keys has a sum of weights: the reference score's own weight is one, but m * scale is rounded in the exponent of
+// the others, which shows from scaled scores of 2^24 on and takes weights out of the range, up or down, from about 2^31 on.
+__device__ __forceinline__ bool sums_up(float m, float l) { return m == -INFINITY || (l >= 0.25f && l < INFINITY); }
+
 // One row over the keys first .. seen - 1, a wavefront: what tiles whose sums are not finite fall back to.  The maximum and the sum of
 // the weights come first, so that values are taken with weights that add up to one and their sum stays where the values are; a
 // key per lane for the scores, then lane l coordinates l, l + 64 for the values.  score(j, q): q.k of key j by this lane, which no

@@ -247,6 +247,7 @@ __global__ __launch_bounds__(NW * 64, 2) void attn_kernel(const Args a) {
             float l_all = 0.0f;
 #pragma unroll
             for (int i = 0; i < NW; ++i) l_all += s_l[i][16 * rt + row] * weight_of(s_m[i][16 * rt + row], m_all, scale_log2);
+            odd |= !sums_up(m_all, l_all);
             const float wt = weight_of(m[rt], m_all, scale_log2);
 #pragma unroll
             for (int db = 0; db < DB; ++db) o[rt][db] *= wt;
@@ -288,7 +289,7 @@ __global__ __launch_bounds__(NW * 64, 2) void attn_kernel(const Args a) {
             if (w == 0 && quarter == 0) {
                 if (whole) {
                     if (a.lse && rr < n_rows)
-                        a.lse[(size_t)head * a.n_tok + sq.q0 + tok] = l_all == 0.0f ? -INFINITY : (m_all * scale_log2 + __log2f(l_all)) * LN2;
+                        a.lse[(size_t)head * a.n_tok + sq.q0 + tok] = lse_of(m_all, l_all, scale_log2);
                 } else {
                     frag[R * D + 16 * rt + row] = m_all;
                     frag[R * D + R + 16 * rt + row] = l_all;
@@ -297,8 +298,8 @@ __global__ __launch_bounds__(NW * 64, 2) void attn_kernel(const Args a) {
             if (odd) s_odd = turn;
             __syncthreads();
         }
-        // Sums that are not finite: a value that a row does not see may have come in as 0 * x (a product of tiles has no other way), or
-        // they have left the range.  Those rows are done again key by key, over the keys that they see.
+        // Sums that are not finite, or none: a value that a row does not see may have come in as 0 * x (a product of tiles has no other
+        // way), or they or the weights have left the range.  Those rows are done again key by key, over the keys that they see.
         if (__builtin_amdgcn_readfirstlane(s_odd) == turn) {
             for (int i = w; i < R && qt * R + i < n_rows; i += NW) {
                 const int rr = qt * R + i, tok = rr / a.group, head = h * a.group + rr - tok * a.group;
@@ -313,7 +314,7 @@ __global__ __launch_bounds__(NW * 64, 2) void attn_kernel(const Args a) {
                 }
                 if (lane == 0) {
                     if (whole) {
-                        if (a.lse) a.lse[(size_t)head * a.n_tok + sq.q0 + tok] = lr == 0.0f ? -INFINITY : (mr * scale_log2 + __log2f(lr)) * LN2;
+                        if (a.lse) a.lse[(size_t)head * a.n_tok + sq.q0 + tok] = lse_of(mr, lr, scale_log2);
                     } else {
                         frag[R * D + i] = mr;
                         frag[R * D + R + i] = -lr;   // its sums add up to one
@@ -378,7 +379,7 @@ __global__ __launch_bounds__(256) void combine_kernel(const Args a) {
     const bf16x4 y = {(__bf16)x[0], (__bf16)x[1], (__bf16)x[2], (__bf16)x[3]};
     *(bf16x4 *)(a.O.p + head * a.O.head + (int64_t)(sq.q0 + tok) * a.O.row + (16 * db + 4 * quarter) * 2) = y;
     if (a.lse && db == 0 && quarter == 0)
-        a.lse[(size_t)head * a.n_tok + sq.q0 + tok] = l == 0.0f ? -INFINITY : (m_all * a.scale_log2 + __log2f(l)) * LN2;
+        a.lse[(size_t)head * a.n_tok + sq.q0 + tok] = lse_of(m_all, l, a.scale_log2);
 }
 
 template <int D, int RT>

@@ -292,7 +292,7 @@ __global__ __launch_bounds__(2 * NWG * 64, 1) void attn_chunk_kernel(const Args 
         const int my_tok_e = my_row_e / a.group, my_head_e = h * a.group + my_row_e - my_tok_e * a.group;
         const float l_lane = l0 + l1;
         const float l = l_lane + shfl_xor(l_lane, 32);
-        bool odd = false;
+        bool odd = !sums_up(m, l);
 #pragma unroll
         for (int db = 0; db < DB; ++db)
 #pragma unroll
@@ -321,7 +321,7 @@ __global__ __launch_bounds__(2 * NWG * 64, 1) void attn_chunk_kernel(const Args 
                 }
             }
             if (a.lse && g_e == 0 && row0_e + col_e < n_rows)
-                a.lse[(size_t)my_head_e * a.n_tok + sq.q0 + my_tok_e] = l == 0.0f ? -INFINITY : (m * scale_log2 + __log2f(l)) * LN2;
+                a.lse[(size_t)my_head_e * a.n_tok + sq.q0 + my_tok_e] = lse_of(m, l, scale_log2);
         } else {   // [wavefront][block of 32 coordinates][q4][lane_e] of four floats, then maxima and sums
 #pragma unroll
             for (int db = 0; db < DB; ++db)
@@ -335,7 +335,7 @@ __global__ __launch_bounds__(2 * NWG * 64, 1) void attn_chunk_kernel(const Args 
                 frag[R * D + R + wave * 32 + col_e] = l;
             }
         }
-        // as in paged_attn.hip: rows whose sums are not finite (here a weight of up to 256 times a value may have left the range too)
+        // as in paged_attn.hip: rows whose sums are not finite, or none (here a weight of up to 256 times a value may have left the range too)
         if (__any(odd)) {
             __threadfence();
             for (int x = 0; x < 32 && row0_e + x < n_rows; ++x) {
@@ -350,7 +350,7 @@ __global__ __launch_bounds__(2 * NWG * 64, 1) void attn_chunk_kernel(const Args 
                 }
                 if (lane_e == 0) {
                     if (whole) {
-                        if (a.lse) a.lse[(size_t)head * a.n_tok + sq.q0 + tok] = lr == 0.0f ? -INFINITY : (mr * scale_log2 + __log2f(lr)) * LN2;
+                        if (a.lse) a.lse[(size_t)head * a.n_tok + sq.q0 + tok] = lse_of(mr, lr, scale_log2);
                     } else {
                         frag[R * D + wave * 32 + x] = mr;
                         frag[R * D + R + wave * 32 + x] = -lr;   // its sums add up to one
@@ -404,7 +404,7 @@ __global__ __launch_bounds__(256) void combine_chunk_kernel(const Args a) {
     const bf16x4 y = {(__bf16)x[0], (__bf16)x[1], (__bf16)x[2], (__bf16)x[3]};
     *(bf16x4 *)(a.O.p + head * a.O.head + (int64_t)(sq.q0 + tok) * a.O.row + (32 * db + 8 * q4 + 4 * g) * 2) = y;
     if (a.lse && db == 0 && q4 == 0 && g == 0)
-        a.lse[(size_t)head * a.n_tok + sq.q0 + tok] = l == 0.0f ? -INFINITY : (m_all * a.scale_log2 + __log2f(l)) * LN2;
+        a.lse[(size_t)head * a.n_tok + sq.q0 + tok] = lse_of(m_all, l, a.scale_log2);
 }
 
 }  // namespace chunk

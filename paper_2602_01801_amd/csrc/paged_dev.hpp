@@ -14,7 +14,6 @@ namespace fastar {
 namespace paged {
 
 constexpr int TK = 64;              // keys per tile
-constexpr float LN2 = 0.6931471805599453f;
 constexpr int MAX_SHARES = 512;
 // Units of work of an item in front of its tiles: what its ends cost (queries, page numbers, first codes, sums put together), in tiles.
 // Without them shares of many short sequences end last.  1 / 6 / 9 / 14 of them, tokens of 48 requests of 100 to 37440 keys 210 / 183 /

@@ -36,7 +36,6 @@ constexpr int NK = 3, NV = 4, OWN_STAGES = 2;
 // 60 workgroups (1000 tokens, causal) 31.8 / 22.2 us, 156 (3000) 73.2 / 49.9, 240 (4680) 111 / 86, not causal 134 / 162; 392 (40 heads on
 // 8, 2 x 1200, causal) 47 / 62.
 constexpr int SPLIT_ITEMS = 128;
-constexpr float LN2 = 0.6931471805599453f;
 
 struct Args {
     View Q, K, V, O;
@@ -285,7 +284,7 @@ __global__ __launch_bounds__(2 * NWG * 64, 1) void attn_bf16_kernel(const Args a
             }
     }
     const float inv = l == 0.0f ? 0.0f : 1.0f / l;
-    bool odd = false;
+    bool odd = !sums_up(m, l);
 #pragma unroll
     for (int db = 0; db < DB; ++db)
 #pragma unroll
@@ -312,9 +311,9 @@ __global__ __launch_bounds__(2 * NWG * 64, 1) void attn_bf16_kernel(const Args a
         }
     }
     if (a.lse && g == 0 && row0 + col < n_rows)
-        a.lse[(size_t)my_head * a.n_tok_q + rq.first + my_tok] = l == 0.0f ? -INFINITY : (m * scale_log2 + __log2f(l)) * LN2;
-    // Sums that are not finite: a value that a row does not see, or key 0's, which fills up the last tile, may have come in as 0 * x
-    // (a product of tiles has no other way), or weights times values have left the range.  Those rows are done again key by key, over
+        a.lse[(size_t)my_head * a.n_tok_q + rq.first + my_tok] = lse_of(m, l, scale_log2);
+    // Sums that are not finite, or none: a value that a row does not see, or key 0's, which fills up the last tile, may have come in as 0 * x
+    // (a product of tiles has no other way), or weights, or weights times values, have left the range.  Those rows are done again key by key, over
     // the keys that they see and with weights that add up to one.
     if (__any(odd)) {
         for (int r = 0; r < 32 && row0 + r < n_rows; ++r) {
@@ -324,7 +323,7 @@ __global__ __launch_bounds__(2 * NWG * 64, 1) void attn_bf16_kernel(const Args a
             __bf16 *op = (__bf16 *)(a.O.p + head * a.O.head + (int64_t)(rq.first + tok) * a.O.row);
 #pragma unroll
             for (int c = 0; c < D / 64; ++c) op[64 * c + lane] = (__bf16)acc[c];
-            if (lane == 0 && a.lse) a.lse[(size_t)head * a.n_tok_q + rq.first + tok] = lr == 0.0f ? -INFINITY : (mr * scale_log2 + __log2f(lr)) * LN2;
+            if (lane == 0 && a.lse) a.lse[(size_t)head * a.n_tok_q + rq.first + tok] = lse_of(mr, lr, scale_log2);
         }
     }
 }

@@ -24,8 +24,6 @@ int launch_prompt_bf16(const View &Q, const View &K, const View &V, const int32_
 
 namespace prompt32 {
 
-constexpr float LN2 = 0.6931471805599453f;
-
 __device__ __forceinline__ f32x4 mfma_16x16x4(float a, float b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x4f32(a, b, c, 0, 0, 0); }
 // LDS reads as assembly: the compiler would wait for the tile loads in flight before each of its own.
 __device__ __forceinline__ f32x4 lds_read(unsigned addr) {
@@ -278,7 +276,7 @@ __global__ __launch_bounds__(TEAMS * RW * 64, 2) void attn_f32_prompt_kernel(con
         }
         m = m_all;
     }
-    bool odd = false;
+    bool odd = !sums_up(m, l);
 #pragma unroll
     for (int c = 0; c < CH; ++c)
 #pragma unroll
@@ -295,7 +293,7 @@ __global__ __launch_bounds__(TEAMS * RW * 64, 2) void attn_f32_prompt_kernel(con
                 *(f32x4 *)(op + (64 * e + 16 * quarter + 4 * v) * 4) = y;
             }
         if (a.lse && quarter == 0)
-            a.lse[(size_t)my_head * a.n_tok_q + rq.first + my_tok] = l == 0.0f ? -INFINITY : (m * scale_log2 + __log2f(l)) * LN2;
+            a.lse[(size_t)my_head * a.n_tok_q + rq.first + my_tok] = lse_of(m, l, scale_log2);
     }
     // as in prompt_attn.hip: rows whose sums are not finite
     if (__any(odd)) {
@@ -306,7 +304,7 @@ __global__ __launch_bounds__(TEAMS * RW * 64, 2) void attn_f32_prompt_kernel(con
             float *op = (float *)(a.O.p + head * a.O.head + (int64_t)(rq.first + tok) * a.O.row);
 #pragma unroll
             for (int c = 0; c < D / 64; ++c) op[64 * c + lane] = acc[c];
-            if (lane == 0 && a.lse) a.lse[(size_t)head * a.n_tok_q + rq.first + tok] = lr == 0.0f ? -INFINITY : (mr * scale_log2 + __log2f(lr)) * LN2;
+            if (lane == 0 && a.lse) a.lse[(size_t)head * a.n_tok_q + rq.first + tok] = lse_of(mr, lr, scale_log2);
         }
     }
 }

@@ -806,3 +806,50 @@ def test_paged_attention_of_values_whose_sums_leave_the_range(Hq, Hkv, P, d, q, 
     want = ref.attend(f64(Q), gather(K, ks, table[0], n, False), gather(V, vs, table[0], n, True), causal, d ** -0.5)
     assert np.isfinite(want[0]).all()
     check_kinds(O, lse, want, n, d, True)
+
+
+def whole_scores(Hq, Hkv, q, n, d, top, sign):
+    """Scores that are whole numbers: 0 to 3 (or -1 to -4), that of key `top` one more than all others."""
+    rng = np.random.default_rng(n)
+    s = rng.integers(0, 4, size=n)
+    s[top] = 4
+    if sign < 0:
+        s -= 5
+    Q, K = torch.zeros((Hq, q, d)), torch.zeros((Hkv, n, d))
+    Q[:, :, 1], K[:, :, 1] = 1.0, torch.from_numpy(s).float()
+    return Q, K, s
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("sign", [1, -1])
+@pytest.mark.parametrize("scale", [2.0 ** 36, 2.0 ** 90, 2.0 ** 125, 2.3e38])
+@pytest.mark.parametrize("Hkv,q,n", [(2, 5, 200), (1, 3, 1), (40, 420, 470)])
+def test_prompt_attention_with_scales_that_leave_one_key(Hkv, q, n, scale, sign, dtype):
+    """Scales as large as they may be: scaled scores beyond the range, whose differences decide all the same."""
+    d, top = 64, n - n // 3 - 1
+    Q, K, s = whole_scores(2 * Hkv, Hkv, q, n, d, top, sign)
+    V = torch.randn((Hkv, n, d), generator=torch.Generator().manual_seed(2))
+    Q, K, V = (x.to(DT[dtype]).cuda() for x in (Q, K, V))
+    O, lse = fa.prompt_attn_fwd(Q, K, V, i32([0, q]), i32([0, n]), causal=False, scale=scale)
+    assert torch.equal(O, V[:, top].repeat_interleave(2, 0)[:, None].expand_as(O))
+    want = float(s[top]) * float(np.float32(scale))
+    got = f64(lse)
+    assert (got == np.copysign(math.inf, want)).all() if abs(want) > 3.4028235e38 else (np.abs(got - want) <= 2.0 ** -22 * abs(want)).all()
+
+
+@pytest.mark.parametrize("Hq,Hkv,P,d,q,n", PAGED_ENDS + [(8, 2, 16, 128, 1, 300), (8, 1, 64, 64, 1, 20000), (6, 2, 32, 128, 7, 900), (12, 1, 16, 128, 2, 5000)])
+@pytest.mark.parametrize("sign,scale", [(1, 2.0 ** 36), (-1, 2.0 ** 36), (1, 2.0 ** 90), (-1, 2.0 ** 125), (1, 2.3e38), (-1, 2.3e38)])
+def test_paged_attention_with_scales_that_leave_one_key(Hq, Hkv, P, d, q, n, sign, scale):
+    top = n - n // 3 - 1
+    Q, Kf, s = whole_scores(Hq, Hkv, q, n, d, top, sign)
+    K, ks, V, vs, table = flat_pages(n, Hkv, P, d, n)
+    rows = np.zeros((K.shape[0], Hkv, P, d), np.uint8)
+    for j in range(n):
+        rows[table[0, j // P], :, j % P] = ref.code_of(Kf[:, j].numpy().astype(np.float64))
+    K, ks = ref.cells_of_rows(rows, False), np.ones_like(ks)
+    O, lse = fa.paged_attn_fwd(Q.bfloat16().cuda(), i32([0, q]), i32([n]), i32(table), on_device(K, ks, V, vs), causal=False, scale=scale)
+    v = gather(V, vs, table[0], n, True)[:, top]
+    assert (f64(O) == np.repeat(v, Hq // Hkv, 0)[:, None]).all()
+    want = float(s[top]) * float(np.float32(scale))
+    got = f64(lse)
+    assert (got == np.copysign(math.inf, want)).all() if abs(want) > 3.4028235e38 else (np.abs(got - want) <= 2.0 ** -22 * abs(want)).all()
