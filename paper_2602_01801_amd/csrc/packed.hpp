@@ -112,6 +112,21 @@ __device__ __forceinline__ bool find_item(const int32_t *__restrict__ cu_q, cons
     return false;
 }
 
+// The kernel's only argument, read again from where the launch left it: what the rare paths behind a loop need of it is then not held
+// in registers over the loop (32760 tokens x 12 heads 2.87 -> 2.79 ms).
+template <class Args>
+__device__ __forceinline__ Args args_anew() {
+    static_assert(sizeof(Args) % 4 == 0);
+    struct Words {
+        unsigned w[sizeof(Args) / 4];
+    } x;
+    auto *p = (const __attribute__((address_space(4))) unsigned *)__builtin_amdgcn_kernarg_segment_ptr();
+    asm volatile("" : "+s"(p));
+#pragma unroll
+    for (unsigned i = 0; i < sizeof(Args) / 4; ++i) x.w[i] = p[i];
+    return __builtin_bit_cast(Args, x);
+}
+
 // ln of a row's sum of weights from its reference score and the sum l against it, from log2 but where scaled scores leave its range.
 __device__ __forceinline__ float lse_of(float m, float l, float scale_log2) {
     constexpr float LN2 = 0.6931471805599453f;

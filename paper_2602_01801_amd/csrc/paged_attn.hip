@@ -300,7 +300,10 @@ __global__ __launch_bounds__(NW * 64, 2) void attn_kernel(const Args a) {
         }
         // Sums that are not finite, or none: a value that a row does not see may have come in as 0 * x (a product of tiles has no other
         // way), or they or the weights have left the range.  Those rows are done again key by key, over the keys that they see.
-        if (__builtin_amdgcn_readfirstlane(s_odd) == turn) {
+        if (__builtin_expect(__builtin_amdgcn_readfirstlane(s_odd) == turn, 0)) {
+            const Args a = args_anew<Args>();
+            const int32_t *pages = a.table + (size_t)r.b * a.max_pages;
+            float *frag = SPLIT ? a.frag + (size_t)(2 * r.share + (begins ? 1 : 0)) * FRAG_FLOATS : nullptr;
             for (int i = w; i < R && qt * R + i < n_rows; i += NW) {
                 const int rr = qt * R + i, tok = rr / a.group, head = h * a.group + rr - tok * a.group;
                 float mr, lr, acc[D / 64];
@@ -314,7 +317,7 @@ __global__ __launch_bounds__(NW * 64, 2) void attn_kernel(const Args a) {
                 }
                 if (lane == 0) {
                     if (whole) {
-                        if (a.lse) a.lse[(size_t)head * a.n_tok + sq.q0 + tok] = lse_of(mr, lr, scale_log2);
+                        if (a.lse) a.lse[(size_t)head * a.n_tok + sq.q0 + tok] = lse_of(mr, lr, a.scale_log2);
                     } else {
                         frag[R * D + i] = mr;
                         frag[R * D + R + i] = -lr;   // its sums add up to one

@@ -336,12 +336,15 @@ __global__ __launch_bounds__(2 * NWG * 64, 1) void attn_chunk_kernel(const Args 
             }
         }
         // as in paged_attn.hip: rows whose sums are not finite, or none (here a weight of up to 256 times a value may have left the range too)
-        if (__any(odd)) {
+        if (__builtin_expect(__any(odd), 0)) {
+            const Args a = args_anew<Args>();
+            const int32_t *pages = a.table + (size_t)r.b * a.max_pages;
+            float *frag = a.frag + (size_t)(2 * r.share + (begins ? 1 : 0)) * FRAG_FLOATS;
             __threadfence();
             for (int x = 0; x < 32 && row0_e + x < n_rows; ++x) {
                 const int rr = row0_e + x, tok = rr / a.group, head = h * a.group + rr - tok * a.group;
                 float mr, lr, acc[D / 64];
-                row_by_paged_keys<D>(a, a.Q.p + head * a.Q.head + (int64_t)(sq.q0 + tok) * a.Q.row, pages, h, ta * TK, min(sees(rr), te * TK), mr, lr, acc);
+                row_by_paged_keys<D>(a, a.Q.p + head * a.Q.head + (int64_t)(sq.q0 + tok) * a.Q.row, pages, h, ta * TK, min(a.causal ? min(max(sq.L - sq.n_q + tok + 1, 0), sq.L) : sq.L, te * TK), mr, lr, acc);
 #pragma unroll
                 for (int c = 0; c < D / 64; ++c) {
                     const int co = 64 * c + lane_e;
@@ -350,7 +353,7 @@ __global__ __launch_bounds__(2 * NWG * 64, 1) void attn_chunk_kernel(const Args 
                 }
                 if (lane_e == 0) {
                     if (whole) {
-                        if (a.lse) a.lse[(size_t)head * a.n_tok + sq.q0 + tok] = lse_of(mr, lr, scale_log2);
+                        if (a.lse) a.lse[(size_t)head * a.n_tok + sq.q0 + tok] = lse_of(mr, lr, a.scale_log2);
                     } else {
                         frag[R * D + wave * 32 + x] = mr;
                         frag[R * D + R + wave * 32 + x] = -lr;   // its sums add up to one

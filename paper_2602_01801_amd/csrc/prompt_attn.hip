@@ -315,15 +315,18 @@ __global__ __launch_bounds__(2 * NWG * 64, 1) void attn_bf16_kernel(const Args a
     // Sums that are not finite, or none: a value that a row does not see, or key 0's, which fills up the last tile, may have come in as 0 * x
     // (a product of tiles has no other way), or weights, or weights times values, have left the range.  Those rows are done again key by key, over
     // the keys that they see and with weights that add up to one.
-    if (__any(odd)) {
+    if (__builtin_expect(__any(odd), 0)) {
+        const Args a = args_anew<Args>();
+        const char *K = a.K.p + h * a.K.head + (int64_t)rk.first * a.K.row, *V = a.V.p + h * a.V.head + (int64_t)rk.first * a.V.row;
         for (int r = 0; r < 32 && row0 + r < n_rows; ++r) {
-            const int rr = row0 + r, tok = rr / a.group, head = h * a.group + rr - tok * a.group, seen = sees(rr);
+            const int rr = row0 + r, tok = rr / a.group, head = h * a.group + rr - tok * a.group;
             float mr, lr, acc[D / 64];
-            row_by_keys<__bf16, D>(a.Q.p + head * a.Q.head + (int64_t)(rq.first + tok) * a.Q.row, Kb, a.K.row, Vb, a.V.row, seen, scale_log2, mr, lr, acc);
+            row_by_keys<__bf16, D>(a.Q.p + head * a.Q.head + (int64_t)(rq.first + tok) * a.Q.row, K, a.K.row, V, a.V.row,
+                                   a.causal ? min(max(n - rq.n + tok + 1, 0), n) : n, a.scale_log2, mr, lr, acc);
             __bf16 *op = (__bf16 *)(a.O.p + head * a.O.head + (int64_t)(rq.first + tok) * a.O.row);
 #pragma unroll
             for (int c = 0; c < D / 64; ++c) op[64 * c + lane] = (__bf16)acc[c];
-            if (lane == 0 && a.lse) a.lse[(size_t)head * a.n_tok_q + rq.first + tok] = lse_of(mr, lr, scale_log2);
+            if (lane == 0 && a.lse) a.lse[(size_t)head * a.n_tok_q + rq.first + tok] = lse_of(mr, lr, a.scale_log2);
         }
     }
 }

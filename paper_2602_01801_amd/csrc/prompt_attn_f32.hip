@@ -296,15 +296,18 @@ __global__ __launch_bounds__(TEAMS * RW * 64, 2) void attn_f32_prompt_kernel(con
             a.lse[(size_t)my_head * a.n_tok_q + rq.first + my_tok] = lse_of(m, l, scale_log2);
     }
     // as in prompt_attn.hip: rows whose sums are not finite
-    if (__any(odd)) {
+    if (__builtin_expect(__any(odd), 0)) {
+        const Args a = args_anew<Args>();
+        const char *K = a.K.p + h * a.K.head + (int64_t)rk.first * a.K.row, *V = a.V.p + h * a.V.head + (int64_t)rk.first * a.V.row;
         for (int r = 0; r < 16 && row0 + r < n_rows; ++r) {
             const int rr = row0 + r, tok = rr / a.group, head = h * a.group + rr - tok * a.group;
             float mr, lr, acc[D / 64];
-            row_by_keys<float, D>(a.Q.p + head * a.Q.head + (int64_t)(rq.first + tok) * a.Q.row, Kb, a.K.row, Vb, a.V.row, sees(rr), scale_log2, mr, lr, acc);
+            row_by_keys<float, D>(a.Q.p + head * a.Q.head + (int64_t)(rq.first + tok) * a.Q.row, K, a.K.row, V, a.V.row,
+                                  a.causal ? min(max(n - rq.n + tok + 1, 0), n) : n, a.scale_log2, mr, lr, acc);
             float *op = (float *)(a.O.p + head * a.O.head + (int64_t)(rq.first + tok) * a.O.row);
 #pragma unroll
             for (int c = 0; c < D / 64; ++c) op[64 * c + lane] = acc[c];
-            if (lane == 0 && a.lse) a.lse[(size_t)head * a.n_tok_q + rq.first + tok] = lse_of(mr, lr, scale_log2);
+            if (lane == 0 && a.lse) a.lse[(size_t)head * a.n_tok_q + rq.first + tok] = lse_of(mr, lr, a.scale_log2);
         }
     }
 }
