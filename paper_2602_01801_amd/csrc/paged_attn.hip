@@ -170,7 +170,8 @@ __global__ __launch_bounds__(NW * 64, 2) void attn_kernel(const Args a) {
 #pragma unroll
                         for (int v = 0; v < 4; ++v)
                             if (!v_ok || t * TK + 16 * quarter + 4 * j + v >= limit[rt]) s[rt][j][v] = -INFINITY;
-                // values that no row sees need not be numbers
+                // values that no row sees need not be numbers, nor page 0's scale
+                if (!v_ok) vs = 1.0f;
                 const u32x4 mask = first_bytes(v_ok ? limit_max - (t * TK + 16 * quarter) : 0);
 #pragma unroll
                 for (int db = 0; db < DB; ++db) vr[db] &= mask;

@@ -133,7 +133,10 @@ __global__ __launch_bounds__(2 * NWG * 64, 1) void attn_chunk_kernel(const Args 
             }
             if (has_v) {
                 const int live = ok ? limit_max - (t * TK + 16 * tb) : 0;
-                if (live < 16) vr &= first_bytes(live);   // uniform; values that no row sees need not be numbers
+                if (live < 16) {   // uniform; values that no row sees need not be numbers, nor page 0's scale
+                    vr &= first_bytes(live);
+                    if (!ok) vs = 1.0f;
+                }
                 unsigned char *p = vbuf + vput;
                 *(bf16x8 *)(p + vw) = widen(vr[0], vr[2], vs);
                 *(bf16x8 *)(p + (vw ^ 16)) = widen(vr[1], vr[3], vs);

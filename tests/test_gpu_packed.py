@@ -853,3 +853,18 @@ def test_paged_attention_with_scales_that_leave_one_key(Hq, Hkv, P, d, q, n, sig
     want = float(s[top]) * float(np.float32(scale))
     got = f64(lse)
     assert (got == np.copysign(math.inf, want)).all() if abs(want) > 3.4028235e38 else (np.abs(got - want) <= 2.0 ** -22 * abs(want)).all()
+
+
+@pytest.mark.parametrize("Hq,Hkv,P,d,q,n", PAGED_ENDS + [(8, 2, 16, 128, 1, 300), (8, 1, 64, 64, 1, 20000), (6, 2, 32, 128, 7, 900), (40, 2, 64, 128, 1, 200)])
+@pytest.mark.parametrize("x", [math.nan, math.inf])
+def test_the_scales_of_page_0_do_not_stand_in_for_those_of_pages_that_do_not_exist(Hq, Hkv, P, d, q, n, x):
+    """Page 0 belongs to nobody and holds no numbers; two pages of the sequence do not exist."""
+    K, ks, V, vs, table = flat_pages(n, Hkv, P, d, n)
+    table[table == 0] = np.setdiff1d(np.arange(1, K.shape[0]), table)[0]
+    table[0, 1], table[0, -1] = -1, 2 ** 30
+    ks[0], vs[0], K[0], V[0] = x, x, 0x7F, 0x7F
+    Q = view(torch.Generator().manual_seed(n), Hq, q, d, torch.bfloat16, "tokens")
+    O, lse = fa.paged_attn_fwd(Q, i32([0, q]), i32([n]), i32(table), on_device(K, ks, V, vs))
+    live = np.repeat([0 <= p < K.shape[0] for p in table[0]], P)[:n]
+    want = ref.attend(f64(Q), gather(K, ks, table[0], n, False), gather(V, vs, table[0], n, True), True, d ** -0.5, live)
+    check_kinds(O, lse, want, n, d, True)
