@@ -457,7 +457,7 @@ typedef struct {
  * bf16: bf16 products (the weights are rounded to bf16; those below 2^-126 of a row's largest are zero), fp32 softmax and
  * sums; fp32: plain fp32 arithmetic.
  * Supported: d in {64, 128}; scale positive, scale * log2(e) finite; rows of K and V at most 2^24 bytes apart;
- * n_tok_q * Hq < 2^30, n_tok_k <= 2^30.  No workspace.  n_tok_q = 0 or B = 0 launches nothing.
+ * n_tok_q * Hq < 2^30, n_tok_k <= 2^30; n_tok_q * Hq / 256 + (B + 1) * Hkv < 2^23 (fp32: n_tok_q * Hq / 64 ... < 2^24).  No workspace.  n_tok_q = 0 or B = 0 launches nothing.
  * Where sums are not finite (infinities or NaN among the keys and values, or values near the end of the range), the queries of the
  * tiles concerned are done again one by one, so that none sees what is masked for it: right, and many times slower.
  */
@@ -516,7 +516,7 @@ int kv_pages_plan(const int32_t *n_new, const int32_t *len, int32_t *table, int 
  * run raises the page's scale to s if that is larger; all other codes of the page and head are then carried over to it (value
  * of the code times the old scale over the new one, rounded to nearest, ties to even).  New codes: x / scale rounded to
  * nearest, ties to even; infinities become the largest code of their sign, NaN stays NaN.
- * Supported: rows of K_new and V_new at most 2^24 bytes apart.
+ * Supported: rows of K_new and V_new at most 2^24 bytes apart, (n_tok + P) * Hkv <= 2^29 - 1.
  */
 int kv_pages_write(const fastar_pages *pages, const fastar_rows *K_new, const fastar_rows *V_new, int dtype,
                    const int32_t *slot, int n_tok, void *stream);

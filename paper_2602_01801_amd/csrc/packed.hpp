@@ -27,6 +27,8 @@ inline bool rows_apart(const fastar_rows *r, int H, int64_t n, int d) {
 constexpr int64_t MAX_PITCH = 1 << 24;   // bytes between rows of keys and values: offsets within a tile of 64 are 32-bit
 constexpr int MAX_KEYS = 1 << 30;        // of a sequence: positions some tiles further than its end are 32-bit too
 inline bool scale_ok(float scale) { return scale > 0.0f && std::isfinite(scale * 1.4426950408889634f); }
+// A launch's threads along its first dimension are counted in 32 bits.
+inline bool launch_ok(int64_t workgroups, int threads) { return workgroups * threads <= UINT32_MAX; }
 inline bool page_size_ok(int P) { return P == 16 || P == 32 || P == 64; }
 
 // Rows [first, first + n) of a sequence, inside the array.

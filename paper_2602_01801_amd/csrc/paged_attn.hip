@@ -440,7 +440,7 @@ extern "C" int paged_attn_fwd(const fastar_rows *Q, const int32_t *cu_q, const i
     if (rows > (int64_t)32 * B) return launch_paged_chunk(a, rows, keys, one_launch, s);
     const int rt = rows <= (int64_t)16 * B ? 1 : 2;
     const int64_t items = ((rows + 16 * rt - 1) / (16 * rt) + B) * pages->Hkv;   // at most
-    const bool split = !one_launch || items > INT32_MAX;
+    const bool split = !one_launch || !launch_ok(items, 512);
     if (pages->d == 128) return rt == 1 ? paged::launch<128, 1>(a, items, split, s) : paged::launch<128, 2>(a, items, split, s);
     return rt == 1 ? paged::launch<64, 1>(a, items, split, s) : paged::launch<64, 2>(a, items, split, s);
 }

@@ -456,7 +456,7 @@ int launch_paged_chunk(const paged::Args &a, int64_t rows, int64_t keys, bool on
     using namespace paged::chunk;
     if (const int rc = paged_chunk_setup(); rc != FASTAR_OK) return rc;
     const int64_t items = ((rows + R - 1) / R + a.B) * a.pg.Hkv;   // at most
-    const bool split = !one_launch || (items < SHARES && keys > FEW_KEYS) || items > INT32_MAX;
+    const bool split = !one_launch || (items < SHARES && keys > FEW_KEYS) || !launch_ok(items, 2 * NWG * 64);
     return a.pg.d == 128 ? launch<128>(a, items, split, s) : launch<64>(a, items, split, s);
 }
 

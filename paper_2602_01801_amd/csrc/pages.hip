@@ -586,7 +586,7 @@ extern "C" int kv_pages_write(const fastar_pages *pages, const fastar_rows *K_ne
     int chunk = pages->P;
     while (chunk > 1 && (int64_t)n_tok * pages->Hkv * 2 / chunk < 4096) chunk /= 2;
     const int64_t units = (int64_t)((n_tok + chunk - 1) / chunk) * pages->Hkv * 2;
-    if (units > INT32_MAX) return FASTAR_ERR_UNSUPPORTED;
+    if (!launch_ok(units, 4 * pages->P)) return FASTAR_ERR_UNSUPPORTED;
     const dim3 grid((unsigned)units);
     const View k = view_of(K_new, elt), v = view_of(V_new, elt);
 #define FASTAR_WRITE(BF16, D, PSHIFT) \

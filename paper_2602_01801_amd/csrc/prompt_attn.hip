@@ -360,10 +360,10 @@ int prompt_setup() {
 int launch_prompt_bf16(const View &Q, const View &K, const View &V, const int32_t *cu_q, const int32_t *cu_k, int B, int n_tok_q,
                        int n_tok_k, int Hq, int Hkv, int d, int causal, float scale_log2, const View &O, float *lse, hipStream_t s) {
     using namespace prompt;
-    if (const int rc = prompt_setup(); rc != FASTAR_OK) return rc;
     const Args a = {Q, K, V, O, cu_q, cu_k, B, n_tok_q, n_tok_k, Hkv, Hq / Hkv, causal, scale_log2, lse};
     auto items = [&](int rows) { return (((int64_t)n_tok_q * a.group + rows - 1) / rows + B) * Hkv; };   // at most
-    if (items(128) > INT32_MAX) return FASTAR_ERR_UNSUPPORTED;
+    if (!launch_ok(items(256), 2 * NWG * 64)) return FASTAR_ERR_UNSUPPORTED;
+    if (const int rc = prompt_setup(); rc != FASTAR_OK) return rc;
     const bool split = items(256) <= (causal ? 2 : 1) * SPLIT_ITEMS;
     if (d == 128) return split ? launch<128, true>(a, items(128), s) : launch<128, false>(a, items(256), s);
     return split ? launch<64, true>(a, items(128), s) : launch<64, false>(a, items(256), s);

@@ -320,9 +320,9 @@ struct Form {
         return hipFuncSetAttribute((const void *)attn_f32_prompt_kernel<D, RW, TEAMS, HB, NS>, hipFuncAttributeMaxDynamicSharedMemorySize, LDS) == hipSuccess ? FASTAR_OK : FASTAR_ERR_HIP;
     }
     static int launch(const Args &a, hipStream_t s) {
-        const int64_t n = items(a);
-        if (n > INT32_MAX) return FASTAR_ERR_UNSUPPORTED;
-        hipLaunchKernelGGL((attn_f32_prompt_kernel<D, RW, TEAMS, HB, NS>), dim3((unsigned)n), dim3(TEAMS * RW * 64), LDS, s, a);
+        if (!launch_ok(items(a), TEAMS * RW * 64)) return FASTAR_ERR_UNSUPPORTED;
+        if (const int rc = prompt_f32_setup(); rc != FASTAR_OK) return rc;
+        hipLaunchKernelGGL((attn_f32_prompt_kernel<D, RW, TEAMS, HB, NS>), dim3((unsigned)items(a)), dim3(TEAMS * RW * 64), LDS, s, a);
         FASTAR_LAUNCH_CHECK();
         return FASTAR_OK;
     }
@@ -370,7 +370,6 @@ extern "C" int prompt_attn_fwd(const fastar_rows *Q, const fastar_rows *K, const
     const float scale_log2 = scale * 1.4426950408889634f;
     if (dtype == FASTAR_BF16)
         return launch_prompt_bf16(q, k, v, cu_q, cu_k, B, n_tok_q, n_tok_k, Hq, Hkv, d, causal, scale_log2, o, lse, (hipStream_t)stream);
-    if (const int rc = prompt_f32_setup(); rc != FASTAR_OK) return rc;
     const prompt32::Args a = {q, k, v, o, cu_q, cu_k, B, n_tok_q, n_tok_k, Hkv, Hq / Hkv, causal, scale_log2, lse};
     return d == 128 ? prompt32::launch<128>(a, (hipStream_t)stream) : prompt32::launch<64>(a, (hipStream_t)stream);
 }

@@ -868,3 +868,28 @@ def test_the_scales_of_page_0_do_not_stand_in_for_those_of_pages_that_do_not_exi
     live = np.repeat([0 <= p < K.shape[0] for p in table[0]], P)[:n]
     want = ref.attend(f64(Q), gather(K, ks, table[0], n, False), gather(V, vs, table[0], n, True), True, d ** -0.5, live)
     check_kinds(O, lse, want, n, d, True)
+
+
+@pytest.mark.parametrize("q", [1, 60])
+def test_paged_attention_of_a_million_sequences_most_of_them_without_queries(q):
+    """As many items as a launch cannot have workgroups for, had each its own."""
+    B, Hkv, P, d = (1 << 20) + 3, 8, 16, 64
+    rng = np.random.default_rng(q)
+    K, ks, V, vs, dev = random_pages(rng, 5, Hkv, P, d)
+    who = [0, 700001, B - 1]
+    cu = torch.zeros(B + 1, dtype=torch.int32, device="cuda")
+    length, table = torch.full((B,), 9, dtype=torch.int32, device="cuda"), torch.zeros((B, 1), dtype=torch.int32, device="cuda")
+    for i, b in enumerate(who):
+        cu[b + 1:] += q
+        length[b], table[b] = 16 - i, 4 - i
+    if q == 1:
+        Q = view(torch.Generator().manual_seed(1), Hkv, len(who), d, torch.bfloat16, "tokens")
+    else:   # rows of nobody, as many as it takes for the kernel of many rows; one query for all
+        Q = view(torch.Generator().manual_seed(2), Hkv, 1, d, torch.bfloat16, "heads").expand(Hkv, 33 * B, d)
+    O = torch.empty((Q.shape[1], Hkv, d), dtype=torch.bfloat16, device="cuda").transpose(0, 1)
+    lse = torch.empty((Hkv, Q.shape[1]), device="cuda")
+    fa.paged_attn_fwd(Q, cu, length, table, dev, causal=False, out=(O, lse))
+    for i, b in enumerate(who):
+        j = slice(i * q, (i + 1) * q)
+        want = ref.attend(f64(Q[:, j]), gather(K, ks, [4 - i], 16 - i, False), gather(V, vs, [4 - i], 16 - i, True), False, d ** -0.5)
+        check(O[:, j], lse[:, j], want, 16 - i, d, True, f"sequence {b}")

@@ -116,6 +116,15 @@ def test_write_of_nothing_is_done_at_once(L):
     assert write(L, n=0) == 0 and write(L, n=0, slot=None) == 0
 
 
+def test_launches_of_more_workgroups_than_there_can_be_are_refused(L):
+    """Threads are counted in 32 bits along a launch's first dimension."""
+    for dtype, B in ((1, 1 << 23), (0, 1 << 24)):
+        assert prompt(L, n_q=1, Hq=1, Hkv=1, B=B, dtype=dtype) == UNSUPPORTED
+        assert prompt(L, n_q=1, Hq=64, Hkv=64, B=B // 64, dtype=dtype) == UNSUPPORTED
+    assert prompt(L, n_q=(1 << 30) - 1, Hq=1, Hkv=1, B=1 << 22) == UNSUPPORTED
+    assert write(L, n=1 << 28) == UNSUPPORTED and write(L, n=1 << 29, pg=pages(Hkv=1, P=16, d=64)) == UNSUPPORTED
+
+
 def test_a_workspace_that_a_kernel_cannot_write_to_is_refused():
     """Its size alone was looked at: the address of a host tensor went to the kernel."""
     import torch
