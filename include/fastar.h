@@ -439,7 +439,7 @@ int sparse_attn_fwd_fp8_ws(const void *Q, int n_q, const uint8_t *K8, const uint
 
 /*
  * A strided view [H, n, d]: element (h, i, t) at p + h*head + i*row + t, strides in elements, >= 0, every row 16-byte
- * aligned.  [H, n, d] and [n, H, d] arrays and the parts of a fused projection's output are such views.  Rows of an
+ * aligned; the stride of a dimension of one may be anything.  [H, n, d] and [n, H, d] arrays and the parts of a fused projection's output are such views.  Rows of an
  * output must not overlap: one of the strides is at least d, the other at least the first one's extent.  An output shares no
  * memory with an input.
  */

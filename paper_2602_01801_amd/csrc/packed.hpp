@@ -12,10 +12,13 @@ struct View {
     char *p;
     int64_t head, row;
 };
-inline View view_of(const fastar_rows *r, int elt) { return View{(char *)r->p, r->head * elt, r->row * elt}; }
-
-inline bool view_ok(const fastar_rows *r, int elt) {
-    return r && r->p && !((uintptr_t)r->p & 15) && r->head >= 0 && r->row >= 0 && !((r->head * elt) & 15) && !((r->row * elt) & 15);
+// The stride of a dimension of one means nothing and may be anything.
+inline View view_of(const fastar_rows *r, int H, int n, int elt) {
+    return View{(char *)r->p, H > 1 ? r->head * elt : 0, n > 1 ? r->row * elt : 0};
+}
+inline bool view_ok(const fastar_rows *r, int H, int n, int elt) {
+    auto stride_ok = [&](int64_t s) { return s >= 0 && !((s * elt) & 15); };
+    return r && r->p && !((uintptr_t)r->p & 15) && (H <= 1 || stride_ok(r->head)) && (n <= 1 || stride_ok(r->row));
 }
 // Rows of an output lie apart: the smaller stride clears a row, the larger one all that the smaller one spans.
 inline bool rows_apart(const fastar_rows *r, int H, int64_t n, int d) {

@@ -427,9 +427,9 @@ extern "C" int paged_attn_fwd(const fastar_rows *Q, const int32_t *cu_q, const i
     if (!ws || ((uintptr_t)ws & 255)) return FASTAR_ERR_INVALID_ARG;
     if (ws_bytes < paged_attn_ws_bytes()) return FASTAR_ERR_WORKSPACE;
     if (n_tok == 0 || B == 0) return FASTAR_OK;
-    if (!cu_q || !len || !table || !view_ok(Q, 2) || !view_ok(O, 2) || !rows_apart(O, Hq, n_tok, pages->d)) return FASTAR_ERR_INVALID_ARG;
+    if (!cu_q || !len || !table || !view_ok(Q, Hq, n_tok, 2) || !view_ok(O, Hq, n_tok, 2) || !rows_apart(O, Hq, n_tok, pages->d)) return FASTAR_ERR_INVALID_ARG;
     const int group = Hq / pages->Hkv;
-    const paged::Args a = {view_of(Q, 2), view_of(O, 2), cu_q, len, table, B, max_pages, n_tok, group, causal,
+    const paged::Args a = {view_of(Q, Hq, n_tok, 2), view_of(O, Hq, n_tok, 2), cu_q, len, table, B, max_pages, n_tok, group, causal,
                            __builtin_ctz((unsigned)pages->P), *pages, scale * 1.4426950408889634f, lse,
                            (paged::Desc *)ws, (float *)((char *)ws + paged::MAX_SHARES * sizeof(paged::Desc))};
     const int64_t rows = (int64_t)n_tok * group;

@@ -579,8 +579,9 @@ extern "C" int kv_pages_write(const fastar_pages *pages, const fastar_rows *K_ne
     if (n_tok < 0) return FASTAR_ERR_INVALID_ARG;
     if (const int rc = pages_check(pages); rc != FASTAR_OK) return rc;
     if (n_tok == 0) return FASTAR_OK;
-    if (!slot || !view_ok(K_new, elt) || !view_ok(V_new, elt)) return FASTAR_ERR_INVALID_ARG;
-    if (K_new->row * elt > MAX_PITCH || V_new->row * elt > MAX_PITCH) return FASTAR_ERR_UNSUPPORTED;
+    if (!slot || !view_ok(K_new, pages->Hkv, n_tok, elt) || !view_ok(V_new, pages->Hkv, n_tok, elt)) return FASTAR_ERR_INVALID_ARG;
+    const View k = view_of(K_new, pages->Hkv, n_tok, elt), v = view_of(V_new, pages->Hkv, n_tok, elt);
+    if (k.row > MAX_PITCH || v.row > MAX_PITCH) return FASTAR_ERR_UNSUPPORTED;
     // Rows per workgroup: a page's where that makes enough of them; fewer, down to one, so that the runs of single tokens are not
     // done one after the other.
     int chunk = pages->P;
@@ -588,7 +589,6 @@ extern "C" int kv_pages_write(const fastar_pages *pages, const fastar_rows *K_ne
     const int64_t units = (int64_t)((n_tok + chunk - 1) / chunk) * pages->Hkv * 2;
     if (!launch_ok(units, 4 * pages->P)) return FASTAR_ERR_UNSUPPORTED;
     const dim3 grid((unsigned)units);
-    const View k = view_of(K_new, elt), v = view_of(V_new, elt);
 #define FASTAR_WRITE(BF16, D, PSHIFT) \
     hipLaunchKernelGGL((pages::write_kernel<BF16, D, PSHIFT>), grid, dim3(4 << PSHIFT), 0, (hipStream_t)stream, k, v, slot, n_tok, chunk, *pages)
 #define FASTAR_WRITE_P(BF16, D)                      \

@@ -361,12 +361,13 @@ extern "C" int prompt_attn_fwd(const fastar_rows *Q, const fastar_rows *K, const
     if (d != 64 && d != 128) return FASTAR_ERR_UNSUPPORTED;
     if ((int64_t)n_tok_q * Hq > INT32_MAX / 2 || n_tok_k > MAX_KEYS) return FASTAR_ERR_UNSUPPORTED;
     if (n_tok_q == 0 || B == 0) return FASTAR_OK;
-    if (!cu_q || !view_ok(Q, elt) || !view_ok(O, elt) || !rows_apart(O, Hq, n_tok_q, d)) return FASTAR_ERR_INVALID_ARG;
-    if (n_tok_k > 0 && (!view_ok(K, elt) || !view_ok(V, elt))) return FASTAR_ERR_INVALID_ARG;
-    if (n_tok_k > 0 && (K->row * elt > MAX_PITCH || V->row * elt > MAX_PITCH)) return FASTAR_ERR_UNSUPPORTED;
+    if (!cu_q || !view_ok(Q, Hq, n_tok_q, elt) || !view_ok(O, Hq, n_tok_q, elt) || !rows_apart(O, Hq, n_tok_q, d)) return FASTAR_ERR_INVALID_ARG;
+    if (n_tok_k > 0 && (!view_ok(K, Hkv, n_tok_k, elt) || !view_ok(V, Hkv, n_tok_k, elt))) return FASTAR_ERR_INVALID_ARG;
     if (!cu_k) cu_k = cu_q;
     const View none{nullptr, 0, 0};
-    const View q = view_of(Q, elt), k = n_tok_k ? view_of(K, elt) : none, v = n_tok_k ? view_of(V, elt) : none, o = view_of(O, elt);
+    const View q = view_of(Q, Hq, n_tok_q, elt), o = view_of(O, Hq, n_tok_q, elt);
+    const View k = n_tok_k ? view_of(K, Hkv, n_tok_k, elt) : none, v = n_tok_k ? view_of(V, Hkv, n_tok_k, elt) : none;
+    if (k.row > MAX_PITCH || v.row > MAX_PITCH) return FASTAR_ERR_UNSUPPORTED;
     const float scale_log2 = scale * 1.4426950408889634f;
     if (dtype == FASTAR_BF16)
         return launch_prompt_bf16(q, k, v, cu_q, cu_k, B, n_tok_q, n_tok_k, Hq, Hkv, d, causal, scale_log2, o, lse, (hipStream_t)stream);

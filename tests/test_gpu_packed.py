@@ -893,3 +893,32 @@ def test_paged_attention_of_a_million_sequences_most_of_them_without_queries(q):
         j = slice(i * q, (i + 1) * q)
         want = ref.attend(f64(Q[:, j]), gather(K, ks, [4 - i], 16 - i, False), gather(V, vs, [4 - i], 16 - i, True), False, d ** -0.5)
         check(O[:, j], lse[:, j], want, 16 - i, d, True, f"sequence {b}")
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_strides_of_dimensions_of_one_mean_nothing(dtype):
+    """What slicing a single row or head out of an odd buffer leaves behind."""
+    g = torch.Generator().manual_seed(5)
+    d, P, dt = 64, 16, DT[dtype]
+    odd = lambda x, dim: x.as_strided(x.shape, [3 if i == dim else s for i, s in enumerate(x.stride())])
+    Q, K, V = (torch.randn((h, 1, d), generator=g).to(dt).cuda() for h in (4, 2, 2))
+    want = fa.prompt_attn_fwd(Q, K, V, i32([0, 1]))
+    O = odd(torch.empty_like(Q), 1)
+    fa.prompt_attn_fwd(odd(Q, 1), odd(K, 1), odd(V, 1), i32([0, 1]), out=(O, None))
+    assert torch.equal(O, want[0])
+    Q, K, V = (torch.randn((1, 40, d), generator=g).to(dt).cuda() for _ in range(3))
+    want = fa.prompt_attn_fwd(Q, K, V, i32([0, 40]))
+    got = fa.prompt_attn_fwd(odd(Q, 0), odd(K, 0), odd(V, 0), i32([0, 40]))
+    assert torch.equal(got[0], want[0])
+    pages = [fa.Pages.empty(3, 1, P, d) for _ in range(2)]
+    slot = torch.arange(40, dtype=torch.int32, device="cuda")
+    for pg, f in zip(pages, (lambda x, dim: x, odd)):
+        fa.kv_pages_write(pg, slot, f(K, 0), f(V, 0))
+        fa.kv_pages_write(pg, i32([40]), f(K[:, 3:4], 1), f(V[:, 3:4], 1))
+    assert all(torch.equal(getattr(pages[0], x), getattr(pages[1], x)) for x in ("K8", "V8", "kscale", "vscale"))
+    if dtype == "bf16":
+        table = i32([[0, 1, 2]])
+        want = fa.paged_attn_fwd(Q, i32([0, 40]), i32([41]), table, pages[0])
+        assert torch.equal(fa.paged_attn_fwd(odd(Q, 0), i32([0, 40]), i32([41]), table, pages[0])[0], want[0])
+        one = fa.paged_attn_fwd(Q[:, :1], i32([0, 1]), i32([41]), table, pages[0])
+        assert torch.equal(fa.paged_attn_fwd(odd(Q[:, :1], 1), i32([0, 1]), i32([41]), table, pages[0])[0], one[0])
