@@ -154,3 +154,27 @@ def code_of(v):
     c = np.searchsorted(order, np.where(np.isnan(a), 0, a))
     c = np.where(np.isnan(v), 127, np.minimum(c, 126))
     return np.where(~np.isnan(v) & np.signbit(v), c | 128, c).astype(np.uint8)
+
+
+def spread_pages(rng, n, Hkv, P, spare=2, d=128):
+    """Pages of n tokens in any order and their block table, for tests that notice a tile of 64 keys that is lost or read wrongly: keys of 0.5 to 2, so that
+    scores of ordinary queries spread by about one and no key rules a row; values of 1 to 2 of either sign and, in one coordinate that is
+    the tile's, of 256.  Page by page a scale of its own."""
+    per = -(-n // P)
+    n_pages = per + spare
+    sign = lambda: 128 * rng.integers(0, 2, size=(n_pages, Hkv, P, d))
+    K = rng.integers(0x30, 0x40, size=(n_pages, Hkv, P, d)) | sign()
+    V = rng.integers(0x38, 0x40, size=K.shape) | sign()
+    table = rng.permutation(n_pages)[:per].astype(np.int32)
+    for j in range(n):
+        V[table[j // P], :, j % P, j // 64 % d] = 0x78
+    scale = lambda: 2.0 ** rng.integers(-1, 2, size=(n_pages, Hkv))
+    return cells_of_rows(K.astype(np.uint8), False), scale(), cells_of_rows(V.astype(np.uint8), True), scale(), table
+
+
+def keys_of_pages(code, scale, table, n, transposed):
+    """[Hkv, n, d] float64 of a sequence; zeros for pages that do not exist."""
+    n_pages = code.shape[0]
+    rows = VALUES[rows_of_cells(code, transposed)] * scale[:, :, None, None]
+    out = [rows[p] if 0 <= p < n_pages else np.zeros_like(rows[0]) for p in table]
+    return np.concatenate(out, 1)[:, :n] if out else rows[0][:, :0]

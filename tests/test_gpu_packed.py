@@ -922,3 +922,85 @@ def test_strides_of_dimensions_of_one_mean_nothing(dtype):
         assert torch.equal(fa.paged_attn_fwd(odd(Q, 0), i32([0, 40]), i32([41]), table, pages[0])[0], want[0])
         one = fa.paged_attn_fwd(Q[:, :1], i32([0, 1]), i32([41]), table, pages[0])
         assert torch.equal(fa.paged_attn_fwd(odd(Q[:, :1], 1), i32([0, 1]), i32([41]), table, pages[0])[0], one[0])
+
+
+# ------------------------------------------------------------------------------------------------ data that shows a lost tile
+
+
+SPREAD = [   # Hq, Hkv, P, d, queries, keys; at most 16 and 32 rows per key head, and more; whole and in pieces
+    (2, 1, 64, 128, [1, 1], [9000, 3]), (5, 1, 16, 64, [1], [2100]), (10, 2, 32, 128, [1] * 4, [100, 1560, 64, 700]), (24, 1, 64, 128, [1, 1], [4097, 700]),
+    (6, 2, 16, 128, [7, 5], [900, 2000]), (4, 1, 64, 64, [6, 8], [7000, 2200]), (4, 2, 32, 128, [60, 90], [300, 1200]), (4, 1, 64, 128, [130], [8200]),
+    (3, 1, 16, 64, [100], [400])]
+
+
+def spread_case(Hq, Hkv, P, d, q, k, seed):
+    """Per sequence its pages and table, numbered on from those of the sequences before; queries [Hq, n, d]."""
+    rng = np.random.default_rng(seed)
+    parts, first = [], 0
+    for n in k:
+        K, ks, V, vs, table = ref.spread_pages(rng, n, Hkv, P, d=d)
+        parts.append((K, ks, V, vs, table + first))
+        first += K.shape[0]
+    K, ks, V, vs = (np.concatenate([p[i] for p in parts]) for i in range(4))
+    mp = max(len(p[4]) for p in parts) + 1
+    table = np.full((len(k), mp), -1, np.int32)
+    for b, p in enumerate(parts):
+        table[b, :len(p[4])] = p[4]
+    Q = torch.randn((sum(q), Hq, d), generator=torch.Generator().manual_seed(seed)).bfloat16().transpose(0, 1)
+    return K, ks, V, vs, table, Q
+
+
+@pytest.mark.parametrize("Hq,Hkv,P,d,q,k", SPREAD)
+@pytest.mark.parametrize("causal", [True, False])
+def test_paged_attention_of_rows_that_need_every_tile(Hq, Hkv, P, d, q, k, causal):
+    """test_packed_host.py shows that losing or exchanging any tile of these would be seen."""
+    K, ks, V, vs, table, Q = spread_case(Hq, Hkv, P, d, q, k, sum(k))
+    O, lse = fa.paged_attn_fwd(Q.cuda(), i32(prefix(q)), i32(k), i32(table), on_device(K, ks, V, vs), causal=causal)
+    for b, n in enumerate(k):
+        i = slice(prefix(q)[b], prefix(q)[b + 1])
+        want = ref.attend(f64(Q[:, i]), ref.keys_of_pages(K, ks, table[b, :-(-n // P)], n, False), ref.keys_of_pages(V, vs, table[b, :-(-n // P)], n, True), causal, d ** -0.5)
+        check(O[:, i], lse[:, i], want, n, d, True, f"sequence {b}")
+
+
+@pytest.mark.parametrize("Hq,Hkv,P,d,q,k", SPREAD + [(8, 1, 16, 64, [1, 1], [9000, 9000]), (8, 1, 32, 128, [3], [9000]), (4, 2, 64, 128, [70], [9000])])
+@pytest.mark.parametrize("causal", [True, False])
+def test_keys_on_runs_of_pages_that_do_not_exist_are_left_out(Hq, Hkv, P, d, q, k, causal):
+    """Single pages, a run of them that is longer than a share of the tiles, the first and the last; and sequences without any page that exists."""
+    K, ks, V, vs, table, Q = spread_case(Hq, Hkv, P, d, q, k, sum(k) + 1)
+    for gone in ([lambda per: [0], lambda per: [per // 2, per - 1], lambda per: list(range(per // 3, max(2 * per // 3, 1)))], [lambda per: list(range(per))] * 3):
+        t = table.copy()
+        for b, n in enumerate(k):
+            t[b, gone[(b + len(k)) % 3](-(-n // P))] = (-1, 2 ** 30, -2 ** 31, K.shape[0])[b % 4]
+        O, lse = fa.paged_attn_fwd(Q.cuda(), i32(prefix(q)), i32(k), i32(t), on_device(K, ks, V, vs), causal=causal)
+        for b, n in enumerate(k):
+            i, ids = slice(prefix(q)[b], prefix(q)[b + 1]), t[b, :-(-n // P)]
+            live = np.repeat([0 <= p < K.shape[0] for p in ids], P)[:n]
+            want = ref.attend(f64(Q[:, i]), ref.keys_of_pages(K, ks, ids, n, False), ref.keys_of_pages(V, vs, ids, n, True), causal, d ** -0.5, live)
+            check(O[:, i], lse[:, i], want, n, d, True, f"sequence {b}")
+
+
+WEIGHTS16 = [(8, 1, 16, 128, 1, 100), (12, 12, 64, 128, 1, 64), (4, 1, 32, 64, 2, 40), (5, 1, 64, 128, 1, 160), (6, 3, 16, 64, 4, 99)]
+
+
+def weights16_case(Hq, Hkv, P, d, q, k):
+    """Even weights and values of 1 and 2 of either sign, which leave little of each other: an output is some per cent of what rounding a
+    weight is relative to.  Returns the pages, the table, the queries, the 64-bit result and the bound of weights of 16 bits: 2^-16 of a weight may be missing."""
+    rng = np.random.default_rng(k)
+    K, ks, V, vs, table = ref.spread_pages(rng, k, Hkv, P, d=d)
+    V = (V & 0x80 | 0x38).astype(np.uint8)
+    vs[:] = 1.0
+    Q = torch.randn((q, Hq, d), generator=torch.Generator().manual_seed(k)).bfloat16().transpose(0, 1)
+    k64, v64 = ref.keys_of_pages(K, ks, table, k, False), ref.keys_of_pages(V, vs, table, k, True)
+    Or, _, A, S, vmax = ref.attend(f64(Q), k64, v64, False, d ** -0.5)
+    delta = 2 * (d + 4) * 2.0 ** -24 * S[..., None] + 2.0 ** -20
+    tol = 2.0 ** -8 * np.abs(Or) + (2.0 ** -16 + delta + k * 2.0 ** -24) * 1.02 * A + 2 * k * 2.0 ** -126 * vmax
+    return (K, ks, V, vs), table, Q, k64, v64, Or, tol
+
+
+@pytest.mark.parametrize("Hq,Hkv,P,d,q,k", WEIGHTS16)
+def test_even_weights_of_few_rows_have_sixteen_bits(Hq, Hkv, P, d, q, k):
+    """test_packed_host.py shows that weights of 8 bits would be seen.  Tables as long as the sequence and of 4096 keys (two launches)."""
+    pages, table, Q, _, _, Or, tol = weights16_case(Hq, Hkv, P, d, q, k)
+    for t in (table, np.concatenate([table, np.full(4096 // P - len(table), -1, np.int32)])):
+        O, _ = fa.paged_attn_fwd(Q.cuda(), i32([0, q]), i32([k]), i32(t[None]), on_device(*pages), causal=False)
+        assert (np.abs(f64(O) - Or) <= tol).all()

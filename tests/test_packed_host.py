@@ -190,3 +190,60 @@ def test_attend_leaves_out_what_a_query_does_not_see():
     assert np.array_equal(O2[:, :4], O[:, :4]) and np.array_equal(lse2[:, :4], lse[:, :4])
     O3 = ref.attend(Q, K, V, False, 0.5, live=np.array([True, False, True]))[0]
     assert np.allclose(O3, ref.attend(Q, K[:, ::2], V[:, ::2], False, 0.5)[0])
+
+
+# ------------------------------------------------------------------------------------------------ what the GPU tests' data shows
+
+
+def spread_cases():
+    from test_gpu_packed import SPREAD
+    return [c for c in SPREAD if sum(c[4]) < 20]   # the chunks' pages are made the same way
+
+
+@pytest.mark.parametrize("case", spread_cases(), ids=str)
+def test_data_of_the_paged_attention_tests_shows_a_lost_tile(case):
+    """Mistakes planted in the 64-bit result: one tile of 64 keys left out, and its values those of the next tile, for every tile."""
+    import torch
+    from test_gpu_packed import check, prefix, spread_case
+    Hq, Hkv, P, d, q, k = case
+    K, ks, V, vs, table, Q = spread_case(*case, sum(k))
+    b = int(np.argmax(k))
+    n, ids = k[b], table[b, :-(-k[b] // P)]
+    Q = Q[:, prefix(q)[b]:prefix(q)[b] + 1].double().numpy()
+    K, V = ref.keys_of_pages(K, ks, ids, n, False), ref.keys_of_pages(V, vs, ids, n, True)
+    want = ref.attend(Q, K, V, False, d ** -0.5)
+    check(torch.from_numpy(want[0]), torch.from_numpy(want[1]), want, n, d, True)
+    for t in range(-(-n // 64)):
+        tile = np.arange(n) // 64 == t
+        lost = ref.attend(Q, K[:, ~tile], V[:, ~tile], False, d ** -0.5)
+        for o, l in ((lost[0], None), (want[0], lost[1])):
+            with pytest.raises(AssertionError):
+                check(torch.from_numpy(o), None if l is None else torch.from_numpy(l), want, n, d, True)
+        if (t + 2) * 64 <= n:
+            V2 = V.copy()
+            V2[:, t * 64:(t + 1) * 64] = V[:, (t + 1) * 64:(t + 2) * 64]
+            with pytest.raises(AssertionError):
+                check(torch.from_numpy(ref.attend(Q, K, V2, False, d ** -0.5)[0]), None, want, n, d, True)
+
+
+def weights16_cases():
+    from test_gpu_packed import WEIGHTS16
+    return WEIGHTS16
+
+
+@pytest.mark.parametrize("case", weights16_cases(), ids=str)
+def test_data_of_the_test_of_sixteen_bits_shows_eight(case):
+    """The 64-bit result with every weight rounded to bf16 is outside of the bound."""
+    import torch
+    from test_gpu_packed import weights16_case
+    Hq, Hkv, P, d, q, k = case
+    _, _, Q, K, V, Or, tol = weights16_case(*case)
+    off = 0
+    for h in range(Hq):
+        for i in range(q):
+            l = K[h // (Hq // Hkv)] @ Q[h, i].double().numpy() * d ** -0.5
+            w = np.exp(l - l.max())
+            r = torch.from_numpy(w).bfloat16().double().numpy()
+            off += (np.abs(r @ V[h // (Hq // Hkv)] / w.sum() - Or[h, i]) > tol[h, i]).sum()
+            assert (np.abs(w @ V[h // (Hq // Hkv)] / w.sum() - Or[h, i]) <= tol[h, i]).all()
+    assert off >= 10, off
