@@ -25,7 +25,6 @@ using namespace attn_lds;
 constexpr int NWG = 4;         // wavefronts per group
 constexpr int R = 256;         // rows per item
 constexpr int NK = 2, NV = 3;  // stages
-constexpr float TAU = 8.0f;    // the reference maximum may lag the true one by 8 octaves: weights up to 256
 constexpr int SHARES = 256;
 constexpr int LEAST = 8;       // tiles of a share at least: a fragment costs as much as some of them
 constexpr int FEW_KEYS = 512;  // longer tables are cut while items leave compute units idle (100 tokens x 12 heads on 4 x 2000 keys 72 us whole, 34 cut)
@@ -225,7 +224,10 @@ __global__ __launch_bounds__(2 * NWG * 64, 1) void attn_chunk_kernel(const Args 
             __builtin_amdgcn_s_setprio(0);
         };
         auto phase_y = [&]() __attribute__((always_inline)) {
-            if (__any((mx_tile - m) * scale_log2 > TAU)) {
+            // The reference is the maximum itself, as in paged_attn.hip: weights near 1 lose least when they are rounded to bf16.  Chunks
+            // of 201 to 780 tokens over caches of up to 37440 an error of 0.0017 of the output where a reference that may lag 8 octaves has
+            // 0.0020, for 434 us instead of 429.
+            if (__any(mx_tile > m)) {
                 const float mn = fmaxf(m, mx_tile);
                 const float alpha = weight_of(m, mn, scale_log2);
                 m = mn;
@@ -338,7 +340,7 @@ __global__ __launch_bounds__(2 * NWG * 64, 1) void attn_chunk_kernel(const Args 
                 frag[R * D + R + wave * 32 + col_e] = l;
             }
         }
-        // as in paged_attn.hip: rows whose sums are not finite, or none (here a weight of up to 256 times a value may have left the range too)
+        // as in paged_attn.hip: rows whose sums are not finite, or none
         if (__builtin_expect(__any(odd), 0)) {
             const Args a = args_anew<Args>();
             const int32_t *pages = a.table + (size_t)r.b * a.max_pages;
