@@ -13,7 +13,7 @@
 // Tables that are so short that there is nothing to cut take one launch (SPLIT = false), a workgroup of eight wavefronts per item.
 // What bounds it: bytes.  Tokens of two requests of 200000 and 230400 keys x 8 key heads x 128, 881 MB: 154 us = 5.7 TB/s and 8 us for
 // the fragments; of 48 requests of 100 to 37440 keys 951 MB in 174 us and 6.  Short ones: the chain lengths, page numbers, codes, sums,
-// each a trip to memory (1560 keys x 12 heads 10.6 us).
+// each a trip to memory (1560 keys x 12 heads 10.8 us).
 #include "paged_dev.hpp"
 
 namespace fastar {
@@ -23,13 +23,16 @@ int pages_check(const fastar_pages *pg);
 namespace paged {
 
 constexpr int SHARES = 512;        // workgroups that share the tiles: two per compute unit
-// Tiles of a share at least, three per wavefront: fragments are put together by few workgroups.  1 / 2 / 4 per wavefront: one sequence
-// of 100000 keys, one key head 37 / 23.7 / 19.4 us, of 16000 keys x 8 key heads 22.8 / 17.6 / 19.7.
+// Units of a share at least (tiles, and the ENDS in front of an item's): few workgroups put fragments together.  3 / 6 / 12 / 24 / 48: one
+// sequence of 100000 keys, one key head 41 / 28 / 20 / 19 / 25 us, of 16000 keys x 8 key heads 27 / 19 / 18 / 19 / 25, 16 of 2100 x 8
+// 25 / 25 / 22.5 / 22.3 / 27.5; launches with more work have longer shares anyway.
 constexpr int LEAST = 12;
 constexpr int MAX_RT = 2;
 constexpr int FRAG_FLOATS = MAX_RT * (16 * 128 + 32);
 static_assert(SHARES <= MAX_SHARES, "descriptors");
-constexpr int ONE_LAUNCH_KEYS = 2048;   // tables of up to this many keys are not cut
+// Tables of up to this many keys are not cut.  Whole / cut, a token each: one request of 12 heads with 1000 keys 9.1 / 14.0 us, 2000
+// 12.3 / 14.1, 4000 18.7 / 13.1; 48 requests of 40 heads on 8 with 1000 24 / 30, 2000 38 / 45, 4000 79 / 89.
+constexpr int ONE_LAUNCH_KEYS = 2048;
 
 __device__ __forceinline__ f32x4 mfma_16x16x32(bf16x8 a, bf16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
 
@@ -74,7 +77,7 @@ __global__ __launch_bounds__(NW * 64, 2) void attn_kernel(const Args a) {
         const int limit_max = a.causal ? min(max(sq.L - sq.n_q + tok1 + 1, 0), sq.L) : sq.L;   // ... the last
         // Up to eight rows leave half of a product's columns empty: column c + 8 then holds row c too, with what rounding takes from its
         // weights in place of the weights, so that these rows have weights of 16 bits without a product more.  One token of 12 heads,
-        // 1560 keys each: an error of 0.0015 (the output's rounding) instead of 0.0018 to 0.0028, for 10.6 us instead of 10.1; 48 tokens
+        // 1560 keys each: an error of 0.0015 (the output's rounding) instead of 0.0018 to 0.0028, for 0.5 us more; 48 tokens
         // x 40 heads 184 us instead of 183.  With more rows peaked ones are fewer among them and products of their own cost 3 to 17 %:
         // weights of 8 bits.
         const bool fold = RT == 1 && n_rows - qt * R <= 8;
@@ -434,7 +437,11 @@ extern "C" int paged_attn_fwd(const fastar_rows *Q, const int32_t *cu_q, const i
                            (paged::Desc *)ws, (float *)((char *)ws + paged::MAX_SHARES * sizeof(paged::Desc))};
     const int64_t rows = (int64_t)n_tok * group;
     const hipStream_t s = (hipStream_t)stream;
-    // By the rows that a sequence has on average: 16 or 32 per item, or the kernel whose wavefronts share their tiles.
+    // By the rows that a sequence has on average: 16 or 32 per item, or the kernel whose wavefronts share their tiles.  8 heads on 8, one
+    // sequence of 1500 keys, 8 of 1500, 8 of 9000 and 48 of 9000: 16 rows an item / 32, at 16 rows 11.3 / 14.5, 11.7 / 14.9, 38.5 / 50, 178 / 205 us,
+    // at 20 11.3 / 14.9, 14.0 / 15.3, 38 / 52, 322 / 207; 32 rows an item / the other kernel, at 32 15.5 / 27, 16 / 34, 52 / 86, 207 / 426, at 40
+    // 15.5 / 28.8, 17.9 / 38, 50 / 90, 354 / 430, at 96 15.6 / 29, 20 / 39, 88 / 92, 453 / 449: long batches decide on the first line; the
+    // second is low for them and for few sequences (64 to 96 rows).
     const int64_t keys = (int64_t)max_pages * pages->P;
     const bool one_launch = keys <= paged::ONE_LAUNCH_KEYS;
     if (rows > (int64_t)32 * B) return launch_paged_chunk(a, rows, keys, one_launch, s);

@@ -8,7 +8,7 @@
 // which is the order that half a wavefront holds P in.  The items' tiles are dealt out as in paged_dev.hpp, a workgroup per compute
 // unit.  What bounds it: the two phases' instructions, 4000 cycles per tile and pair of wavefronts, 2048 of them matrix instructions;
 // rows that no token fills (8 % of five chunks of 201 to 780 tokens x 3 heads); 14 us of fragments.  Those chunks over caches of 4680
-// to 37440 keys x 4 key heads: 460 us = 845 TFLOP/s (paged_attn.hip's way with 64 rows per wavefront took 790).
+// to 37440 keys x 4 key heads: 430 to 460 us from box to box, 840 to 900 TFLOP/s (paged_attn.hip's way with 64 rows per wavefront took 790).
 #include "attn_lds.hpp"
 #include "paged_dev.hpp"
 
@@ -26,8 +26,10 @@ constexpr int NWG = 4;         // wavefronts per group
 constexpr int R = 256;         // rows per item
 constexpr int NK = 2, NV = 3;  // stages
 constexpr int SHARES = 256;
-constexpr int LEAST = 8;       // tiles of a share at least: a fragment costs as much as some of them
-constexpr int FEW_KEYS = 512;  // longer tables are cut while items leave compute units idle (100 tokens x 12 heads on 4 x 2000 keys 72 us whole, 34 cut)
+// Units of a share at least (tiles, and the ENDS in front of an item's): a fragment costs as much as some tiles.  4 / 8 / 16 / 32: 100 tokens x
+// 12 heads on 4 x 2000 keys 27 / 31 / 43 / 67 us, 300 on 9000 68 / 68 / 52 / 76, 130 x 4 heads on one x 100000 94 / 95 / 95 / 99.
+constexpr int LEAST = 8;
+constexpr int FEW_KEYS = 512;  // longer tables are cut while items leave compute units idle (100 tokens x 12 heads on 4 x 2000 keys 72 us whole, 31 cut)
 constexpr int FRAG_FLOATS = R * 128 + 2 * R;
 static_assert(SHARES <= MAX_SHARES, "descriptors");
 

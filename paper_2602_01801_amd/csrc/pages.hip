@@ -40,7 +40,7 @@ __device__ __forceinline__ int slot_of(const int32_t *__restrict__ row, long lon
 // request to another by way of the pool are looked up where they come from, and tables, pool and slots are written side by side:
 // two rounds of loads in all (one for lengths, one for pages), against six of the kernel for more requests.  With many tokens more
 // workgroups repeat the sums and write slots only; that needs the lengths to stay in place, so not if len_out or pool_n_out is an input.
-// 192 requests, a token each 14.1 -> 6.0 us, 64 prompts of 90122 tokens 13 -> 4.6.
+// 192 requests, a token each 14.1 -> 6.0 us, 64 prompts of 90122 tokens 13 -> 4.6; 1024 requests 5.8, 1025 by the other kernel 51, 10000 249.
 constexpr int SMALL_LIMIT = 1 << 20;   // PT times this much stays below 2^31
 __global__ __launch_bounds__(PT) void plan_small_kernel(const int32_t *__restrict__ n_new, const int32_t *len, int32_t *table, int B,
                                                         int max_pages, int32_t *pool, const int32_t *pool_n, int n_pages, int pshift,
@@ -530,7 +530,9 @@ extern "C" int kv_pages_plan(const int32_t *n_new, const int32_t *len, int32_t *
     const int pshift = __builtin_ctz((unsigned)P);
     const hipStream_t s = (hipStream_t)stream;
     if (B <= pages::PT && n_tok < pages::SMALL_LIMIT && max_pages < pages::SMALL_LIMIT) {
-        // one workgroup writes ONE_SLOTS slots beside the rest; beyond that there are more workgroups, or a launch of their own
+        // One workgroup writes ONE_SLOTS slots beside the rest; beyond that there are more workgroups, or a launch of their own where the
+        // call works in place.  64 prompts of 2048 / 3840 / 6400 / 16000 slots in all: one workgroup 5.6 / 6.8 / 8.7 / 14.5 us, more of them 4.9
+        // each; in place one 4.5 / 5.7 / 7.6 / 13.8, a second launch 6.2 / 6.7 / 6.5 / 6.7.
         constexpr int ONE_SLOTS = 4096;
         const bool alone = len_out == len || pool_n_out == pool_n;
         const int wgs = n_tok <= ONE_SLOTS || alone ? 1 : (n_tok + pages::PT - 1) / pages::PT;
@@ -583,7 +585,8 @@ extern "C" int kv_pages_write(const fastar_pages *pages, const fastar_rows *K_ne
     const View k = view_of(K_new, pages->Hkv, n_tok, elt), v = view_of(V_new, pages->Hkv, n_tok, elt);
     if (k.row > MAX_PITCH || v.row > MAX_PITCH) return FASTAR_ERR_UNSUPPORTED;
     // Rows per workgroup: a page's where that makes enough of them; fewer, down to one, so that the runs of single tokens are not
-    // done one after the other.
+    // done one after the other.  At least 1024 / 4096 / 16384 workgroups, pages of 64, 8 heads: 512 single tokens 17.5 / 19.4 / 21.7 us, 16 runs
+    // of 16 4.5 / 6.0 / 6.0, 8 of 200 6.3 / 9.2 / 18.6, 8 of 4680 38.6 / 37.4 / 52; 30000 tokens of one head 9.5 / 23 / 49: for runs fewer would do.
     int chunk = pages->P;
     while (chunk > 1 && (int64_t)n_tok * pages->Hkv * 2 / chunk < 4096) chunk /= 2;
     const int64_t units = (int64_t)((n_tok + chunk - 1) / chunk) * pages->Hkv * 2;

@@ -15,7 +15,7 @@
 // Three stages of K and four of V make room for tiles that one group still reads while the other has asked for the next ones.
 // What bounds it: 3200 cycles per tile and pair of wavefronts, 2048 of them matrix instructions, at the 1.6 to 1.7 GHz that the chip
 // holds under it (matrix instructions alone reach 1.73 PFLOP/s on such data): 32760 tokens x 12 heads on 4 key heads, causal,
-// 2.71 to 2.75 ms = 1.2 PFLOP/s.  Short sequences add 5 us of a workgroup's ends (lengths, queries and first tiles 2.5, output 1.2).
+// 2.71 to 2.80 ms = 1.2 PFLOP/s.  Short sequences add 5 us of a workgroup's ends (lengths, queries and first tiles 2.5, output 1.2).
 #include "attn_lds.hpp"
 #include "packed.hpp"
 
