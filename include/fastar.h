@@ -458,8 +458,8 @@ typedef struct {
  * sums; fp32: plain fp32 arithmetic.
  * Supported: d in {64, 128}; scale positive, scale * log2(e) finite; rows of K and V at most 2^24 bytes apart;
  * n_tok_q * Hq < 2^30, n_tok_k <= 2^30; n_tok_q * Hq / 256 + (B + 1) * Hkv < 2^23 (fp32: n_tok_q * Hq / 64 ... < 2^24).  No workspace.  n_tok_q = 0 or B = 0 launches nothing.
- * Where sums are not finite (infinities or NaN among the keys and values, or values near the end of the range), the queries of the
- * tiles concerned are done again one by one, so that none sees what is masked for it: right, and many times slower.
+ * Where a causal call meets infinities or NaN among the values, or any call values near the end of the range, the queries of the tiles
+ * concerned are done again one by one, so that none sees what is masked for it and no mean is lost: right, and many times slower.
  */
 int prompt_attn_fwd(const fastar_rows *Q, const fastar_rows *K, const fastar_rows *V, const int32_t *cu_q,
                     const int32_t *cu_k, int B, int n_tok_q, int n_tok_k, int Hq, int Hkv, int d, int dtype, int causal,

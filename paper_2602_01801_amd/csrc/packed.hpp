@@ -141,6 +141,23 @@ __device__ __forceinline__ float lse_of(float m, float l, float scale_log2) {
 // Whether a row with keys has a sum of weights: the reference score's own weight is one, but m * scale is rounded in the exponent of
 // the others, which shows from scaled scores of 2^24 on and takes weights out of the range, up or down, from about 2^31 on.
 __device__ __forceinline__ bool sums_up(float m, float l) { return m == -INFINITY || (l >= 0.25f && l < INFINITY); }
+// Whether a sum of weights that does not add up is no number because some score is none, which is what the row is then.
+__device__ __forceinline__ bool no_number(float m, float l, float scale_log2) { return l != l && fabsf(m * scale_log2) < 0x1p24f; }
+// Whether sums of rows that see all n values stand, finite or not: each value is below 2^88, so that 2^30 of them with weights of up
+// to 256 stay in the range, or not finite, and then no infinity of the first key if that fills up a tile.  A wavefront, lane l coordinates l, l + 64.
+constexpr float VALUES_ADD_UP = 0x1p88f;
+template <typename T, int D>
+__device__ __forceinline__ bool sums_stand(const char *V, int64_t pitch, int n, bool filled) {
+    const int lane = lane_id();
+    bool bad = false;
+    for (int j = 0; j < n; ++j)
+#pragma unroll
+        for (int c = 0; c < D / 64; ++c) {
+            const float x = fabsf((float)((const T *)(V + (int64_t)j * pitch))[64 * c + lane]);
+            bad |= x < INFINITY ? x >= VALUES_ADD_UP : j == 0 && filled && x == INFINITY;
+        }
+    return !__any(bad);
+}
 
 // One row over the keys first .. seen - 1, a wavefront: what tiles whose sums are not finite fall back to.  The maximum and the sum of
 // the weights come first, so that values are taken with weights that add up to one and their sum stays where the values are; a

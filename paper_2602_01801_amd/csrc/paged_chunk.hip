@@ -347,8 +347,10 @@ __global__ __launch_bounds__(2 * NWG * 64, 1) void attn_chunk_kernel(const Args 
             const Args a = args_anew<Args>();
             const int32_t *pages = a.table + (size_t)r.b * a.max_pages;
             float *frag = a.frag + (size_t)(2 * r.share + (begins ? 1 : 0)) * FRAG_FLOATS;
+            const bool again = (a.causal && sq.n_q > 1) || __any(!sums_up(m, l) && !no_number(m, l, a.scale_log2)) ||
+                               !paged_sums_stand(a, pages, h, ta * TK, min(sq.L, te * TK));
             __threadfence();
-            for (int x = 0; x < 32 && row0_e + x < n_rows; ++x) {
+            for (int x = 0; again && x < 32 && row0_e + x < n_rows; ++x) {
                 const int rr = row0_e + x, tok = rr / a.group, head = h * a.group + rr - tok * a.group;
                 float mr, lr, acc[D / 64];
                 row_by_paged_keys<D>(a, a.Q.p + head * a.Q.head + (int64_t)(sq.q0 + tok) * a.Q.row, pages, h, ta * TK, min(a.causal ? min(max(sq.L - sq.n_q + tok + 1, 0), sq.L) : sq.L, te * TK), mr, lr, acc);

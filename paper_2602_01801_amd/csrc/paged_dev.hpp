@@ -251,6 +251,14 @@ __device__ __forceinline__ void row_by_paged_keys(const Args &a, const char *q, 
         m, l, o);
 }
 
+// The same of rows that see all keys first .. seen - 1: tiles are filled up with zeros here.
+__device__ __forceinline__ bool paged_sums_stand(const Args &a, const int32_t *pages, int h, int first, int seen) {
+    bool bad = false;
+    for (int i = (first >> a.pshift) + lane_id(); i <= (seen - 1) >> a.pshift; i += 64)
+        if (page_exists(a, pages[i])) bad |= !(a.pg.vscale[(size_t)pages[i] * a.pg.Hkv + h] < VALUES_ADD_UP / 512.0f);
+    return !__any(bad);
+}
+
 // What a fragment's sums count for against the others': its weight; sums of rows that were done again add up to one, which the sign of
 // their sum of weights says (theirs is that times its size).
 __device__ __forceinline__ float parts_of(float l, float weight) { return l < 0.0f ? -l * weight : weight; }

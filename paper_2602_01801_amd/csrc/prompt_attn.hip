@@ -316,11 +316,12 @@ __global__ __launch_bounds__(2 * NWG * 64, 1) void attn_bf16_kernel(const Args a
     if (a.lse && g == 0 && row0 + col < n_rows)
         a.lse[(size_t)my_head * a.n_tok_q + rq.first + my_tok] = lse_of(m, l, scale_log2);
     // Sums that are not finite, or none: a value that a row does not see, or key 0's, which fills up the last tile, may have come in as 0 * x
-    // (a product of tiles has no other way), or weights, or weights times values, have left the range.  Those rows are done again key by key, over
-    // the keys that they see and with weights that add up to one.
+    // (a product of tiles has no other way), or weights, or weights times values, have left the range.  Those rows are done again one by one, over
+    // the keys that they see and with weights that add up to one; where all rows see all keys, only if the sums may be wrong.
     if (__builtin_expect(__any(odd), 0)) {
         const Args a = args_anew<Args>();
         const char *K = a.K.p + h * a.K.head + (int64_t)rk.first * a.K.row, *V = a.V.p + h * a.V.head + (int64_t)rk.first * a.V.row;
+        if (!a.causal && !__any(!sums_up(m, l) && !no_number(m, l, a.scale_log2)) && sums_stand<__bf16, D>(V, a.V.row, n, n % TK != 0)) return;
         for (int r = 0; r < 32 && row0 + r < n_rows; ++r) {
             const int rr = row0 + r, tok = rr / a.group, head = h * a.group + rr - tok * a.group;
             float mr, lr, acc[D / 64];

@@ -299,6 +299,7 @@ __global__ __launch_bounds__(TEAMS * RW * 64, 2) void attn_f32_prompt_kernel(con
     if (__builtin_expect(__any(odd), 0)) {
         const Args a = args_anew<Args>();
         const char *K = a.K.p + h * a.K.head + (int64_t)rk.first * a.K.row, *V = a.V.p + h * a.V.head + (int64_t)rk.first * a.V.row;
+        if (!a.causal && !__any(!sums_up(m, l) && !no_number(m, l, a.scale_log2)) && sums_stand<float, D>(V, a.V.row, n, n % TK != 0)) return;
         for (int r = 0; r < 16 && row0 + r < n_rows; ++r) {
             const int rr = row0 + r, tok = rr / a.group, head = h * a.group + rr - tok * a.group;
             float mr, lr, acc[D / 64];

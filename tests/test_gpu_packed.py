@@ -692,6 +692,8 @@ def check_kinds(O, lse, want, n, d, bf16, what=""):
     for kind in (np.isnan, np.isposinf, np.isneginf):
         assert (kind(o) == kind(Or)).all(), (what, kind.__name__, np.argwhere(kind(o) != kind(Or))[:4], o[kind(o) != kind(Or)][:4])
     fin = np.isfinite(Or)
+    assert (np.isfinite(S) | ~fin.any(-1)).all()   # a row without a bound has no finite output
+    S = np.where(np.isfinite(S), S, 0.0)
     check(torch.from_numpy(np.where(fin, o, 0.0)), lse, (np.where(fin, Or, 0.0), lr, np.where(fin, A, 0.0), S, vmax), n, d, bf16, what)
 
 
@@ -1004,3 +1006,38 @@ def test_even_weights_of_few_rows_have_sixteen_bits(Hq, Hkv, P, d, q, k):
     for t in (table, np.concatenate([table, np.full(4096 // P - len(table), -1, np.int32)])):
         O, _ = fa.paged_attn_fwd(Q.cuda(), i32([0, q]), i32([k]), i32(t[None]), on_device(*pages), causal=False)
         assert (np.abs(f64(O) - Or) <= tol).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("large", [1.0, 2.0 ** 127])
+@pytest.mark.parametrize("Hkv,q,n", [(2, 5, 200), (2, 5, 256), (40, 420, 470)])
+def test_infinities_and_no_numbers_that_every_query_sees(Hkv, q, n, large, dtype):
+    """Not causal: sums that are not finite stand, unless values are so large that they may have left the range by themselves."""
+    g = torch.Generator().manual_seed(n)
+    d, Hq = 128, 2 * Hkv
+    Q, K = (view(g, h, m, d, DT[dtype], "tokens") for h, m in ((Hq, q), (Hkv, n)))
+    V = ((torch.rand((Hkv, n, d), generator=g) + 1.0) * large * 0.99).to(DT[dtype]).cuda()
+    V[:, 9, 3], V[:, 100, 4], V[:, 101, 5], V[:, 102, 5], V[:, n - 1, 77] = math.inf, math.nan, math.inf, -math.inf, -math.inf
+    K[Hkv - 1, 150] = math.nan     # a head whose rows are no numbers at all
+    O, lse = fa.prompt_attn_fwd(Q, K, V, i32([0, q]), i32([0, n]), causal=False)
+    for h in (0, Hq - 1):
+        with np.errstate(invalid="ignore"):
+            want = ref.attend(f64(Q[h:h + 1]), f64(K[h // 2:h // 2 + 1]), f64(V[h // 2:h // 2 + 1]), False, d ** -0.5)
+        check_kinds(O[h:h + 1], lse[h:h + 1], want, n, d, dtype == "bf16", f"head {h}")
+
+
+@pytest.mark.parametrize("Hq,Hkv,P,d,q,n", PAGED_ENDS + [(8, 2, 16, 128, 1, 300), (8, 1, 64, 64, 1, 20000)])
+@pytest.mark.parametrize("vexp", [0, 119])
+def test_codes_that_are_no_numbers_and_every_query_sees(Hq, Hkv, P, d, q, n, vexp):
+    K, ks, V, vs, table = flat_pages(n, Hkv, P, d, n)
+    V = ((V & 0x07) | 0x70).astype(np.uint8)
+    V[V == 0x77] = 0x7E
+    vs[:] = 2.0 ** vexp
+    rows = ref.rows_of_cells(V, True).copy()
+    for j, c in ((9, 3), (n // 2, 40), (n - 1, 41)):
+        rows[table[0, j // P], :, j % P, c] = 0x7F
+    V = ref.cells_of_rows(rows, True)
+    Q = view(torch.Generator().manual_seed(n), Hq, q, d, torch.bfloat16, "tokens")
+    O, lse = fa.paged_attn_fwd(Q, i32([0, q]), i32([n]), i32(table), on_device(K, ks, V, vs), causal=False)
+    want = ref.attend(f64(Q), gather(K, ks, table[0], n, False), gather(V, vs, table[0], n, True), False, d ** -0.5)
+    check_kinds(O, lse, want, n, d, True)
