@@ -183,8 +183,8 @@ __global__ __launch_bounds__(2 * NWG * 64, 1) void attn_bf16_kernel(const Args a
     auto phase_y = [&](int t) __attribute__((always_inline)) {
         issue_k(t + 2);
         issue_v(SPLIT ? t + 1 : t + 2);
-        // The reference may lag the maximum by 8 octaves.  The maximum itself (error of the output 0.0019 instead of 0.0022, most of both its
-        // rounding) rescales sums in most tiles: 14 ragged prompts 357 us instead of 337, 32760 tokens 2.90 ms instead of 2.79; a lag of 3
+        // The reference may lag the maximum by 8 octaves.  The maximum itself (error of the output 0.0018 to 0.0020 instead of 0.0020 to
+        // 0.0022 on the same inputs, 0.0016 of either its rounding) rescales sums in most tiles: 14 ragged prompts 357 us instead of 337, 32760 tokens 2.90 ms instead of 2.79; a lag of 3
         // octaves 346 and 2.80.  Sums of the rounded weights beside those that lse needs, for a row's own key to have weight 1: 349 and 2.91.
         if (__any((mx_tile - m) * scale_log2 > 8.0f)) {
             const float mn = fmaxf(m, mx_tile);
