@@ -14,6 +14,11 @@
  *   kv_pages_plan        block tables and slot maps of a paged cache from the requests' lengths
  *   kv_pages_write       new keys and values into its pages: E4M3 codes with a scale per page and head
  *   paged_attn_fwd       attention over those pages, for single tokens and chunks
+ *   qk_norm_rope         queries and keys normed per head and rotated by their positions
+ *   kv_pages_write_rope  the same, the keys and values going straight into pages
+ *   kv_pages_fork        new requests that begin with another one's tokens and share its full pages
+ *   kv_pages_free        requests that end or are cut back give up pages that nobody else holds
+ *   kv_pages_compact     the tokens that a mask keeps move together, into fewer pages
  *
  * Conventions (all entry points):
  *   - Every pointer is a DEVICE pointer unless it points to one of the small structs below, which
@@ -68,6 +73,7 @@ extern "C" {
 #define FASTAR_OP_SELECT_BUCKETS 5 /* pass the number of prompt tokens as r */
 #define FASTAR_OP_ATTN 6           /* sparse_attn_fwd_ws, sparse_attn_fwd_fp8_ws: a fixed amount, whatever the shape */
 #define FASTAR_OP_PAGED_ATTN 7     /* paged_attn_fwd: a fixed amount, whatever the shape */
+#define FASTAR_OP_PAGES 8          /* kv_pages_free, kv_pages_compact: pass B as H, max_pages as n_q, n_pages as n_k, P as r */
 
 /* representative key of a merged TempCache group (tempcache_compress, rep_mode) */
 #define FASTAR_REP_LAST 0
@@ -537,6 +543,115 @@ int kv_pages_write(const fastar_pages *pages, const fastar_rows *K_new, const fa
 int paged_attn_fwd(const fastar_rows *Q, const int32_t *cu_q, const int32_t *len, const int32_t *table, int B, int max_pages,
                    int n_tok, int Hq, const fastar_pages *pages, int dtype, int causal, float scale, const fastar_rows *O,
                    float *lse, void *ws, size_t ws_bytes, void *stream);
+
+/* ---- norm and rotation ---- */
+
+/*
+ * What is done to every row x [d] of queries and keys.
+ *   Norm:      y_c = x_c w_c / sqrt(mean(x^2) + eps)
+ *   Rotation:  of the first rot coordinates, in pairs (a, b) -> (a cos t - b sin t, a sin t + b cos t), t = position * freq[pair];
+ *              the others stay as they are
+ * All in 32 bits, angles in 64 before they are reduced to a turn, rounded once to the type of the output.
+ */
+typedef struct {
+    const float *qw, *kw;   /* [d] weights of queries and of keys, or NULL: ones (device)                      */
+    const double *freq;     /* [rot/2] radians per position (device)                                           */
+    const int32_t *axis;    /* [rot/2] which row of `pos` a pair goes by (device), or NULL: row 0               */
+    float eps;              /* >= 0                                                                            */
+    int32_t norm;           /* 0: no norm (qw, kw and eps mean nothing);  1: as above                           */
+    int32_t rot;            /* 0 .. d, a multiple of 16;  0: no rotation (freq and axis mean nothing)           */
+    int32_t interleaved;    /* pair i is (i, i + rot/2);  1: (2i, 2i + 1)                                      */
+    int32_t n_axes;         /* rows of `pos`, 1 .. 4                                                           */
+} fastar_rope;
+
+/*
+ * Norm and rotation of packed queries and keys.
+ *   Q, Qo [Hq,n_tok,d], K, Ko [Hkv,n_tok,d] views of dtype; either pair may be missing (Hq = 0 or Hkv = 0, pointers NULL).
+ *   pos [n_axes, n_tok] int32 positions, negative ones too; an axis that is none goes as the nearest.  NULL: row i of the a rows
+ *       of sequence b is at position len[b] - a + i on every axis (the last row is the sequence's last token).
+ *   cu [B+1], len [B]: the sequences, where pos is NULL.  With pos: cu NULL (and B = 0): all rows;  otherwise rows outside of every
+ *       sequence are neither read nor written, and len may be NULL.
+ * An output may be its input (the same address and strides); otherwise they share no memory.
+ * Rows that hold infinities or NaN give what the formula gives, in that row alone; a row of zeros with eps = 0 is NaN.
+ * Supported: d in {64, 128}; n_tok <= 2^30; n_tok times 1 .. (Hq + Hkv) * d / 512 wavefronts in 2^32 threads.  No workspace.
+ */
+int qk_norm_rope(const fastar_rows *Q, const fastar_rows *K, const int32_t *pos, const int32_t *cu, const int32_t *len, int B,
+                 int n_tok, int Hq, int Hkv, int d, int dtype, const fastar_rope *rope, const fastar_rows *Qo, const fastar_rows *Ko,
+                 void *stream);
+
+/*
+ * qk_norm_rope of Q into Qo and of the keys, and kv_pages_write of those keys and of V_new, without the keys between the two: they are
+ * rounded once, from 32 bits to their codes (the two calls round them to dtype first).  Q and Qo may be missing (Hq = 0).
+ * Arguments as for the two; slots of rows outside of every sequence (cu) are passed over whatever they say.  Supported as both.
+ */
+int kv_pages_write_rope(const fastar_pages *pages, const fastar_rows *Q, const fastar_rows *K_new, const fastar_rows *V_new, int dtype,
+                        const int32_t *slot, const int32_t *pos, const int32_t *cu, const int32_t *len, int B, int n_tok, int Hq,
+                        const fastar_rope *rope, const fastar_rows *Qo, void *stream);
+
+/* ---- requests that share pages ---- */
+/*
+ * A page may be in several block tables: it is held as often as tables name it (their first ceil(len/P) entries; entries outside of
+ * [0, n_pages) name nothing).  Only full pages come to be shared, and kv_pages_write writes behind a request's last token, so that
+ * nobody writes to a page that others hold.  kv_pages_plan gives the pages of an ended request back whoever else holds them:
+ * where requests share, they end by kv_pages_free.
+ */
+
+/*
+ * Requests that begin with the tokens of another one.  Fork i: request child[i], which holds nothing, gets the first
+ * m = min(keep[i], len[parent[i]]) tokens of request parent[i] (keep NULL: all; negative: none): its full pages by their numbers,
+ * and, if m is no multiple of P, a page of its own from the pool, into which the page with the last of them is copied (all its codes
+ * and scales).  An entry of the parent's table that names no page is taken over as it is.  The parents are those before the call.
+ *   parent, child, keep [n];  len [B];  table [B, max_pages]: the children's rows are written up to ceil(m/P) entries
+ *   pool [n_pages], pool_n [1]: as for kv_pages_plan; pages are taken from the top, in the order of the forks
+ *   len_out [B]       tokens after the call; may be len itself
+ *   pool_n_out [1]    free pages after it; may be pool_n itself
+ *   status [n]        0;  1: it needs a page, and those needed up to and including it are more than there are;  2: parent or child is no
+ *                     request, the child holds tokens, or an earlier fork of the call names the same child.  Refused forks change nothing.
+ * Lengths and counts are cut to what the arrays hold.
+ * Supported: n <= 1024; B * max_pages < 2^31; P and n_pages as for kv_pages_plan.  No workspace.
+ */
+int kv_pages_fork(const fastar_pages *pages, const int32_t *parent, const int32_t *child, const int32_t *keep, int n, const int32_t *len,
+                  int32_t *table, int B, int max_pages, const int32_t *pool, const int32_t *pool_n, int32_t *len_out, int32_t *pool_n_out,
+                  int32_t *status, void *stream);
+
+/*
+ * Requests that end or are cut back: request b keeps its first keep[b] tokens (none if negative, all if there are no more).  It gives up
+ * the pages behind them; those that nobody holds any more go on top of the pool, in the order of the requests and of their
+ * tables, each at the place of its last holder.  Cutting into a page that others hold is refused, as the next token would be written
+ * to it (kv_pages_fork makes a request that may): by the tables before the call, whoever else gives the page up.
+ *   keep, len [B];  table [B, max_pages] (not changed);  pool [n_pages], pool_n [1]: as for kv_pages_plan
+ *   len_out [B]       tokens after the call; may be len itself
+ *   pool_n_out [1]    free pages after it; may be pool_n itself
+ *   status [B]        0, or 1: refused, the request keeps what it has
+ *   ws / ws_bytes     fastar_workspace_bytes(FASTAR_OP_PAGES, B, max_pages, n_pages, P, ...) bytes, 256-byte aligned; contents need not be
+ *                     kept.  Calls that may be in flight at the same time need a workspace each.
+ * Lengths and counts are cut to what the arrays hold; pages beyond what the pool can hold are lost.
+ * Supported: B * max_pages < 2^31; P and n_pages as for kv_pages_plan.
+ */
+int kv_pages_free(const int32_t *keep, const int32_t *len, const int32_t *table, int B, int max_pages, int32_t *pool, const int32_t *pool_n,
+                  int n_pages, int P, int32_t *len_out, int32_t *pool_n_out, int32_t *status, void *ws, size_t ws_bytes, void *stream);
+
+/*
+ * Requests that thin out their caches: the tokens i < len[b] of request b with keep[b][i] != 0 that lie on pages become its tokens
+ * 0, 1, .. in their order.  A new page whose tokens are all those that the request holds in one old page, at the same places, is that
+ * page.  Any other is a fresh one from the pool, its scale per head the largest of its tokens' old ones, codes carried over to it (value of
+ * the code times the old scale over the new one, rounded to nearest, ties to even), codes behind the last token zero.
+ * Request b needs as many pages as it has fresh ones; they are taken from the top of the pool, in the order of the requests and of their
+ * tables.  A request is refused, and keeps what it has (status 1), if it needs pages and those needed up to and including it are more than
+ * there are.  Then the old pages that are not kept are given up as in kv_pages_free, on top of what is left.
+ *   keep [B, max_pages * P] uint8, 16-byte aligned;  len [B];  table [B, max_pages];  pool [n_pages], pool_n [1]
+ *   len_out [B]               tokens after the call;  may be len itself
+ *   table_out [B, max_pages]  block tables after it, -1 behind a request's last page (rows of refused requests as they were);  may be table itself
+ *   pool_out [n_pages]        the pool after it; entries that nothing was put into as they were;  may be pool itself
+ *   pool_n_out [1]            free pages after it; may be pool_n itself
+ *   status [B]                0 or 1
+ *   ws / ws_bytes             as for kv_pages_free
+ * Keys keep the positions that they were rotated by.  Lengths and counts are cut to what the arrays hold.
+ * Supported: as for kv_pages_free.
+ */
+int kv_pages_compact(const fastar_pages *pages, const uint8_t *keep, const int32_t *len, const int32_t *table, int B, int max_pages,
+                     const int32_t *pool, const int32_t *pool_n, int32_t *len_out, int32_t *table_out, int32_t *pool_out, int32_t *pool_n_out,
+                     int32_t *status, void *ws, size_t ws_bytes, void *stream);
 
 #ifdef __cplusplus
 }

@@ -17,7 +17,7 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libfastar.so")
 
 F32, BF16 = 0, 1
-OP_COMPRESS, OP_SELECT_SELF, OP_SELECT_CROSS, OP_SELECT_LSH, OP_SELECT_BUCKETS, OP_ATTN, OP_PAGED_ATTN = 1, 2, 3, 4, 5, 6, 7
+OP_COMPRESS, OP_SELECT_SELF, OP_SELECT_CROSS, OP_SELECT_LSH, OP_SELECT_BUCKETS, OP_ATTN, OP_PAGED_ATTN, OP_PAGES = 1, 2, 3, 4, 5, 6, 7, 8
 REP_LAST, REP_MEAN, REP_MEDOID = 0, 1, 2
 
 _lib = None
@@ -44,6 +44,12 @@ class _RowsStruct(ctypes.Structure):
 class _PagesStruct(ctypes.Structure):
     _fields_ = [("K8", ctypes.c_void_p), ("V8", ctypes.c_void_p), ("kscale", ctypes.c_void_p), ("vscale", ctypes.c_void_p),
                 ("n_pages", ctypes.c_int32), ("Hkv", ctypes.c_int32), ("P", ctypes.c_int32), ("d", ctypes.c_int32)]
+
+
+class _RopeStruct(ctypes.Structure):
+    _fields_ = [("qw", ctypes.c_void_p), ("kw", ctypes.c_void_p), ("freq", ctypes.c_void_p), ("axis", ctypes.c_void_p),
+                ("eps", ctypes.c_float), ("norm", ctypes.c_int32), ("rot", ctypes.c_int32), ("interleaved", ctypes.c_int32),
+                ("n_axes", ctypes.c_int32)]
 
 
 def lib() -> ctypes.CDLL:
@@ -143,6 +149,17 @@ def lib() -> ctypes.CDLL:
         L.paged_attn_fwd.argtypes = [rows, ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p] + [ctypes.c_int] * 4 + \
             [ctypes.POINTER(_PagesStruct), ctypes.c_int, ctypes.c_int, ctypes.c_float, rows, ctypes.c_void_p, ctypes.c_void_p,
              ctypes.c_size_t, ctypes.c_void_p]
+        ptr, i32, pages, rope = ctypes.c_void_p, ctypes.c_int, ctypes.POINTER(_PagesStruct), ctypes.POINTER(_RopeStruct)
+        L.qk_norm_rope.restype = i32
+        L.qk_norm_rope.argtypes = [rows, rows, ptr, ptr, ptr] + [i32] * 6 + [rope, rows, rows, ptr]
+        L.kv_pages_write_rope.restype = i32
+        L.kv_pages_write_rope.argtypes = [pages, rows, rows, rows, i32, ptr, ptr, ptr, ptr, i32, i32, i32, rope, rows, ptr]
+        L.kv_pages_fork.restype = i32
+        L.kv_pages_fork.argtypes = [pages, ptr, ptr, ptr, i32, ptr, ptr, i32, i32, ptr, ptr, ptr, ptr, ptr, ptr]
+        L.kv_pages_free.restype = i32
+        L.kv_pages_free.argtypes = [ptr, ptr, ptr, i32, i32, ptr, ptr, i32, i32, ptr, ptr, ptr, ptr, ctypes.c_size_t, ptr]
+        L.kv_pages_compact.restype = i32
+        L.kv_pages_compact.argtypes = [pages, ptr, ptr, ptr, i32, i32] + [ptr] * 8 + [ctypes.c_size_t, ptr]
         L.fastar_probe_mfma_bf16.restype = ctypes.c_int
         L.fastar_probe_mfma_bf16.argtypes = [ctypes.c_int, ctypes.c_int, ctypes.c_void_p, ctypes.POINTER(ctypes.c_double), ctypes.c_void_p]
         L.fastar_probe_copy.restype = ctypes.c_int
@@ -159,7 +176,8 @@ EXPORTS = ("fastar_init", "fastar_version", "fastar_strerror", "fastar_workspace
            "ann_cross_attn_fwd",
            "ann_select_self", "ann_select_self_forced", "ann_select_self_static", "ann_prompt_buckets", "ann_select_buckets", "fastar_encode_packed", "ann_select_self_packed", "ann_select_cross", "sparse_attn_fwd", "sparse_attn_fwd_ws", "fastar_kv_to_fp8",
            "sparse_attn_fwd_fp8", "sparse_attn_fwd_fp8_ws", "fastar_encode_sign", "ann_select_lsh", "ann_select_lsh_buckets",
-           "prompt_attn_fwd", "kv_pages_plan", "kv_pages_write", "paged_attn_fwd",
+           "prompt_attn_fwd", "kv_pages_plan", "kv_pages_write", "paged_attn_fwd", "qk_norm_rope", "kv_pages_write_rope", "kv_pages_fork", "kv_pages_free",
+           "kv_pages_compact",
            "fastar_probe_mfma_bf16", "fastar_probe_copy", "fastar_probe_attn_route", "fastar_debug_plan_wait")
 
 
@@ -750,6 +768,136 @@ def paged_attn_fwd(Q, cu_q, length, table, pages: Pages, causal: bool = True, sc
                                 d ** -0.5 if scale is None else float(scale), _rows(O, Hq, n, ps.d, dt, dev),
                                 _lse_out(lse, Hq, n, dev), ws.data_ptr(), ws.numel() * ws.element_size(), _stream()), "paged_attn_fwd")
     return O, lse
+
+
+@dataclass(frozen=True)
+class Rope:
+    """Norm and rotation of queries and keys (fastar_rope); checked once, when it is made."""
+    freq: torch.Tensor | None                # [rot/2] float64: radians per position of every pair; None: no rotation
+    axis: torch.Tensor | None = None         # [rot/2] int32: row of the positions that a pair goes by; None: row 0
+    n_axes: int = 1                          # rows of the positions
+    norm: bool = True                        # root mean square per head
+    q_weight: torch.Tensor | None = None     # [d] float32; None: ones
+    k_weight: torch.Tensor | None = None
+    eps: float = 1e-6
+    interleaved: bool = False                # pairs (2i, 2i+1) instead of (i, i + rot/2)
+
+    def __post_init__(self):
+        rot = 0 if self.freq is None else 2 * _dev(self.freq, torch.float64).numel()
+        if self.axis is not None and _dev(self.axis, torch.int32).numel() * 2 != rot:
+            raise ValueError("axis must name one row of the positions per pair")
+        d = {_dev(w, torch.float32).numel() for w in (self.q_weight, self.k_weight) if w is not None}
+        if len({t.device for t in (self.freq, self.axis, self.q_weight, self.k_weight) if t is not None}) > 1 or len(d) > 1:
+            raise ValueError("frequencies, axes and weights must be on one device, and the weights as many as a head's coordinates")
+        device = next((t.get_device() for t in (self.freq, self.axis, self.q_weight, self.k_weight) if t is not None), None)
+        for name, value in (("rot", rot), ("d", d.pop() if d else None), ("device", device), (
+                "_struct", _RopeStruct(_ptr(self.q_weight), _ptr(self.k_weight), _ptr(self.freq), _ptr(self.axis), float(self.eps),
+                                       int(self.norm), rot, int(self.interleaved), self.n_axes))):
+            object.__setattr__(self, name, value)
+
+    def struct(self, d: int, dev: int) -> _RopeStruct:
+        if (self.d is not None and self.d != d) or (self.device is not None and self.device != dev):
+            raise ValueError(f"expected weights of {d} coordinates on the current device, got {self.d} on {self.device}")
+        return self._struct
+
+
+def _positions(rope: Rope, pos, cu, length, n: int, dev: int):
+    """Pointers of pos, cu and length, and the number of sequences."""
+    if pos is not None and pos.shape != (rope.n_axes, n):
+        raise ValueError(f"pos must be [{rope.n_axes}, {n}], got {tuple(pos.shape)}")
+    if cu is None:
+        return None if pos is None else _ints(pos, rope.n_axes * n, dev), None, None, 0
+    B = cu.numel() - 1
+    return (None if pos is None else _ints(pos, rope.n_axes * n, dev), _ints(cu, B + 1, dev),
+            None if length is None else _ints(length, B, dev), B)
+
+
+def qk_norm_rope(Q, K, rope: Rope, pos=None, cu=None, length=None, out=None):
+    """Queries [Hq,n,d] and keys [Hkv,n,d] (views of any head and row strides; either may be None) normed per head and rotated by
+    their positions pos [n_axes,n] int32.  pos None: row i of the a rows of a sequence (cu [B+1] int32) is at length - a + i (length
+    [B] int32).  Returns (Q, K) in their type, in `out`, which may be (Q, K) itself; rows outside of every sequence are not written."""
+    some = Q if Q is not None else K
+    if some is None or some.dim() != 3:
+        raise ValueError("Q and K must be [heads, n, d]")
+    n, d, dt, code, dev = some.shape[1], some.shape[2], some.dtype, _dtype_code(some), _here()
+    if out is None:
+        out = tuple(None if x is None else torch.empty_like(x) for x in (Q, K))
+    Hq, Hkv = (0 if x is None else x.shape[0] for x in (Q, K))
+    q, qo, k, ko = (None if x is None else _rows(x, H, n, d, dt, dev) for x, H in ((Q, Hq), (out[0], Hq), (K, Hkv), (out[1], Hkv)))
+    pos, cu, length, B = _positions(rope, pos, cu, length, n, dev)
+    _check(lib().qk_norm_rope(q, k, pos, cu, length, B, n, Hq, Hkv, d, code, rope.struct(d, dev), qo, ko, _stream()), "qk_norm_rope")
+    return out
+
+
+def kv_pages_write_rope(pages: Pages, slot, Q, K_new, V_new, rope: Rope, pos=None, cu=None, length=None, out=None):
+    """qk_norm_rope of Q [Hq,n,d] (None: keys only) and K_new [Hkv,n,d], and kv_pages_write of those keys and V_new into the slots [n].
+    Returns Q normed and rotated, in `out`, which may be Q itself."""
+    dev = _here()
+    ps = pages.struct(dev)
+    n, dt, code = slot.numel(), K_new.dtype, _dtype_code(K_new)
+    if Q is not None and out is None:
+        out = torch.empty_like(Q)
+    Hq = 0 if Q is None else Q.shape[0]
+    q, qo = (None if Q is None else _rows(x, Hq, n, ps.d, dt, dev) for x in (Q, out))
+    pos, cu, length, B = _positions(rope, pos, cu, length, n, dev)
+    _check(lib().kv_pages_write_rope(ps, q, _rows(K_new, ps.Hkv, n, ps.d, dt, dev), _rows(V_new, ps.Hkv, n, ps.d, dt, dev), code,
+                                     _ints(slot, n, dev), pos, cu, length, B, n, Hq, rope.struct(ps.d, dev), qo, _stream()),
+           "kv_pages_write_rope")
+    return out
+
+
+def kv_pages_fork(pages: Pages, parent, child, length, table, pool, pool_n, keep=None, out=None):
+    """Requests child [n] begin with the first keep [n] (None: all) tokens of requests parent [n] and share their full pages: length
+    [B], table [B,max_pages] (the children's rows are written), pool [n_pages], pool_n [1].  Returns (length after, pool_n after,
+    status [n]), all int32; out may name `length` and `pool_n` themselves for the first two."""
+    dev = _here()
+    ps = pages.struct(dev)
+    n, (B, max_pages) = parent.numel(), table.shape
+    if out is None:
+        out = tuple(torch.empty(m, dtype=torch.int32, device=table.device) for m in (B, 1, n))
+    after, free, status = out
+    _check(lib().kv_pages_fork(ps, _ints(parent, n, dev), _ints(child, n, dev), None if keep is None else _ints(keep, n, dev), n,
+                               _ints(length, B, dev), _ints(table, B * max_pages, dev), B, max_pages, _ints(pool, ps.n_pages, dev),
+                               _ints(pool_n, 1, dev), _ints(after, B, dev), _ints(free, 1, dev), _ints(status, n, dev), _stream()),
+           "kv_pages_fork")
+    return out
+
+
+def kv_pages_free(keep, length, table, pool, pool_n, P: int, out=None, ws=None):
+    """Requests keep their first keep [B] tokens; pages that no table names any more go to the pool [n_pages] (updated in place):
+    length [B], table [B,max_pages], pool_n [1], all int32.  Returns (length after, pool_n after, status [B]); out may name `length` and
+    `pool_n` themselves for the first two.  ws: workspace of workspace_bytes(OP_PAGES, B, max_pages, n_pages, P); calls that may be in
+    flight at the same time need one each."""
+    (B, max_pages), n_pages, dev = table.shape, pool.numel(), _here()
+    ws = _workspace(ws, workspace_bytes(OP_PAGES, B, max_pages, n_pages, P), table.device)
+    if out is None:
+        out = tuple(torch.empty(m, dtype=torch.int32, device=table.device) for m in (B, 1, B))
+    after, free, status = out
+    _check(lib().kv_pages_free(_ints(keep, B, dev), _ints(length, B, dev), _ints(table, B * max_pages, dev), B, max_pages,
+                               _ints(pool, n_pages, dev), _ints(pool_n, 1, dev), n_pages, P, _ints(after, B, dev), _ints(free, 1, dev),
+                               _ints(status, B, dev), ws.data_ptr(), ws.numel() * ws.element_size(), _stream()), "kv_pages_free")
+    return out
+
+
+def kv_pages_compact(pages: Pages, keep, length, table, pool, pool_n, out=None, ws=None):
+    """The tokens with keep [B, max_pages * P] (uint8 or bool) other than zero move together: length [B], table [B,max_pages], pool
+    [n_pages], pool_n [1], all int32.  Returns (length, table, pool, pool_n after, status [B]); out may name the inputs themselves for the
+    first four.  ws as for kv_pages_free."""
+    dev = _here()
+    ps = pages.struct(dev)
+    B, max_pages = table.shape
+    if keep.dtype not in (torch.uint8, torch.bool) or keep.shape != (B, max_pages * ps.P) or keep.get_device() != dev or not keep.is_contiguous():
+        raise ValueError(f"keep must be [{B}, {max_pages * ps.P}] bytes, contiguous on the current device")
+    ws = _workspace(ws, workspace_bytes(OP_PAGES, B, max_pages, ps.n_pages, ps.P), table.device)
+    if out is None:
+        i = lambda *n: torch.empty(n, dtype=torch.int32, device=table.device)
+        out = (i(B), i(B, max_pages), i(ps.n_pages), i(1), i(B))
+    after, table_out, pool_out, free, status = out
+    _check(lib().kv_pages_compact(ps, keep.data_ptr(), _ints(length, B, dev), _ints(table, B * max_pages, dev), B, max_pages,
+                                  _ints(pool, ps.n_pages, dev), _ints(pool_n, 1, dev), _ints(after, B, dev),
+                                  _ints(table_out, B * max_pages, dev), _ints(pool_out, ps.n_pages, dev), _ints(free, 1, dev),
+                                  _ints(status, B, dev), ws.data_ptr(), ws.numel() * ws.element_size(), _stream()), "kv_pages_compact")
+    return out
 
 
 def probe_mfma_bf16(iters: int = 20000, random_operands: bool = False) -> float:

@@ -1,6 +1,6 @@
 // The paged 8-bit cache: block tables and slot maps from the requests' lengths (kv_pages_plan), and new keys and values into
-// its pages (kv_pages_write).
-#include "packed.hpp"
+// its pages (kv_pages_write), the keys normed and rotated on the way (kv_pages_write_rope).
+#include "rope_dev.hpp"
 
 namespace fastar {
 
@@ -356,15 +356,46 @@ __device__ __forceinline__ void write_odd_run(const char *row0, int64_t pitch, i
     if (lane == 0) *scale_out = scale;
 }
 
+// The same of keys that are normed and rotated: roped(r, x) gives a lane's eight coordinates of row o + r * RPI + its own.
+template <int D, class Roped>
+__device__ __forceinline__ void write_odd_roped_run(Roped roped, int o, int e, uint8_t *cell0, int page_bytes, float old_scale,
+                                                    float *scale_out) {
+    constexpr int LPR = D / 8, RPI = 64 / LPR;
+    const int lane = threadIdx.x & 63, lr = lane / LPR, c = lane % LPR * 8;
+    float amax = 0.0f, x[8];
+    for (int r = o; r < e; r += RPI) {   // rows beyond the last are the last again
+        roped(min(r + lr, e - 1), x);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) amax = fmaxf(amax, finite_abs(x[i]));
+    }
+    const float scale = fmaxf(pow2(scale_exp(wave_max(amax))), old_scale), inv = 1.0f / scale, ratio = old_scale * inv;
+    if (o > 0 && ratio < 1.0f) {
+        for (int i = lane; i < page_bytes / 4; i += 64) ((unsigned *)cell0)[i] = rescaled(((unsigned *)cell0)[i], ratio);
+        __threadfence();   // before other lanes' new codes go to the same words
+    }
+    for (int r0 = o; r0 < e; r0 += RPI) {
+        const int r = r0 + lr;
+        roped(min(r, e - 1), x);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i] *= inv;
+        if (r < e)
+            *(u32x2 *)(cell0 + ((r >> 4) * (D / 16) + (c >> 4)) * 256 + (r & 15) * 16 + (c & 15)) =
+                u32x2{f8_of(x[0], x[1], x[2], x[3]), f8_of(x[4], x[5], x[6], x[7])};
+    }
+    if (lane == 0) *scale_out = scale;
+}
+
 // A workgroup looks at `chunk` rows of one head of K or V and writes the runs that begin there, a wavefront for every 16 tokens of
 // a page, whose rows stay in registers between the run's maximum and the codes.  Bound by memory: every row is read once and every
 // code written once, in whole lines: K by rows, whose halves of a cell's 16 bytes neighbouring lanes exchange; V two coordinates of
 // every row per lane, whose codes over the rows are the lane's 32 consecutive bytes of the page (d = 64: twice 8), exchanged within
 // the lane.  (A wavefront per page and tensor with 64 registers of data, K in pieces of 64 bytes, V of 16: 76 us where this takes
 // 43 for 34612 tokens x 8 heads; a third of the wavefronts were resident, and they read and wrote in turn.)
-template <bool BF16, int D, int PSHIFT>
+// ROPE: keys are normed and rotated in 32 bits between the load and the maximum; rows outside of every sequence are passed over.
+struct NoRope {};
+template <bool BF16, int D, int PSHIFT, bool ROPE>
 __global__ __launch_bounds__(4 << PSHIFT) void write_kernel(View Kn, View Vn, const int32_t *__restrict__ slot, int n_tok, int chunk,
-                                                            fastar_pages pg) {
+                                                            fastar_pages pg, std::conditional_t<ROPE, RopeArgs, NoRope> rope) {
     constexpr int P = 1 << PSHIFT, ELT = BF16 ? 2 : 4, NW = P / 16;
     __shared__ unsigned s_top[2][NW];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -377,7 +408,18 @@ __global__ __launch_bounds__(4 << PSHIFT) void write_kernel(View Kn, View Vn, co
     float *scales = is_v ? pg.vscale : pg.kscale;
     const unsigned n_slots = (unsigned)pg.n_pages << PSHIFT, pitch = (unsigned)x.row;
     // rows first - 1 .. first + 127: which are valid, and which go on where the row before them ended
-    auto at = [&](int t) { return t >= 0 && t < n_tok ? slot[t] : -1; };
+    int t_lo = 0, t_hi = n_tok;
+    if constexpr (ROPE)
+        if (rope.cu) t_lo = max(rope.cu[0], 0), t_hi = min(rope.cu[rope.B], n_tok);
+    auto at = [&](int t) { return t >= t_lo && t < t_hi ? slot[t] : -1; };
+    RopeLane rl;
+    float kw[8];
+    if constexpr (ROPE)
+        if (!is_v) {
+            rl = rope_lane<D>(rope);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) kw[i] = rope.norm && rope.kw ? rope.kw[lane % (D / 8) * 8 + i] : 1.0f;
+        }
     const int s0 = at(first + lane), s1 = at(first + 64 + lane);
     const int s_before = at(first - 1);
     const bool ok0 = (unsigned)s0 < n_slots, ok1 = (unsigned)s1 < n_slots;
@@ -407,18 +449,53 @@ __global__ __launch_bounds__(4 << PSHIFT) void write_kernel(View Kn, View Vn, co
         constexpr int LPR = D / 8, RPI = 64 / LPR, IT = 16 / RPI, VL = D / 2, VR = 16 * VL / 64;
         const int lr = lane / LPR, lc = lane % LPR, vc = lane % VL, vg = lane / VL;
         Piece<BF16, 8> k[IT];
+        Piece<false, 8> kr[ROPE ? IT : 1];   // normed and rotated
         Piece<BF16, 2> v[VR];
         u32x2 old[4];   // of V: what is there of a block that the run covers in part
         u32x2 *vp = (u32x2 *)(blk + vc * 32 + vg * VR);   // a coordinate's VR bytes; the next one's are 16 bytes on
         auto vword = [&](int i) -> u32x2 & { return D == 128 ? vp[i] : vp[2 * i]; };   // 8 bytes: D = 128: two per coordinate
         constexpr int VW = VR / 4;   // such words: 4 or 2
         unsigned top = 0;
+        int b = 0;
+        if constexpr (ROPE)
+            if (!is_v && rope.rot > 0 && !rope.pos) b = sequence_of(rope.cu, rope.B, t0);
+        auto roped = [&](int t, float (&x)[8]) __attribute__((always_inline)) {   // of row t, whose coordinates x holds
+          if constexpr (ROPE) {
+            double pos[4] = {0.0, 0.0, 0.0, 0.0};
+            if (rope.rot > 0) {
+                if (rope.pos) {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) pos[i] = rope.pos[(size_t)rl.axis[i] * n_tok + t];
+                } else {
+                    int bt = b;   // the run's first row's; others can only be later ones'
+                    while (bt < rope.B - 1 && rope.cu[bt + 1] <= t) ++bt;
+                    const double p = (double)((long long)rope.len[bt] - min(rope.cu[bt + 1], n_tok) + t);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) pos[i] = p;
+                }
+            }
+            norm_and_turn<D>(rope, rl, turn_of(rl, pos), kw, x);
+          }
+        };
         if (touches) {
             if (!is_v) {
 #pragma unroll
                 for (int i = 0; i < IT; ++i) k[i].load(row_of(i * RPI + lr) + lc * 8 * ELT);
+                if constexpr (ROPE) {
 #pragma unroll
-                for (int i = 0; i < IT; ++i) top = k[i].top(top);
+                    for (int i = 0; i < IT; ++i) {
+                        float x[8];
+#pragma unroll
+                        for (int j = 0; j < 8; ++j) x[j] = k[i][j];
+                        roped(t0 + min(max(r0 + i * RPI + lr, o), e - 1) - o, x);
+#pragma unroll
+                        for (int j = 0; j < 8; ++j) kr[i].w[j] = __float_as_uint(x[j]);
+                        top = kr[i].top(top);
+                    }
+                } else {
+#pragma unroll
+                    for (int i = 0; i < IT; ++i) top = k[i].top(top);
+                }
             } else {
 #pragma unroll
                 for (int i = 0; i < VR; ++i) v[i].load(row_of(vg * VR + i) + vc * 2 * ELT);
@@ -430,7 +507,8 @@ __global__ __launch_bounds__(4 << PSHIFT) void write_kernel(View Kn, View Vn, co
                 for (int i = 0; i < VR; ++i) top = v[i].top(top);
             }
         }
-        if constexpr (BF16) top = max(top & 0xFFFFu, top >> 16) << 16;
+        if constexpr (BF16)
+            if (!ROPE || is_v) top = max(top & 0xFFFFu, top >> 16) << 16;
         top = (unsigned)__builtin_amdgcn_readlane((int)wave_max_last(top), 63);
         if constexpr (NW > 1) {
             if (lane == 0) s_top[turn][wave] = top;
@@ -439,7 +517,16 @@ __global__ __launch_bounds__(4 << PSHIFT) void write_kernel(View Kn, View Vn, co
             for (int i = 0; i < NW; ++i) top = max(top, s_top[turn][i]);
         }
         if (top >= 0x7F800000u) {   // some number is not finite
-            if (wave == 0) write_odd_run<BF16, D>(row0, x.row, o, e, is_v, page0, D * P, old_scale, scales + ph);
+            if (wave != 0) continue;
+            if constexpr (ROPE)
+                if (!is_v) {
+                    write_odd_roped_run<D>([&](int r, float (&y)[8]) __attribute__((always_inline)) {
+                        load8<BF16>(row0 + r * x.row + lc * 8 * ELT, y);
+                        roped(t0 + r - o, y);
+                    }, o, e, page0, D * P, old_scale, scales + ph);
+                    continue;
+                }
+            write_odd_run<BF16, D>(row0, x.row, o, e, is_v, page0, D * P, old_scale, scales + ph);
             continue;
         }
         const float scale = fmaxf(pow2(scale_exp(__uint_as_float(top))), old_scale), ratio = old_scale / scale;
@@ -451,10 +538,14 @@ __global__ __launch_bounds__(4 << PSHIFT) void write_kernel(View Kn, View Vn, co
 #pragma unroll
             for (int i = 0; i < IT; ++i) {
                 unsigned w0 = 0, w1 = 0;
-                k[i].template codes<false>(0, scale, w0);
-                k[i].template codes<true>(2, scale, w0);
-                k[i].template codes<false>(4, scale, w1);
-                k[i].template codes<true>(6, scale, w1);
+                auto codes_of = [&](const auto &x) __attribute__((always_inline)) {
+                    x.template codes<false>(0, scale, w0);
+                    x.template codes<true>(2, scale, w0);
+                    x.template codes<false>(4, scale, w1);
+                    x.template codes<true>(6, scale, w1);
+                };
+                if constexpr (ROPE) codes_of(kr[i]);
+                else codes_of(k[i]);
                 c[i] = u32x2{w0, w1};
             }
 #pragma unroll
@@ -573,14 +664,11 @@ int pages_check(const fastar_pages *pg) {
 }
 }  // namespace fastar
 
-extern "C" int kv_pages_write(const fastar_pages *pages, const fastar_rows *K_new, const fastar_rows *V_new, int dtype,
-                              const int32_t *slot, int n_tok, void *stream) {
-    using namespace fastar;
-    if (dtype != FASTAR_F32 && dtype != FASTAR_BF16) return FASTAR_ERR_INVALID_ARG;
+namespace fastar {
+// kv_pages_write, or with a rotation (rope) of the keys and of Hq heads of queries.
+static int pages_write(const fastar_pages *pages, const fastar_rows *K_new, const fastar_rows *V_new, int dtype, const int32_t *slot,
+                       int n_tok, const RopeArgs *rope, const fastar_rows *Q, int Hq, const fastar_rows *Qo, hipStream_t s) {
     const int elt = dtype == FASTAR_BF16 ? 2 : 4;
-    if (n_tok < 0) return FASTAR_ERR_INVALID_ARG;
-    if (const int rc = pages_check(pages); rc != FASTAR_OK) return rc;
-    if (n_tok == 0) return FASTAR_OK;
     if (!slot || !view_ok(K_new, pages->Hkv, n_tok, elt) || !view_ok(V_new, pages->Hkv, n_tok, elt)) return FASTAR_ERR_INVALID_ARG;
     const View k = view_of(K_new, pages->Hkv, n_tok, elt), v = view_of(V_new, pages->Hkv, n_tok, elt);
     if (k.row > MAX_PITCH || v.row > MAX_PITCH) return FASTAR_ERR_UNSUPPORTED;
@@ -591,9 +679,14 @@ extern "C" int kv_pages_write(const fastar_pages *pages, const fastar_rows *K_ne
     while (chunk > 1 && (int64_t)n_tok * pages->Hkv * 2 / chunk < 4096) chunk /= 2;
     const int64_t units = (int64_t)((n_tok + chunk - 1) / chunk) * pages->Hkv * 2;
     if (!launch_ok(units, 4 * pages->P)) return FASTAR_ERR_UNSUPPORTED;
+    if (Hq > 0)
+        if (const int rc = rope_launch(Q, nullptr, *rope, Hq, 0, pages->d, dtype, Qo, nullptr, s); rc != FASTAR_OK) return rc;
     const dim3 grid((unsigned)units);
-#define FASTAR_WRITE(BF16, D, PSHIFT) \
-    hipLaunchKernelGGL((pages::write_kernel<BF16, D, PSHIFT>), grid, dim3(4 << PSHIFT), 0, (hipStream_t)stream, k, v, slot, n_tok, chunk, *pages)
+#define FASTAR_WRITE(BF16, D, PSHIFT)                                                                                                \
+    do {                                                                                                                             \
+        if (rope) hipLaunchKernelGGL((pages::write_kernel<BF16, D, PSHIFT, true>), grid, dim3(4 << PSHIFT), 0, s, k, v, slot, n_tok, chunk, *pages, *rope); \
+        else hipLaunchKernelGGL((pages::write_kernel<BF16, D, PSHIFT, false>), grid, dim3(4 << PSHIFT), 0, s, k, v, slot, n_tok, chunk, *pages, pages::NoRope{}); \
+    } while (0)
 #define FASTAR_WRITE_P(BF16, D)                      \
     do {                                             \
         if (pages->P == 64) FASTAR_WRITE(BF16, D, 6); \
@@ -611,4 +704,28 @@ extern "C" int kv_pages_write(const fastar_pages *pages, const fastar_rows *K_ne
 #undef FASTAR_WRITE
     FASTAR_LAUNCH_CHECK();
     return FASTAR_OK;
+}
+}  // namespace fastar
+
+extern "C" int kv_pages_write(const fastar_pages *pages, const fastar_rows *K_new, const fastar_rows *V_new, int dtype,
+                              const int32_t *slot, int n_tok, void *stream) {
+    using namespace fastar;
+    if (dtype != FASTAR_F32 && dtype != FASTAR_BF16) return FASTAR_ERR_INVALID_ARG;
+    if (n_tok < 0) return FASTAR_ERR_INVALID_ARG;
+    if (const int rc = pages_check(pages); rc != FASTAR_OK) return rc;
+    if (n_tok == 0) return FASTAR_OK;
+    return pages_write(pages, K_new, V_new, dtype, slot, n_tok, nullptr, nullptr, 0, nullptr, (hipStream_t)stream);
+}
+
+extern "C" int kv_pages_write_rope(const fastar_pages *pages, const fastar_rows *Q, const fastar_rows *K_new, const fastar_rows *V_new,
+                                   int dtype, const int32_t *slot, const int32_t *pos, const int32_t *cu, const int32_t *len, int B, int n_tok,
+                                   int Hq, const fastar_rope *rope, const fastar_rows *Qo, void *stream) {
+    using namespace fastar;
+    if (dtype != FASTAR_F32 && dtype != FASTAR_BF16) return FASTAR_ERR_INVALID_ARG;
+    if (Hq < 0) return FASTAR_ERR_INVALID_ARG;
+    if (const int rc = pages_check(pages); rc != FASTAR_OK) return rc;
+    if (const int rc = rope_check(rope, pos, cu, len, B, n_tok, pages->d); rc != FASTAR_OK) return rc;
+    if (n_tok == 0 || (cu && B == 0)) return FASTAR_OK;
+    const RopeArgs r = rope_args(rope, pos, cu, len, B, n_tok);
+    return pages_write(pages, K_new, V_new, dtype, slot, n_tok, &r, Q, Hq, Qo, (hipStream_t)stream);
 }
