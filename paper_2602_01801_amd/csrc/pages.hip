@@ -1,6 +1,6 @@
 // The paged 8-bit cache: block tables and slot maps from the requests' lengths (kv_pages_plan), and new keys and values into
-// its pages (kv_pages_write), the keys normed and rotated on the way (kv_pages_write_rope).
-#include "rope_dev.hpp"
+// its pages (kv_pages_write).
+#include "pages_dev.hpp"
 
 namespace fastar {
 
@@ -256,353 +256,29 @@ __global__ __launch_bounds__(256) void slots_kernel(const int32_t *__restrict__ 
 
 // ---- writing ----------------------------------------------------------------------------------------------------
 
-constexpr float F8_MAX = 448.0f;
-
-__device__ __forceinline__ float f8_in_range(float x) { return x != x ? x : fminf(fmaxf(x, -F8_MAX), F8_MAX); }
-__device__ __forceinline__ unsigned f8_of(float a, float b, float c, float d) {
-    int w = 0;
-    w = __builtin_amdgcn_cvt_pk_fp8_f32(f8_in_range(a), f8_in_range(b), w, false);
-    w = __builtin_amdgcn_cvt_pk_fp8_f32(f8_in_range(c), f8_in_range(d), w, true);
-    return (unsigned)w;
-}
-__device__ __forceinline__ float finite_abs(float x) {
-    x = fabsf(x);
-    return x < INFINITY ? x : 0.0f;
-}
-// Exponent of the least power of two, 2^-100 at least, whose 448-fold is not below amax.
-__device__ __forceinline__ int scale_exp(float amax) {
-    int e;
-    const float m = frexpf(amax, &e);   // 448 = 0.875 * 2^9
-    return max(-100, amax == 0.0f ? -100 : m <= 0.875f ? e - 9 : e - 8);
-}
-__device__ __forceinline__ float pow2(int e) { return __uint_as_float((unsigned)(e + 127) << 23); }
-
-typedef __attribute__((ext_vector_type(2))) unsigned short u16x2;
-typedef __attribute__((ext_vector_type(2))) short s16x2;
-
-// EPL consecutive elements of a row as they lie in memory.
-template <bool BF16, int EPL>
-struct Piece {
-    static constexpr int W = EPL * (BF16 ? 2 : 4) / 4;
-    unsigned w[W];
-    __device__ __forceinline__ void load(const char *p) {
-        if constexpr (W == 1) {
-            w[0] = *(const unsigned *)p;
-        } else if constexpr (W == 2) {
-            const u32x2 x = *(const u32x2 *)p;
-            w[0] = x[0], w[1] = x[1];
-        } else {
-#pragma unroll
-            for (int q = 0; q < W / 4; ++q) {
-                const u32x4 x = ((const u32x4 *)p)[q];
-#pragma unroll
-                for (int e = 0; e < 4; ++e) w[4 * q + e] = x[e];
-            }
-        }
-    }
-    __device__ __forceinline__ float operator[](int i) const {
-        if constexpr (BF16) return i & 1 ? bf16_hi(w[i / 2]) : bf16_lo(w[i / 2]);
-        else return __uint_as_float(w[i]);
-    }
-    // Largest |x| by its bits, with what `top` holds (two 16-bit maxima for bf16): numbers that are not finite come out on top.
-    __device__ __forceinline__ unsigned top(unsigned top) const {
-#pragma unroll
-        for (int i = 0; i < W; ++i) {
-            if constexpr (BF16) top = __builtin_bit_cast(unsigned, __builtin_elementwise_max(__builtin_bit_cast(u16x2, top), __builtin_bit_cast(u16x2, w[i] & 0x7FFF7FFFu)));
-            else top = max(top, w[i] & 0x7FFFFFFFu);
-        }
-        return top;
-    }
-    // Codes of elements i, i + 1, in the lower or the upper half of r: the conversion instructions divide by a power of two and round
-    // to nearest, ties to even (what goes beyond 464 becomes no number; here nothing goes beyond 448).
-    template <bool UPPER>
-    __device__ __forceinline__ void codes(int i, float scale, unsigned &r) const {
-        const s16x2 old = __builtin_bit_cast(s16x2, r);
-        if constexpr (BF16) r = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(old, __builtin_bit_cast(bf16x2, w[i / 2]), scale, UPPER));
-        else r = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(old, (*this)[i], (*this)[i + 1], scale, UPPER));
-    }
-};
-// Codes carried over to a scale 1 / ratio times as large.
-__device__ __forceinline__ unsigned rescaled(unsigned w, float ratio) {
-    return f8_of(__builtin_amdgcn_cvt_f32_fp8((int)w, 0) * ratio, __builtin_amdgcn_cvt_f32_fp8((int)w, 1) * ratio,
-                 __builtin_amdgcn_cvt_f32_fp8((int)w, 2) * ratio, __builtin_amdgcn_cvt_f32_fp8((int)w, 3) * ratio);
-}
-__device__ __forceinline__ float wave_max(float x) {   // of numbers that are not negative
-    return __uint_as_float((unsigned)__builtin_amdgcn_readlane((int)wave_max_last(__float_as_uint(x)), 63));
-}
-// Rows o .. e - 1 of a page where some number is not finite, one after the other.
-template <bool BF16, int D>
-__device__ __forceinline__ void write_odd_run(const char *row0, int64_t pitch, int o, int e, bool is_v, uint8_t *cell0, int page_bytes,
-                                              float old_scale, float *scale_out) {
-    const int lane = threadIdx.x & 63;
-    auto at = [&](int r, int c) {
-        const char *p = row0 + r * pitch;
-        if constexpr (BF16) return bf16_bits_to_f32(((const unsigned short *)p)[c]);
-        else return ((const float *)p)[c];
-    };
-    float amax = 0.0f;
-    for (int r = o; r < e; ++r)
-        for (int c = lane; c < D; c += 64) amax = fmaxf(amax, finite_abs(at(r, c)));
-    const float scale = fmaxf(pow2(scale_exp(wave_max(amax))), old_scale), inv = 1.0f / scale, ratio = old_scale * inv;
-    if (o > 0 && ratio < 1.0f) {
-        for (int i = lane; i < page_bytes / 4; i += 64) ((unsigned *)cell0)[i] = rescaled(((unsigned *)cell0)[i], ratio);
-        __threadfence();   // before other lanes' new codes go to the same words
-    }
-    for (int r = o; r < e; ++r)
-        for (int c = lane; c < D; c += 64) {
-            const float x = at(r, c) * inv;
-            cell0[((r >> 4) * (D / 16) + (c >> 4)) * 256 + (is_v ? (c & 15) * 16 + (r & 15) : (r & 15) * 16 + (c & 15))] = (uint8_t)f8_of(x, x, x, x);
-        }
-    if (lane == 0) *scale_out = scale;
-}
-
-// The same of keys that are normed and rotated: roped(r, x) gives a lane's eight coordinates of row o + r * RPI + its own.
-template <int D, class Roped>
-__device__ __forceinline__ void write_odd_roped_run(Roped roped, int o, int e, uint8_t *cell0, int page_bytes, float old_scale,
-                                                    float *scale_out) {
-    constexpr int LPR = D / 8, RPI = 64 / LPR;
-    const int lane = threadIdx.x & 63, lr = lane / LPR, c = lane % LPR * 8;
-    float amax = 0.0f, x[8];
-    for (int r = o; r < e; r += RPI) {   // rows beyond the last are the last again
-        roped(min(r + lr, e - 1), x);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) amax = fmaxf(amax, finite_abs(x[i]));
-    }
-    const float scale = fmaxf(pow2(scale_exp(wave_max(amax))), old_scale), inv = 1.0f / scale, ratio = old_scale * inv;
-    if (o > 0 && ratio < 1.0f) {
-        for (int i = lane; i < page_bytes / 4; i += 64) ((unsigned *)cell0)[i] = rescaled(((unsigned *)cell0)[i], ratio);
-        __threadfence();   // before other lanes' new codes go to the same words
-    }
-    for (int r0 = o; r0 < e; r0 += RPI) {
-        const int r = r0 + lr;
-        roped(min(r, e - 1), x);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) x[i] *= inv;
-        if (r < e)
-            *(u32x2 *)(cell0 + ((r >> 4) * (D / 16) + (c >> 4)) * 256 + (r & 15) * 16 + (c & 15)) =
-                u32x2{f8_of(x[0], x[1], x[2], x[3]), f8_of(x[4], x[5], x[6], x[7])};
-    }
-    if (lane == 0) *scale_out = scale;
-}
-
 // A workgroup looks at `chunk` rows of one head of K or V and writes the runs that begin there, a wavefront for every 16 tokens of
 // a page, whose rows stay in registers between the run's maximum and the codes.  Bound by memory: every row is read once and every
 // code written once, in whole lines: K by rows, whose halves of a cell's 16 bytes neighbouring lanes exchange; V two coordinates of
 // every row per lane, whose codes over the rows are the lane's 32 consecutive bytes of the page (d = 64: twice 8), exchanged within
 // the lane.  (A wavefront per page and tensor with 64 registers of data, K in pieces of 64 bytes, V of 16: 76 us where this takes
 // 43 for 34612 tokens x 8 heads; a third of the wavefronts were resident, and they read and wrote in turn.)
-// ROPE: keys are normed and rotated in 32 bits between the load and the maximum; rows outside of every sequence are passed over.
-struct NoRope {};
-template <bool BF16, int D, int PSHIFT, bool ROPE>
+template <bool BF16, int D, int PSHIFT>
 __global__ __launch_bounds__(4 << PSHIFT) void write_kernel(View Kn, View Vn, const int32_t *__restrict__ slot, int n_tok, int chunk,
-                                                            fastar_pages pg, std::conditional_t<ROPE, RopeArgs, NoRope> rope) {
-    constexpr int P = 1 << PSHIFT, ELT = BF16 ? 2 : 4, NW = P / 16;
+                                                            fastar_pages pg) {
+    constexpr int P = 1 << PSHIFT, NW = P / 16;
     __shared__ unsigned s_top[2][NW];
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int h = blockIdx.x % pg.Hkv, rest = blockIdx.x / pg.Hkv;
     const bool is_v = rest & 1;
-    const int first = (rest >> 1) * chunk;
     const View x = is_v ? Vn : Kn;
-    const char *xh = x.p + h * x.head;
     uint8_t *codes = is_v ? pg.V8 : pg.K8;
     float *scales = is_v ? pg.vscale : pg.kscale;
-    const unsigned n_slots = (unsigned)pg.n_pages << PSHIFT, pitch = (unsigned)x.row;
-    // rows first - 1 .. first + 127: which are valid, and which go on where the row before them ended
-    int t_lo = 0, t_hi = n_tok;
-    if constexpr (ROPE)
-        if (rope.cu) t_lo = max(rope.cu[0], 0), t_hi = min(rope.cu[rope.B], n_tok);
-    auto at = [&](int t) { return t >= t_lo && t < t_hi ? slot[t] : -1; };
-    RopeLane rl;
-    float kw[8];
-    if constexpr (ROPE)
-        if (!is_v) {
-            rl = rope_lane<D>(rope);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) kw[i] = rope.norm && rope.kw ? rope.kw[lane % (D / 8) * 8 + i] : 1.0f;
-        }
-    const int s0 = at(first + lane), s1 = at(first + 64 + lane);
-    const int s_before = at(first - 1);
-    const bool ok0 = (unsigned)s0 < n_slots, ok1 = (unsigned)s1 < n_slots;
-    int p0 = __shfl_up(s0, 1, 64), p1 = __shfl_up(s1, 1, 64);   // all lanes together: a lane that is not there gives nothing
-    if (lane == 0) {
-        p0 = s_before;
-        p1 = __builtin_amdgcn_readlane(s0, 63);
-    }
-    const unsigned long long valid = __ballot(ok0);
-    const unsigned long long go0 = __ballot(ok0 && (s0 & (P - 1)) && p0 == s0 - 1), go1 = __ballot(ok1 && (s1 & (P - 1)) && p1 == s1 - 1);
-    unsigned long long begin = valid & ~go0;
-    if (chunk < 64) begin &= (1ull << chunk) - 1ull;
-    for (int turn = 0; begin; begin &= begin - 1ull, turn ^= 1) {   // uniform over the workgroup
-        const int pos = __builtin_ctzll(begin);
-        const unsigned long long after = pos == 63 ? go1 : (go0 >> (pos + 1)) | (go1 << (63 - pos));   // bit i: row pos + 1 + i goes on
-        const int n = 1 + (~after ? __builtin_ctzll(~after) : 63);   // at most P: a run ends with its page
-        const int t0 = first + pos, sl = __builtin_amdgcn_readlane(s0, pos);
-        const int page = sl >> PSHIFT, o = sl & (P - 1), e = o + n;
-        const size_t ph = (size_t)page * pg.Hkv + h;
-        uint8_t *page0 = codes + ph * (size_t)(D * P), *blk = page0 + wave * (16 * D);
-        const float old_scale = o > 0 ? scales[ph] : 0.0f;
-        const char *row0 = xh + (int64_t)(t0 - o) * x.row;   // of offset 0
-        const int r0 = 16 * wave;
-        const bool touches = r0 < e && r0 + 16 > o, all = r0 >= o && r0 + 16 <= e;   // rows of the run among the wavefront's 16
-        auto row_of = [&](int r) { return row0 + (unsigned)min(max(r0 + r, o), e - 1) * pitch; };   // rows beside the run: one of its own again
-        // K: row i RPI + lr, coordinates 8 lc .. ; V: rows VR g .., coordinates 2 c
-        constexpr int LPR = D / 8, RPI = 64 / LPR, IT = 16 / RPI, VL = D / 2, VR = 16 * VL / 64;
-        const int lr = lane / LPR, lc = lane % LPR, vc = lane % VL, vg = lane / VL;
-        Piece<BF16, 8> k[IT];
-        Piece<false, 8> kr[ROPE ? IT : 1];   // normed and rotated
-        Piece<BF16, 2> v[VR];
-        u32x2 old[4];   // of V: what is there of a block that the run covers in part
-        u32x2 *vp = (u32x2 *)(blk + vc * 32 + vg * VR);   // a coordinate's VR bytes; the next one's are 16 bytes on
-        auto vword = [&](int i) -> u32x2 & { return D == 128 ? vp[i] : vp[2 * i]; };   // 8 bytes: D = 128: two per coordinate
-        constexpr int VW = VR / 4;   // such words: 4 or 2
-        unsigned top = 0;
-        int b = 0;
-        if constexpr (ROPE)
-            if (!is_v && rope.rot > 0 && !rope.pos) b = sequence_of(rope.cu, rope.B, t0);
-        auto roped = [&](int t, float (&x)[8]) __attribute__((always_inline)) {   // of row t, whose coordinates x holds
-          if constexpr (ROPE) {
-            double pos[4] = {0.0, 0.0, 0.0, 0.0};
-            if (rope.rot > 0) {
-                if (rope.pos) {
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) pos[i] = rope.pos[(size_t)rl.axis[i] * n_tok + t];
-                } else {
-                    int bt = b;   // the run's first row's; others can only be later ones'
-                    while (bt < rope.B - 1 && rope.cu[bt + 1] <= t) ++bt;
-                    const double p = (double)((long long)rope.len[bt] - min(rope.cu[bt + 1], n_tok) + t);
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) pos[i] = p;
-                }
-            }
-            norm_and_turn<D>(rope, rl, turn_of(rl, pos), kw, x);
-          }
-        };
-        if (touches) {
-            if (!is_v) {
-#pragma unroll
-                for (int i = 0; i < IT; ++i) k[i].load(row_of(i * RPI + lr) + lc * 8 * ELT);
-                if constexpr (ROPE) {
-#pragma unroll
-                    for (int i = 0; i < IT; ++i) {
-                        float x[8];
-#pragma unroll
-                        for (int j = 0; j < 8; ++j) x[j] = k[i][j];
-                        roped(t0 + min(max(r0 + i * RPI + lr, o), e - 1) - o, x);
-#pragma unroll
-                        for (int j = 0; j < 8; ++j) kr[i].w[j] = __float_as_uint(x[j]);
-                        top = kr[i].top(top);
-                    }
-                } else {
-#pragma unroll
-                    for (int i = 0; i < IT; ++i) top = k[i].top(top);
-                }
-            } else {
-#pragma unroll
-                for (int i = 0; i < VR; ++i) v[i].load(row_of(vg * VR + i) + vc * 2 * ELT);
-                if (!all) {
-#pragma unroll
-                    for (int i = 0; i < VW; ++i) old[i] = vword(i);
-                }
-#pragma unroll
-                for (int i = 0; i < VR; ++i) top = v[i].top(top);
-            }
-        }
-        if constexpr (BF16)
-            if (!ROPE || is_v) top = max(top & 0xFFFFu, top >> 16) << 16;
-        top = (unsigned)__builtin_amdgcn_readlane((int)wave_max_last(top), 63);
-        if constexpr (NW > 1) {
-            if (lane == 0) s_top[turn][wave] = top;
-            __syncthreads();   // the other half of s_top is free by the next one
-#pragma unroll
-            for (int i = 0; i < NW; ++i) top = max(top, s_top[turn][i]);
-        }
-        if (top >= 0x7F800000u) {   // some number is not finite
-            if (wave != 0) continue;
-            if constexpr (ROPE)
-                if (!is_v) {
-                    write_odd_roped_run<D>([&](int r, float (&y)[8]) __attribute__((always_inline)) {
-                        load8<BF16>(row0 + r * x.row + lc * 8 * ELT, y);
-                        roped(t0 + r - o, y);
-                    }, o, e, page0, D * P, old_scale, scales + ph);
-                    continue;
-                }
-            write_odd_run<BF16, D>(row0, x.row, o, e, is_v, page0, D * P, old_scale, scales + ph);
-            continue;
-        }
-        const float scale = fmaxf(pow2(scale_exp(__uint_as_float(top))), old_scale), ratio = old_scale / scale;
-        const bool grows = o > 0 && ratio < 1.0f;
-        if (lane == 0 && wave == 0) scales[ph] = scale;
-        if (!touches && !grows) continue;
-        if (!is_v) {
-            u32x2 c[IT];
-#pragma unroll
-            for (int i = 0; i < IT; ++i) {
-                unsigned w0 = 0, w1 = 0;
-                auto codes_of = [&](const auto &x) __attribute__((always_inline)) {
-                    x.template codes<false>(0, scale, w0);
-                    x.template codes<true>(2, scale, w0);
-                    x.template codes<false>(4, scale, w1);
-                    x.template codes<true>(6, scale, w1);
-                };
-                if constexpr (ROPE) codes_of(kr[i]);
-                else codes_of(k[i]);
-                c[i] = u32x2{w0, w1};
-            }
-#pragma unroll
-            for (int i = 0; i < IT; i += 2) {   // even lanes take row i of the pair's cell, odd ones row i + 1
-                const bool odd = lane & 1;
-                const u32x2 give = odd ? c[i] : c[i + 1], keep = odd ? c[i + 1] : c[i];
-                const u32x2 got = {lane_of_eight<0>(give[0]), lane_of_eight<0>(give[1])};
-                const int r = (i + (odd ? 1 : 0)) * RPI + lr;
-                u32x4 y = odd ? u32x4{got[0], got[1], keep[0], keep[1]} : u32x4{keep[0], keep[1], got[0], got[1]};
-                u32x4 *p = (u32x4 *)(blk + (lc >> 1) * 256 + r * 16);
-                const bool mine = r0 + r >= o && r0 + r < e;
-                if (!mine && grows) {
-                    y = *p;
-#pragma unroll
-                    for (int q = 0; q < 4; ++q) y[q] = rescaled(y[q], ratio);
-                }
-                if (mine || grows) *p = y;
-            }
-        } else {
-            unsigned c[VR / 2];   // of rows 2 i, 2 i + 1: codes of the two coordinates
-#pragma unroll
-            for (int i = 0; i < VR / 2; ++i) {
-                c[i] = 0;
-                v[2 * i].template codes<false>(0, scale, c[i]);
-                v[2 * i + 1].template codes<true>(0, scale, c[i]);
-            }
-            u32x2 y[VW];   // coordinate by coordinate, four rows a word
-#pragma unroll
-            for (int co = 0; co < 2; ++co)
-#pragma unroll
-                for (int q = 0; q < VR / 4; ++q)
-                    y[(co * (VR / 4) + q) / 2][(co * (VR / 4) + q) % 2] = __builtin_amdgcn_perm(c[2 * q + 1], c[2 * q], co ? 0x07050301u : 0x06040200u);
-            if (!all) {
-#pragma unroll
-                for (int i = 0; i < VW; ++i) {
-                    u32x2 w = touches ? old[i] : vword(i);
-#pragma unroll
-                    for (int j = 0; j < 2; ++j) {
-                        if (grows) w[j] = rescaled(w[j], ratio);
-                        const int row = r0 + vg * VR + ((2 * i + j) % (VR / 4)) * 4;   // of the word's first byte
-                        unsigned mask = 0;
-#pragma unroll
-                        for (int b = 0; b < 4; ++b) mask |= row + b >= o && row + b < e ? 0xFFu << (8 * b) : 0u;
-                        w[j] = touches ? (y[i][j] & mask) | (w[j] & ~mask) : w[j];
-                    }
-                    y[i] = w;
-                }
-            }
-            if constexpr (D == 128) {
-                ((u32x4 *)vp)[0] = u32x4{y[0][0], y[0][1], y[1][0], y[1][1]};
-                ((u32x4 *)vp)[1] = u32x4{y[2][0], y[2][1], y[3][0], y[3][1]};
-            } else {
-#pragma unroll
-                for (int i = 0; i < VW; ++i) vword(i) = y[i];
-            }
-        }
-    }
+    for_runs<PSHIFT>(slot, n_tok, (rest >> 1) * chunk, chunk, (unsigned)pg.n_pages << PSHIFT, 0, n_tok, [&](int t0, int sl, int n, int turn) __attribute__((always_inline)) {
+        const int o = sl & (P - 1);
+        const size_t ph = (size_t)(sl >> PSHIFT) * pg.Hkv + h;
+        const Run run{x.p + h * x.head + (int64_t)(t0 - o) * x.row, x.row, o, o + n, codes + ph * (size_t)(D * P), scales + ph, o > 0 ? scales[ph] : 0.0f};
+        if (is_v) v_run<BF16, D, PSHIFT>(run, s_top, turn);
+        else k_run<BF16, D, PSHIFT>(run, s_top, turn);
+    });
 }
 
 }  // namespace pages
@@ -664,29 +340,23 @@ int pages_check(const fastar_pages *pg) {
 }
 }  // namespace fastar
 
-namespace fastar {
-// kv_pages_write, or with a rotation (rope) of the keys and of Hq heads of queries.
-static int pages_write(const fastar_pages *pages, const fastar_rows *K_new, const fastar_rows *V_new, int dtype, const int32_t *slot,
-                       int n_tok, const RopeArgs *rope, const fastar_rows *Q, int Hq, const fastar_rows *Qo, hipStream_t s) {
+extern "C" int kv_pages_write(const fastar_pages *pages, const fastar_rows *K_new, const fastar_rows *V_new, int dtype,
+                              const int32_t *slot, int n_tok, void *stream) {
+    using namespace fastar;
+    if (dtype != FASTAR_F32 && dtype != FASTAR_BF16) return FASTAR_ERR_INVALID_ARG;
     const int elt = dtype == FASTAR_BF16 ? 2 : 4;
+    if (n_tok < 0) return FASTAR_ERR_INVALID_ARG;
+    if (const int rc = pages_check(pages); rc != FASTAR_OK) return rc;
+    if (n_tok == 0) return FASTAR_OK;
     if (!slot || !view_ok(K_new, pages->Hkv, n_tok, elt) || !view_ok(V_new, pages->Hkv, n_tok, elt)) return FASTAR_ERR_INVALID_ARG;
     const View k = view_of(K_new, pages->Hkv, n_tok, elt), v = view_of(V_new, pages->Hkv, n_tok, elt);
     if (k.row > MAX_PITCH || v.row > MAX_PITCH) return FASTAR_ERR_UNSUPPORTED;
-    // Rows per workgroup: a page's where that makes enough of them; fewer, down to one, so that the runs of single tokens are not
-    // done one after the other.  At least 1024 / 4096 / 16384 workgroups, pages of 64, 8 heads: 512 single tokens 17.5 / 19.4 / 21.7 us, 16 runs
-    // of 16 4.5 / 6.0 / 6.0, 8 of 200 6.3 / 9.2 / 18.6, 8 of 4680 38.6 / 37.4 / 52; 30000 tokens of one head 9.5 / 23 / 49: for runs fewer would do.
-    int chunk = pages->P;
-    while (chunk > 1 && (int64_t)n_tok * pages->Hkv * 2 / chunk < 4096) chunk /= 2;
+    const int chunk = pages::rows_per_workgroup(n_tok, pages->Hkv, pages->P);
     const int64_t units = (int64_t)((n_tok + chunk - 1) / chunk) * pages->Hkv * 2;
     if (!launch_ok(units, 4 * pages->P)) return FASTAR_ERR_UNSUPPORTED;
-    if (Hq > 0)
-        if (const int rc = rope_launch(Q, nullptr, *rope, Hq, 0, pages->d, dtype, Qo, nullptr, s); rc != FASTAR_OK) return rc;
     const dim3 grid((unsigned)units);
-#define FASTAR_WRITE(BF16, D, PSHIFT)                                                                                                \
-    do {                                                                                                                             \
-        if (rope) hipLaunchKernelGGL((pages::write_kernel<BF16, D, PSHIFT, true>), grid, dim3(4 << PSHIFT), 0, s, k, v, slot, n_tok, chunk, *pages, *rope); \
-        else hipLaunchKernelGGL((pages::write_kernel<BF16, D, PSHIFT, false>), grid, dim3(4 << PSHIFT), 0, s, k, v, slot, n_tok, chunk, *pages, pages::NoRope{}); \
-    } while (0)
+#define FASTAR_WRITE(BF16, D, PSHIFT) \
+    hipLaunchKernelGGL((pages::write_kernel<BF16, D, PSHIFT>), grid, dim3(4 << PSHIFT), 0, (hipStream_t)stream, k, v, slot, n_tok, chunk, *pages)
 #define FASTAR_WRITE_P(BF16, D)                      \
     do {                                             \
         if (pages->P == 64) FASTAR_WRITE(BF16, D, 6); \
@@ -704,28 +374,4 @@ static int pages_write(const fastar_pages *pages, const fastar_rows *K_new, cons
 #undef FASTAR_WRITE
     FASTAR_LAUNCH_CHECK();
     return FASTAR_OK;
-}
-}  // namespace fastar
-
-extern "C" int kv_pages_write(const fastar_pages *pages, const fastar_rows *K_new, const fastar_rows *V_new, int dtype,
-                              const int32_t *slot, int n_tok, void *stream) {
-    using namespace fastar;
-    if (dtype != FASTAR_F32 && dtype != FASTAR_BF16) return FASTAR_ERR_INVALID_ARG;
-    if (n_tok < 0) return FASTAR_ERR_INVALID_ARG;
-    if (const int rc = pages_check(pages); rc != FASTAR_OK) return rc;
-    if (n_tok == 0) return FASTAR_OK;
-    return pages_write(pages, K_new, V_new, dtype, slot, n_tok, nullptr, nullptr, 0, nullptr, (hipStream_t)stream);
-}
-
-extern "C" int kv_pages_write_rope(const fastar_pages *pages, const fastar_rows *Q, const fastar_rows *K_new, const fastar_rows *V_new,
-                                   int dtype, const int32_t *slot, const int32_t *pos, const int32_t *cu, const int32_t *len, int B, int n_tok,
-                                   int Hq, const fastar_rope *rope, const fastar_rows *Qo, void *stream) {
-    using namespace fastar;
-    if (dtype != FASTAR_F32 && dtype != FASTAR_BF16) return FASTAR_ERR_INVALID_ARG;
-    if (Hq < 0) return FASTAR_ERR_INVALID_ARG;
-    if (const int rc = pages_check(pages); rc != FASTAR_OK) return rc;
-    if (const int rc = rope_check(rope, pos, cu, len, B, n_tok, pages->d); rc != FASTAR_OK) return rc;
-    if (n_tok == 0 || (cu && B == 0)) return FASTAR_OK;
-    const RopeArgs r = rope_args(rope, pos, cu, len, B, n_tok);
-    return pages_write(pages, K_new, V_new, dtype, slot, n_tok, &r, Q, Hq, Qo, (hipStream_t)stream);
 }

@@ -1,8 +1,8 @@
 // Norm and rotation of a row: what qk_norm_rope and kv_pages_write_rope share, so that both compute the same numbers.
 //   y = x (mean x^2 + eps)^-1/2 w;   pair (a, b) of coordinates -> (a cos t - b sin t, a sin t + b cos t), t = pos * freq
-// A row is eight coordinates per lane (one 16-byte load in bf16), d / 8 neighbouring lanes.  Every lane of the rotated part
-// turns four pairs: interleaved ones lie in its own coordinates; where pairs are rot / 2 apart, the lanes of the lower and the
-// upper half swap four coordinates before and after, so that no angle is computed twice within a row.
+// A row is d / 8 neighbouring lanes with two pieces of four coordinates each, rot / 2 apart where pairs are, so that every lane has both
+// coordinates of its four pairs and none are exchanged.  (Eight neighbouring coordinates per lane, swapped with the lane of the other
+// half before and after, took 176 vector instructions per lane where this takes 75: 34612 tokens x 40 heads 134 us, of which 100 were these.)
 #pragma once
 
 #include "packed.hpp"
@@ -15,12 +15,11 @@ struct RopeArgs {
     const int32_t *axis, *pos, *cu, *len;
     const float *qw, *kw;
     float eps;
-    int32_t norm, rot, interleaved, n_axes, B, n_tok;
+    int32_t norm, rot, n_axes, B, n_tok;
 };
 int rope_check(const fastar_rope *r, const int32_t *pos, const int32_t *cu, const int32_t *len, int B, int n_tok, int d);
 RopeArgs rope_args(const fastar_rope *r, const int32_t *pos, const int32_t *cu, const int32_t *len, int B, int n_tok);
-int rope_launch(const fastar_rows *Q, const fastar_rows *K, const RopeArgs &r, int Hq, int Hkv, int d, int dtype, const fastar_rows *Qo,
-                const fastar_rows *Ko, hipStream_t s);
+int rope_parts(int n_tok, int Hq, int Hkv, int d);
 
 // Sum over the LPR (8 or 16) neighbouring lanes of a row; every lane has the same bits, as each step adds the same two numbers.
 template <int LPR>
@@ -32,10 +31,13 @@ __device__ __forceinline__ float row_sum(float v) {
     return v;
 }
 template <int LPR>
-__device__ __forceinline__ double row_sum(double v) {
-#pragma unroll
-    for (int o = 1; o < LPR; o *= 2) v += __shfl_xor(v, o, 64);
-    return v;
+__device__ __forceinline__ float row_max(float v) {   // of numbers that are not negative, by their bits: what is not finite comes out on top
+    unsigned u = __float_as_uint(v);
+    u = max(u, lane_of_eight<0>(u));
+    u = max(u, lane_of_eight<1>(u));
+    u = max(u, lane_of_eight<2>(u));
+    if constexpr (LPR == 16) u = max(u, (unsigned)__builtin_amdgcn_update_dpp(0, (int)u, 0x140, 0xF, 0xF, false));
+    return __uint_as_float(u);
 }
 
 // Sequence of row t, cu[0] <= t < cu[B]: the number of the offsets cu[1 ..] that are not beyond t.  A wavefront together, 64 offsets a round.
@@ -52,129 +54,278 @@ __device__ __forceinline__ int sequence_of(const int32_t *__restrict__ cu, int B
     }
     return lo;
 }
+// The sequences of a call, a lane each while there are no more than 64: their offsets and lengths are asked for at once, so that a wavefront
+// waits for one trip to memory instead of three.
+struct Places {
+    int begin, end, len;
+};
+// Whether a row t is a sequence's, how far ahead of t its position is where that goes by the sequence's length, and where the sequence ends.
+struct Place {
+    bool there;
+    int ahead, end;
+};
+// Differences and sums of lengths that are the caller's, whatever they are.
+__device__ __forceinline__ int less(int a, int b) { return (int)((unsigned)a - (unsigned)b); }
+__device__ __forceinline__ int plus(int a, int b) { return (int)((unsigned)a + (unsigned)b); }
+__device__ __forceinline__ Places places_of(const RopeArgs &r) {
+    if (!r.cu || r.B > 64) return Places{0, 0, 0};
+    const int b = min(lane_id(), r.B - 1);   // lanes beyond the sequences repeat the last one
+    return Places{r.cu[b], r.cu[b + 1], r.rot > 0 && !r.pos ? r.len[b] : 0};
+}
+__device__ __forceinline__ Place place_of(const RopeArgs &r, const Places &p, int t) {
+    if (!r.cu) return Place{true, 0, r.n_tok};
+    if (r.B > 64) {
+        if (t < r.cu[0] || t >= r.cu[r.B]) return Place{false, 0, 0};
+        if (r.rot == 0 || r.pos) return Place{true, 0, r.n_tok};
+        const int b = sequence_of(r.cu, r.B, t), end = min(r.cu[b + 1], r.n_tok);
+        return Place{true, less(r.len[b], end), end};
+    }
+    const unsigned long long here = __ballot(p.begin <= t && t < p.end);
+    if (!here) return Place{false, 0, 0};
+    const int l = __builtin_ctzll(here), end = min(__builtin_amdgcn_readlane(p.end, l), r.n_tok);
+    return Place{true, less(__builtin_amdgcn_readlane(p.len, l), end), end};
+}
 
-// What a lane needs of the rotation: its pairs and their frequencies in turns per position.
+// What a lane needs of the rotation: its pieces' first coordinates, its pairs' frequencies in turns per position (0: they do not turn).
+// INTER: pairs lie side by side.
 struct RopeLane {
+    int a, b;
     double freq[4];
     int axis[4];
-    bool turns, lower;   // takes part; has the first coordinates of its pairs
-    int partner;         // the lane it swaps with
+    bool turn_a, turn_b;   // whether the piece's coordinates turn
 };
-template <int D>
-__device__ __forceinline__ RopeLane rope_lane(const RopeArgs &a) {
+template <int D, bool INTER>
+__device__ __forceinline__ RopeLane rope_lane(const RopeArgs &r) {
     constexpr int LPR = D / 8;
-    RopeLane r;
-    const int lane = lane_id(), lc = lane % LPR, h = a.rot / 16;
-    r.turns = lc < 2 * h;
-    r.lower = lc < h;
-    r.partner = !r.turns ? lane : r.lower ? lane + h : lane - h;
-    const int p0 = a.interleaved ? 4 * lc : r.lower ? 8 * lc : 8 * (lc - h) + 4;
+    RopeLane l;
+    const int i = lane_id() % LPR, half = INTER ? LPR : r.rot / 8;   // lanes with both coordinates of pairs
+    l.a = 4 * (i < half ? i : half + i);
+    l.b = 4 * (i < half ? i + half : LPR + i);
+    l.turn_a = l.a < r.rot;
+    l.turn_b = l.b < r.rot;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        r.freq[i] = r.turns ? a.freq[p0 + i] * 0.15915494309189533577 : 0.0;   // 1 / (2 pi)
-        r.axis[i] = r.turns && a.axis && a.pos ? min(max(a.axis[p0 + i], 0), a.n_axes - 1) : 0;
+    for (int j = 0; j < 4; ++j) {
+        const int pair = INTER ? (j < 2 ? l.a / 2 + j : l.b / 2 + j - 2) : l.a + j;
+        const bool turns = INTER && j >= 2 ? l.turn_b : l.turn_a;
+        l.freq[j] = turns ? r.freq[pair] * 0.15915494309189533577 : 0.0;   // 1 / (2 pi)
+        l.axis[j] = turns && r.axis && r.pos ? min(max(r.axis[pair], 0), r.n_axes - 1) : 0;
     }
-    return r;
+    return l;
 }
 // The angles of a lane's pairs at a row.  Positions times frequencies in 64 bits, of which the part of a turn is kept: at position
-// 200000 a product in 32 bits is off by 0.01.
+// 200000 a product in 32 bits is off by 0.01.  (64-bit arithmetic has the rate of unpacked 32-bit arithmetic here.)  The instructions for sine and
+// cosine take turns and are within 2^-22.9 (measured at 2^22 points of a turn), as are series to the 13th power, for 26 instructions more.
 struct Turn {
     float c[4], s[4];
 };
-__device__ __forceinline__ Turn turn_of(const RopeLane &r, const double (&pos)[4]) {
-    Turn t;
+struct Fractions {   // of a turn, of a lane's pairs
+    float f[4];
+    __device__ __forceinline__ Turn turn() const {
+        Turn t;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const double x = pos[i] * r.freq[i];
-        sincospif(2.0f * (float)(x - __builtin_rint(x)), &t.s[i], &t.c[i]);
+        for (int i = 0; i < 4; ++i) t.s[i] = __builtin_amdgcn_sinf(f[i]), t.c[i] = __builtin_amdgcn_cosf(f[i]);
+        return t;
     }
-    return t;
+};
+__device__ __forceinline__ float fraction(const RopeLane &l, int i, int pos) {
+    const double x = (double)pos * l.freq[i];
+    return (float)(x - __builtin_rint(x));
 }
-
-// A lane's eight coordinates of a row with their weights: normed and turned.  All lanes of a row together.
+__device__ __forceinline__ Fractions fractions(const RopeLane &l, int pos) {   // one position on every axis
+    return Fractions{fraction(l, 0, pos), fraction(l, 1, pos), fraction(l, 2, pos), fraction(l, 3, pos)};
+}
+__device__ __forceinline__ Fractions fractions(const RopeArgs &r, const RopeLane &l, int t) {   // those of row t
+    int p[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) p[i] = r.pos[(size_t)l.axis[i] * r.n_tok + t];
+    return Fractions{fraction(l, 0, p[0]), fraction(l, 1, p[1]), fraction(l, 2, p[2]), fraction(l, 3, p[3])};
+}
+// A lane's weights.
+struct Weights {
+    float w[8];
+    __device__ __forceinline__ void load(const float *p, const RopeLane &l) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) w[e] = p ? p[l.a + e] : 1.0f, w[4 + e] = p ? p[l.b + e] : 1.0f;
+    }
+};
 template <int D>
-__device__ __forceinline__ void norm_and_turn(const RopeArgs &a, const RopeLane &r, const Turn &t, const float (&w)[8], float (&x)[8]) {
-    constexpr int LPR = D / 8;
-    if (a.norm) {
-        float ss = 0.0f;
+__device__ __forceinline__ float squares(const float (&x)[8]) {
+    float ss = 0.0f;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) ss = fmaf(x[e], x[e], ss);
-        ss = row_sum<LPR>(ss);
-        // squares that leave the range of 32 bits, upwards or, where eps does not rule them, downwards
-        const bool odd = !(ss < 0x1p120f) || (ss < 0x1p-80f && a.eps < 0x1p-80f);
-        if (__any(odd)) {
-            double s2 = 0.0;
-#pragma unroll
-            for (int e = 0; e < 8; ++e) s2 = fma((double)x[e], (double)x[e], s2);
-            s2 = row_sum<LPR>(s2);
-            const double inv = 1.0 / sqrt(s2 * (1.0 / D) + (double)a.eps);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const float y = (float)((double)x[e] * inv);
-                if (odd) x[e] = y * w[e];
-            }
-        }
-        const float inv = 1.0f / sqrtf(fmaf(ss, 1.0f / D, a.eps));
-#pragma unroll
-        for (int e = 0; e < 8; ++e)
-            if (!odd) x[e] = x[e] * inv * w[e];
-    }
-    if (a.rot == 0) return;
-    float p[4], q[4];   // pairs (p, q)
-    if (a.interleaved) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) p[i] = x[2 * i], q[i] = x[2 * i + 1];
-    } else {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const float mine = r.lower ? x[i] : x[4 + i], got = __shfl(r.lower ? x[4 + i] : x[i], r.partner, 64);
-            p[i] = r.lower ? mine : got;
-            q[i] = r.lower ? got : mine;
-        }
-    }
-    float u[4], v[4];
+    for (int e = 0; e < 8; ++e) ss = fmaf(x[e], x[e], ss);
+    return row_sum<D / 8>(ss);
+}
+// 1 / sqrt(mean + eps): one step from the instruction's approximation.
+template <int D>
+__device__ __forceinline__ float inverse_root(float ss, float eps) {
+    const float v = fmaf(ss, 1.0f / D, eps), q = __builtin_amdgcn_rsqf(v);
+    return fmaf(0.5f * q, fmaf(-v * q, q, 1.0f), q);
+}
+// x w turned and times inv; pairs that do not turn have c = 1, s = 0.
+template <bool INTER>
+__device__ __forceinline__ void turned(const Turn &t, const Weights &w, float inv, float (&x)[8]) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        u[i] = fmaf(p[i], t.c[i], -(q[i] * t.s[i]));
-        v[i] = fmaf(p[i], t.s[i], q[i] * t.c[i]);
+        const int ia = INTER ? 2 * i : i, ib = INTER ? 2 * i + 1 : 4 + i;
+        const float a = x[ia] * w.w[ia], b = x[ib] * w.w[ib];
+        x[ia] = fmaf(a, t.c[i], -(b * t.s[i])) * inv;
+        x[ib] = fmaf(a, t.s[i], b * t.c[i]) * inv;
     }
-    if (a.interleaved) {
+}
+// A lane's eight coordinates of a row: normed and turned, all lanes of a row together.  Not of rows whose squares leave the range or that hold
+// infinities or NaN: those come back true, and are done again by norm_and_turn_odd.
+template <int D, bool INTER>
+__device__ __forceinline__ bool norm_and_turn(const RopeArgs &r, const Turn &t, const Weights &w, float (&x)[8]) {
+    const float ss = squares<D>(x);
+    const bool odd = !(ss >= (r.norm ? 0x1p-80f : 0.0f) && ss < 0x1p120f);
+    turned<INTER>(t, w, r.norm ? inverse_root<D>(ss, r.eps) : 1.0f, x);
+    return odd;
+}
+// The same of any row.  The row and the root of eps are taken times a power of two that brings the larger one near 1; without a finite number
+// but zero to bring there, what the formula gives.  Coordinates that do not turn are kept apart, as 0 times infinity is no number.
+template <int D, bool INTER>
+__device__ __forceinline__ void norm_and_turn_odd(const RopeArgs &r, const RopeLane &l, const Turn &t, const Weights &w, float (&x)[8]) {
+    float inv = 1.0f;
+    if (r.norm) {
+        unsigned m = 0;
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-            if (r.turns) x[2 * i] = u[i], x[2 * i + 1] = v[i];
-    } else {
+        for (int e = 0; e < 8; ++e) m = max(m, __float_as_uint(fabsf(x[e])));
+        const float most = row_max<D / 8>(__uint_as_float(m)), top = most < INFINITY ? fmaxf(most, sqrtf(r.eps)) : most;
+        if (top < INFINITY) {
+            const int n = top > 0.0f ? -__builtin_amdgcn_frexp_expf(top) : 0;   // top * 2^n is in [1/2, 1)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const float keep = r.lower ? u[i] : v[i], got = __shfl(r.lower ? v[i] : u[i], r.partner, 64);
-            if (r.turns) {
-                x[i] = r.lower ? keep : got;
-                x[4 + i] = r.lower ? got : keep;
+            for (int e = 0; e < 8; ++e) x[e] = __builtin_amdgcn_ldexpf(x[e], n);
+            inv = inverse_root<D>(squares<D>(x), __builtin_amdgcn_ldexpf(__builtin_amdgcn_ldexpf(r.eps, n), n));
+        } else {
+            squares<D>(x);   // rows beside this one
+#pragma unroll
+            for (int e = 0; e < 8; ++e) x[e] = top == INFINITY && fabsf(x[e]) < INFINITY ? 0.0f : NAN;
+        }
+    }
+    float z[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) z[e] = r.norm ? x[e] * inv * w.w[e] : x[e];
+    turned<INTER>(t, w, inv, x);
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+        if (!(e < 4 ? l.turn_a : l.turn_b)) x[e] = z[e];
+}
+
+// A lane's two pieces as they lie in memory.
+template <bool BF16>
+struct Raw8 {
+    static constexpr int W = BF16 ? 2 : 4;
+    typedef __attribute__((ext_vector_type(W))) unsigned Piece;
+    Piece a, b;
+    __device__ __forceinline__ void load(const char *row, const RopeLane &l) {
+        a = *(const Piece *)(row + l.a * (BF16 ? 2 : 4));
+        b = *(const Piece *)(row + l.b * (BF16 ? 2 : 4));
+    }
+    __device__ __forceinline__ void to(float (&x)[8]) const {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            if constexpr (BF16) {
+                x[e] = e & 1 ? bf16_hi(a[e / 2]) : bf16_lo(a[e / 2]);
+                x[4 + e] = e & 1 ? bf16_hi(b[e / 2]) : bf16_lo(b[e / 2]);
+            } else {
+                x[e] = __uint_as_float(a[e]);
+                x[4 + e] = __uint_as_float(b[e]);
             }
         }
+    }
+    static __device__ __forceinline__ void store(char *row, const RopeLane &l, const float (&x)[8]) {
+        Piece u, v;
+        if constexpr (BF16) {
+            u = Piece{cvt_bf16x2(x[0], x[1]), cvt_bf16x2(x[2], x[3])};
+            v = Piece{cvt_bf16x2(x[4], x[5]), cvt_bf16x2(x[6], x[7])};
+        } else {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) u[e] = __float_as_uint(x[e]), v[e] = __float_as_uint(x[4 + e]);
+        }
+        *(Piece *)(row + l.a * (BF16 ? 2 : 4)) = u;
+        *(Piece *)(row + l.b * (BF16 ? 2 : 4)) = v;
+    }
+};
+
+// Groups of 64 / (d / 8) heads of one token, first, first + step, .. of those of queries and then keys.  A wavefront together: the token's angles
+// are computed once for all of them, and AHEAD groups are asked for ahead.  At most ROPE_GROUPS groups.
+constexpr int ROPE_GROUPS = 32;
+struct RopeViews {
+    View q, k, qo, ko;
+    int Hq, Hkv;
+};
+template <int D>
+__host__ __device__ __forceinline__ int rope_groups(int H) { return (int)(((long long)H + 512 / D - 1) / (512 / D)); }
+template <bool BF16, int D, bool INTER, int AHEAD>
+__device__ __forceinline__ void rope_token(const RopeArgs &r, const RopeViews &a, int t, int first, int step) {
+    constexpr int LPR = D / 8, RPW = 64 / LPR;
+    const int lr = lane_id() / LPR;
+    const int gq = rope_groups<D>(a.Hq), n = gq + rope_groups<D>(a.Hkv);
+    const Places places = places_of(r);
+    const RopeLane rl = rope_lane<D, INTER>(r);
+    Fractions at{};
+    if (r.rot > 0 && r.pos) at = fractions(r, rl, t);
+    auto weights_of = [&](bool is_k) __attribute__((always_inline)) {
+        Weights w;
+        w.load(r.norm ? is_k ? r.kw : r.qw : nullptr, rl);
+        return w;
+    };
+    const bool first_k = first >= gq;
+    Weights w = weights_of(first_k);
+    Raw8<BF16> raw[AHEAD];
+    auto ask = [&](int g, Raw8<BF16> &x) __attribute__((always_inline)) {
+        const bool is_k = g >= gq;
+        const int h = (is_k ? g - gq : g) * RPW + lr;
+        const char *p = (is_k ? a.k.p : a.q.p) + t * (is_k ? a.k.row : a.q.row);
+        if (h < (is_k ? a.Hkv : a.Hq)) x.load(p + h * (is_k ? a.k.head : a.q.head), rl);
+        else x.a = 0, x.b = 0;
+    };
+    auto put = [&](int g, bool mine, const float (&x)[8]) __attribute__((always_inline)) {
+        const bool is_k = g >= gq;
+        const int h = (is_k ? g - gq : g) * RPW + lr;
+        char *p = (is_k ? a.ko.p : a.qo.p) + t * (is_k ? a.ko.row : a.qo.row);
+        if (mine && h < (is_k ? a.Hkv : a.Hq)) Raw8<BF16>::store(p + h * (is_k ? a.ko.head : a.qo.head), rl, x);
+    };
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i)
+        if (first + i * step < n) ask(first + i * step, raw[i]);
+    const Place place = place_of(r, places, t);
+    if (!place.there) return;
+    if (r.rot > 0 && !r.pos) at = fractions(rl, plus(place.ahead, t));
+    const Turn turn = at.turn();
+    bool keys = first_k;
+    unsigned odds = 0;   // bit i: the lane's row of the wavefront's i-th group is to be done again
+    int i0 = 0;
+    for (int g0 = first; g0 < n; g0 += AHEAD * step, i0 += AHEAD)
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i) {
+            const int g = g0 + i * step;
+            if (g >= n) break;   // uniform
+            if (g >= gq && !keys) {
+                keys = true;
+                w = weights_of(true);
+            }
+            float x[8];
+            raw[i].to(x);
+            if (g + AHEAD * step < n) ask(g + AHEAD * step, raw[i]);
+            const bool odd = norm_and_turn<D, INTER>(r, turn, w, x);
+            put(g, !odd, x);
+            odds |= odd ? 1u << (i0 + i) : 0u;
+        }
+    if (!__any(odds)) return;
+#pragma unroll 1
+    for (int i = 0, g = first; g < n; ++i, g += step) {   // the others' rows are left out: an output may be its input
+        if (!__any(odds >> i & 1)) continue;
+        float x[8];
+        ask(g, raw[0]);
+        raw[0].to(x);
+        w = weights_of(g >= gq);
+        norm_and_turn_odd<D, INTER>(r, rl, turn, w, x);
+        put(g, odds >> i & 1, x);
     }
 }
 
-// A lane's eight coordinates from memory and back, in one or two 16-byte pieces.
-template <bool BF16>
-__device__ __forceinline__ void load8(const char *p, float (&x)[8]) {
-    if constexpr (BF16) {
-        const u32x4 w = *(const u32x4 *)p;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) x[2 * e] = bf16_lo(w[e]), x[2 * e + 1] = bf16_hi(w[e]);
-    } else {
-        const f32x4 u = ((const f32x4 *)p)[0], v = ((const f32x4 *)p)[1];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) x[e] = u[e], x[4 + e] = v[e];
-    }
-}
-template <bool BF16>
-__device__ __forceinline__ void store8(char *p, const float (&x)[8]) {
-    if constexpr (BF16) {
-        *(u32x4 *)p = u32x4{cvt_bf16x2(x[0], x[1]), cvt_bf16x2(x[2], x[3]), cvt_bf16x2(x[4], x[5]), cvt_bf16x2(x[6], x[7])};
-    } else {
-        ((f32x4 *)p)[0] = f32x4{x[0], x[1], x[2], x[3]};
-        ((f32x4 *)p)[1] = f32x4{x[4], x[5], x[6], x[7]};
-    }
-}
+// qk_norm_rope's launch (rope.hip).
+int rope_launch(const RopeArgs &r, const RopeViews &v, int d, int dtype, int interleaved, hipStream_t s);
 
 }  // namespace fastar
