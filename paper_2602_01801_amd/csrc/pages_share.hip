@@ -1,5 +1,6 @@
 // Pages that requests share: forking (kv_pages_fork), giving pages up (kv_pages_free) and thinning out (kv_pages_compact).
 #include <algorithm>
+#include <type_traits>
 
 #include "packed.hpp"
 
@@ -141,29 +142,36 @@ __global__ __launch_bounds__(FT) void fork_kernel(ForkArgs a, bool finish_here) 
 // ---- giving pages up --------------------------------------------------------------------------------------------
 
 // Table entries are looked at in blocks of ET, each within a request's row: entry e of request b has number b * max_pages + e.
-constexpr int ET = 1024;
+constexpr int ET = 256;
 
+// A page in the call: its holders before it, those that give it up, and the last of them.  Together, so that an entry meets one line of memory.
+struct PageState {
+    int32_t hold, gone, last, unused;
+};
+// 16 tokens of a request in its mask: which are kept, and how many before them.
+struct Group {
+    int32_t rank;
+    uint32_t bits;
+};
 // What a call needs in memory between its launches, cut out of the workspace.
 struct Work {
-    int32_t *hold, *gone, *last;             // [n_pages] holders before the call; those that give the page up; the last of them
+    PageState *state;                        // [n_pages]
+    Group *group;                            // [B, max_pages * P / 16]
     int32_t *have, *stay, *need, *base;      // [B] pages and tokens before and after, fresh pages needed and where they begin (-1: refused)
     int32_t *head;                           // [4] free pages before, fresh pages in all
-    int32_t *block;                          // pages that a block gives back, then those before it
-    int32_t *old, *link, *from;              // [B, max_pages] table before the call; new page of an old one; old page of a new one, or ~(which fresh one)
+    int32_t *block;                          // pages that a block gives back
+    int32_t *old, *link, *from, *start;      // [B, max_pages] table before the call; new page of an old one; old page of a new one, or ~(which fresh one), and the group of its first token
     int32_t *made, *page;                    // [n_pages] fresh pages: entry of the new table, number
-    int32_t *token;                          // [B, max_pages * P] old place of the request's new tokens
 };
-inline size_t rounded(size_t n) { return (n + 63) / 64 * 64; }   // 256 bytes
-inline size_t lay_out(Work &w, int32_t *p, int64_t B, int64_t max_pages, int64_t n_pages, int64_t P) {
+inline size_t lay_out(Work &w, char *p, int64_t B, int64_t max_pages, int64_t n_pages, int64_t P) {
     size_t at = 0;
-    auto take = [&](int32_t *&x, size_t n) {
-        x = p ? p + at : nullptr;
-        at += rounded(n);
+    auto take = [&](auto *&x, size_t n) {
+        using T = std::remove_reference_t<decltype(*x)>;
+        x = p ? (T *)(p + at) : nullptr;
+        at += (n * sizeof(T) + 255) / 256 * 256;
     };
     take(w.head, 4);
-    take(w.hold, n_pages);
-    take(w.gone, n_pages);
-    take(w.last, n_pages);
+    take(w.state, n_pages);
     take(w.have, B);
     take(w.stay, B);
     take(w.need, B);
@@ -172,125 +180,122 @@ inline size_t lay_out(Work &w, int32_t *p, int64_t B, int64_t max_pages, int64_t
     take(w.old, B * max_pages);
     take(w.link, B * max_pages);
     take(w.from, B * max_pages);
+    take(w.start, B * max_pages);
     take(w.made, n_pages);
     take(w.page, n_pages);
-    take(w.token, (size_t)(B * max_pages) * P);
-    return at * sizeof(int32_t);
+    take(w.group, (size_t)(B * max_pages) * P / 16);
+    return at;
 }
 
 struct Args {
-    fastar_pages pg;   // compaction only
+    fastar_pages pg;   // thinning out only
     const uint8_t *mask;
     const int32_t *keep, *len, *table, *pool, *pool_n;
     int32_t *len_out, *table_out, *pool_out, *pool_n_out, *status;
     int32_t B, max_pages, n_pages, pshift, segs;   // segs: blocks of entries per row
+    bool summed, admitted;                         // block, and base and status, have been worked out by a launch of their own
     Work w;
 };
 
-__global__ __launch_bounds__(256) void clear_kernel(Work w, int n_pages) {
-    const int i = blockIdx.x * 256 + threadIdx.x;
-    if (i >= n_pages) return;
-    w.hold[i] = 0;
-    w.gone[i] = 0;
-    w.last[i] = -1;
+__device__ __forceinline__ void clear_states(const Args &a) {
+    for (size_t i = (size_t)blockIdx.x * blockDim.x + threadIdx.x; i < (size_t)a.n_pages; i += (size_t)gridDim.x * blockDim.x)
+        *(i32x4 *)&a.w.state[i] = i32x4{0, 0, -1, 0};
 }
+__global__ __launch_bounds__(256) void clear_kernel(Args a) { clear_states(a); }
 
-// A block of entries: request, first entry.
-__device__ __forceinline__ void block_of(const Args &a, int &b, int &e0) {
-    b = blockIdx.x / a.segs;
-    e0 = blockIdx.x % a.segs * ET;
+// A block of entries: request, and the thread's entry.
+__device__ __forceinline__ void entry_of(const Args &a, int block, int &b, int &e) {
+    b = block / a.segs;
+    e = block % a.segs * ET + threadIdx.x;
 }
 __device__ __forceinline__ int tokens_of(const Args &a, int b) {
     return (int)min((long long)max(a.len[b], 0), (long long)a.max_pages << a.pshift);
 }
+__device__ __forceinline__ bool is_page(const Args &a, int p) { return (unsigned)p < (unsigned)a.n_pages; }
 
-__global__ __launch_bounds__(256) void hold_kernel(Args a) {
-    int b, e0;
-    block_of(a, b, e0);
-    const int have = (tokens_of(a, b) + (1 << a.pshift) - 1) >> a.pshift;
-    const int32_t *row = a.table + (size_t)b * a.max_pages;
-    for (int e = e0 + threadIdx.x; e < min(e0 + ET, have); e += 256) {
-        const int p = row[e];
-        if ((unsigned)p < (unsigned)a.n_pages) atomicAdd(&a.w.hold[p], 1);
-    }
+__global__ __launch_bounds__(ET) void hold_kernel(Args a) {
+    int b, e;
+    entry_of(a, blockIdx.x, b, e);
+    if (e >= (tokens_of(a, b) + (1 << a.pshift) - 1) >> a.pshift) return;
+    const int p = a.table[(size_t)b * a.max_pages + e];
+    if (is_page(a, p)) atomicAdd(&a.w.state[p].hold, 1);
 }
 
 __device__ __forceinline__ void give_up(const Args &a, int p, int number) {
-    atomicAdd(&a.w.gone[p], 1);
-    atomicMax(&a.w.last[p], number);
+    atomicAdd(&a.w.state[p].gone, 1);
+    atomicMax(&a.w.state[p].last, number);
 }
 // Which requests are refused, and the pages that the others give up.
-__global__ __launch_bounds__(256) void cut_kernel(Args a) {
-    int b, e0;
-    block_of(a, b, e0);
+__global__ __launch_bounds__(ET) void cut_kernel(Args a) {
+    int b, e;
+    entry_of(a, blockIdx.x, b, e);
     const int P = 1 << a.pshift, L = tokens_of(a, b), have = (L + P - 1) >> a.pshift;
     const int32_t *row = a.table + (size_t)b * a.max_pages;
-    int stay = min(max(a.keep[b], 0), L);
+    const int p = e < have ? row[e] : -1;
+    int stay = clipped(a.keep[b], L);
     bool refused = false;
     if (stay < L && (stay & (P - 1))) {
-        const int p = row[stay >> a.pshift];
-        refused = (unsigned)p < (unsigned)a.n_pages && a.w.hold[p] > 1;
+        const int q = row[stay >> a.pshift];
+        refused = is_page(a, q) && a.w.state[q].hold > 1;
     }
     if (refused) stay = L;
-    if (e0 == 0 && threadIdx.x == 0) {
+    if (e == 0) {
         a.w.have[b] = have;
         a.w.stay[b] = stay;
         a.status[b] = refused;
         if (b == 0) a.w.head[0] = clipped(a.pool_n[0], a.n_pages);
     }
-    const int left = (stay + P - 1) >> a.pshift;
-    for (int e = max(e0, left / 256 * 256) + threadIdx.x; e < min(e0 + ET, have); e += 256) {
-        if (e < left) continue;
-        const int p = row[e];
-        if ((unsigned)p < (unsigned)a.n_pages) give_up(a, p, b * a.max_pages + e);
-    }
+    if (e >= (stay + P - 1) >> a.pshift && is_page(a, p)) give_up(a, p, b * a.max_pages + e);
 }
 
 // The page of entry e, if the call gives it back to the pool there: all its holders give it up, and this is the last one.
 template <bool COMPACT>
-__device__ __forceinline__ int given_back(const Args &a, int b, int e, int left, int have) {
-    if (e < left || e >= have) return -1;
+__device__ __forceinline__ int given_back(const Args &a, int b, int e) {
+    const int have = a.w.have[b];
+    if (e >= have) return -1;
+    if (COMPACT ? a.w.base[b] < 0 : e < (a.w.stay[b] + (1 << a.pshift) - 1) >> a.pshift) return -1;   // refused;  kept
     const size_t at = (size_t)b * a.max_pages + e;
     const int p = COMPACT ? a.w.old[at] : a.table[at];
-    if ((unsigned)p >= (unsigned)a.n_pages || (COMPACT && a.w.link[at] >= 0)) return -1;
-    return a.w.gone[p] == a.w.hold[p] && a.w.last[p] == (int)at ? p : -1;
+    if (!is_page(a, p) || (COMPACT && a.w.link[at] >= 0)) return -1;
+    const PageState s = a.w.state[p];
+    return s.gone == s.hold && s.last == (int)at ? p : -1;
 }
+// How many pages a block gives back.
 template <bool COMPACT>
-__device__ __forceinline__ int first_given(const Args &a, int b, int have) {
-    if (COMPACT) return a.w.base[b] < 0 ? have : 0;   // refused requests give nothing up
-    return (a.w.stay[b] + (1 << a.pshift) - 1) >> a.pshift;
+__device__ __forceinline__ void count_block(const Args &a, int block) {
+    __shared__ int n;
+    int b, e;
+    entry_of(a, block, b, e);
+    if (threadIdx.x == 0) n = 0;
+    __syncthreads();
+    const int c = __builtin_popcountll(__ballot(given_back<COMPACT>(a, b, e) >= 0));
+    if ((threadIdx.x & 63) == 0 && c) atomicAdd(&n, c);
+    __syncthreads();
+    if (threadIdx.x == 0) a.w.block[block] = n;
 }
-// PUSH false: how many pages every block gives back;  true: they go to the pool.
-template <bool COMPACT, bool PUSH>
-__global__ __launch_bounds__(256) void give_kernel(Args a) {
-    __shared__ int part[4];
-    int b, e0;
-    block_of(a, b, e0);
-    const int have = a.w.have[b], left = first_given<COMPACT>(a, b, have);
-    int p[ET / 256], n = 0;
-#pragma unroll
-    for (int i = 0; i < ET / 256; ++i) {
-        p[i] = given_back<COMPACT>(a, b, e0 + (ET / 256) * (int)threadIdx.x + i, left, have);
-        n += p[i] >= 0;
-    }
+__global__ __launch_bounds__(ET) void count_kernel(Args a) { count_block<false>(a, blockIdx.x); }
+// They go to the pool, behind those of the blocks before, and what is known only now is written over what may be the call's input.
+template <bool COMPACT>
+__global__ __launch_bounds__(ET) void push_kernel(Args a) {
+    __shared__ int part[ET / 64], s_before;
+    int b, e;
+    entry_of(a, blockIdx.x, b, e);
+    const int p = given_back<COMPACT>(a, b, e), blocks = a.B * a.segs;
+    if (threadIdx.x == 0) s_before = a.summed ? a.w.block[blockIdx.x] : 0;
     int all;
-    const int upto = wg_incl_scan<256>(n, part, &all);
-    if constexpr (!PUSH) {
-        if (threadIdx.x == 0) a.w.block[blockIdx.x] = all;
-    } else {
-        const int top = a.w.head[0] - (COMPACT ? a.w.head[1] : 0);
-        long long at = (long long)top + a.w.block[blockIdx.x] + upto - n;
-#pragma unroll
-        for (int i = 0; i < ET / 256; ++i)
-            if (p[i] >= 0) {
-                if (at < a.n_pages) a.pool_out[at] = p[i];
-                ++at;
-            }
-        if (threadIdx.x == 0) {
-            if (e0 == 0) a.len_out[b] = a.w.stay[b];
-            if (blockIdx.x == 0) a.pool_n_out[0] = (int)min((long long)top + a.w.block[(size_t)a.B * a.segs], (long long)a.n_pages);
-        }
+    const int upto = wg_incl_scan<ET>(p >= 0, part, &all);
+    const bool last = blockIdx.x == blocks - 1;
+    if (!a.summed && (all || last)) {
+        int sum = 0;
+        for (int i = threadIdx.x; i < (int)blockIdx.x; i += ET) sum += a.w.block[i];
+        if (sum) atomicAdd(&s_before, sum);
     }
+    __syncthreads();
+    const int top = a.w.head[0] - (COMPACT ? a.w.head[1] : 0);
+    const long long at = (long long)top + s_before + upto - 1;
+    if (p >= 0 && at < a.n_pages) a.pool_out[at] = p;
+    if (e == 0) a.len_out[b] = a.w.stay[b];
+    if (last && threadIdx.x == 0) a.pool_n_out[0] = (int)min((long long)top + s_before + all, (long long)a.n_pages);
 }
 // Exclusive prefix sums of n numbers, and their sum behind them.
 __global__ __launch_bounds__(1024) void scan_kernel(int32_t *x, int n) {
@@ -305,7 +310,6 @@ __global__ __launch_bounds__(1024) void scan_kernel(int32_t *x, int n) {
     }
     if (threadIdx.x == 0) x[n] = sum;
 }
-
 // Of no requests: the free pages as they are.
 __global__ __launch_bounds__(256) void nothing_kernel(Args a) {
     const size_t i = (size_t)blockIdx.x * 256 + threadIdx.x;
@@ -315,61 +319,77 @@ __global__ __launch_bounds__(256) void nothing_kernel(Args a) {
 
 // ---- thinning out -----------------------------------------------------------------------------------------------
 
-// A workgroup per request goes through its mask: where every token goes, which pages stay whole, which of the new ones are fresh.
-// It keeps the old table row, as the new one may be written over it.
+// A workgroup per request goes through its mask, 64 tokens per thread: how many are kept before every group of 16, which pages stay whole,
+// which of the new ones are fresh and where their tokens begin.  It keeps the old table row, as the new one may be written over it.  Whoever has a
+// new page's first token writes about that page, so that nothing has to be cleared before, and all loads of a round are one trip to memory.
 __global__ __launch_bounds__(1024) void mask_kernel(Args a) {
     __shared__ int part[16];
     const int b = blockIdx.x, tid = threadIdx.x, P = 1 << a.pshift;
     const int L = tokens_of(a, b), have = (L + P - 1) >> a.pshift;
     const size_t row = (size_t)b * a.max_pages;
-    int32_t *token = a.w.token + (row << a.pshift);
     const u32x4 *mask = (const u32x4 *)(a.mask + (row << a.pshift));
-    for (int e = tid; e < have; e += 1024) {
-        const int p = a.table[row + e];
-        a.w.old[row + e] = p;
-        a.w.link[row + e] = -1;
-        a.w.from[row + e] = -1;
-        if ((unsigned)p < (unsigned)a.n_pages) atomicAdd(&a.w.hold[p], 1);
-    }
-    __syncthreads();
-    const int per = P / 16;   // threads that look at a page: 1, 2 or 4 neighbours
-    int kept = 0;
-    for (int i0 = 0; i0 * 16 < L; i0 += 1024) {
-        const int u = i0 + tid, t0 = 16 * u;   // 16 tokens of one page
-        unsigned bits = 0, there = 0;
-        if (t0 < L) {
-            const u32x4 x = mask[u];
-            there = t0 + 16 <= L ? 0xFFFFu : (1u << (L - t0)) - 1u;
-            if ((unsigned)a.w.old[row + (t0 >> a.pshift)] < (unsigned)a.n_pages)
+    Group *group = a.w.group + (row << a.pshift) / 16;
+    clear_states(a);
+    const int per = P / 16;   // groups of a page: 1, 2 or 4
+    int kept = 0, fresh = 0;
+    for (int i0 = 0; i0 < L; i0 += 64 * 1024) {
+        const int t0 = i0 + 64 * tid;
+        u32x4 x[4];
+        int page[4];
 #pragma unroll
-                for (int i = 0; i < 16; ++i) bits |= (x[i / 4] >> (8 * (i % 4)) & 0xFFu) ? 1u << i : 0u;
-            bits &= there;
+        for (int q = 0; q < 4; ++q) {
+            const bool here = t0 + 16 * q < L;   // so that the group's bytes are the row's
+            x[q] = here ? mask[t0 / 16 + q] : u32x4{0, 0, 0, 0};
+            page[q] = here ? a.table[row + ((t0 + 16 * q) >> a.pshift)] : -1;
         }
-        const int n = __builtin_popcount(bits);
+        unsigned bits[4], there[4];
+        int n = 0;
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            const int left = L - t0 - 16 * q;
+            there[q] = left >= 16 ? 0xFFFFu : left > 0 ? (1u << left) - 1u : 0u;
+            bits[q] = 0;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) bits[q] |= (x[q][i / 4] >> (8 * (i % 4)) & 0xFFu) ? 1u << i : 0u;
+            bits[q] = is_page(a, page[q]) ? bits[q] & there[q] : 0;
+            n += __builtin_popcount(bits[q]);
+        }
         int all;
-        const int rank = kept + wg_incl_scan<1024>(n, part, &all) - n;
-        int at = rank;
-        for (unsigned m = bits; m; m &= m - 1) token[at++] = t0 + __builtin_ctz(m);
-        // the whole of a page, at a page's beginning, and to its end unless the request ends there too
-        unsigned lost = bits != there;
-        if (per >= 2) lost |= (unsigned)__shfl_xor((int)lost, 1, 64);
-        if (per >= 4) lost |= (unsigned)__shfl_xor((int)lost, 2, 64);
-        if (t0 < L && !lost && !(u & (per - 1)) && !(rank & (P - 1))) {
-            const int s = t0 >> a.pshift, j = rank >> a.pshift;
-            a.w.link[row + s] = j;
-            a.w.from[row + j] = s;
-        }
+        int rank = kept + wg_incl_scan<1024>(n, part, &all) - n;
         kept += all;
-    }
-    __syncthreads();
-    const int pages = (kept + P - 1) >> a.pshift;
-    int fresh = 0;
-    for (int j0 = 0; j0 < pages; j0 += 1024) {
-        const int j = j0 + tid, n = j < pages && a.w.from[row + j] < 0;
-        int all;
-        const int upto = wg_incl_scan<1024>(n, part, &all);
-        if (n) a.w.from[row + j] = ~(fresh + upto - 1);
+        // the new page whose first token is in the group, and the old page that it is, or -1
+        int j[4], s[4], n_fresh = 0;
+        bool first[4];
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            const int u = t0 / 16 + q, c = __builtin_popcount(bits[q]), end = rank + c;
+            first[q] = c && ((end - 1) >> a.pshift << a.pshift) >= rank;
+            j[q] = (end - 1) >> a.pshift;
+            // whole: begins at a page's beginning, nothing missing up to the page's or the request's end
+            bool whole = there[q] && !(u & (per - 1)) && !(rank & (P - 1));
+#pragma unroll
+            for (int i = 0; i < 4; ++i) whole = whole && (i < q || i >= q + per || bits[i] == there[i]);
+            s[q] = first[q] && whole ? (16 * u) >> a.pshift : -1;
+            n_fresh += first[q] && s[q] < 0;
+            if (there[q]) {
+                group[u] = Group{rank, bits[q]};
+                if (!(u & (per - 1))) {
+                    const size_t at = row + ((16 * u) >> a.pshift);
+                    a.w.old[at] = page[q];
+                    a.w.link[at] = whole ? rank >> a.pshift : -1;
+                }
+            }
+            rank = end;
+        }
+        int f = fresh + wg_incl_scan<1024>(n_fresh, part, &all) - n_fresh;
         fresh += all;
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+            if (first[q]) {
+                a.w.from[row + j[q]] = s[q] >= 0 ? s[q] : ~f;
+                a.w.start[row + j[q]] = t0 / 16 + q;
+                f += s[q] < 0;
+            }
     }
     if (tid == 0) {
         a.w.have[b] = have;
@@ -378,7 +398,8 @@ __global__ __launch_bounds__(1024) void mask_kernel(Args a) {
     }
 }
 
-// Which requests are refused, and where the fresh pages of the others begin.
+// Which requests are refused, and where the fresh pages of the others begin.  One workgroup, where there are too many requests for each to do so.
+constexpr int ADMIT_ALL = 1024;
 __global__ __launch_bounds__(1024) void admit_kernel(Args a) {
     __shared__ int part[16];
     __shared__ int s_taken;
@@ -405,37 +426,63 @@ __global__ __launch_bounds__(1024) void admit_kernel(Args a) {
     }
 }
 
-// New table rows, the list of fresh pages, the old pages that are given up, and the pool as it was.
-__global__ __launch_bounds__(256) void relink_kernel(Args a) {
-    int b, e0;
-    block_of(a, b, e0);
-    const int base = a.w.base[b], have = a.w.have[b], stay = a.w.stay[b], free0 = a.w.head[0];
-    const int pages = (stay + (1 << a.pshift) - 1) >> a.pshift;
-    const size_t row = (size_t)b * a.max_pages;
-    for (int e = e0 + threadIdx.x; e < min(e0 + ET, a.max_pages); e += 256) {
-        if (base < 0) {
-            if (a.table_out != a.table) a.table_out[row + e] = a.table[row + e];
-            continue;
+// New table rows, the list of fresh pages, the holders of old pages and those that give them up, and the pool as it was.
+__global__ __launch_bounds__(ET) void relink_kernel(Args a) {
+    __shared__ int part[ET / 64];
+    int b, e;
+    entry_of(a, blockIdx.x, b, e);
+    const size_t at = (size_t)b * a.max_pages + e;
+    const int have = a.w.have[b];
+    int stay = a.w.stay[b];
+    const int old = e < have ? a.w.old[at] : -1, link = e < have ? a.w.link[at] : 0, was = e < a.max_pages ? a.table[at] : -1;
+    const bool is_new = e < (stay + (1 << a.pshift) - 1) >> a.pshift;   // unless the request is refused
+    const int from = is_new ? a.w.from[at] : 0;
+    const int free0 = clipped(a.pool_n[0], a.n_pages);
+    int base;
+    if (a.admitted) base = a.w.base[b];
+    else {   // the sums up to the request, and for the first workgroup up to the last one that is not refused
+        int mine = 0, before = 0, taken = 0;
+        for (int i0 = 0; i0 < a.B; i0 += ET) {
+            const int i = i0 + threadIdx.x, need = i < a.B ? a.w.need[i] : 0;
+            int all;
+            const int upto = before + wg_incl_scan<ET>(need, part, &all);
+            if (i == b) mine = need > 0 && upto > free0 ? -1 : min(upto - need, free0);
+            if (need > 0 && upto <= free0) taken = upto;
+            before += all;
         }
+        __shared__ int s_base, s_taken;
+        if (threadIdx.x == 0) s_taken = 0;
+        __syncthreads();
+        if (threadIdx.x == b % ET) s_base = mine;
+        if (taken) atomicMax(&s_taken, taken);
+        __syncthreads();
+        base = s_base;
+        if (e == 0) {
+            a.w.base[b] = base;
+            a.status[b] = base < 0;
+            if (base < 0) a.w.stay[b] = tokens_of(a, b);
+            if (b == 0) a.w.head[0] = free0, a.w.head[1] = s_taken;
+        }
+    }
+    if (is_page(a, old)) atomicAdd(&a.w.state[old].hold, 1);
+    if (base < 0) {
+        if (e < a.max_pages && a.table_out != a.table) a.table_out[at] = was;
+    } else if (e < a.max_pages) {
         int p = -1;
-        if (e < pages) {
-            const int f = a.w.from[row + e];
-            if (f >= 0) p = a.w.old[row + f];
+        if (is_new) {
+            if (from >= 0) p = a.w.old[(size_t)b * a.max_pages + from];
             else {
-                const int k = base + ~f;
+                const int k = base + ~from;
                 p = a.pool[free0 - 1 - k];
-                a.w.made[k] = (int)(row + e);
+                a.w.made[k] = (int)at;
                 a.w.page[k] = p;
             }
         }
-        a.table_out[row + e] = p;
-        if (e < have && a.w.link[row + e] < 0) {
-            const int q = a.w.old[row + e];
-            if ((unsigned)q < (unsigned)a.n_pages) give_up(a, q, (int)(row + e));
-        }
+        a.table_out[at] = p;
+        if (link < 0 && is_page(a, old)) give_up(a, old, (int)at);
     }
     if (a.pool_out != a.pool)
-        for (size_t i = (size_t)blockIdx.x * 256 + threadIdx.x; i < (size_t)a.n_pages; i += (size_t)gridDim.x * 256) a.pool_out[i] = a.pool[i];
+        for (size_t i = (size_t)blockIdx.x * ET + threadIdx.x; i < (size_t)a.n_pages; i += (size_t)gridDim.x * ET) a.pool_out[i] = a.pool[i];
 }
 
 __device__ __forceinline__ float largest(float a, float b) { return a > b ? a : b; }
@@ -446,80 +493,108 @@ __device__ __forceinline__ unsigned carried(unsigned w, float ratio) {
     y = __builtin_amdgcn_cvt_pk_fp8_f32(__builtin_amdgcn_cvt_f32_fp8((int)w, 2) * ratio, __builtin_amdgcn_cvt_f32_fp8((int)w, 3) * ratio, y, true);
     return (unsigned)y;
 }
+__device__ __forceinline__ u32x4 carried(u32x4 w, float ratio) {
+    return u32x4{carried(w[0], ratio), carried(w[1], ratio), carried(w[2], ratio), carried(w[3], ratio)};
+}
 
-// A workgroup takes one head of a fresh page after the other: its tokens' places, then the 16 bytes of a token (K) or of a
-// coordinate (V) per thread.
-__global__ __launch_bounds__(256) void gather_kernel(Args a) {
-    __shared__ int s_src[64], s_off[64];
-    __shared__ float s_ratio[2][64];
-    const int tid = threadIdx.x, P = 1 << a.pshift, d = a.pg.d, Hkv = a.pg.Hkv;
-    const long long items = (long long)a.w.head[1] * Hkv;
-    for (long long it = blockIdx.x; it < items; it += gridDim.x) {
-        const int k = (int)(it / Hkv), h = (int)(it % Hkv), entry = a.w.made[k], dst = a.w.page[k];
-        if ((unsigned)dst >= (unsigned)a.n_pages) continue;   // the caller's pool names no page: nothing is written
-        const int b = entry / a.max_pages, j = entry % a.max_pages;
-        const int n = min(P, a.w.stay[b] - j * P);
-        __syncthreads();
-        if (tid < 64) {
-            float ks = 0.0f, vs = 0.0f;
-            int src = 0, off = 0;
-            if (tid < n) {
-                const int t = a.w.token[(((size_t)b * a.max_pages + j) << a.pshift) + tid];
-                src = a.w.old[(size_t)b * a.max_pages + (t >> a.pshift)];
-                off = t & (P - 1);
-                ks = a.pg.kscale[(size_t)src * Hkv + h];
-                vs = a.pg.vscale[(size_t)src * Hkv + h];
+// The first workgroups count the pages that blocks of entries give back; the others fill fresh pages, one with HEADS heads after the other: its tokens'
+// places, their scales, then the 16 bytes of a token (K) or of a coordinate (V) per thread.
+constexpr int HEADS = 2;
+__global__ __launch_bounds__(256) void gather_kernel(Args a, int blocks) {
+    if ((int)blockIdx.x < blocks) {
+        count_block<true>(a, blockIdx.x);
+        return;
+    }
+    __shared__ int s_token[64];
+    __shared__ size_t s_head[64];                  // of a token's page: number * Hkv
+    __shared__ float s_ratio[2][HEADS][64];
+    __shared__ unsigned s_runs[4];                 // bit i of word t: token 16 t + i begins a run of neighbours in one cell
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int P = 1 << a.pshift, d = a.pg.d, Hkv = a.pg.Hkv, parts = (Hkv + HEADS - 1) / HEADS;
+    const size_t head_bytes = (size_t)P * d;
+    const long long items = (long long)a.w.head[1] * parts;
+    for (long long it = blockIdx.x - blocks; it < items; it += gridDim.x - blocks) {
+        const int k = (int)(it / parts), h0 = (int)(it % parts) * HEADS, entry = a.w.made[k], dst = a.w.page[k];
+        if (!is_page(a, dst)) continue;   // the caller's pool names no page: nothing is written
+        const int b = entry / a.max_pages, j = entry % a.max_pages, n = min(P, a.w.stay[b] - j * P);
+        const size_t row = (size_t)b * a.max_pages;
+        __syncthreads();   // what the last item had in LDS has been read
+        if (wave == 0) {
+            const Group *group = a.w.group + (row << a.pshift) / 16;
+            const int groups = (tokens_of(a, b) + 15) / 16;
+            int u = a.w.start[row + j];
+            bool more = true;
+            while (more) {   // 64 groups a round, until the page's last token
+                const Group g = u + lane < groups ? group[u + lane] : Group{0, 0};
+                int o = g.rank - j * P;
+                for (unsigned m = g.bits; m; m &= m - 1, ++o)
+                    if (o >= 0 && o < n) s_token[o] = 16 * (u + lane) + __builtin_ctz(m);
+                u += 64;
+                more = u < groups && __builtin_amdgcn_readlane(o, 63) < n;
             }
-            float km = ks, vm = vs;
+            __builtin_amdgcn_wave_barrier();
+            const int t = lane < n ? s_token[lane] : -2, before = __shfl_up(t, 1, 64);
+            const unsigned long long runs = __ballot(lane < n && ((lane & 15) == 0 || (t & 15) == 0 || t != before + 1));
+            if (lane < 4) s_runs[lane] = (unsigned)(runs >> (16 * lane)) & 0xFFFFu;
+            const size_t src = lane < n ? (size_t)a.w.old[row + (t >> a.pshift)] * Hkv : 0;
+            s_head[lane] = src;
 #pragma unroll
-            for (int o = 1; o < 64; o *= 2) {
-                km = largest(km, shfl_xor(km, o));
-                vm = largest(vm, shfl_xor(vm, o));
-            }
-            s_src[tid] = src;
-            s_off[tid] = off;
-            s_ratio[0][tid] = ks / km;
-            s_ratio[1][tid] = vs / vm;
-            if (tid == 0) {
-                a.pg.kscale[(size_t)dst * Hkv + h] = km;
-                a.pg.vscale[(size_t)dst * Hkv + h] = vm;
-            }
-        }
-        __syncthreads();
-        const size_t head = (size_t)P * d;
-        auto at = [&](uint8_t *x, int page) { return x + ((size_t)page * Hkv + h) * head; };
-        for (int u = tid; u < P * d / 16; u += 256) {   // K: cell (tb, db), token o of it
-            const int tb = u / d, db = u / 16 % (d / 16), t = tb * 16 + u % 16;
-            u32x4 y = {0, 0, 0, 0};
-            if (t < n) {
-                const int off = s_off[t];
-                const float ratio = s_ratio[0][t];
-                y = *(const u32x4 *)(at(a.pg.K8, s_src[t]) + ((off >> 4) * (d / 16) + db) * 256 + (off & 15) * 16);
-                if (ratio != 1.0f)
+            for (int i = 0; i < HEADS; ++i) {
+                const int h = min(h0 + i, Hkv - 1);
+                const float ks = lane < n ? a.pg.kscale[src + h] : 0.0f, vs = lane < n ? a.pg.vscale[src + h] : 0.0f;
+                float km = ks, vm = vs;
 #pragma unroll
-                    for (int q = 0; q < 4; ++q) y[q] = carried(y[q], ratio);
-            }
-            ((u32x4 *)at(a.pg.K8, dst))[u] = y;
-        }
-        for (int u = tid; u < P * d / 16; u += 256) {   // V: cell (tb, db), coordinate c of it
-            const int tb = u / d, db = u / 16 % (d / 16), c = u % 16;
-            u32x4 y;
-#pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                unsigned w = 0;
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const int t = tb * 16 + 4 * q + i;
-                    if (t >= n) continue;
-                    const int off = s_off[t];
-                    const float ratio = s_ratio[1][t];
-                    unsigned x = at(a.pg.V8, s_src[t])[((off >> 4) * (d / 16) + db) * 256 + c * 16 + (off & 15)];
-                    if (ratio != 1.0f) x = carried(x, ratio) & 0xFFu;
-                    w |= x << (8 * i);
+                for (int o = 1; o < 64; o *= 2) {
+                    km = largest(km, shfl_xor(km, o));
+                    vm = largest(vm, shfl_xor(vm, o));
                 }
-                y[q] = w;
+                s_ratio[0][i][lane] = ks / km;
+                s_ratio[1][i][lane] = vs / vm;
+                if (lane == 0) {
+                    a.pg.kscale[(size_t)dst * Hkv + h] = km;
+                    a.pg.vscale[(size_t)dst * Hkv + h] = vm;
+                }
             }
-            ((u32x4 *)at(a.pg.V8, dst))[u] = y;
+        }
+        __syncthreads();
+        const int units = P * d / 16;   // 16-byte pieces of a head: in cell (tb, db), token or coordinate u % 16 of it
+        for (int i = 0; i < HEADS; ++i) {
+            const int h = h0 + i;
+            if (h >= Hkv) break;
+            const size_t to = ((size_t)dst * Hkv + h) * head_bytes;
+            for (int u = tid; u < units; u += 256) {
+                const int tb = u / d, db = u / 16 % (d / 16), t = tb * 16 + u % 16;
+                u32x4 y = {0, 0, 0, 0};
+                if (t < n) {
+                    const int off = s_token[t] & (P - 1);
+                    const float ratio = s_ratio[0][i][t];
+                    y = *(const u32x4 *)(a.pg.K8 + (s_head[t] + h) * head_bytes + ((off >> 4) * (d / 16) + db) * 256 + (off & 15) * 16);
+                    if (ratio != 1.0f) y = carried(y, ratio);
+                }
+                ((u32x4 *)(a.pg.K8 + to))[u] = y;
+            }
+            // V: a wavefront's pieces are of the same 16 tokens; a run's bytes are brought to their places by the address that they are loaded from
+            for (int u = tid; u < units; u += 256) {
+                const int tb = __builtin_amdgcn_readfirstlane(u / d), db = u / 16 % (d / 16), c = u % 16;
+                const unsigned runs = __builtin_amdgcn_readfirstlane(s_runs[tb]);
+                const int there = min(max(n - 16 * tb, 0), 16);
+                u32x4 y = {0, 0, 0, 0};
+                for (unsigned m = runs; m; m &= m - 1) {
+                    const int o = __builtin_ctz(m), rest = m & (m - 1) ? __builtin_ctz(m & (m - 1)) : there;   // the run is [o, rest)
+                    const int t = 16 * tb + o, off = __builtin_amdgcn_readfirstlane(s_token[t]) & (P - 1);
+                    const float ratio = s_ratio[1][i][t];
+                    const uint8_t *p = a.pg.V8 + (s_head[t] + h) * head_bytes + ((off >> 4) * (d / 16) + db) * 256 + c * 16;
+                    u32x4 w = *(const u32x4 *)p;
+                    if (ratio != 1.0f) w = carried(w, ratio);
+                    const int s = o - (off & 15);   // bytes up (or down)
+                    __uint128_t v = ((__uint128_t)((uint64_t)w[3] << 32 | w[2]) << 64) | ((uint64_t)w[1] << 32 | w[0]);
+                    v = s >= 0 ? v << (8 * s) : v >> (-8 * s);
+                    const __uint128_t all = ~(__uint128_t)0, mask = (rest < 16 ? ~(all << (8 * rest)) : all) & (all << (8 * o));
+                    v &= mask;
+                    y[0] |= (unsigned)v, y[1] |= (unsigned)(v >> 32), y[2] |= (unsigned)(v >> 64), y[3] |= (unsigned)(v >> 96);
+                }
+                ((u32x4 *)(a.pg.V8 + to))[u] = y;
+            }
         }
     }
 }
@@ -531,6 +606,8 @@ size_t pages_ws_bytes(int B, int max_pages, int n_pages, int P) {
     share::Work w;
     return share::lay_out(w, nullptr, B, max_pages, n_pages, P);
 }
+
+constexpr int SUM_ALL = 4096;   // blocks of entries up to which each sums up the counts of those before it
 
 // What kv_pages_free and kv_pages_compact ask of their arguments alike.
 static int share_check(const int32_t *len, const int32_t *table, int B, int max_pages, const int32_t *pool, const int32_t *pool_n, int n_pages,
@@ -552,7 +629,9 @@ static share::Args share_args(const int32_t *len, const int32_t *table, int B, i
     a.len_out = len_out, a.pool_out = pool_out, a.pool_n_out = pool_n_out, a.status = status;
     a.B = B, a.max_pages = max_pages, a.n_pages = n_pages, a.pshift = __builtin_ctz((unsigned)P);
     a.segs = (max_pages + share::ET - 1) / share::ET;
-    share::lay_out(a.w, (int32_t *)ws, B, max_pages, n_pages, P);
+    a.summed = B * a.segs > SUM_ALL;
+    a.admitted = B > share::ADMIT_ALL;
+    share::lay_out(a.w, (char *)ws, B, max_pages, n_pages, P);
     return a;
 }
 static int nothing(const share::Args &a, hipStream_t s) {
@@ -560,15 +639,14 @@ static int nothing(const share::Args &a, hipStream_t s) {
     FASTAR_LAUNCH_CHECK();
     return FASTAR_OK;
 }
-// Pages given back by the blocks of entries: counted, summed up, pushed.
+// The blocks' counts summed up, if there are too many for every block to do so, and the pages pushed.
 template <bool COMPACT>
-static int give_back(const share::Args &a, hipStream_t s) {
-    const dim3 grid((unsigned)(a.B * a.segs));
-    hipLaunchKernelGGL((share::give_kernel<COMPACT, false>), grid, dim3(256), 0, s, a);
-    FASTAR_LAUNCH_CHECK();
-    hipLaunchKernelGGL(share::scan_kernel, dim3(1), dim3(1024), 0, s, a.w.block, a.B * a.segs);
-    FASTAR_LAUNCH_CHECK();
-    hipLaunchKernelGGL((share::give_kernel<COMPACT, true>), grid, dim3(256), 0, s, a);
+static int push(const share::Args &a, hipStream_t s) {
+    if (a.summed) {
+        hipLaunchKernelGGL(share::scan_kernel, dim3(1), dim3(1024), 0, s, a.w.block, a.B * a.segs);
+        FASTAR_LAUNCH_CHECK();
+    }
+    hipLaunchKernelGGL((share::push_kernel<COMPACT>), dim3((unsigned)(a.B * a.segs)), dim3(share::ET), 0, s, a);
     FASTAR_LAUNCH_CHECK();
     return FASTAR_OK;
 }
@@ -617,13 +695,15 @@ extern "C" int kv_pages_free(const int32_t *keep, const int32_t *len, const int3
     a.keep = keep;
     const hipStream_t s = (hipStream_t)stream;
     const dim3 grid((unsigned)(B * a.segs));
-    hipLaunchKernelGGL(share::clear_kernel, dim3((unsigned)((n_pages + 255) / 256)), dim3(256), 0, s, a.w, n_pages);
+    hipLaunchKernelGGL(share::clear_kernel, dim3((unsigned)((n_pages + 255) / 256)), dim3(256), 0, s, a);
     FASTAR_LAUNCH_CHECK();
-    hipLaunchKernelGGL(share::hold_kernel, grid, dim3(256), 0, s, a);
+    hipLaunchKernelGGL(share::hold_kernel, grid, dim3(share::ET), 0, s, a);
     FASTAR_LAUNCH_CHECK();
-    hipLaunchKernelGGL(share::cut_kernel, grid, dim3(256), 0, s, a);
+    hipLaunchKernelGGL(share::cut_kernel, grid, dim3(share::ET), 0, s, a);
     FASTAR_LAUNCH_CHECK();
-    return give_back<false>(a, s);
+    hipLaunchKernelGGL(share::count_kernel, grid, dim3(share::ET), 0, s, a);
+    FASTAR_LAUNCH_CHECK();
+    return push<false>(a, s);
 }
 
 extern "C" int kv_pages_compact(const fastar_pages *pages, const uint8_t *keep, const int32_t *len, const int32_t *table, int B, int max_pages,
@@ -641,15 +721,16 @@ extern "C" int kv_pages_compact(const fastar_pages *pages, const uint8_t *keep, 
     a.mask = keep;
     a.table_out = table_out;
     const hipStream_t s = (hipStream_t)stream;
-    hipLaunchKernelGGL(share::clear_kernel, dim3((unsigned)((a.n_pages + 255) / 256)), dim3(256), 0, s, a.w, a.n_pages);
-    FASTAR_LAUNCH_CHECK();
+    const unsigned blocks = (unsigned)(B * a.segs);
     hipLaunchKernelGGL(share::mask_kernel, dim3((unsigned)B), dim3(1024), 0, s, a);
     FASTAR_LAUNCH_CHECK();
-    hipLaunchKernelGGL(share::admit_kernel, dim3(1), dim3(1024), 0, s, a);
+    if (a.admitted) {
+        hipLaunchKernelGGL(share::admit_kernel, dim3(1), dim3(1024), 0, s, a);
+        FASTAR_LAUNCH_CHECK();
+    }
+    hipLaunchKernelGGL(share::relink_kernel, dim3(blocks), dim3(share::ET), 0, s, a);
     FASTAR_LAUNCH_CHECK();
-    hipLaunchKernelGGL(share::relink_kernel, dim3((unsigned)(B * a.segs)), dim3(256), 0, s, a);
+    hipLaunchKernelGGL(share::gather_kernel, dim3(blocks + 2048), dim3(256), 0, s, a, (int)blocks);
     FASTAR_LAUNCH_CHECK();
-    hipLaunchKernelGGL(share::gather_kernel, dim3(2048), dim3(256), 0, s, a);
-    FASTAR_LAUNCH_CHECK();
-    return give_back<true>(a, s);
+    return push<true>(a, s);
 }
