@@ -84,6 +84,7 @@ extern "C" int fastar_init(void) {
     if (rc == FASTAR_OK) rc = fastar::prompt_setup();
     if (rc == FASTAR_OK) rc = fastar::prompt_f32_setup();
     if (rc == FASTAR_OK) rc = fastar::paged_chunk_setup();
+    if (rc == FASTAR_OK) rc = fastar::share_setup();
     return rc;
 }
 

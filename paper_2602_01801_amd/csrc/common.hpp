@@ -228,6 +228,7 @@ int attn_fp8_setup();
 int prompt_setup();
 int prompt_f32_setup();
 int paged_chunk_setup();
+int share_setup();
 
 // Host-side launch check shared by the entry points.
 #define FASTAR_LAUNCH_CHECK()                          \

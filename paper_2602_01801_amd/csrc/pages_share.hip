@@ -153,6 +153,11 @@ struct Group {
     int32_t rank;
     uint32_t bits;
 };
+// A fresh page: its number, its request and how many groups that has, the group of its first token, which of the request's new tokens that is,
+// and how many it holds.
+struct Fresh {
+    int32_t page, b, groups, start, first, n, unused[2];
+};
 // What a call needs in memory between its launches, cut out of the workspace.
 struct Work {
     PageState *state;                        // [n_pages]
@@ -161,7 +166,7 @@ struct Work {
     int32_t *head;                           // [4] free pages before, fresh pages in all
     int32_t *block;                          // pages that a block gives back
     int32_t *old, *link, *from, *start;      // [B, max_pages] table before the call; new page of an old one; old page of a new one, or ~(which fresh one), and the group of its first token
-    int32_t *made, *page;                    // [n_pages] fresh pages: entry of the new table, number
+    Fresh *made;                             // [n_pages]
 };
 inline size_t lay_out(Work &w, char *p, int64_t B, int64_t max_pages, int64_t n_pages, int64_t P) {
     size_t at = 0;
@@ -182,7 +187,6 @@ inline size_t lay_out(Work &w, char *p, int64_t B, int64_t max_pages, int64_t n_
     take(w.from, B * max_pages);
     take(w.start, B * max_pages);
     take(w.made, n_pages);
-    take(w.page, n_pages);
     take(w.group, (size_t)(B * max_pages) * P / 16);
     return at;
 }
@@ -193,6 +197,7 @@ struct Args {
     const int32_t *keep, *len, *table, *pool, *pool_n;
     int32_t *len_out, *table_out, *pool_out, *pool_n_out, *status;
     int32_t B, max_pages, n_pages, pshift, segs;   // segs: blocks of entries per row
+    bool one_pushes;                               // a workgroup pushes for all blocks
     bool summed, admitted;                         // block, and base and status, have been worked out by a launch of their own
     Work w;
 };
@@ -274,6 +279,82 @@ __device__ __forceinline__ void count_block(const Args &a, int block) {
     if (threadIdx.x == 0) a.w.block[block] = n;
 }
 __global__ __launch_bounds__(ET) void count_kernel(Args a) { count_block<false>(a, blockIdx.x); }
+
+// All of kv_pages_free by one workgroup, where no more than ONE_TABLE entries can be held and pages' states fit its LDS: entries of all requests in
+// one sequence, ONE_ENTRIES per thread, whose pages stay in registers from one round of atomics to the next.  Three trips to memory instead of
+// five launches: 50 / 640 / 7872 entries 5.0 / 7.7 / 12.6 us, and 8.7 / 10.7 / 11.9 by launches that follow one another at once; a program that
+// launches each by itself waits 20 us for five.  (In more rounds, 15360 entries 43 us and 12.)
+constexpr int ONE = 1024, ONE_ENTRIES = 8, ONE_TABLE = ONE * ONE_ENTRIES, ONE_PAGES = 16384;   // threads, also requests; pages: 128 KB
+__global__ __launch_bounds__(ONE) void free_one_kernel(Args a) {
+    extern __shared__ int s_left[];          // holders, less those that give the page up
+    int *s_last = s_left + a.n_pages;        // the last of the latter
+    __shared__ int part[ONE / 64], s_have[ONE], s_stay[ONE];   // s_have: inclusive sums of the requests' pages
+    const int tid = threadIdx.x, P = 1 << a.pshift, free0 = clipped(a.pool_n[0], a.n_pages);
+    int L = 0, stay = 0;
+    if (tid < a.B) {
+        L = tokens_of(a, tid);
+        stay = clipped(a.keep[tid], L);
+    }
+    const int have = (L + P - 1) >> a.pshift;
+    const int cut = stay < L && (stay & (P - 1)) ? a.table[(size_t)tid * a.max_pages + (stay >> a.pshift)] : -1;
+    for (int i = tid; i < a.n_pages; i += ONE) s_left[i] = 0, s_last[i] = -1;
+    int total;
+    s_have[tid] = wg_incl_scan<ONE>(have, part, &total);
+    __syncthreads();
+    int page[ONE_ENTRIES], who[ONE_ENTRIES], at[ONE_ENTRIES];   // neighbours in the sequence, so that sums over threads go by it
+#pragma unroll
+    for (int i = 0; i < ONE_ENTRIES; ++i) {
+        const int x = tid * ONE_ENTRIES + i;
+        page[i] = -1;
+        if (x >= total) continue;
+        int lo = 0, hi = a.B - 1;
+        while (lo < hi) {
+            const int mid = (lo + hi) >> 1;
+            if (s_have[mid] > x) hi = mid;
+            else lo = mid + 1;
+        }
+        who[i] = lo;
+        at[i] = x - (lo ? s_have[lo - 1] : 0);
+        page[i] = a.table[(size_t)lo * a.max_pages + at[i]];
+    }
+#pragma unroll
+    for (int i = 0; i < ONE_ENTRIES; ++i)
+        if (is_page(a, page[i])) atomicAdd(&s_left[page[i]], 1);
+    __syncthreads();
+    const bool refused = is_page(a, cut) && s_left[cut] > 1;
+    if (refused) stay = L;
+    s_stay[tid] = (stay + P - 1) >> a.pshift;
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < ONE_ENTRIES; ++i) {
+        if (!is_page(a, page[i])) continue;
+        if (at[i] < s_stay[who[i]]) page[i] = -1;
+        else {
+            atomicAdd(&s_left[page[i]], -1);
+            atomicMax(&s_last[page[i]], tid * ONE_ENTRIES + i);
+        }
+    }
+    __syncthreads();
+    int n = 0;
+#pragma unroll
+    for (int i = 0; i < ONE_ENTRIES; ++i) {
+        if (is_page(a, page[i]) && (s_left[page[i]] != 0 || s_last[page[i]] != tid * ONE_ENTRIES + i)) page[i] = -1;
+        n += is_page(a, page[i]);
+    }
+    int all;
+    int to = free0 + wg_incl_scan<ONE>(n, part, &all) - n;
+#pragma unroll
+    for (int i = 0; i < ONE_ENTRIES; ++i)
+        if (is_page(a, page[i])) {
+            if (to < a.n_pages) a.pool_out[to] = page[i];
+            ++to;
+        }
+    if (tid < a.B) {
+        a.len_out[tid] = stay;
+        a.status[tid] = refused;
+    }
+    if (tid == 0) a.pool_n_out[0] = min(free0 + all, a.n_pages);
+}
 // They go to the pool, behind those of the blocks before, and what is known only now is written over what may be the call's input.
 template <bool COMPACT>
 __global__ __launch_bounds__(ET) void push_kernel(Args a) {
@@ -296,6 +377,30 @@ __global__ __launch_bounds__(ET) void push_kernel(Args a) {
     if (p >= 0 && at < a.n_pages) a.pool_out[at] = p;
     if (e == 0) a.len_out[b] = a.w.stay[b];
     if (last && threadIdx.x == 0) a.pool_n_out[0] = (int)min((long long)top + s_before + all, (long long)a.n_pages);
+}
+// Few blocks: a workgroup pushes for all of them, without counts;  thinning out, beside the workgroups that move tokens.
+constexpr int PUSH_ALL = 16;
+template <bool COMPACT>
+__device__ __forceinline__ void push_all(const Args &a, int blocks) {
+    __shared__ int s_part[ET / 64];
+    int top = a.w.head[0] - (COMPACT ? a.w.head[1] : 0);
+    int p[PUSH_ALL];
+#pragma unroll
+    for (int i = 0; i < PUSH_ALL; ++i) {
+        int b, e;
+        entry_of(a, i, b, e);
+        p[i] = i < blocks ? given_back<COMPACT>(a, b, e) : -1;
+        if (i < blocks && e == 0) a.len_out[b] = a.w.stay[b];
+    }
+#pragma unroll
+    for (int i = 0; i < PUSH_ALL; ++i) {
+        if (i >= blocks) break;
+        int all;
+        const long long at = (long long)top + wg_incl_scan<ET>(p[i] >= 0, s_part, &all) - 1;
+        if (p[i] >= 0 && at < a.n_pages) a.pool_out[at] = p[i];
+        top = (int)min((long long)top + all, (long long)a.n_pages);
+    }
+    if (threadIdx.x == 0) a.pool_n_out[0] = top;
 }
 // Exclusive prefix sums of n numbers, and their sum behind them.
 __global__ __launch_bounds__(1024) void scan_kernel(int32_t *x, int n) {
@@ -436,7 +541,7 @@ __global__ __launch_bounds__(ET) void relink_kernel(Args a) {
     int stay = a.w.stay[b];
     const int old = e < have ? a.w.old[at] : -1, link = e < have ? a.w.link[at] : 0, was = e < a.max_pages ? a.table[at] : -1;
     const bool is_new = e < (stay + (1 << a.pshift) - 1) >> a.pshift;   // unless the request is refused
-    const int from = is_new ? a.w.from[at] : 0;
+    const int from = is_new ? a.w.from[at] : 0, start = is_new ? a.w.start[at] : 0;
     const int free0 = clipped(a.pool_n[0], a.n_pages);
     int base;
     if (a.admitted) base = a.w.base[b];
@@ -474,8 +579,7 @@ __global__ __launch_bounds__(ET) void relink_kernel(Args a) {
             else {
                 const int k = base + ~from;
                 p = a.pool[free0 - 1 - k];
-                a.w.made[k] = (int)at;
-                a.w.page[k] = p;
+                a.w.made[k] = Fresh{p, b, (tokens_of(a, b) + 15) / 16, start, e << a.pshift, min(1 << a.pshift, stay - (e << a.pshift)), {0, 0}};
             }
         }
         a.table_out[at] = p;
@@ -497,110 +601,189 @@ __device__ __forceinline__ u32x4 carried(u32x4 w, float ratio) {
     return u32x4{carried(w[0], ratio), carried(w[1], ratio), carried(w[2], ratio), carried(w[3], ratio)};
 }
 
-// The first workgroups count the pages that blocks of entries give back; the others fill fresh pages, one with HEADS heads after the other: its tokens'
-// places, their scales, then the 16 bytes of a token (K) or of a coordinate (V) per thread.
-constexpr int HEADS = 2;
-__global__ __launch_bounds__(256) void gather_kernel(Args a, int blocks) {
-    if ((int)blockIdx.x < blocks) {
+// A mask of the bytes below n of eight.
+__device__ __forceinline__ uint64_t bytes_below(int n) { return n >= 8 ? ~0ull : n > 0 ? (1ull << (8 * n)) - 1ull : 0ull; }
+struct __attribute__((packed, aligned(1))) Bytes16 {
+    u32x4 w;
+};
+
+// The first workgroups count the pages that blocks of entries give back; the others fill fresh pages, `heads` heads of one after the other, PIECES
+// times 16 bytes per thread: of a token (K) and of a coordinate (V).  Bound by the trips to memory of an item: what it is -> groups of tokens -> old pages ->
+// codes and, beside them, scales;  so codes are asked for before the scales are there, all of an item's K and the first two runs of its V.
+// (An item's heads one after the other, scales first: 54 us for 109 MB of codes in whole pages, 75 for 96 MB in short runs.)
+constexpr int PIECES = 4, MAX_HEADS = 16;   // 1024 pieces of a page are 2 heads of 64 x 128, 16 of 16 x 64
+__global__ __launch_bounds__(256, 4) void gather_kernel(Args a, int blocks, int heads) {
+    if (a.one_pushes) {
+        if (blockIdx.x == 0) {
+            push_all<true>(a, blocks);
+            return;
+        }
+        blocks = 1;   // the workgroups before those that move tokens
+    } else if ((int)blockIdx.x < blocks) {
         count_block<true>(a, blockIdx.x);
         return;
     }
     __shared__ int s_token[64];
     __shared__ size_t s_head[64];                  // of a token's page: number * Hkv
-    __shared__ float s_ratio[2][HEADS][64];
+    __shared__ float s_ratio[2][MAX_HEADS][64];
+    __shared__ int s_edges;                        // whether some are of the first or the last page
     __shared__ unsigned s_runs[4];                 // bit i of word t: token 16 t + i begins a run of neighbours in one cell
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int P = 1 << a.pshift, d = a.pg.d, Hkv = a.pg.Hkv, parts = (Hkv + HEADS - 1) / HEADS;
-    const size_t head_bytes = (size_t)P * d;
+    const int P = 1 << a.pshift, dshift = a.pg.d == 128 ? 7 : 6, ushift = a.pshift + dshift - 4, Hkv = a.pg.Hkv, parts = (Hkv + heads - 1) / heads;
+    const size_t head_bytes = (size_t)P << dshift;
     const long long items = (long long)a.w.head[1] * parts;
+    auto uniform = [](int x) { return __builtin_amdgcn_readfirstlane(x); };
     for (long long it = blockIdx.x - blocks; it < items; it += gridDim.x - blocks) {
-        const int k = (int)(it / parts), h0 = (int)(it % parts) * HEADS, entry = a.w.made[k], dst = a.w.page[k];
+        const int h0 = (int)(it % parts) * heads, mine = min(heads, Hkv - h0);
+        const Fresh f = a.w.made[it / parts];
+        const int dst = uniform(f.page), n = uniform(f.n);
         if (!is_page(a, dst)) continue;   // the caller's pool names no page: nothing is written
-        const int b = entry / a.max_pages, j = entry % a.max_pages, n = min(P, a.w.stay[b] - j * P);
-        const size_t row = (size_t)b * a.max_pages;
+        const size_t row = (size_t)f.b * a.max_pages;
         __syncthreads();   // what the last item had in LDS has been read
         if (wave == 0) {
             const Group *group = a.w.group + (row << a.pshift) / 16;
-            const int groups = (tokens_of(a, b) + 15) / 16;
-            int u = a.w.start[row + j];
+            int u = f.start;
             bool more = true;
             while (more) {   // 64 groups a round, until the page's last token
-                const Group g = u + lane < groups ? group[u + lane] : Group{0, 0};
-                int o = g.rank - j * P;
+                const Group g = u + lane < f.groups ? group[u + lane] : Group{0, 0};
+                int o = g.rank - f.first;
                 for (unsigned m = g.bits; m; m &= m - 1, ++o)
                     if (o >= 0 && o < n) s_token[o] = 16 * (u + lane) + __builtin_ctz(m);
                 u += 64;
-                more = u < groups && __builtin_amdgcn_readlane(o, 63) < n;
+                more = u < f.groups && __builtin_amdgcn_readlane(o, 63) < n;
             }
             __builtin_amdgcn_wave_barrier();
             const int t = lane < n ? s_token[lane] : -2, before = __shfl_up(t, 1, 64);
             const unsigned long long runs = __ballot(lane < n && ((lane & 15) == 0 || (t & 15) == 0 || t != before + 1));
             if (lane < 4) s_runs[lane] = (unsigned)(runs >> (16 * lane)) & 0xFFFFu;
-            const size_t src = lane < n ? (size_t)a.w.old[row + (t >> a.pshift)] * Hkv : 0;
-            s_head[lane] = src;
+            const int src = lane < n ? a.w.old[row + (t >> a.pshift)] : -1;
+            s_head[lane] = (size_t)max(src, 0) * Hkv;
+            const bool edge = __any(src == 0 || src == a.n_pages - 1);
+            if (lane == 0) s_edges = edge;
+        }
+        __syncthreads();
+        const bool edges = uniform(s_edges);
+        float ks[MAX_HEADS / 4], vs[MAX_HEADS / 4];   // a token per lane, every fourth head
 #pragma unroll
-            for (int i = 0; i < HEADS; ++i) {
-                const int h = min(h0 + i, Hkv - 1);
-                const float ks = lane < n ? a.pg.kscale[src + h] : 0.0f, vs = lane < n ? a.pg.vscale[src + h] : 0.0f;
-                float km = ks, vm = vs;
+        for (int i = 0; i < MAX_HEADS / 4; ++i)
+            if (wave + 4 * i < mine) {
+                const size_t at = s_head[lane] + h0 + wave + 4 * i;
+                ks[i] = lane < n ? a.pg.kscale[at] : 0.0f;
+                vs[i] = lane < n ? a.pg.vscale[at] : 0.0f;
+            }
+        // pieces tid + 256 r of the item's: head, cell (tb, db), token or coordinate of it.  A wavefront's are of the same 16 tokens.
+        u32x4 k[PIECES], v[PIECES][2];
+        int hh[PIECES], tb[PIECES], c[PIECES], first[PIECES], behind[PIECES], last[PIECES];
+        unsigned m[PIECES];
+        auto run_of = [&](int r, int &o, int &e) __attribute__((always_inline)) {   // the next run: [o, e) of the 16 tokens
+            o = __builtin_ctz(m[r]);
+            m[r] &= m[r] - 1;
+            e = m[r] ? __builtin_ctz(m[r]) : min(n - 16 * tb[r], 16);
+        };
+        // A run's bytes are brought to their places by the address that they are loaded from, some bytes in front of or behind their coordinate's.
+        // In the array's first and last page those may lie outside of it: such runs are brought there by shifts, when they are put.
+        auto place_of = [&](int r, int o, int &s) __attribute__((always_inline)) {
+            const int t = 16 * tb[r] + o, off = uniform(s_token[t]) & (P - 1);
+            s = o - (off & 15);
+            return a.pg.V8 + (s_head[t] + h0 + hh[r]) * head_bytes + ((off >> 4) << (dshift + 4)) + c[r];
+        };
+        auto ask = [&](int r, int o) __attribute__((always_inline)) {
+            int s;
+            const uint8_t *p = place_of(r, o, s);
+            const uint8_t *q = p - s;   // without a branch, behind which loads would be waited for one by one
+            if (edges) q = p;
+            return ((const Bytes16 *)q)->w;
+        };
+        auto shifted = [&](int r, int o, u32x4 x) __attribute__((always_inline)) {
+            int s;
+            place_of(r, o, s);
+            __uint128_t y = ((__uint128_t)((uint64_t)x[3] << 32 | x[2]) << 64) | ((uint64_t)x[1] << 32 | x[0]);
+            y = s >= 0 ? y << (8 * s) : y >> (-8 * s);
+            return u32x4{(unsigned)y, (unsigned)(y >> 32), (unsigned)(y >> 64), (unsigned)(y >> 96)};
+        };
+#pragma unroll
+        for (int r = 0; r < PIECES; ++r) {
+            const int x = tid + 256 * r, u = x & ((1 << ushift) - 1), t = (u >> dshift) * 16 + u % 16;
+            hh[r] = uniform(x >> ushift);
+            tb[r] = uniform(u >> dshift);
+            c[r] = (u >> 4 & ((1 << dshift) / 16 - 1)) * 256 + u % 16 * 16;
+            k[r] = u32x4{0, 0, 0, 0};
+            if (hh[r] < mine && t < n) {
+                const int off = s_token[t] & (P - 1);
+                k[r] = *(const u32x4 *)(a.pg.K8 + (s_head[t] + h0 + hh[r]) * head_bytes + ((off >> 4) << (dshift + 4)) + (c[r] & ~255) + (off & 15) * 16);
+            }
+        }
+#pragma unroll
+        for (int r = 0; r < PIECES; ++r) {
+            m[r] = hh[r] < mine ? uniform(s_runs[tb[r]]) : 0;
+            first[r] = behind[r] = last[r] = 0;
+            if (m[r]) {
+                int o;
+                run_of(r, o, behind[r]);
+                v[r][0] = ask(r, o);
+                if (m[r]) {
+                    run_of(r, first[r], last[r]);
+                    v[r][1] = ask(r, first[r]);
+                }
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < MAX_HEADS / 4; ++i)
+            if (wave + 4 * i < mine) {
+                const int h = wave + 4 * i;
+                float km = ks[i], vm = vs[i];
 #pragma unroll
                 for (int o = 1; o < 64; o *= 2) {
                     km = largest(km, shfl_xor(km, o));
                     vm = largest(vm, shfl_xor(vm, o));
                 }
-                s_ratio[0][i][lane] = ks / km;
-                s_ratio[1][i][lane] = vs / vm;
+                s_ratio[0][h][lane] = ks[i] / km;
+                s_ratio[1][h][lane] = vs[i] / vm;
                 if (lane == 0) {
-                    a.pg.kscale[(size_t)dst * Hkv + h] = km;
-                    a.pg.vscale[(size_t)dst * Hkv + h] = vm;
+                    a.pg.kscale[(size_t)dst * Hkv + h0 + h] = km;
+                    a.pg.vscale[(size_t)dst * Hkv + h0 + h] = vm;
                 }
             }
-        }
         __syncthreads();
-        const int units = P * d / 16;   // 16-byte pieces of a head: in cell (tb, db), token or coordinate u % 16 of it
-        for (int i = 0; i < HEADS; ++i) {
-            const int h = h0 + i;
-            if (h >= Hkv) break;
-            const size_t to = ((size_t)dst * Hkv + h) * head_bytes;
-            for (int u = tid; u < units; u += 256) {
-                const int tb = u / d, db = u / 16 % (d / 16), t = tb * 16 + u % 16;
-                u32x4 y = {0, 0, 0, 0};
-                if (t < n) {
-                    const int off = s_token[t] & (P - 1);
-                    const float ratio = s_ratio[0][i][t];
-                    y = *(const u32x4 *)(a.pg.K8 + (s_head[t] + h) * head_bytes + ((off >> 4) * (d / 16) + db) * 256 + (off & 15) * 16);
-                    if (ratio != 1.0f) y = carried(y, ratio);
-                }
-                ((u32x4 *)(a.pg.K8 + to))[u] = y;
+#pragma unroll
+        for (int r = 0; r < PIECES; ++r) {
+            if (hh[r] >= mine) continue;
+            const int x = tid + 256 * r, u = x & ((1 << ushift) - 1), t = tb[r] * 16 + u % 16;
+            const float ratio = s_ratio[0][hh[r]][min(t, n - 1)];
+            if (ratio != 1.0f) k[r] = carried(k[r], ratio);
+            const size_t to = ((size_t)dst * Hkv + h0 + hh[r]) * head_bytes + (size_t)u * 16;
+            *(u32x4 *)(a.pg.K8 + to) = k[r];
+            u32x4 y = {0, 0, 0, 0};
+            auto put = [&](u32x4 w, int o, int e) __attribute__((always_inline)) {
+                if (edges) w = shifted(r, o, w);
+                const float by = s_ratio[1][hh[r]][16 * tb[r] + o];
+                if (by != 1.0f) w = carried(w, by);
+                const uint64_t lo = bytes_below(e) & ~bytes_below(o), hi = bytes_below(e - 8) & ~bytes_below(o - 8);
+                y[0] |= w[0] & (unsigned)lo, y[1] |= w[1] & (unsigned)(lo >> 32), y[2] |= w[2] & (unsigned)hi, y[3] |= w[3] & (unsigned)(hi >> 32);
+            };
+            if (behind[r]) put(v[r][0], 0, behind[r]);   // the first run begins a cell
+            if (last[r]) put(v[r][1], first[r], last[r]);
+            while (m[r]) {
+                int o, e;
+                run_of(r, o, e);
+                put(ask(r, o), o, e);
             }
-            // V: a wavefront's pieces are of the same 16 tokens; a run's bytes are brought to their places by the address that they are loaded from
-            for (int u = tid; u < units; u += 256) {
-                const int tb = __builtin_amdgcn_readfirstlane(u / d), db = u / 16 % (d / 16), c = u % 16;
-                const unsigned runs = __builtin_amdgcn_readfirstlane(s_runs[tb]);
-                const int there = min(max(n - 16 * tb, 0), 16);
-                u32x4 y = {0, 0, 0, 0};
-                for (unsigned m = runs; m; m &= m - 1) {
-                    const int o = __builtin_ctz(m), rest = m & (m - 1) ? __builtin_ctz(m & (m - 1)) : there;   // the run is [o, rest)
-                    const int t = 16 * tb + o, off = __builtin_amdgcn_readfirstlane(s_token[t]) & (P - 1);
-                    const float ratio = s_ratio[1][i][t];
-                    const uint8_t *p = a.pg.V8 + (s_head[t] + h) * head_bytes + ((off >> 4) * (d / 16) + db) * 256 + c * 16;
-                    u32x4 w = *(const u32x4 *)p;
-                    if (ratio != 1.0f) w = carried(w, ratio);
-                    const int s = o - (off & 15);   // bytes up (or down)
-                    __uint128_t v = ((__uint128_t)((uint64_t)w[3] << 32 | w[2]) << 64) | ((uint64_t)w[1] << 32 | w[0]);
-                    v = s >= 0 ? v << (8 * s) : v >> (-8 * s);
-                    const __uint128_t all = ~(__uint128_t)0, mask = (rest < 16 ? ~(all << (8 * rest)) : all) & (all << (8 * o));
-                    v &= mask;
-                    y[0] |= (unsigned)v, y[1] |= (unsigned)(v >> 32), y[2] |= (unsigned)(v >> 64), y[3] |= (unsigned)(v >> 96);
-                }
-                ((u32x4 *)(a.pg.V8 + to))[u] = y;
-            }
+            *(u32x4 *)(a.pg.V8 + to) = y;
         }
     }
 }
 
 }  // namespace share
 
+// Lets kv_pages_free use as much LDS as its pages' states need.
+int share_setup() {
+    static DeviceOnce once;
+    return once.run([](int) {
+        return hipFuncSetAttribute((const void *)share::free_one_kernel, hipFuncAttributeMaxDynamicSharedMemorySize, 2 * sizeof(int) * share::ONE_PAGES) == hipSuccess
+                   ? FASTAR_OK
+                   : FASTAR_ERR_HIP;
+    });
+}
 size_t pages_ws_bytes(int B, int max_pages, int n_pages, int P) {
     if (B < 0 || max_pages <= 0 || n_pages <= 0 || !page_size_ok(P)) return 0;
     share::Work w;
@@ -629,6 +812,7 @@ static share::Args share_args(const int32_t *len, const int32_t *table, int B, i
     a.len_out = len_out, a.pool_out = pool_out, a.pool_n_out = pool_n_out, a.status = status;
     a.B = B, a.max_pages = max_pages, a.n_pages = n_pages, a.pshift = __builtin_ctz((unsigned)P);
     a.segs = (max_pages + share::ET - 1) / share::ET;
+    a.one_pushes = B * a.segs <= share::PUSH_ALL;
     a.summed = B * a.segs > SUM_ALL;
     a.admitted = B > share::ADMIT_ALL;
     share::lay_out(a.w, (char *)ws, B, max_pages, n_pages, P);
@@ -694,6 +878,12 @@ extern "C" int kv_pages_free(const int32_t *keep, const int32_t *len, const int3
     if (B == 0) return nothing(a, (hipStream_t)stream);
     a.keep = keep;
     const hipStream_t s = (hipStream_t)stream;
+    if (B <= share::ONE && (int64_t)B * max_pages <= share::ONE_TABLE && n_pages <= share::ONE_PAGES) {
+        if (const int rc = share_setup(); rc != FASTAR_OK) return rc;
+        hipLaunchKernelGGL(share::free_one_kernel, dim3(1), dim3(share::ONE), 2 * sizeof(int) * (size_t)n_pages, s, a);
+        FASTAR_LAUNCH_CHECK();
+        return FASTAR_OK;
+    }
     const dim3 grid((unsigned)(B * a.segs));
     hipLaunchKernelGGL(share::clear_kernel, dim3((unsigned)((n_pages + 255) / 256)), dim3(256), 0, s, a);
     FASTAR_LAUNCH_CHECK();
@@ -730,7 +920,9 @@ extern "C" int kv_pages_compact(const fastar_pages *pages, const uint8_t *keep, 
     }
     hipLaunchKernelGGL(share::relink_kernel, dim3(blocks), dim3(share::ET), 0, s, a);
     FASTAR_LAUNCH_CHECK();
-    hipLaunchKernelGGL(share::gather_kernel, dim3(blocks + 2048), dim3(256), 0, s, a, (int)blocks);
+    const int heads = std::min(pages->Hkv, 256 * share::PIECES * 16 / (pages->P * pages->d));
+    const int64_t items = std::min<int64_t>((int64_t)B * max_pages, a.n_pages) * ((pages->Hkv + heads - 1) / heads);   // at most
+    hipLaunchKernelGGL(share::gather_kernel, dim3((a.one_pushes ? 1 : blocks) + (unsigned)std::min<int64_t>(items, 2048)), dim3(256), 0, s, a, (int)blocks, heads);
     FASTAR_LAUNCH_CHECK();
-    return push<true>(a, s);
+    return a.one_pushes ? FASTAR_OK : push<true>(a, s);
 }
