@@ -153,6 +153,38 @@ def test_many_sequences_and_heads():
     check_rows(ok, K, rope.k_weight, rope, freq, at, True)
 
 
+def test_more_heads_than_a_wavefront_takes():
+    """264 heads of 64 and 4100 tokens, some rows of magnitudes that are done again; the same in place."""
+    g = torch.Generator().manual_seed(13)
+    Hq, n, d = 264, 4100, 64
+    Q = torch.randn((n, Hq, d), generator=g).bfloat16().cuda()
+    rows = [0, 1, 77, 2050, 4099]
+    for r in rows:
+        Q[r, ::3] *= 1e30
+        Q[r, 1::7] *= 1e-30
+    rope, freq, _ = make_rope(g, d, 32, True)
+    pos = i32([list(range(n))])
+    Q = Q.transpose(0, 1)
+    out = fa.qk_norm_rope(Q, None, rope, pos=pos)[0]
+    some = rows + [5, 1000, 3333]
+    check_rows(out[:, some], Q[:, some], rope.q_weight, rope, freq, np.array(some, float)[:, None] * np.ones(16), True)
+    fa.qk_norm_rope(Q, None, rope, pos=pos, out=(Q, None))
+    assert torch.equal(Q, out)
+
+
+@pytest.mark.parametrize("weight", [1e-25, 1e25])
+def test_in_place_rows_are_done_once(weight):
+    """Rows whose outputs would be done again if they were inputs."""
+    g = torch.Generator().manual_seed(14)
+    d, n = 128, 9
+    Q = view(g, 6, n, d, torch.float32, "tokens")
+    Q[:, 4] *= 1e30
+    rope = fa.Rope(torch.from_numpy(sref.frequencies(d)).cuda(), q_weight=weights(g, d) * weight)
+    out = fa.qk_norm_rope(Q, None, rope, pos=i32([list(range(n))]))[0]
+    fa.qk_norm_rope(Q, None, rope, pos=i32([list(range(n))]), out=(Q, None))
+    assert torch.equal(Q, out) and torch.isfinite(Q).all()
+
+
 # ------------------------------------------------------------------------------------------------ into pages
 
 
@@ -240,6 +272,26 @@ def test_write_rope_of_numbers_that_are_not_finite(dtype, d, P):
             a, b = getattr(pages, name), getattr(want, name)
             assert torch.equal(torch.where(a & 127 == 127, 127, a), torch.where(b & 127 == 127, 127, b)), name
         assert torch.equal(pages.kscale, want.kscale) and torch.equal(pages.vscale, want.vscale)
+
+
+def test_prompts_whose_queries_have_a_launch_of_their_own():
+    g = torch.Generator().manual_seed(15)
+    rng = np.random.default_rng(15)
+    q, k, P, d, Hq, Hkv = [5000, 3, 3700], [0, 9, 5], 64, 128, 64, 2
+    n = sum(q)
+    slot, n_pages = slots_of(rng, q, k, P)
+    x = torch.randn((n, Hq + 2 * Hkv, d), generator=g).bfloat16().cuda()
+    assert x.numel() * 2 >= 150000000
+    Q, K, V = (y.transpose(0, 1) for y in x.split([Hq, Hkv, Hkv], 1))
+    rope, _, _ = make_rope(g, d, d)
+    cu, length = i32(prefix(q).tolist()), i32([a + b for a, b in zip(q, k)])
+    pages = make_pages(rng, n_pages, Hkv, P, d)
+    want = clone(pages)
+    out = fa.kv_pages_write_rope(pages, i32(slot), Q, K, V, rope, cu=cu, length=length)
+    assert torch.equal(out, fa.qk_norm_rope(Q, None, rope, cu=cu, length=length)[0])
+    fa.kv_pages_write(want, i32(slot), fa.qk_norm_rope(None, K.float(), rope, cu=cu, length=length)[1], V.float())
+    for name in ("K8", "kscale", "V8", "vscale"):
+        assert torch.equal(getattr(pages, name), getattr(want, name)), name
 
 
 def test_positions_on_axes_into_pages():

@@ -225,6 +225,28 @@ def test_compact_of_many_requests():
     assert 0 in want[4] and 1 in want[4]
 
 
+def test_more_requests_than_workgroups_sum_up():
+    """Blocks of entries whose counts are summed by a launch of their own."""
+    rng = np.random.default_rng(8)
+    P, W, B = 16, 2, 4500
+    lens = [int(rng.integers(0, W * P + 1)) for _ in range(B)]
+    table, pool, free, n_pages = layout(rng, lens, W, P, 5000, share=0.2)
+    keep = [int(rng.choice([0, n, max(0, n - 1), n // 2])) for n in lens]
+    run_free(keep, lens, table, pool, free, P)
+    pages = make_pages(rng, n_pages, 1, P, 64)
+    run_compact(pages, rng.random((B, W * P)) < 0.7, lens, table, pool, free, P, in_place=True)
+
+
+@pytest.mark.parametrize("P,d,Hkv", [(16, 64, 20), (32, 64, 9), (16, 128, 9), (64, 128, 1), (32, 128, 4)])
+def test_compact_of_many_heads(P, d, Hkv):
+    """More heads than an item takes, and fewer."""
+    rng = np.random.default_rng(P + Hkv)
+    lens = [5 * P - 2, 3 * P + 1]
+    table, pool, free, n_pages = layout(rng, lens, 6, P, 12)
+    pages = make_pages(rng, n_pages, Hkv, P, d)
+    run_compact(pages, rng.random((2, 6 * P)) < 0.6, lens, table, pool, free, P)
+
+
 def test_compact_keeps_what_a_code_says():
     """Every code, NaN and both zeros among them, over pages of equal scales: carried bit by bit, and rounded where the scales differ."""
     rng = np.random.default_rng(5)
