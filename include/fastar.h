@@ -570,7 +570,7 @@ typedef struct {
  *   pos [n_axes, n_tok] int32 positions, negative ones too; an axis that is none goes as the nearest.  NULL: row i of the a rows
  *       of sequence b is at position len[b] - a + i on every axis (the last row is the sequence's last token).
  *   cu [B+1], len [B]: the sequences, where pos is NULL.  With pos: cu NULL (and B = 0): all rows;  otherwise rows outside of every
- *       sequence are neither read nor written, and len may be NULL.
+ *       sequence are not written, whatever they hold, and len may be NULL.
  * An output may be its input (the same address and strides); otherwise they share no memory.
  * Rows that hold infinities or NaN give what the formula gives, in that row alone; a row of zeros with eps = 0 is NaN.
  * Supported: d in {64, 128}; n_tok <= 2^30; n_tok times 1 .. (Hq + Hkv) * d / 512 wavefronts in 2^32 threads.  No workspace.
@@ -647,7 +647,7 @@ int kv_pages_free(const int32_t *keep, const int32_t *len, const int32_t *table,
  *   status [B]                0 or 1
  *   ws / ws_bytes             as for kv_pages_free
  * Keys keep the positions that they were rotated by.  Lengths and counts are cut to what the arrays hold.
- * Supported: as for kv_pages_free.
+ * Supported: as for kv_pages_free, max_pages * P <= 2^30.
  */
 int kv_pages_compact(const fastar_pages *pages, const uint8_t *keep, const int32_t *len, const int32_t *table, int B, int max_pages,
                      const int32_t *pool, const int32_t *pool_n, int32_t *len_out, int32_t *table_out, int32_t *pool_out, int32_t *pool_n_out,

@@ -904,6 +904,7 @@ extern "C" int kv_pages_compact(const fastar_pages *pages, const uint8_t *keep, 
     if (const int rc = share_check(len, table, B, max_pages, pool, pool_n, pages->n_pages, pages->P, len_out, pool_n_out, status, ws, ws_bytes);
         rc != FASTAR_OK)
         return rc;
+    if ((int64_t)max_pages * pages->P > MAX_KEYS) return FASTAR_ERR_UNSUPPORTED;   // positions a round beyond a request's end are 32-bit
     if (!pool_out || (B > 0 && (!keep || ((uintptr_t)keep & 15) || !table_out))) return FASTAR_ERR_INVALID_ARG;
     share::Args a = share_args(len, table, B, max_pages, pool, pool_n, pages->n_pages, pages->P, len_out, pool_out, pool_n_out, status, ws);
     if (B == 0) return nothing(a, (hipStream_t)stream);

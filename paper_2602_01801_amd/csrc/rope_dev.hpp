@@ -40,22 +40,8 @@ __device__ __forceinline__ float row_max(float v) {   // of numbers that are not
     return __uint_as_float(u);
 }
 
-// Sequence of row t, cu[0] <= t < cu[B]: the number of the offsets cu[1 ..] that are not beyond t.  A wavefront together, 64 offsets a round.
-__device__ __forceinline__ int sequence_of(const int32_t *__restrict__ cu, int B, int t) {
-    const int lane = lane_id();
-    int lo = 0, n = B;
-    while (n > 1) {   // uniform; n falls to ceil(n / 64)
-        const int step = (n + 63) / 64;
-        const long long j = (long long)(lane + 1) * step;
-        const bool passed = j < n && cu[lo + j] <= t;
-        const int c = __builtin_popcountll(__ballot(passed));
-        lo += c * step;
-        n = min(step, n - c * step);
-    }
-    return lo;
-}
-// The sequences of a call, a lane each while there are no more than 64: their offsets and lengths are asked for at once, so that a wavefront
-// waits for one trip to memory instead of three.
+// Sequences of a call, a lane each: their offsets and lengths are asked for at once, so that a wavefront waits for one trip to memory while there are
+// no more than 64, and for one more for every factor of 64.
 struct Places {
     int begin, end, len;
 };
@@ -67,18 +53,24 @@ struct Place {
 // Differences and sums of lengths that are the caller's, whatever they are.
 __device__ __forceinline__ int less(int a, int b) { return (int)((unsigned)a - (unsigned)b); }
 __device__ __forceinline__ int plus(int a, int b) { return (int)((unsigned)a + (unsigned)b); }
-__device__ __forceinline__ Places places_of(const RopeArgs &r) {
-    if (!r.cu || r.B > 64) return Places{0, 0, 0};
-    const int b = min(lane_id(), r.B - 1);   // lanes beyond the sequences repeat the last one
+__device__ __forceinline__ Places places_from(const RopeArgs &r, int lo, int n) {
+    const int b = lo + min(lane_id(), n - 1);   // lanes beyond the sequences repeat the last one
     return Places{r.cu[b], r.cu[b + 1], r.rot > 0 && !r.pos ? r.len[b] : 0};
 }
-__device__ __forceinline__ Place place_of(const RopeArgs &r, const Places &p, int t) {
+__device__ __forceinline__ Places places_of(const RopeArgs &r) { return !r.cu || r.B > 64 ? Places{0, 0, 0} : places_from(r, 0, r.B); }
+__device__ __forceinline__ Place place_of(const RopeArgs &r, Places p, int t) {
     if (!r.cu) return Place{true, 0, r.n_tok};
     if (r.B > 64) {
-        if (t < r.cu[0] || t >= r.cu[r.B]) return Place{false, 0, 0};
-        if (r.rot == 0 || r.pos) return Place{true, 0, r.n_tok};
-        const int b = sequence_of(r.cu, r.B, t), end = min(r.cu[b + 1], r.n_tok);
-        return Place{true, less(r.len[b], end), end};
+        int lo = 0, n = r.B;   // t is a row of sequences lo .. lo + n - 1, if of any
+        while (n > 64) {       // uniform; every step leaves a 64th
+            const int step = (n + 63) / 64;
+            const long long j = (long long)(lane_id() + 1) * step;
+            const bool passed = j < n && r.cu[lo + j] <= t;
+            const int c = __builtin_popcountll(__ballot(passed));
+            lo += c * step;
+            n = min(step, n - c * step);
+        }
+        p = places_from(r, lo, n);
     }
     const unsigned long long here = __ballot(p.begin <= t && t < p.end);
     if (!here) return Place{false, 0, 0};
@@ -220,6 +212,10 @@ struct Raw8 {
     __device__ __forceinline__ void load(const char *row, const RopeLane &l) {
         a = *(const Piece *)(row + l.a * (BF16 ? 2 : 4));
         b = *(const Piece *)(row + l.b * (BF16 ? 2 : 4));
+    }
+    __device__ __forceinline__ void load(const char *base, unsigned row, const RopeLane &l) {   // from a uniform base
+        a = *(const Piece *)(base + (row + (unsigned)l.a * (BF16 ? 2 : 4)));
+        b = *(const Piece *)(base + (row + (unsigned)l.b * (BF16 ? 2 : 4)));
     }
     __device__ __forceinline__ void to(float (&x)[8]) const {
 #pragma unroll

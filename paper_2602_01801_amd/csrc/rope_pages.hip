@@ -78,7 +78,7 @@ __device__ __forceinline__ void rope_k_run(const RopeArgs &r, const Run &run, in
     Raw8<BF16> raw[IT];
     if (touches) {
 #pragma unroll
-        for (int i = 0; i < IT; ++i) raw[i].load(run.row0 + (unsigned)row_at(i * RPI + lr) * (unsigned)run.pitch, rl);
+        for (int i = 0; i < IT; ++i) raw[i].load(run.row0, (unsigned)row_at(i * RPI + lr) * (unsigned)run.pitch, rl);
     }
     const Place place = place_of(r, places, t0);
     const bool derived = !r.pos && t0 + e - o <= place.end;   // positions follow one another

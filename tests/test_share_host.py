@@ -129,6 +129,10 @@ def test_compact_refuses(L, over, code):
     assert thin(L, **over) == code
 
 
+def test_positions_of_a_mask_stay_in_32_bits_a_round_ahead(L):
+    assert thin(L, B=1, max_pages=(1 << 24) + 1) == UNSUPPORTED and thin(L, B=1, max_pages=(1 << 25) - 1) == UNSUPPORTED
+
+
 def test_workspace_of_shared_pages(L):
     from paper_2602_01801_amd import OP_PAGES, workspace_bytes
     need = workspace_bytes(OP_PAGES, 3, 4, 10, 64)
