@@ -47,7 +47,9 @@ struct ForkArgs {
 
 // Every workgroup works the whole call out for itself: which forks are refused, and which pages the others take.  Then the first one
 // of a fork writes its table row, the others a part each of its last page's copy, and the first of all lengths and counts,
-// or, where those are written in place, a workgroup of a second launch (FINISH), so that nobody reads them changed.
+// or, where those are written in place, a workgroup of a second launch (FINISH), so that nobody reads them changed.  Bound by the trips to memory before the
+// copies (forks -> lengths -> tables -> pool), which a launch of its own would only put in front of another one's: 4 forks 4.8 us, 128 forks with 33 MB of last pages
+// 8.6 (3.8 TB/s).
 template <bool FINISH>
 __global__ __launch_bounds__(FT) void fork_kernel(ForkArgs a, bool finish_here) {
     __shared__ int part[FT / 64];
@@ -141,6 +143,9 @@ __global__ __launch_bounds__(FT) void fork_kernel(ForkArgs a, bool finish_here) 
 
 // ---- giving pages up --------------------------------------------------------------------------------------------
 
+// Who holds a page is counted from the tables, by atomics whose order does not show: holders (hold_kernel), who is refused and who gives up (cut_kernel), how many pages
+// each block gives back (count_kernel), where they go (push_kernel).  Bound by trips to memory and by the launches: 192 requests on 8000 entries 2.4 + 2.8 + 3.5 + 3.7 + 4.8 us,
+// 96 on 102000 3.0 + 5.8 + 7.0 + 4.0 + 5.8.
 // Table entries are looked at in blocks of ET, each within a request's row: entry e of request b has number b * max_pages + e.
 constexpr int ET = 256;
 
@@ -426,7 +431,8 @@ __global__ __launch_bounds__(256) void nothing_kernel(Args a) {
 
 // A workgroup per request goes through its mask, 64 tokens per thread: how many are kept before every group of 16, which pages stay whole,
 // which of the new ones are fresh and where their tokens begin.  It keeps the old table row, as the new one may be written over it.  Whoever has a
-// new page's first token writes about that page, so that nothing has to be cleared before, and all loads of a round are one trip to memory.
+// new page's first token writes about that page, so that nothing has to be cleared before, and all loads of a round are one trip to memory: three requests of up
+// to 37440 tokens 5.3 us.  (16 tokens per thread and a list of every token's place: 15; its stores, four bytes apart by lanes sixteen apart, were most of it.)
 __global__ __launch_bounds__(1024) void mask_kernel(Args a) {
     __shared__ int part[16];
     const int b = blockIdx.x, tid = threadIdx.x, P = 1 << a.pshift;
@@ -531,7 +537,8 @@ __global__ __launch_bounds__(1024) void admit_kernel(Args a) {
     }
 }
 
-// New table rows, the list of fresh pages, the holders of old pages and those that give them up, and the pool as it was.
+// New table rows, the list of fresh pages, the holders of old pages and those that give them up, and the pool as it was.  A trip to memory after the
+// other, 5.5 us.
 __global__ __launch_bounds__(ET) void relink_kernel(Args a) {
     __shared__ int part[ET / 64];
     int b, e;
@@ -610,7 +617,8 @@ struct __attribute__((packed, aligned(1))) Bytes16 {
 // The first workgroups count the pages that blocks of entries give back; the others fill fresh pages, `heads` heads of one after the other, PIECES
 // times 16 bytes per thread: of a token (K) and of a coordinate (V).  Bound by the trips to memory of an item: what it is -> groups of tokens -> old pages ->
 // codes and, beside them, scales;  so codes are asked for before the scales are there, all of an item's K and the first two runs of its V.
-// (An item's heads one after the other, scales first: 54 us for 109 MB of codes in whole pages, 75 for 96 MB in short runs.)
+// 112 MB of codes of three windows 52 us (4.1 TB/s read and written), 98 MB in runs of 14 tokens 58 (whole cells of V are read: 4.2 TB/s).  (An item's heads one after the
+// other, scales first: 54 and 75;  a branch between the loads, so that each is waited for: 65 and 75;  three wavefronts per SIMD 55 and 65, five spill: 93.)
 constexpr int PIECES = 4, MAX_HEADS = 16;   // 1024 pieces of a page are 2 heads of 64 x 128, 16 of 16 x 64
 __global__ __launch_bounds__(256, 4) void gather_kernel(Args a, int blocks, int heads) {
     if (a.one_pushes) {

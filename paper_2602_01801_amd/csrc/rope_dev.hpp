@@ -2,7 +2,7 @@
 //   y = x (mean x^2 + eps)^-1/2 w;   pair (a, b) of coordinates -> (a cos t - b sin t, a sin t + b cos t), t = pos * freq
 // A row is d / 8 neighbouring lanes with two pieces of four coordinates each, rot / 2 apart where pairs are, so that every lane has both
 // coordinates of its four pairs and none are exchanged.  (Eight neighbouring coordinates per lane, swapped with the lane of the other
-// half before and after, took 176 vector instructions per lane where this takes 75: 34612 tokens x 40 heads 134 us, of which 100 were these.)
+// half before and after, took 176 vector instructions per lane and row where this takes 75, which was most of the time: 34612 tokens x 40 heads 100 us of 134.)
 #pragma once
 
 #include "packed.hpp"
