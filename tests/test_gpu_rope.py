@@ -274,6 +274,31 @@ def test_write_rope_of_numbers_that_are_not_finite(dtype, d, P):
         assert torch.equal(pages.kscale, want.kscale) and torch.equal(pages.vscale, want.vscale)
 
 
+@pytest.mark.parametrize("dtype,d,P,eps", [("bf16", 128, 64, 1e-6), ("f32", 64, 16, 0.0), ("f32", 128, 32, 1e-6)])
+def test_write_rope_of_rows_of_any_magnitude(dtype, d, P, eps):
+    """Keys of zeros, and those whose squares leave the range, among others of their pages and alone on one."""
+    g = torch.Generator().manual_seed(16)
+    rng = np.random.default_rng(16)
+    q, k, Hkv = [70, 1, 33, 64], [5, 30, 0, 0], 2
+    n = sum(q)
+    slot, n_pages = slots_of(rng, q, k, P)
+    K, V = view(g, Hkv, n, d, torch.float32, "tokens"), view(g, Hkv, n, d, torch.float32, "tokens")
+    for t, x in ((3, 1e30), (20, 1e-30), (40, 1e-38), (70, 1e25), (80, 1e37), (81, 1e-45)):
+        K[:, t] *= x
+    if eps:
+        K[:, 50], K[1, 104:168], V[0, 104:168] = 0.0, 0.0, 0.0
+    K, V = K.to(DT[dtype]), V.to(DT[dtype])
+    for norm in (True, False):
+        rope, _, _ = make_rope(g, d, d // 2, norm, eps=eps)
+        cu, length = i32(prefix(q).tolist()), i32([a + b for a, b in zip(q, k)])
+        pages = make_pages(rng, n_pages, Hkv, P, d)
+        want = clone(pages)
+        fa.kv_pages_write_rope(pages, i32(slot), None, K, V, rope, cu=cu, length=length)
+        fa.kv_pages_write(want, i32(slot), fa.qk_norm_rope(None, K.float(), rope, cu=cu, length=length)[1], V.float())
+        for name in ("K8", "kscale", "V8", "vscale"):
+            assert torch.equal(getattr(pages, name), getattr(want, name)), (norm, name)
+
+
 def test_prompts_whose_queries_have_a_launch_of_their_own():
     g = torch.Generator().manual_seed(15)
     rng = np.random.default_rng(15)
