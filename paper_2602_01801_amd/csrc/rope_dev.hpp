@@ -153,23 +153,23 @@ __device__ __forceinline__ float inverse_root(float ss, float eps) {
     const float v = fmaf(ss, 1.0f / D, eps), q = __builtin_amdgcn_rsqf(v);
     return fmaf(0.5f * q, fmaf(-v * q, q, 1.0f), q);
 }
-// x w turned and times inv; pairs that do not turn have c = 1, s = 0.
+// x inv w turned; pairs that do not turn have c = 1, s = 0.
 template <bool INTER>
 __device__ __forceinline__ void turned(const Turn &t, const Weights &w, float inv, float (&x)[8]) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         const int ia = INTER ? 2 * i : i, ib = INTER ? 2 * i + 1 : 4 + i;
-        const float a = x[ia] * w.w[ia], b = x[ib] * w.w[ib];
-        x[ia] = fmaf(a, t.c[i], -(b * t.s[i])) * inv;
-        x[ib] = fmaf(a, t.s[i], b * t.c[i]) * inv;
+        const float a = x[ia] * inv * w.w[ia], b = x[ib] * inv * w.w[ib];
+        x[ia] = fmaf(a, t.c[i], -(b * t.s[i]));
+        x[ib] = fmaf(a, t.s[i], b * t.c[i]);
     }
 }
-// A lane's eight coordinates of a row: normed and turned, all lanes of a row together.  Not of rows whose squares leave the range or that hold
-// infinities or NaN: those come back true, and are done again by norm_and_turn_odd.
+// A lane's eight coordinates of a row: normed and turned, all lanes of a row together.  Not of rows whose squares leave the range (upwards or, where eps does
+// not rule them, downwards) or that hold infinities or NaN: those come back true, and are done again by norm_and_turn_odd.
 template <int D, bool INTER>
 __device__ __forceinline__ bool norm_and_turn(const RopeArgs &r, const Turn &t, const Weights &w, float (&x)[8]) {
     const float ss = squares<D>(x);
-    const bool odd = !(ss >= (r.norm ? 0x1p-80f : 0.0f) && ss < 0x1p120f);
+    const bool odd = !(ss >= (r.norm && r.eps < 0x1p-80f ? 0x1p-80f : 0.0f) && ss < 0x1p120f);
     turned<INTER>(t, w, r.norm ? inverse_root<D>(ss, r.eps) : 1.0f, x);
     return odd;
 }
