@@ -626,7 +626,7 @@ int kv_pages_fork(const fastar_pages *pages, const int32_t *parent, const int32_
  *   ws / ws_bytes     fastar_workspace_bytes(FASTAR_OP_PAGES, B, max_pages, n_pages, P, ...) bytes, 256-byte aligned; contents need not be
  *                     kept.  Calls that may be in flight at the same time need a workspace each.
  * Lengths and counts are cut to what the arrays hold; pages beyond what the pool can hold are lost.
- * Supported: B * max_pages < 2^31; P and n_pages as for kv_pages_plan.
+ * Supported: B * max_pages < 2^31; B * ceil(max_pages / 256) < 2^22; P and n_pages as for kv_pages_plan.
  */
 int kv_pages_free(const int32_t *keep, const int32_t *len, const int32_t *table, int B, int max_pages, int32_t *pool, const int32_t *pool_n,
                   int n_pages, int P, int32_t *len_out, int32_t *pool_n_out, int32_t *status, void *ws, size_t ws_bytes, void *stream);

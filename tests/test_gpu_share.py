@@ -359,6 +359,51 @@ def test_requests_that_share_grow_thin_out_and_end():
     accounts()
 
 
+@pytest.mark.parametrize("seed,P,B,W,n_pages", [(0, 16, 9, 14, 40), (1, 32, 40, 6, 150), (2, 16, 20, 500, 3000), (3, 64, 3, 9, 20)])
+def test_a_long_life_of_many_requests(seed, P, B, W, n_pages):
+    """Plans, forks, cuts and masks in any order, everything in place, step by step against the references; codes go where tables say."""
+    rng = np.random.default_rng(seed)
+    pages = make_pages(rng, n_pages, 1, P, 64)
+    K, ks, V, vs = (x.cpu().numpy().copy() for x in (pages.K8, pages.kscale, pages.V8, pages.vscale))
+    table, length = [[-1] * W for _ in range(B)], [0] * B
+    pool, free = [int(p) for p in rng.permutation(n_pages)], n_pages
+    dt, dl, dp, dn = i32(table), i32(length), i32(pool), i32([free])
+    for step in range(80):
+        what = rng.choice(4, p=[0.4, 0.25, 0.15, 0.2])
+        if what == 0:
+            n_new = [int(rng.choice([0, 1, P, rng.integers(0, W * P // 2 + 1)])) for _ in range(B)]
+            after, free, _, _, status = ref.plan(n_new, length, table, pool, free, P, 10 ** 6)
+            got = fa.kv_pages_plan(i32(n_new), dl, dt, dp, dn, P, sum(n_new), out=(dl, dn, i32([0] * (B + 1)), i32([-1] * sum(n_new)), i32([0] * B)))[4]
+        elif what == 1:
+            n = int(rng.integers(1, 6))
+            parent, empty = rng.integers(-1, B + 1, n).tolist(), [b for b in range(B) if not length[b]]
+            child, keep = rng.choice(empty + [-1, B, 0], n).tolist(), rng.integers(-3, W * P, n).tolist()
+            after, free, status, copies = sref.fork(parent, child, keep, length, table, pool, free, P, n_pages)
+            for x in (K, ks, V, vs):
+                old = x.copy()
+                for a, b in copies:
+                    x[b] = old[a]
+            got = fa.kv_pages_fork(pages, i32(parent), i32(child), dl, dt, dp, dn, keep=i32(keep), out=(dl, dn, i32([9] * n)))[2]
+        elif what == 2:
+            keep = [int(rng.choice([0, n, max(0, n - rng.integers(40))], p=[0.2, 0.4, 0.4])) for n in length]
+            after, free, status = sref.free(keep, length, table, pool, free, P, n_pages)
+            got = fa.kv_pages_free(i32(keep), dl, dt, dp, dn, P, out=(dl, dn, i32([9] * B)))[2]
+        else:
+            keep = np.repeat(rng.random((B, W * P // 16)) < rng.choice([0.5, 0.9]), 16, 1) ^ (rng.random((B, W * P)) < 0.01)
+            after, table, pool, free, status, made = sref.compact(keep, length, table, pool, free, P, n_pages)
+            sref.compact_codes(K, ks, False, made)
+            sref.compact_codes(V, vs, True, made)
+            got = fa.kv_pages_compact(pages, torch.from_numpy(keep.astype(np.uint8)).cuda(), dl, dt, dp, dn, out=(dl, dt, dp, dn, i32([9] * B)))[4]
+        length = after
+        assert ints(got) == status, step
+        assert ints(dl) == length and ints(dn) == [free] and ints(dp)[:free] == pool[:free], step
+        assert sref.held(ints(dt), length, n_pages, P) == sref.held(table, length, n_pages, P), step
+        for x, y in ((pages.K8, K), (pages.kscale, ks), (pages.V8, V), (pages.vscale, vs)):
+            assert np.array_equal(x.cpu().numpy(), y), step
+        holders = [p for row in sref.held(table, length, n_pages, P) for p in row]
+        assert not set(holders) & set(pool[:free]) and sorted(set(holders) | set(pool[:free])) == list(range(n_pages)), step
+
+
 def test_replayed_from_a_graph():
     """Fork, thin out and end, captured once with everything in place and replayed on other lengths and masks."""
     rng = np.random.default_rng(6)
