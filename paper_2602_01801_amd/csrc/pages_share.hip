@@ -745,8 +745,8 @@ __global__ __launch_bounds__(256, 4) void gather_kernel(Args a, int blocks, int 
                     km = largest(km, shfl_xor(km, o));
                     vm = largest(vm, shfl_xor(vm, o));
                 }
-                s_ratio[0][h][lane] = ks[i] / km;
-                s_ratio[1][h][lane] = vs[i] / vm;
+                s_ratio[0][h][lane] = ks[i] == km ? 1.0f : ks[i] / km;   // both may be 0: of a page that nothing has been written to
+                s_ratio[1][h][lane] = vs[i] == vm ? 1.0f : vs[i] / vm;
                 if (lane == 0) {
                     a.pg.kscale[(size_t)dst * Hkv + h0 + h] = km;
                     a.pg.vscale[(size_t)dst * Hkv + h0 + h] = vm;

@@ -273,6 +273,22 @@ def test_compact_keeps_what_a_code_says():
     assert np.array_equal(pages.kscale.cpu().numpy(), ks) and np.array_equal(pages.vscale.cpu().numpy(), vs)
 
 
+def test_compact_of_pages_that_nothing_was_written_to():
+    """Tokens that have been counted but not written: scales are zero, alone in a fresh page or beside others."""
+    rng = np.random.default_rng(12)
+    P, W = 16, 5
+    table, pool, free, n_pages = layout(rng, [5 * P, 4 * P + 3], W, P, 12)
+    pages = make_pages(rng, n_pages, 3, P, 64)
+    for code, scale in ((pages.K8, pages.kscale), (pages.V8, pages.vscale)):
+        for p in table[0][1:] + table[1][3:]:
+            if 0 <= p < n_pages:
+                code[p], scale[p] = 0, 0
+    keep = np.ones((2, W * P), bool)
+    keep[:, ::3] = False
+    run_compact(pages, keep, [5 * P, 4 * P + 3], table, pool, free, P)
+    assert (pages.kscale == 0).any() and not ((pages.K8 & 127) == 127).any() and not ((pages.V8 & 127) == 127).any()
+
+
 def test_compact_of_nobody():
     pages = fa.Pages.empty(4, 1, 16, 64)
     got = fa.kv_pages_compact(pages, torch.zeros((0, 32), dtype=torch.uint8, device="cuda"), i32([]), i32([]).view(0, 2), i32([1, 2, 3, -1]), i32([3]))
