@@ -289,6 +289,27 @@ def test_compact_of_pages_that_nothing_was_written_to():
     assert (pages.kscale == 0).any() and not ((pages.K8 & 127) == 127).any() and not ((pages.V8 & 127) == 127).any()
 
 
+@pytest.mark.parametrize("P,B,W", [(16, 4, 9), (16, 300, 30), (64, 12, 1000), (16, 4500, 2)])
+def test_more_pages_than_the_pool_can_hold(P, B, W):
+    """A count that says that more is free than the tables leave: pages are lost, and nothing is written behind the pool, which is longer than the call's."""
+    rng = np.random.default_rng(B + W)
+    lens = [int(rng.integers(1, min(W, 40) * P + 1)) for _ in range(B)]
+    table, pool, free, n_pages = layout(rng, lens, W, P, 9, share=0.3)
+    held = n_pages - free
+    pool = [p if p >= 0 else int(rng.integers(n_pages)) for p in pool]
+    for pool_n in (n_pages, n_pages - 1, n_pages - held // 3):
+        behind = i32(pool + [-77] * 5000)
+        want_pool = list(pool)
+        after, n, status = sref.free([0] * B, lens, table, want_pool, pool_n, P, n_pages)
+        got = fa.kv_pages_free(i32([0] * B), i32(lens), i32(table), behind[:n_pages], i32([pool_n]), P)
+        assert n == n_pages and ints(got[1]) == [n] and ints(got[0]) == after and ints(got[2]) == status
+        assert ints(behind) == want_pool + [-77] * 5000
+    pages = make_pages(rng, n_pages, 1, P, 64)
+    keep = np.zeros((B, W * P), bool)
+    keep[:, :P] = True      # whole pages stay: no page is taken
+    run_compact(pages, keep, [n // P * P for n in lens], table, pool, n_pages - held // 3, P, in_place=True)
+
+
 def test_compact_of_nobody():
     pages = fa.Pages.empty(4, 1, 16, 64)
     got = fa.kv_pages_compact(pages, torch.zeros((0, 32), dtype=torch.uint8, device="cuda"), i32([]), i32([]).view(0, 2), i32([1, 2, 3, -1]), i32([3]))
