@@ -572,7 +572,8 @@ typedef struct {
  *   cu [B+1], len [B]: the sequences, where pos is NULL.  With pos: cu NULL (and B = 0): all rows;  otherwise rows outside of every
  *       sequence are not written, whatever they hold, and len may be NULL.
  * An output may be its input (the same address and strides); otherwise they share no memory.
- * Rows that hold infinities or NaN give what the formula gives, in that row alone; a row of zeros with eps = 0 is NaN.
+ * Rows that hold infinities or NaN give what the formula gives, in that row alone; a row of zeros with eps = 0 is NaN.  Weights that are infinite or
+ * NaN reach the coordinates that the formula brings them to, and no others.
  * Supported: d in {64, 128}; n_tok <= 2^30; n_tok times 1 .. (Hq + Hkv) * d / 512 wavefronts in 2^32 threads.  No workspace.
  */
 int qk_norm_rope(const fastar_rows *Q, const fastar_rows *K, const int32_t *pos, const int32_t *cu, const int32_t *len, int B,

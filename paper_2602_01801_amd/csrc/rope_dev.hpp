@@ -139,6 +139,15 @@ struct Weights {
 #pragma unroll
         for (int e = 0; e < 4; ++e) w[e] = p ? p[l.a + e] : 1.0f, w[4 + e] = p ? p[l.b + e] : 1.0f;
     }
+    // Whether some of the row's weights are so large that a normed coordinate times them may leave the range, or are no numbers.  A coordinate that does not
+    // turn goes through the turn with c = 1, s = 0 like any other, where its lane's other coordinate times 0 has to be 0; so every row is then done as
+    // norm_and_turn_odd does it.  The same in all lanes, as a row is done again as a whole (an output may be its input).
+    __device__ __forceinline__ bool wild() const {
+        unsigned top = 0;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) top = max(top, __float_as_uint(fabsf(w[e])));
+        return __any(top >= __float_as_uint(0x1p100f));
+    }
 };
 template <int D>
 __device__ __forceinline__ float squares(const float (&x)[8]) {
@@ -287,6 +296,7 @@ __device__ __forceinline__ void rope_token(const RopeArgs &r, const RopeViews &a
         if (first + i * step < n) ask(first + i * step, raw[i]);
     const Place place = place_of(r, places, t);
     if (!place.there) return;
+    bool wild = w.wild();
     if (r.rot > 0 && !r.pos) at = fractions(rl, plus(place.ahead, t));
     const Turn turn = at.turn();
     bool keys = first_k;
@@ -300,11 +310,12 @@ __device__ __forceinline__ void rope_token(const RopeArgs &r, const RopeViews &a
             if (g >= gq && !keys) {
                 keys = true;
                 w = weights_of(true);
+                wild = w.wild();
             }
             float x[8];
             raw[i].to(x);
             if (g + AHEAD * step < n) ask(g + AHEAD * step, raw[i]);
-            const bool odd = norm_and_turn<D, INTER>(r, turn, w, x);
+            const bool odd = norm_and_turn<D, INTER>(r, turn, w, x) || wild;
             put(g, !odd, x);
             odds |= odd ? 1u << (i0 + i) : 0u;
         }

@@ -91,9 +91,10 @@ __device__ __forceinline__ void rope_k_run(const RopeArgs &r, const Run &run, in
         while (b < r.B - 1 && r.cu[b + 1] <= t) ++b;
         return fractions(rl, plus(less(r.len[b], min(r.cu[b + 1], r.n_tok)), t)).turn();
     };
+    const bool wild = kw.wild();
     unsigned top = 0;
     if (touches) {
-        bool odd = false;
+        bool odd = wild;
 #pragma unroll
         for (int i = 0; i < IT; ++i) {
             float x[8];
@@ -117,7 +118,7 @@ __device__ __forceinline__ void rope_k_run(const RopeArgs &r, const Run &run, in
                 w.to(x);
                 w.to(z);
                 const Turn at = turn_at(row);
-                const bool odd = norm_and_turn<D, INTER>(r, at, kw, z);
+                const bool odd = norm_and_turn<D, INTER>(r, at, kw, z) || wild;
                 norm_and_turn_odd<D, INTER>(r, rl, at, kw, x);
 #pragma unroll
                 for (int j = 0; j < 8; ++j) x[j] = odd ? x[j] : z[j];
