@@ -636,7 +636,8 @@ int kv_pages_free(const int32_t *keep, const int32_t *len, const int32_t *table,
  * Requests that thin out their caches: the tokens i < len[b] of request b with keep[b][i] != 0 that lie on pages become its tokens
  * 0, 1, .. in their order.  A new page whose tokens are all those that the request holds in one old page, at the same places, is that
  * page.  Any other is a fresh one from the pool, its scale per head the largest of its tokens' old ones, codes carried over to it (value of
- * the code times the old scale over the new one, rounded to nearest, ties to even), codes behind the last token zero.
+ * the code times the old scale over the new one, rounded to nearest, ties to even), codes behind the last token zero.  Old
+ * scales that are NaN (of pages that nothing was written to) are passed over as zeros; their tokens' codes become NaN.
  * Request b needs as many pages as it has fresh ones; they are taken from the top of the pool, in the order of the requests and of their
  * tables.  A request is refused, and keeps what it has (status 1), if it needs pages and those needed up to and including it are more than
  * there are.  Then the old pages that are not kept are given up as in kv_pages_free, on top of what is left.

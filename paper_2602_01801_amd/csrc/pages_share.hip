@@ -596,7 +596,6 @@ __global__ __launch_bounds__(ET) void relink_kernel(Args a) {
         for (size_t i = (size_t)blockIdx.x * ET + threadIdx.x; i < (size_t)a.n_pages; i += (size_t)gridDim.x * ET) a.pool_out[i] = a.pool[i];
 }
 
-__device__ __forceinline__ float largest(float a, float b) { return a > b ? a : b; }
 // Codes carried over to a scale 1 / ratio times as large; NaN stays.
 __device__ __forceinline__ unsigned carried(unsigned w, float ratio) {
     int y = 0;
@@ -739,11 +738,11 @@ __global__ __launch_bounds__(256, 4) void gather_kernel(Args a, int blocks, int 
         for (int i = 0; i < MAX_HEADS / 4; ++i)
             if (wave + 4 * i < mine) {
                 const int h = wave + 4 * i;
-                float km = ks[i], vm = vs[i];
+                float km = fmaxf(ks[i], 0.0f), vm = fmaxf(vs[i], 0.0f);   // of those that are numbers: the same in all lanes
 #pragma unroll
                 for (int o = 1; o < 64; o *= 2) {
-                    km = largest(km, shfl_xor(km, o));
-                    vm = largest(vm, shfl_xor(vm, o));
+                    km = fmaxf(km, shfl_xor(km, o));
+                    vm = fmaxf(vm, shfl_xor(vm, o));
                 }
                 s_ratio[0][h][lane] = ks[i] == km ? 1.0f : ks[i] / km;   // both may be 0: of a page that nothing has been written to
                 s_ratio[1][h][lane] = vs[i] == vm ? 1.0f : vs[i] / vm;
