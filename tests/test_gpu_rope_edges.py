@@ -1,5 +1,6 @@
-"""Norm and rotation, and the same on the way into pages, where a call is at an edge of what it allows: weights that are not ordinary numbers.
-References and tolerances are those of share_ref.py."""
+"""Norm and rotation, and the same on the way into pages, where a call is at an edge of what it allows: weights that are not ordinary numbers, more
+sequences than one look finds, angles whose sine or cosine is all that is left.  References are those of share_ref.py, and its tolerances unless a test
+derives its own."""
 import math
 
 import numpy as np
@@ -52,3 +53,78 @@ def test_weights_that_are_not_finite_stay_in_their_coordinates(dtype, d, rot, in
         a, b = getattr(pages, name), getattr(want, name)
         assert torch.equal(torch.where(a & 127 == 127, 127, a), torch.where(b & 127 == 127, 127, b)), name
     assert torch.equal(pages.kscale, want.kscale) and torch.equal(pages.vscale, want.vscale)
+
+
+# Sine and cosine take a fraction of a turn of at most 1/2 in 32 bits, whose rounding is 2^-26 at most, 2 pi times that of the angle; the instructions' own
+# error is 2^-22.92 at most (2^26 fractions at random).  Absolute errors, of which the sum is the bound.
+TURN = 2.0 ** -22.92 + 2 * math.pi * 2.0 ** -26
+
+
+@pytest.mark.parametrize("interleaved,d", [(False, 128), (True, 64)])
+def test_sine_and_cosine(interleaved, d):
+    """Pairs (1, 0) and (0, 1): the outputs are the two themselves.  Angles in 64 bits are off by 2^-52 of themselves, here and in the reference; the
+    product with 1 and the sum with 0 are exact."""
+    rng = np.random.default_rng(d)
+    n = 4096
+    pos = np.concatenate([np.arange(n // 2), rng.integers(-2 ** 31, 2 ** 31, n // 2)])
+    freq = np.concatenate([sref.frequencies(d)[: d // 4], rng.random(d // 4) * 7.0])
+    Q = torch.zeros((2, n, d))
+    first = torch.arange(0, d, 2) if interleaved else torch.arange(d // 2)
+    second = first + 1 if interleaved else first + d // 2
+    Q[0, :, first] = Q[1, :, second] = 1.0
+    rope = fa.Rope(torch.from_numpy(freq).cuda(), norm=False, interleaved=interleaved)
+    got = f64(fa.qk_norm_rope(Q.cuda(), None, rope, pos=i32([pos.tolist()]))[0])
+    t = pos[:, None].astype(float) * freq
+    for row, at, want in ((0, first, np.cos(t)), (0, second, np.sin(t)), (1, first, -np.sin(t)), (1, second, np.cos(t))):
+        assert (np.abs(got[row][:, at.numpy()] - want) <= TURN + np.abs(t) * 2.0 ** -51).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_products_that_cancel(dtype):
+    """Angles at which a pair turns into (0, r): what is left of the first is the error of the angle, which is as small where the type is short.  The
+    products and their sum in 32 bits are off by 2^-24 of the largest each, then the rounding to the type."""
+    g = torch.Generator().manual_seed(21)
+    d, n = 128, 9
+    x = torch.randn((1, 1, d), generator=g).to(DT[dtype])
+    a, b = f64(x)[0, 0, :64], f64(x)[0, 0, 64:]
+    freq = np.arctan2(a, b)
+    rope = fa.Rope(torch.from_numpy(freq).cuda(), norm=False)
+    got = f64(fa.qk_norm_rope(x.cuda().expand(3, n, d), None, rope, pos=i32([[1] * n]))[0])
+    r = np.hypot(a, b)
+    size = np.abs(a) + np.abs(b)
+    assert (np.abs(got[..., :64]) <= (TURN + 3 * 2.0 ** -24) * size * (1 + 2.0 ** -8)).all()
+    unit = 2.0 ** -8 if dtype == "bf16" else 2.0 ** -24
+    assert (np.abs(got[..., 64:] - r) <= (TURN + 3 * 2.0 ** -24) * size + unit * r).all()
+
+
+@pytest.mark.parametrize("B,P,d,dtype,interleaved", [(64, 16, 64, "bf16", False), (65, 16, 64, "f32", True), (67, 64, 128, "bf16", False),
+                                                     (130, 32, 128, "f32", False), (4500, 16, 64, "bf16", True), (5000, 64, 64, "bf16", False)])
+def test_write_rope_of_many_sequences(B, P, d, dtype, interleaved):
+    """More sequences than one look finds, empty ones among them, at positions that differ: codes and scales of qk_norm_rope in fp32 and
+    kv_pages_write, queries of qk_norm_rope, and keys against 64 bits."""
+    g = torch.Generator().manual_seed(B)
+    rng = np.random.default_rng(B)
+    q = rng.choice([0, 1, 1, 1, 2, 5, P + 3], size=B, p=[0.2, 0.3, 0.2, 0.1, 0.1, 0.08, 0.02]).tolist()
+    k = rng.integers(0, 9999, size=B).tolist()
+    pad, n, Hq, Hkv = 2, sum(q) + 4, 3, 1
+    slot, n_pages = slots_of(rng, q, k, P)
+    Q, K, V = view(g, Hq, n, d, DT[dtype], "fused"), view(g, Hkv, n, d, DT[dtype], "tokens"), view(g, Hkv, n, d, DT[dtype], "tokens", 0.2)
+    freq = sref.frequencies(d)
+    rope = fa.Rope(torch.from_numpy(freq).cuda(), q_weight=weights(g, d), k_weight=weights(g, d), interleaved=interleaved)
+    cu, length = i32((prefix(q) + pad).tolist()), i32([a + b for a, b in zip(q, k)])
+    pages = make_pages(rng, n_pages, Hkv, P, d)
+    want = clone(pages)
+    out = torch.full_like(Q, 7.0)
+    fa.kv_pages_write_rope(pages, i32([n_pages * P - 1] * pad + slot + [n_pages * P - 1] * pad), Q, K, V, rope, cu=cu, length=length, out=out)
+    both = torch.full_like(Q, 7.0)
+    turned = torch.zeros_like(K, dtype=torch.float32)
+    fa.qk_norm_rope(Q, None, rope, cu=cu, length=length, out=(both, None))
+    fa.qk_norm_rope(None, K.float(), rope, cu=cu, length=length, out=(None, turned))
+    fa.kv_pages_write(want, i32([-1] * pad + slot + [-1] * pad), turned, V.float())
+    for name in ("K8", "kscale", "V8", "vscale"):
+        assert torch.equal(getattr(pages, name), getattr(want, name)), name
+    assert torch.equal(out, both)
+    at = np.concatenate([b + np.arange(a) for a, b in zip(q, k)])[:, None].astype(float) * np.ones(d // 2)
+    rows = slice(pad, n - pad)
+    check_rows(turned[:, rows], K[:, rows], rope.k_weight, rope, freq, at, False)
+    check_rows(out[:, rows], Q[:, rows], rope.q_weight, rope, freq, at, dtype == "bf16")

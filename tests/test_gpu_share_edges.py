@@ -10,7 +10,7 @@ import paper_2602_01801_amd as fa
 import share_ref as sref
 from test_gpu_packed import i32
 from test_gpu_rope import make_pages
-from test_gpu_share import ints, layout
+from test_gpu_share import ints, layout, run_compact, run_free
 
 pytestmark = pytest.mark.gpu
 
@@ -48,3 +48,119 @@ def test_scales_that_are_no_numbers_stay_with_their_tokens(P, d, Hkv):
                         else:
                             want = ref.round_e4m3(ref.VALUES[was[p, h, o]] * (xs[p, h] / numbers[h]))
                             assert np.array_equal(value, want, equal_nan=True)
+
+
+# ------------------------------------------------------------------------------------------------ masks of several rounds
+
+ROUND = 65536   # tokens of a request that its mask's workgroup looks at before it goes on
+
+
+@pytest.mark.parametrize("P,beside", [(16, True), (16, False), (64, True), (64, False)])
+def test_compact_of_requests_of_several_rounds(P, beside):
+    """Two requests of more than twice as many tokens as a round has, neither a multiple of 64: counts of tokens and of fresh pages go from one round to the
+    next.  Whole pages and fresh ones on both sides of every round's end, or a stretch of fresh ones across it."""
+    rng = np.random.default_rng(P + beside)
+    W = (2 * ROUND + 4000) // P
+    T = W * P
+    lens = [T - 27, 2 * ROUND + 1001]
+    keep = np.repeat(rng.random((2, T // P)) < 0.9, P, 1)
+    for b in range(2):
+        for end in (ROUND, 2 * ROUND):
+            keep[b, end - 1024:end + 1024] = True
+            for lo, hi in ([(end - 512, end - 320), (end + 320, end + 512)] if beside else [(end - 192, end + 192)]):
+                keep[b, lo:hi] = rng.random(hi - lo) < 0.5
+                spare = np.flatnonzero(keep[b, lo:hi])[: int(keep[b, :hi].sum() % P)]   # so that the pages behind are whole again
+                keep[b, lo + spare] = False
+    table, pool, free, n_pages = layout(rng, lens, W, P, 200)
+    pages = make_pages(rng, n_pages, 1, P, 64)
+    want = run_compact(pages, keep, lens, table, pool, free, P)
+    assert want[4] == [0, 0] and len(want[5]) >= 2 * 2 * 192 // P // 2
+    for b in range(2):   # what the mask was made for
+        rank = np.concatenate([[0], np.cumsum(keep[b])])
+        old = {p: j for j, p in enumerate(table[b][: -(-lens[b] // P)])}
+        kind = [old.get(p, -1) >= 0 for p in want[1][b][: -(-want[0][b] // P)]]
+        for end in (ROUND, 2 * ROUND):
+            at = int(rank[end]) // P
+            before, behind = kind[at - 768 // P:at], kind[at + 1:at + 768 // P]
+            assert any(before) and any(behind)
+            assert not all(before) and not all(behind) if beside else not kind[at]
+
+
+@pytest.mark.parametrize("B,first", [(700, 300), (700, 600), (1000, 800), (257, 256), (700, 255), (512, 511)])
+@pytest.mark.parametrize("in_place", [False, True])
+def test_compact_of_requests_whose_pages_run_out_in_a_later_round(B, first, in_place):
+    """Fresh pages are summed up 256 requests a round: the pool suffices for the requests before `first`."""
+    rng = np.random.default_rng(B + first)
+    P, W = 16, 2
+    lens = [int(rng.integers(1, W * P + 1)) for _ in range(B)]
+    table, pool, free, n_pages = layout(rng, lens, W, P, 2 * B, share=0.2)
+    keep = rng.random((B, W * P)) < 0.6
+    keep[first, :] = [0, 1] * P      # needs one
+    lens[first] = max(lens[first], 5)
+    all_of_it = sref.compact(keep, lens, table, pool, free, P, n_pages)
+    assert 1 not in all_of_it[4]
+    have = [set(p for p in row if p is not None) for row in sref.held(table, lens, n_pages, P)]
+    need = [sum(p not in have[b] for p in all_of_it[1][b][: -(-all_of_it[0][b] // P)]) for b in range(B)]
+    assert need[first] > 0
+    pages = make_pages(rng, n_pages, 1, P, 64)
+    want = run_compact(pages, keep, lens, table, pool, sum(need[:first]), P, in_place=in_place)
+    assert want[4].index(1) == first and all(s == 0 or need[b] for b, s in enumerate(want[4]))
+
+
+# ------------------------------------------------------------------------------------------------ freeing by one workgroup and by several launches
+
+
+@pytest.mark.parametrize("B,W,n_pages,share", [
+    (1024, 8, 0, 0.5), (1024, 8, 0, 0.0), (1, 8192, 0, 0.0), (64, 128, 0, 0.7), (1023, 8, 16384, 0.0), (3, 5, 16384, 0.0),    # the most that one workgroup does
+    (1025, 7, 0, 0.5), (2731, 3, 0, 0.5), (1, 8193, 0, 0.0), (1025, 8, 0, 0.0), (3, 5, 16385, 0.0), (1024, 8, 16385, 0.0)])   # the least that it does not
+@pytest.mark.parametrize("full", [True, False])
+def test_free_on_both_sides_of_what_one_workgroup_does(B, W, n_pages, share, full):
+    rng = np.random.default_rng(B + W + n_pages)
+    P = 16
+    lens = [W * P - int(rng.integers(0, P)) if full else int(rng.choice([0, 1, P, rng.integers(0, W * P + 1)])) for _ in range(B)]
+    held = sum(-(-n // P) for n in lens)
+    table, pool, free, got = layout(rng, lens, W, P, n_pages - held if n_pages else 5, share=share, junk=not full)
+    assert not n_pages or got == n_pages
+    for in_place in (False, True):
+        keep = [int(rng.choice([-5, 0, n, max(0, n - 1), rng.integers(0, n + 9), 2 ** 31 - 1], p=[0.1, 0.3, 0.2, 0.15, 0.15, 0.1])) for n in lens]
+        status = run_free(keep, lens, table, pool, free, P, in_place=in_place)
+        assert share == 0 or full is False or 1 in status
+    run_free([0] * B, lens, table, pool, free, P)
+
+
+# ------------------------------------------------------------------------------------------------ two calls at once
+
+
+def test_two_calls_at_once():
+    """Two caches on two streams, with a workspace each, step by step in turn: neither sees the other."""
+    rng = np.random.default_rng(9)
+    P, B, W = 16, 30, 12
+    sides = []
+    for i in range(2):
+        lens = [int(rng.integers(1, W * P + 1)) for _ in range(B)]
+        table, pool, free, n_pages = layout(rng, lens, W, P, 200, share=0.3)
+        pages = make_pages(rng, n_pages, 2, P, 64)
+        mask = rng.random((B, W * P)) < 0.6
+        keep = [int(rng.integers(0, W * P)) for _ in range(B)]
+        after, t, pl, n, s0, made = sref.compact(mask, lens, table, pool, free, P, n_pages)
+        K, ks = pages.K8.cpu().numpy().copy(), pages.kscale.cpu().numpy().copy()
+        sref.compact_codes(K, ks, False, made)
+        after, n, s1 = sref.free(keep, after, t, pl, n, P, n_pages)
+        state = dict(length=i32(lens), table=i32(table), pool=i32(pool), pool_n=i32([free]), mask=torch.from_numpy(mask.astype(np.uint8)).cuda(), keep=i32(keep),
+                     status=[i32([9] * B), i32([9] * B)], pages=pages, stream=torch.cuda.Stream(),
+                     ws=torch.empty(fa.workspace_bytes(fa.OP_PAGES, B, W, n_pages, P), dtype=torch.uint8, device="cuda"))
+        sides.append((state, (after, n, pl, s0, s1, K, ks)))
+    torch.cuda.synchronize()
+    for what in range(2):
+        for s, _ in sides:
+            with torch.cuda.stream(s["stream"]):
+                if what == 0:
+                    fa.kv_pages_compact(s["pages"], s["mask"], s["length"], s["table"], s["pool"], s["pool_n"],
+                                        out=(s["length"], s["table"], s["pool"], s["pool_n"], s["status"][0]), ws=s["ws"])
+                else:
+                    fa.kv_pages_free(s["keep"], s["length"], s["table"], s["pool"], s["pool_n"], P, out=(s["length"], s["pool_n"], s["status"][1]), ws=s["ws"])
+    torch.cuda.synchronize()
+    for s, (after, n, pl, s0, s1, K, ks) in sides:
+        assert ints(s["length"]) == after and ints(s["pool_n"]) == [n] and ints(s["pool"])[:n] == pl[:n]
+        assert [ints(x) for x in s["status"]] == [s0, s1]
+        assert np.array_equal(s["pages"].K8.cpu().numpy(), K) and np.array_equal(s["pages"].kscale.cpu().numpy(), ks)
