@@ -46,10 +46,6 @@ __device__ __forceinline__ void write_odd_roped_run(Roped roped, const RopeLane 
 // lanes that read the same group of eight cells meet all banks, as those that write neighbouring groups do.
 __device__ __forceinline__ int lds_group(int group) { return group ^ (group >> 3 & 3); }
 
-// Bytes of new rows from which on the queries have a launch of their own: beside the keys they run at four wavefronts per SIMD instead of eight,
-// which shows where they come from memory.  Both ways, 40 heads on 8, 8192 / 16384 tokens (117 / 235 MB) 47.7 / 105.6 us in one launch, 59.0 / 103.6 in two;
-// 12 on 12 (75 / 151 MB) 40.0 / 60.2 and 43.2 / 59.0; 34612 tokens, 40 on 8, 224 and 206.  Few tokens save the second launch: 5.1 and 7.9.
-constexpr int64_t APART = 150000000;
 struct RopeWriteArgs {
     RopeArgs r;
     RopeViews q;          // Hkv = 0: the keys go another way
@@ -157,7 +153,8 @@ __device__ __forceinline__ void rope_k_run(const RopeArgs &r, const Run &run, in
 }
 
 // Workgroups of keys, of values and of queries, evenly mixed over the launch: those of keys compute more than they move, the others the
-// other way round.  Keys and values of 34612 tokens x 8 heads take 77 us behind other work, where writing them as they are takes 53: 29 of these are the vector
+// other way round, and few tokens save a launch.  (Queries by a launch of their own, at eight wavefronts per SIMD instead of four: 34612 tokens, 40 heads on 8, 204 us
+// where one takes 196, in fp32 349 and 339, 12 on 12 146 and 146, in fp32 199 and 182; 96 tokens 13.7 and 11.1.)  Keys and values of 34612 tokens x 8 heads take 77 us behind other work, where writing them as they are takes 53: 29 of these are the vector
 // instructions of the keys, at the four wavefronts per SIMD that their LDS and registers leave (five spill, 87).  96 single tokens with their queries 8.0 us.
 template <bool BF16, int D, int PSHIFT, bool INTER>
 __global__ __launch_bounds__(4 << PSHIFT, 4) void write_rope_kernel(RopeWriteArgs a) {
@@ -224,19 +221,18 @@ extern "C" int kv_pages_write_rope(const fastar_pages *pages, const fastar_rows 
     a.kv = (int64_t)((n_tok + a.chunk - 1) / a.chunk) * Hkv * 2;
     a.all = a.kv;
     const hipStream_t s = (hipStream_t)stream;
-    bool apart = false;
     if (Hq > 0) {
         a.q = RopeViews{view_of(Q, Hq, n_tok, elt), View{}, view_of(Qo, Hq, n_tok, elt), View{}, Hq, 0};
-        apart = (int64_t)n_tok * (Hq + 2 * (int64_t)Hkv) * d * elt >= pages::APART;
-        if (!apart) {
-            a.parts = rope_parts(n_tok, Hq, 0, d);
-            const int waves = pages->P / 16;
-            a.all += ((int64_t)n_tok * a.parts + waves - 1) / waves;
+        a.parts = rope_parts(n_tok, Hq, 0, d);
+        const int waves = pages->P / 16;
+        a.all += ((int64_t)n_tok * a.parts + waves - 1) / waves;
+        if (!launch_ok(a.all, 4 * pages->P)) {   // more than a launch can have: the queries by themselves
+            if (!launch_ok(a.kv, 4 * pages->P)) return FASTAR_ERR_UNSUPPORTED;
+            if (const int rc = rope_launch(a.r, a.q, d, dtype, rope->interleaved, s); rc != FASTAR_OK) return rc;
+            a.all = a.kv;
         }
     }
     if (!launch_ok(a.all, 4 * pages->P)) return FASTAR_ERR_UNSUPPORTED;
-    if (apart)
-        if (const int rc = rope_launch(a.r, a.q, d, dtype, rope->interleaved, s); rc != FASTAR_OK) return rc;
     const dim3 grid((unsigned)a.all);
 #define FASTAR_WRITE(BF16, D, PSHIFT) \
     do {                                                                                                                                 \

@@ -128,3 +128,31 @@ def test_write_rope_of_many_sequences(B, P, d, dtype, interleaved):
     rows = slice(pad, n - pad)
     check_rows(turned[:, rows], K[:, rows], rope.k_weight, rope, freq, at, False)
     check_rows(out[:, rows], Q[:, rows], rope.q_weight, rope, freq, at, dtype == "bf16")
+
+
+def test_more_tokens_than_one_launch_takes_with_their_queries():
+    """62 million tokens of one request, of which a few go into pages: the queries take a launch of their own, and rows lie beyond 2^32 bytes."""
+    g = torch.Generator().manual_seed(31)
+    rng = np.random.default_rng(31)
+    n, d, P = 62_000_000, 64, 64
+    some = [0, 1, 4097, 2 ** 25 - 1, 2 ** 25, 33_554_433 + 70, n - 66, n - 1]
+    x = torch.randn((3, len(some), d), generator=g).bfloat16().cuda()
+    Q, K, V, out = (torch.zeros((1, n, d), dtype=torch.bfloat16, device="cuda") for _ in range(4))
+    slot = torch.full((n,), -1, dtype=torch.int32, device="cuda")
+    for i, t in enumerate(some):
+        Q[0, t], K[0, t], V[0, t] = x[0, i], x[1, i], x[2, i]
+        slot[t] = i * P + (1 if i == 1 else 0)
+    slot[1] = 1   # goes on where row 0 ended
+    freq = sref.frequencies(d)
+    rope = fa.Rope(torch.from_numpy(freq).cuda(), q_weight=weights(g, d), k_weight=weights(g, d))
+    pages = make_pages(rng, len(some), 1, P, d)
+    want = clone(pages)
+    fa.kv_pages_write_rope(pages, slot, Q, K, V, rope, cu=i32([0, n]), length=i32([n]), out=out)
+    pos = i32([some])
+    turned = fa.qk_norm_rope(None, x[1][None].float(), rope, pos=pos)[1]
+    fa.kv_pages_write(want, slot[some], turned, x[2][None].float())
+    for name in ("K8", "kscale", "V8", "vscale"):
+        assert torch.equal(getattr(pages, name), getattr(want, name)), name
+    assert torch.equal(out[0, some], fa.qk_norm_rope(x[0][None], None, rope, pos=pos)[0][0])
+    out[0, some] = 0
+    assert not out.any()
