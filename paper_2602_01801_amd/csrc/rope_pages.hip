@@ -212,12 +212,12 @@ extern "C" int kv_pages_write_rope(const fastar_pages *pages, const fastar_rows 
     if (a.k.row > MAX_PITCH || a.v.row > MAX_PITCH) return FASTAR_ERR_UNSUPPORTED;
     a.pg = *pages;
     a.slot = slot;
-    // Of a few sequences a workgroup takes as many rows as one has on average, even if that leaves few workgroups: the runs of a workgroup are done one
-    // after the other, 2.8 us each, and there are no more of them than sequences.  Four sequences of 256 / 512 / 1024 tokens in all, 12 heads on 12, pages of 64:
-    // 6.4 / 7.5 / 9.7 us, where chunks for 4096 workgroups take 12.0 / 14.2 / 16.9.
-    a.chunk = pages::rows_per_workgroup(n_tok, Hkv, pages->P);
-    if (cu && B <= 4)
-        while (a.chunk < pages->P && a.chunk * 2 <= n_tok / B) a.chunk *= 2;
+    // The runs of a workgroup are done one after the other, 2.8 us each, and one whose rows begin none has been there for nothing.  Of up to four sequences few runs can
+    // meet in one, so that a workgroup per compute unit suffices; of more, it depends on their lengths, which the host does not know.  Rows for 256 / for 4096
+    // workgroups: a sequence of 64 / 256 / 1024 tokens, 12 heads on 12, pages of 64, 6.3 / 6.8 / 11.0 us and 6.8 / 13.2 / 17.9, four of them 7.8 / 12.6 / 22.4 and
+    // 13.5 / 18.3 / 27.2; one, 12 heads on 4, pages of 16, 5.6 / 6.1 / 9.1 and 5.6 / 6.7 / 10.7.  Eight of 256 19 and 23, sixteen 26 and 28; but four of 500 beside 60 single
+    // tokens 148 and 41, 96 single tokens 14.8 and 8.3.
+    a.chunk = pages::rows_per_workgroup(n_tok, Hkv, pages->P, cu && B <= 4 ? 256 : 4096);
     a.kv = (int64_t)((n_tok + a.chunk - 1) / a.chunk) * Hkv * 2;
     a.all = a.kv;
     const hipStream_t s = (hipStream_t)stream;
