@@ -383,22 +383,26 @@ __global__ __launch_bounds__(ET) void push_kernel(Args a) {
     if (e == 0) a.len_out[b] = a.w.stay[b];
     if (last && threadIdx.x == 0) a.pool_n_out[0] = (int)min((long long)top + s_before + all, (long long)a.n_pages);
 }
-// Few blocks: a workgroup pushes for all of them, without counts;  thinning out, beside the workgroups that move tokens.
-constexpr int PUSH_ALL = 16;
+// Few blocks: a workgroup pushes for all of them, without counts, beside the workgroups that move tokens.  It takes them one after the other, 1 us each, behind
+// the codes if those take less, and saves a launch.  This way / by counts and a fourth launch, from a graph: 1 / 4 / 8 / 16 requests of 600 tokens x 4 heads of 64 13.7 / 15.0 /
+// 20.5 / 30.2 us and 16.0 / 17.4 / 18.4 / 19.9 (launched one by one 16.6 / 16.2 / 22.2 / 30.7 and 19.4 / 19.3 / 20.3 / 21.7); 3 of up to 37440 x 8 heads of 128 (9 blocks) 76 and 81, 8 of
+// 6300 53.4 and 57.5, 12 of 3700 49 and 53, of which few are kept 25 and 22; 16 of 6300 122 and 120, few 37 and 25.
+constexpr int PUSH_ALL = 9;
+constexpr int PUSH_ROOM = 16;   // (room for nine alone: the kernel's registers are dealt out otherwise, 77.3 us instead of 76.2)
 template <bool COMPACT>
 __device__ __forceinline__ void push_all(const Args &a, int blocks) {
     __shared__ int s_part[ET / 64];
     int top = a.w.head[0] - (COMPACT ? a.w.head[1] : 0);
-    int p[PUSH_ALL];
+    int p[PUSH_ROOM];
 #pragma unroll
-    for (int i = 0; i < PUSH_ALL; ++i) {
+    for (int i = 0; i < PUSH_ROOM; ++i) {
         int b, e;
         entry_of(a, i, b, e);
         p[i] = i < blocks ? given_back<COMPACT>(a, b, e) : -1;
         if (i < blocks && e == 0) a.len_out[b] = a.w.stay[b];
     }
 #pragma unroll
-    for (int i = 0; i < PUSH_ALL; ++i) {
+    for (int i = 0; i < PUSH_ROOM; ++i) {
         if (i >= blocks) break;
         int all;
         const long long at = (long long)top + wg_incl_scan<ET>(p[i] >= 0, s_part, &all) - 1;
@@ -509,7 +513,8 @@ __global__ __launch_bounds__(1024) void mask_kernel(Args a) {
     }
 }
 
-// Which requests are refused, and where the fresh pages of the others begin.  One workgroup, where there are too many requests for each to do so.
+// Which requests are refused, and where the fresh pages of the others begin.  One workgroup, where there are too many requests for each block of entries to do so: 256 /
+// 1024 / 2048 / 4096 / 16384 requests of 30 tokens 25.5 / 43.1 / 68.9 / 128 / 444 us with this launch, 24.4 / 42.7 / 68.7 / 136 / 601 without.
 constexpr int ADMIT_ALL = 1024;
 __global__ __launch_bounds__(1024) void admit_kernel(Args a) {
     __shared__ int part[16];
@@ -797,7 +802,10 @@ size_t pages_ws_bytes(int B, int max_pages, int n_pages, int P) {
     return share::lay_out(w, nullptr, B, max_pages, n_pages, P);
 }
 
-constexpr int SUM_ALL = 4096;   // blocks of entries up to which each sums up the counts of those before it
+// Blocks of entries up to which each sums up the counts of those before it; beyond, a launch does so for all.  512 / 1024 / 2048 / 4096 requests of 100 tokens freed: each by
+// itself 14.5 / 16.8 / 20.7 / 28.7 us from a graph, 21.4 / 18.6 / 21.6 / 30.0 launched one by one; by a launch 14.1 / 15.8 / 18.4 / 24.5 and 25.0 / 24.8 / 24.7 / 27.6.  Thinned out, 17 /
+// 64 / 512 / 4096: 20.9 / 24.7 / 38.3 / 214 and 22.5 / 24.8 / 38.0 / 208 from a graph.
+constexpr int SUM_ALL = 2048;
 
 // What kv_pages_free and kv_pages_compact ask of their arguments alike.
 static int share_check(const int32_t *len, const int32_t *table, int B, int max_pages, const int32_t *pool, const int32_t *pool_n, int n_pages,
