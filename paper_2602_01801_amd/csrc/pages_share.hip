@@ -203,6 +203,7 @@ struct Args {
     int32_t *len_out, *table_out, *pool_out, *pool_n_out, *status;
     int32_t B, max_pages, n_pages, pshift, segs;   // segs: blocks of entries per row
     bool one_pushes;                               // a workgroup pushes for all blocks
+    bool copies;                                   // relink_kernel copies the pool
     bool summed, admitted;                         // block, and base and status, have been worked out by a launch of their own
     Work w;
 };
@@ -436,10 +437,17 @@ __global__ __launch_bounds__(256) void nothing_kernel(Args a) {
 // A workgroup per request goes through its mask, 64 tokens per thread: how many are kept before every group of 16, which pages stay whole,
 // which of the new ones are fresh and where their tokens begin.  It keeps the old table row, as the new one may be written over it.  Whoever has a
 // new page's first token writes about that page, so that nothing has to be cleared before, and all loads of a round are one trip to memory: three requests of up
-// to 37440 tokens 5.3 us.  (16 tokens per thread and a list of every token's place: 15; its stores, four bytes apart by lanes sixteen apart, were most of it.)
+// to 37440 tokens 5.3 us.  More workgroups than there are requests help with the pages' states and copy the pool.  (16 tokens per thread and a list of
+// every token's place: 15; its stores, four bytes apart by lanes sixteen apart, were most of it.)
 __global__ __launch_bounds__(1024) void mask_kernel(Args a) {
     __shared__ int part[16];
     const int b = blockIdx.x, tid = threadIdx.x, P = 1 << a.pshift;
+    if (b >= a.B) {
+        clear_states(a);
+        if (a.pool_out != a.pool)
+            for (size_t i = (size_t)(b - a.B) * 1024 + tid; i < (size_t)a.n_pages; i += (size_t)(gridDim.x - a.B) * 1024) a.pool_out[i] = a.pool[i];
+        return;
+    }
     const int L = tokens_of(a, b), have = (L + P - 1) >> a.pshift;
     const size_t row = (size_t)b * a.max_pages;
     const u32x4 *mask = (const u32x4 *)(a.mask + (row << a.pshift));
@@ -597,7 +605,7 @@ __global__ __launch_bounds__(ET) void relink_kernel(Args a) {
         a.table_out[at] = p;
         if (link < 0 && is_page(a, old)) give_up(a, old, (int)at);
     }
-    if (a.pool_out != a.pool)
+    if (a.copies)
         for (size_t i = (size_t)blockIdx.x * ET + threadIdx.x; i < (size_t)a.n_pages; i += (size_t)gridDim.x * ET) a.pool_out[i] = a.pool[i];
 }
 
@@ -928,7 +936,11 @@ extern "C" int kv_pages_compact(const fastar_pages *pages, const uint8_t *keep, 
     a.table_out = table_out;
     const hipStream_t s = (hipStream_t)stream;
     const unsigned blocks = (unsigned)(B * a.segs);
-    hipLaunchKernelGGL(share::mask_kernel, dim3((unsigned)B), dim3(1024), 0, s, a);
+    // Workgroups beside those of the requests where the pool is so large that these would go on for it.  One request of 600 tokens, pools of
+    // 2000 / 16384 / 131072 / 1048576 pages: 14.7 / 13.5 / 13.8 / 16.0 us, 14.5 / 22.4 / 88 / 1140 with none; 64 requests 27.6 / 31.2 / 32.6 / 35.4 and 27.5 / 31.1 / 32.4 / 48.2.
+    const unsigned room = UINT32_MAX / 1024 - (unsigned)B, more = a.n_pages / 4096 > B ? std::min((unsigned)std::min(a.n_pages / 1024, 1024), room) : 0u;
+    a.copies = more == 0 && pool_out != pool;
+    hipLaunchKernelGGL(share::mask_kernel, dim3((unsigned)B + more), dim3(1024), 0, s, a);
     FASTAR_LAUNCH_CHECK();
     if (a.admitted) {
         hipLaunchKernelGGL(share::admit_kernel, dim3(1), dim3(1024), 0, s, a);

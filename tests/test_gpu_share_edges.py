@@ -107,6 +107,26 @@ def test_compact_of_requests_whose_pages_run_out_in_a_later_round(B, first, in_p
     assert want[4].index(1) == first and all(s == 0 or need[b] for b, s in enumerate(want[4]))
 
 
+@pytest.mark.parametrize("n_free,lens", [(150_000, [37]), (150_000, [40, 0, 1, 33]), (1_100_000, [48])])
+def test_compact_of_few_tokens_in_a_large_pool(n_free, lens):
+    """Far more pages than the tables name, a workspace full of junk, and the same one again."""
+    rng = np.random.default_rng(n_free + len(lens))
+    P, W = 16, 3
+    table, pool, free, n_pages = layout(rng, lens, W, P, n_free)
+    pages = fa.Pages(*(torch.zeros(s, dtype=t, device="cuda") for s, t in (((n_pages, 1, 1, 4, 16, 16), torch.uint8), ((n_pages, 1), torch.float32)) * 2))
+    ws = torch.randint(0, 256, (fa.workspace_bytes(fa.OP_PAGES, len(lens), W, n_pages, P),), dtype=torch.uint8, device="cuda")
+    for turn in range(3):
+        keep = rng.random((len(lens), W * P)) < 0.6
+        keep[:, :P] = True
+        want = sref.compact(keep, lens, table, pool, free, P, n_pages)
+        t, ln, pn, pl = i32(table), i32(lens), i32([free]), i32(pool)
+        out = (ln, t, pl, pn, i32([9] * len(lens))) if turn == 1 else None
+        got = fa.kv_pages_compact(pages, torch.from_numpy(keep.astype(np.uint8)).cuda(), ln, t, pl, pn, out=out, ws=ws)
+        for x, y in zip(got, want[:5]):
+            assert torch.equal(x.cpu().view(-1), torch.tensor(y, dtype=torch.int32).view(-1))
+        assert len(want[5])
+
+
 # ------------------------------------------------------------------------------------------------ freeing by one workgroup and by several launches
 
 
