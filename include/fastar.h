@@ -641,6 +641,7 @@ int kv_pages_free(const int32_t *keep, const int32_t *len, const int32_t *table,
  * Request b needs as many pages as it has fresh ones; they are taken from the top of the pool, in the order of the requests and of their
  * tables.  A request is refused, and keeps what it has (status 1), if it needs pages and those needed up to and including it are more than
  * there are.  Then the old pages that are not kept are given up as in kv_pages_free, on top of what is left.
+ * A mask that keeps or drops whole pages (the last one as far as its tokens go) needs none: with an empty pool, cut at multiples of P.
  *   keep [B, max_pages * P] uint8, 16-byte aligned;  len [B];  table [B, max_pages];  pool [n_pages], pool_n [1]
  *   len_out [B]               tokens after the call;  may be len itself
  *   table_out [B, max_pages]  block tables after it, -1 behind a request's last page (rows of refused requests as they were);  may be table itself

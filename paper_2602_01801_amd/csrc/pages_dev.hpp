@@ -111,7 +111,8 @@ __device__ __forceinline__ void write_odd_run(const char *row0, int64_t pitch, i
 
 // Rows per workgroup: a page's where that makes enough of them; fewer, down to one, so that the runs of single tokens are not
 // done one after the other.  At least 1024 / 4096 / 16384 workgroups, pages of 64, 8 heads: 512 single tokens 17.5 / 19.4 / 21.7 us, 16 runs
-// of 16 4.5 / 6.0 / 6.0, 8 of 200 6.3 / 9.2 / 18.6, 8 of 4680 38.6 / 37.4 / 52; 30000 tokens of one head 9.5 / 23 / 49: for runs fewer would do.
+// of 16 4.5 / 6.0 / 6.0, 8 of 200 6.3 / 9.2 / 18.6, 8 of 4680 38.6 / 37.4 / 52; 30000 tokens of one head 9.5 / 23 / 49: for runs fewer would do
+// (`least` says so where that is known).
 inline int rows_per_workgroup(int n_tok, int Hkv, int P, int least = 4096) {
     int chunk = P;
     while (chunk > 1 && (int64_t)n_tok * Hkv * 2 / chunk < least) chunk /= 2;

@@ -629,8 +629,9 @@ struct __attribute__((packed, aligned(1))) Bytes16 {
 // The first workgroups count the pages that blocks of entries give back; the others fill fresh pages, `heads` heads of one after the other, PIECES
 // times 16 bytes per thread: of a token (K) and of a coordinate (V).  Bound by the trips to memory of an item: what it is -> groups of tokens -> old pages ->
 // codes and, beside them, scales;  so codes are asked for before the scales are there, all of an item's K and the first two runs of its V.
-// 112 MB of codes of three windows 52 us (4.1 TB/s read and written), 98 MB in runs of 14 tokens 58 (whole cells of V are read: 4.2 TB/s).  (An item's heads one after the
-// other, scales first: 54 and 75;  a branch between the loads, so that each is waited for: 65 and 75;  three wavefronts per SIMD 55 and 65, five spill: 93.)
+// 112 MB of codes of three windows 52 us (4.1 TB/s read and written), 98 MB in runs of 14 tokens 58 (whole cells of V are read: 4.2 TB/s) on the same pages again and again, of
+// which some are in the last-level cache; 64 and 70 (3.5 TB/s) from memory.  (An item's heads one after the other, scales first: 54 and 75;  a branch between the loads, so that each is
+// waited for: 65 and 75;  three wavefronts per SIMD 55 and 65, five spill: 93.)
 constexpr int PIECES = 4, MAX_HEADS = 16;   // 1024 pieces of a page are 2 heads of 64 x 128, 16 of 16 x 64
 __global__ __launch_bounds__(256, 4) void gather_kernel(Args a, int blocks, int heads) {
     if (a.one_pushes) {

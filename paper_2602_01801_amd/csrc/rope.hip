@@ -16,8 +16,8 @@ struct Args {
 };
 
 // Bound by memory: every row is read and written once.  A wavefront per token and as many groups of its heads as the rule below leaves it, asked for four
-// ahead, so that its angles and its trip to the sequences' offsets are paid once: 13683 tokens x 48 heads 66 us (5.1 TB/s; 120 with four groups per wavefront, each
-// with its own), 4680 x 24 in fp32 20 (115 MB, from the last-level cache), one token 2.6.
+// ahead, so that its angles and its trip to the sequences' offsets are paid once: 13683 tokens x 48 heads 68 us (4.9 TB/s; 120 with four groups per wavefront, each
+// with its own), 4680 x 24 in fp32 25.6 (4.5 TB/s; 20 from the last-level cache), one token 2.7.
 template <bool BF16, int D, bool INTER>
 __global__ __launch_bounds__(64 * WAVES) void rope_kernel(Args a) {
     const long long unit = (long long)blockIdx.x * WAVES + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);

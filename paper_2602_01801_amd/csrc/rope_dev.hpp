@@ -106,7 +106,11 @@ __device__ __forceinline__ RopeLane rope_lane(const RopeArgs &r) {
 }
 // The angles of a lane's pairs at a row.  Positions times frequencies in 64 bits, of which the part of a turn is kept: at position
 // 200000 a product in 32 bits is off by 0.01.  (64-bit arithmetic has the rate of unpacked 32-bit arithmetic here.)  The instructions for sine and
-// cosine take turns and are within 2^-22.9 (measured at 2^22 points of a turn), as are series to the 13th power, for 26 instructions more.
+// cosine take turns.  They are within 2^-22.92 of those of their operand (2^26 at random, small sines within 2^-20 of themselves), with the operand's rounding to 32 bits within
+// 2^-22.36; the bound of both is 2^-22.1.  That is a choice: quarter turns taken off in 64 bits and polynomials on the rest would make the error of fp32 outputs 6.4e-8 of their
+// norm, where it is 7.7 to 8.6e-8 (the plain form's in fp32 7e-8), at no cost to qk_norm_rope in fp32 (28.9 us and 28.8); but keys on their way into pages, whose angles are
+// computed for every head, would take 102 us instead of 74 (34612 tokens x 8 heads; rows one after the other, so that none spill, 94), for codes of four bits, and both
+// calls write the same bits.
 struct Turn {
     float c[4], s[4];
 };
@@ -182,8 +186,8 @@ __device__ __forceinline__ bool norm_and_turn(const RopeArgs &r, const Turn &t, 
     turned<INTER>(t, w, r.norm ? inverse_root<D>(ss, r.eps) : 1.0f, x);
     return odd;
 }
-// The same of any row.  The row and the root of eps are taken times a power of two that brings the larger one near 1; without a finite number
-// but zero to bring there, what the formula gives.  Coordinates that do not turn are kept apart, as 0 times infinity is no number.
+// The same of any row.  The row and the root of eps are taken times a power of two that brings the larger one near 1, after which the squares add up in 32 bits
+// as any row's do; without a finite number but zero to bring there, what the formula gives.  Coordinates that do not turn are kept apart, as 0 times infinity is no number.
 template <int D, bool INTER>
 __device__ __forceinline__ void norm_and_turn_odd(const RopeArgs &r, const RopeLane &l, const Turn &t, const Weights &w, float (&x)[8]) {
     float inv = 1.0f;
@@ -198,7 +202,6 @@ __device__ __forceinline__ void norm_and_turn_odd(const RopeArgs &r, const RopeL
             for (int e = 0; e < 8; ++e) x[e] = __builtin_amdgcn_ldexpf(x[e], n);
             inv = inverse_root<D>(squares<D>(x), __builtin_amdgcn_ldexpf(__builtin_amdgcn_ldexpf(r.eps, n), n));
         } else {
-            squares<D>(x);   // rows beside this one
 #pragma unroll
             for (int e = 0; e < 8; ++e) x[e] = top == INFINITY && fabsf(x[e]) < INFINITY ? 0.0f : NAN;
         }

@@ -153,9 +153,10 @@ __device__ __forceinline__ void rope_k_run(const RopeArgs &r, const Run &run, in
 }
 
 // Workgroups of keys, of values and of queries, evenly mixed over the launch: those of keys compute more than they move, the others the
-// other way round, and few tokens save a launch.  (Queries by a launch of their own, at eight wavefronts per SIMD instead of four: 34612 tokens, 40 heads on 8, 204 us
-// where one takes 196, in fp32 349 and 339, 12 on 12 146 and 146, in fp32 199 and 182; 96 tokens 13.7 and 11.1.)  Keys and values of 34612 tokens x 8 heads take 77 us behind other work, where writing them as they are takes 53: 29 of these are the vector
-// instructions of the keys, at the four wavefronts per SIMD that their LDS and registers leave (five spill, 87).  96 single tokens with their queries 8.0 us.
+// other way round, and few tokens save a launch.  34612 tokens, 40 heads on 8, 193 to 198 us (4.7 TB/s), in fp32 339 (5.2), 12 on 12 146 (3.6), in fp32 182 (5.3); 96 single tokens with
+// their queries 8.2.  (Queries by a launch of their own, at eight wavefronts per SIMD instead of four: 203, 349, 146 and 199; 96 tokens 13.7 instead of 11.1 a call.)  Without queries
+// keys and values of 34612 tokens x 8 heads take 74, where writing them as they are takes 45: 29 are the vector instructions of the keys, at the four wavefronts per SIMD that
+// their LDS and registers leave (five spill, 87); of 12 heads 94 (3.4 TB/s), in fp32 120 (4.4).
 template <bool BF16, int D, int PSHIFT, bool INTER>
 __global__ __launch_bounds__(4 << PSHIFT, 4) void write_rope_kernel(RopeWriteArgs a) {
     constexpr int P = 1 << PSHIFT, NW = P / 16;
