@@ -10,7 +10,7 @@ import paper_2602_01801_amd as fa
 import share_ref as sref
 from test_gpu_packed import i32
 from test_gpu_rope import make_pages
-from test_gpu_share import ints, layout, run_compact, run_free
+from test_gpu_share import ints, layout, run_compact, run_fork, run_free
 
 pytestmark = pytest.mark.gpu
 
@@ -184,3 +184,105 @@ def test_two_calls_at_once():
         assert ints(s["length"]) == after and ints(s["pool_n"]) == [n] and ints(s["pool"])[:n] == pl[:n]
         assert [ints(x) for x in s["status"]] == [s0, s1]
         assert np.array_equal(s["pages"].K8.cpu().numpy(), K) and np.array_equal(s["pages"].kscale.cpu().numpy(), ks)
+
+
+# ------------------------------------------------------------------------------------------------ pages named twice, pages far out, many requests from a graph
+
+
+@pytest.mark.parametrize("B,W", [(1, 6), (9, 5), (40, 300)])
+def test_pages_that_a_table_names_twice(B, W):
+    """Any entry may name any page, its own request's among them: holders are counted by entries."""
+    rng = np.random.default_rng(B + W)
+    P, n_pages = 16, 8 * B + 30
+    held = 2 * B + 3
+    for turn in range(6):
+        lens = [int(rng.choice([0, 1, P, W * P, rng.integers(0, W * P + 1)])) for _ in range(B)]
+        order = rng.permutation(n_pages).tolist()
+        table = [[order[int(rng.integers(held))] for _ in range(W)] for _ in range(B)]
+        pool, free = order[held:] + [-1] * held, n_pages - held
+        keep = [int(rng.choice([0, n, max(0, n - 1), n // 2, n // P * P])) for n in lens]
+        run_free(keep, lens, table, pool, free, P, in_place=turn % 2 == 1)
+        pages = make_pages(rng, n_pages, 2, P, 64)
+        mask = np.repeat(rng.random((B, W)) < 0.7, P, 1) & (rng.random((B, W * P)) < (1.0 if turn < 3 else 0.97))
+        run_compact(pages, mask, lens, table, pool, free, P, in_place=turn % 2 == 1)
+        empty = [b for b in range(B) if lens[b] == 0]
+        run_fork(rng, pages, rng.integers(0, B, len(empty)).tolist(), empty, rng.integers(0, W * P, len(empty)).tolist(), lens, table, pool, free, P)
+
+
+def test_pages_beyond_32_bits():
+    """Caches of more than 2^32 bytes: the last pages are forked, and move to each other."""
+    rng = np.random.default_rng(17)
+    P, d, Hkv, n_pages = 64, 128, 8, 70_000
+    assert n_pages * P * d * Hkv > 2 ** 32
+    pages = fa.Pages(*(torch.zeros(s, dtype=t, device="cuda") for s, t in (((n_pages, Hkv, P // 16, d // 16, 16, 16), torch.uint8), ((n_pages, Hkv), torch.float32)) * 2))
+    few = 12
+    at = [n_pages - 1, 0, n_pages - 2, 1, 65_535, 65_536, 65_537, n_pages - 3, 33_000, 2, n_pages - 4, 32_767]   # where the pages of a small cache lie in the large one
+    small = make_pages(rng, few, Hkv, P, d)
+    for big, x in ((pages.K8, small.K8), (pages.kscale, small.kscale), (pages.V8, small.V8), (pages.vscale, small.vscale)):
+        big[at] = x
+    def far(rows):
+        return [[at[p] if 0 <= p < few else -1 for p in row] for row in rows]
+    # a fork of 2 P + 5 tokens, then both requests thinned out
+    table, pool = [[0, 1, 2, -1], [-1] * 4], [3, 4, 5, 6, 7, 8, 9, 10, 11, -1, -1, -1]
+    lens, keep = i32([2 * P + 50, 0]), i32([2 * P + 5])
+    st, tb, pl, pn = i32(table), i32(far(table)), i32([at[p] if p >= 0 else -1 for p in pool] + [-1] * (n_pages - few)), i32([9])
+    spl, spn = i32(pool), i32([9])
+    mask = torch.from_numpy((rng.random((2, 4 * P)) < 0.7).astype(np.uint8)).cuda()
+    for pg, t, pool_t, n in ((small, st, spl, spn), (pages, tb, pl, pn)):
+        ln = lens.clone()
+        fa.kv_pages_fork(pg, i32([0]), i32([1]), ln, t, pool_t, n, keep=keep, out=(ln, n, i32([9])))
+        got = fa.kv_pages_compact(pg, mask, ln, t, pool_t, n)
+        t.copy_(got[1])
+        assert ints(got[4]) == [0, 0]
+    assert ints(tb) == far(ints(st))
+    for name in ("K8", "kscale", "V8", "vscale"):
+        assert torch.equal(getattr(pages, name)[at], getattr(small, name)), name
+    for x in (pages.K8, pages.V8):
+        x[at] = 0
+        assert all(not x[a:a + 4096].any() for a in range(0, n_pages, 4096))
+
+
+@pytest.mark.parametrize("B,W", [(1100, 3), (300, 30), (2100, 2)])
+def test_many_requests_replayed_from_a_graph(B, W):
+    """Thinning out and freeing by their launches for many requests, captured once, replayed on other lengths and masks with the program's own work between."""
+    rng = np.random.default_rng(B)
+    P, n_pages = 16, 3 * B * W
+    state = dict(length=i32([0] * B), table=i32([[-1] * W] * B), pool=i32([0] * n_pages), pool_n=i32([0]), stay=i32([0] * B),
+                 mask=torch.zeros((B, W * P), dtype=torch.uint8, device="cuda"))
+    pages = make_pages(rng, n_pages, 1, P, 64)
+    ws = torch.empty(fa.workspace_bytes(fa.OP_PAGES, B, W, n_pages, P), dtype=torch.uint8, device="cuda")
+    st = [i32([0] * B), i32([0] * B)]
+    side = torch.cuda.Stream()
+
+    def calls(s):
+        fa.kv_pages_compact(pages, s["mask"], s["length"], s["table"], s["pool"], s["pool_n"], out=(s["length"], s["table"], s["pool"], s["pool_n"], st[0]), ws=ws)
+        fa.kv_pages_free(s["stay"], s["length"], s["table"], s["pool"], s["pool_n"], P, out=(s["length"], s["pool_n"], st[1]), ws=ws)
+
+    fa.init()
+    with torch.cuda.stream(side):
+        calls(state)
+        side.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=side):
+            calls(state)
+        for turn in range(4):
+            lens = [int(rng.integers(0, W * P + 1)) for _ in range(B)]
+            table, pool, _, total = layout(rng, lens, W, P, 10, share=0.3)
+            assert total <= n_pages
+            table = [[p if 0 <= p < total else -1 for p in row] for row in table]
+            free = [10, B // 3 + 10, n_pages - total + 10, 0][turn]   # from then on pages that no table names
+            pool = pool[:10] + list(range(total, n_pages)) + [-1] * (total - 10)
+            stay = [int(rng.integers(0, W * P + 9)) for _ in range(B)]
+            mask = rng.random((B, W * P)) < 0.7
+            K, ks = pages.K8.cpu().numpy().copy(), pages.kscale.cpu().numpy().copy()
+            for name, x in dict(length=lens, table=table, pool=pool, pool_n=[free], stay=stay).items():
+                state[name].copy_(i32(x))
+            state["mask"].copy_(torch.from_numpy(mask.astype(np.uint8)))
+            graph.replay()
+            side.synchronize()
+            after, t, pool, n, s0, made = sref.compact(mask, lens, table, pool, free, P, n_pages)
+            sref.compact_codes(K, ks, False, made)
+            after, n, s1 = sref.free(stay, after, t, pool, n, P, n_pages)
+            assert [ints(x) for x in st] == [s0, s1]
+            assert ints(state["length"]) == after and ints(state["pool_n"]) == [n] and ints(state["pool"])[:n] == pool[:n]
+            assert np.array_equal(pages.K8.cpu().numpy(), K) and np.array_equal(pages.kscale.cpu().numpy(), ks)
